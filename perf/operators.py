@@ -308,6 +308,7 @@ def prepare(case, seed):
         s.ctx_len = _i32(np.concatenate([ctx, np.zeros(n, np.int64)]))
         s.src = _i32(np.repeat(np.arange(P), c["children"]))
         s.dst = _i32(P + r.permutation(n))
+        s.result = torch.zeros(n, dtype=torch.int32, device=DEV)
         s.k_cache = _cache(layers, s.num_pages, hkv, d, gen)
         s.v_cache = _cache(layers, s.num_pages, hkv, d, gen)
     elif c["kind"] == "compact":
@@ -324,9 +325,13 @@ def prepare(case, seed):
             keep[j, :k] = np.concatenate([[0], 1 + np.sort(r.choice(c["window"] - 1, k - 1,
                                                                     replace=False))])
         s.keep, s.keep_len = _i32(keep), _i32(kept[s.row.cpu().numpy()])
+        s.pages = torch.zeros(n, dtype=torch.int32, device=DEV)
         s.result = torch.zeros(n, dtype=torch.int32, device=DEV)
         s.k_cache = _cache(layers, s.num_pages, hkv, d, gen)
         s.v_cache = _cache(layers, s.num_pages, hkv, d, gen)
+        if own:
+            s.ws = torch.empty(pic.pic_page_compact_workspace_size(s.geom, n, c["keep"]),
+                               dtype=torch.uint8, device=DEV)
     else:
         n = c["pages"]
         s.num_pages = 2 * n
@@ -387,11 +392,12 @@ def run(s):
     if s.kind == "fork":
         (_fork_own if own else _fork_plain)(s)
         return {"block_table": s.block_table, "refs": s.refs, "ctx_len": s.ctx_len,
-                "k_cache": s.k_cache, "v_cache": s.v_cache}
+                "result": s.result, "k_cache": s.k_cache, "v_cache": s.v_cache}
     if s.kind == "compact":
         (_compact_own if own else _compact_plain)(s)
         return {"block_table": s.block_table, "refs": s.refs, "ctx_len": s.ctx_len,
-                "result": s.result, "k_cache": s.k_cache, "v_cache": s.v_cache}
+                "pages": s.pages, "result": s.result, "k_cache": s.k_cache,
+                "v_cache": s.v_cache}
     (_copy_own if own else _copy_plain)(s)
     return {"k": s.k_to, "v": s.v_to}
 
@@ -413,15 +419,16 @@ def _fork_own(s):
     import paper_2607_28069_gb300 as pic
     pic.pic_page_free(s.dst, s.block_table, s.num_pages, s.refs, s.ctx_len)
     pic.pic_page_fork(s.geom, s.src, s.dst, s.ctx_len, s.block_table, s.num_pages, s.refs,
-                      s.k_cache, s.v_cache, reserve=s.c["reserve"])
+                      s.k_cache, s.v_cache, s.result, reserve=s.c["reserve"])
 
 
 def _compact_own(s):
     import paper_2607_28069_gb300 as pic
-    pic.pic_page_reserve(s.row, s.c["window"], s.ctx_len, s.block_table, s.num_pages, s.refs)
+    pic.pic_page_reserve(s.row, s.c["window"], s.ctx_len, s.block_table, s.num_pages, s.refs,
+                         s.pages)
     pic.pic_page_compact(s.geom, s.row, s.keep, s.keep_len, s.ctx_len, s.block_table, s.num_pages,
                          s.refs, s.k_cache, s.v_cache, s.result, start=s.start,
-                         rotate=s.c["rotate"])
+                         rotate=s.c["rotate"], workspace=s.ws)
 
 
 def _copy_own(s):
@@ -577,6 +584,7 @@ def _fork_plain(s):
     s.refs.index_add_(0, table.clamp(min=0).long().flatten(), (shared | fresh).int().flatten())
     s.block_table[dst] = table
     s.ctx_len[dst] = ctx.int()
+    s.result.copy_(ctx)
     # the rows of the page that the context ends in, where it ends inside one
     # (elsewhere the context's first page is written back to itself)
     part = ctx % PAGE > 0
@@ -601,6 +609,7 @@ def _compact_plain(s):
     at = (n.cumsum(0) - n)[:, None] + lack.cumsum(-1) - 1
     table = torch.where(lack, free[at.clamp(0, s.num_pages - 1)].int(), table)
     s.refs.index_add_(0, table.clamp(min=0).long().flatten(), lack.int().flatten())
+    s.pages.copy_(want)
     # the kept positions move together
     keep = s.keep.long()
     i = torch.arange(c["keep"], device=DEV)
@@ -670,7 +679,8 @@ def exact(case, seed):
                 page = int(bt[a, int(ctx[a]) // PAGE])
                 k[:, mine[0], :, :rows] = k[:, page, :, :rows]
                 v[:, mine[0], :, :rows] = v[:, page, :, :rows]
-        return {"block_table": None, "refs": None, "ctx_len": None, "k_cache": k, "v_cache": v}
+        return {"block_table": None, "refs": None, "ctx_len": None, "result": None, "k_cache": k,
+                "v_cache": v}
     if c["kind"] == "compact":
         return _exact_compact(s, c, host)
     out = torch.zeros(s.out.shape, dtype=torch.float64, device=DEV)
@@ -723,5 +733,5 @@ def _exact_compact(s, c, host):
                                 device=DEV)
         k[:, table[w // PAGE], :, w % PAGE] = x
         v[:, table[w // PAGE], :, w % PAGE] = y
-    return {"block_table": None, "refs": None, "ctx_len": None, "result": None, "k_cache": k,
-            "v_cache": v}
+    return {"block_table": None, "refs": None, "ctx_len": None, "pages": None, "result": None,
+            "k_cache": k, "v_cache": v}
