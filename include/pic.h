@@ -71,6 +71,8 @@ typedef enum {
 #define PIC_DEV_BAD_PAGE 6          /* page id outside [0, num_pages)        */
 #define PIC_DEV_BAD_POSITION 7      /* logical position out of range         */
 #define PIC_DEV_TIMEOUT 8           /* a bounded wait inside a kernel expired */
+#define PIC_DEV_SHARED_PAGE 9       /* a page to be written has other users   */
+#define PIC_DEV_NO_FREE_PAGE 10     /* fewer free pages than were asked for   */
 
 /* RoPE pairing: element i with i + d/2 (half-split), or 2i with 2i+1. */
 #define PIC_ROPE_HALF 0
@@ -546,6 +548,204 @@ pic_status_t pic_attend_decode_noalloc(const pic_geom_t *geom, int32_t layer, in
                                        int64_t num_pages, void *k_cache, void *v_cache, void *out,
                                        float *lse, int32_t max_ctx, int32_t num_splits,
                                        pic_stream_t stream);
+
+/* ===========================================================================
+ * Speculative decoding over the linked cache.  The paper ends its serving path
+ * with ordinary decoding (appendix "Position-Independent Linking"); these calls
+ * continue it with several drafted tokens per step: pic_page_reserve (room for
+ * them), pic_attend_draft (each layer), pic_verify_draft (which of them the
+ * target keeps), pic_page_compact (their keys and values move together, the
+ * pages behind them go back), and pic_page_fork / pic_page_free / pic_page_copy
+ * for branches of a context.
+ * ======================================================================== */
+
+/*
+ * pic_attend_draft -- one layer of one step over drafted tokens: the append of
+ * a request's drafts and their attention over its cache.
+ *
+ * Request b has n_b = draft_len[b] drafted tokens (0 <= n_b <= max_draft <=
+ * 64; token 0 is usually the last sampled one, whose key is not in the cache
+ * yet), behind ctx_len[b] cached positions.  parent[b][i] (< i, or -1: none)
+ * is the token that token i continues, so the drafts form a tree (or several);
+ * parent NULL: a chain, parent i - 1.  With depth d_i (0 without a parent, else
+ * the parent's + 1), position p_i = ctx_len[b] + d_i and slot t_i =
+ * ctx_len[b] + i (t / page and t % page through the block table, as always):
+ *     k_cache[layer][slot t_i] = R(p_i) k_new[b][i], v_cache... = v_new[b][i]
+ *     out[b][i][h] = sum over the keys of slots < ctx_len[b], of token i and of
+ *         its ancestors:  softmax(R(p_i) q[b][i][h] . k / sqrt(d)) v
+ * (the key of a rejected branch never shows).  lse[b][i][h] (nullable): the
+ * natural-log sum-exp of those scores.  Rows i >= n_b of out and lse are not
+ * written.  A drafted token's key and value have to be finite: those of another
+ * branch of its own request enter with weight zero.  Slots behind the drafts
+ * may hold anything.
+ *
+ * q: bf16 [batch][max_draft][Hq][d]; k_new, v_new: bf16
+ * [batch][max_draft][Hkv][d] (un-rotated); ctx_len, draft_len: int32 [batch];
+ * parent: int32 [batch][max_draft] or NULL; block_table: int32
+ * [batch][max_pages]; out: bf16 [batch][max_draft][Hq][d]; lse: float
+ * [batch][max_draft][Hq] or NULL.
+ * workspace: >= pic_draft_workspace_size(...) bytes, 256-byte aligned; its
+ * contents do not matter before or after.  Runs on the tensor cores
+ * (tcgen05.mma, TMEM, TMA).  The key tiles of the whole batch are dealt to the
+ * GPU's SMs in equal shares by the kernel itself, so ragged batches need no
+ * split count and the sizes may change on the device between calls (a captured
+ * graph stays valid).  Launches: append, attention, merge.
+ * Device checks: lengths and parents (PIC_DEV_BAD_REQUEST; a bad parent is read
+ * as -1), slots past the block table (PIC_DEV_BLOCK_TABLE_SHORT), page ids
+ * (PIC_DEV_BAD_PAGE; such a page's keys and values read as zeros).  A request
+ * with a bad length or a short table is left alone.
+ */
+size_t pic_draft_workspace_size(const pic_geom_t *geom, int32_t batch, int32_t max_draft);
+
+pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, int32_t batch,
+                              int32_t max_draft, const void *q, const void *k_new,
+                              const void *v_new, const int32_t *ctx_len,
+                              const int32_t *draft_len, const int32_t *parent,
+                              const int32_t *block_table, int32_t max_pages, int64_t num_pages,
+                              void *k_cache, void *v_cache, void *out, float *lse,
+                              void *workspace, size_t workspace_bytes, pic_stream_t stream);
+
+/*
+ * pic_verify_draft -- which drafted tokens the target keeps, and the token that
+ * follows them, from given random numbers; the kept tokens and the next one are
+ * distributed as the target's own sampling would be.
+ *
+ * Request b has draft_len[b] tokens (0 .. max_draft <= 64), token 0 the root: a
+ * token already sampled, whose successor is wanted.  target_prob row (b, i) is
+ * the target's distribution after token i, vocab floats at target_prob + b *
+ * target_stride[0] + i * target_stride[1] (strides in floats, HOST array).
+ *  - With draft_prob: a chain (parent has to be NULL) of tokens sampled from
+ *    the draft's own distributions; row (b, i - 1), i >= 1, is the one token i
+ *    was drawn from.  Tokens 1, 2, ... are accepted while
+ *        uniform[b][i - 1] * draft_prob[i - 1][x_i] < target_prob[i - 1][x_i]
+ *    (single-precision product).  After the first refusal, of token i, the next
+ *    token is drawn from max(target_prob[i - 1] - draft_prob[i - 1], 0) (from
+ *    target_prob[i - 1] where that is zero everywhere); if all are accepted,
+ *    from the last token's target_prob row.  The draw uses
+ *    uniform[b][draft_len[b] - 1].
+ *  - Without: tokens of any origin (for instance a draft's most likely ones), a
+ *    tree by parent as in pic_attend_draft or (NULL) a chain.  From token 0 on,
+ *    a token x is drawn from the present token's target_prob row with
+ *    uniform[b][depth]; if one of its children carries x, that child (the first)
+ *    is accepted and becomes the present token, else x is the next token.
+ * A draw from weights w with the number u: w is taken as the whole numbers
+ * trunc(2^36 min(max(w, 0), 1)) (NaN as 0), and the token is the first whose
+ * running sum exceeds floor(S floor(2^24 u) / 2^24), S the sum of all; u is
+ * taken into [0, 1 - 2^-24].  Whole numbers have no order of summation, so the
+ * result is the same on every run and any implementation of this rule.  S = 0
+ * gives the token -1.
+ *
+ * tokens, parent: int32 [batch][max_draft]; uniform: float [batch][max_draft].
+ * Outputs: path int32 [batch][max_draft], the accepted tokens' indices from 0
+ *   (the root) on, then -1; path_len int32 [batch], their number (the root
+ *   counts; 0 for a request without tokens); next_token int32 [batch].  path and
+ *   path_len are the keep list of pic_page_compact.
+ * vocab <= 2^24.  A drafted token outside [0, vocab) is never accepted, a parent
+ * not below its child never followed.  One launch, no workspace.  Device check:
+ * draft_len (PIC_DEV_BAD_REQUEST, the request is treated as empty).
+ */
+pic_status_t pic_verify_draft(int32_t batch, int32_t max_draft, int32_t vocab,
+                              const int32_t *tokens, const int32_t *parent,
+                              const int32_t *draft_len, const float *target_prob,
+                              const int64_t *target_stride, const float *draft_prob,
+                              const int64_t *draft_stride, const float *uniform, int32_t *path,
+                              int32_t *path_len, int32_t *next_token, pic_stream_t stream);
+
+/*
+ * Pages of a cache.  page_refs int32 [num_pages] holds how many block-table
+ * rows use each page; a page is free when that is 0.  block_table int32
+ * [rows][max_pages] lists a row's pages in logical order, then -1; ctx_len int32
+ * [rows] is a row's length in positions.  Calls name rows by index; a row may
+ * be named once per call.  Free pages are taken lowest number first, in the
+ * order of the call's list, so page numbers depend on the state alone.  A row a
+ * call cannot serve is left as it is, reported through pic_device_status
+ * (detail: its index in the list) and gets -1 in `result`.  At most 4096 rows a
+ * call.
+ */
+
+/*
+ * pic_page_reserve -- room for `extra` more positions behind each listed row's
+ * ctx_len: missing pages up to position ctx_len + extra - 1 are allocated.
+ * result int32 [n]: the pages the row then needs.  One launch.
+ * Device checks: rows, lengths (BAD_REQUEST), max_pages (BLOCK_TABLE_SHORT),
+ * free pages (NO_FREE_PAGE).
+ */
+pic_status_t pic_page_reserve(int32_t n, const int32_t *row, int32_t extra, int32_t rows,
+                              const int32_t *ctx_len, int32_t *block_table, int32_t max_pages,
+                              int64_t num_pages, int32_t *page_refs, int32_t *result,
+                              pic_stream_t stream);
+
+/*
+ * pic_page_fork -- branches of linked contexts: for each i, row dst_row[i]
+ * (empty: no pages) becomes a copy of row src_row[i].  The pages that the
+ * context fills are shared (one more user each); the rows of a last, partly
+ * filled page are copied, layers [layer_begin, layer_end), into a page of the
+ * branch's own, which also gets pages for `reserve` further positions; the
+ * branch's ctx_len is set.  So both can append without touching each other.
+ * result int32 [n]: the branch's length.  Two launches.
+ * Device checks: rows, an empty destination, lengths (BAD_REQUEST), max_pages
+ * (BLOCK_TABLE_SHORT), page ids (BAD_PAGE), free pages (NO_FREE_PAGE).
+ */
+pic_status_t pic_page_fork(const pic_geom_t *geom, int32_t n, const int32_t *src_row,
+                           const int32_t *dst_row, int32_t reserve, int32_t rows,
+                           int32_t *ctx_len, int32_t *block_table, int32_t max_pages,
+                           int64_t num_pages, int32_t *page_refs, void *k_cache, void *v_cache,
+                           int32_t layer_begin, int32_t layer_end, int32_t *result,
+                           pic_stream_t stream);
+
+/*
+ * pic_page_compact -- keep some of the positions from start on, in place: for
+ * each listed row (s = start[i], or its ctx_len where start is NULL) and
+ * j < keep_len[i], position s + j takes the key and value of position
+ * s + keep[i][j] (keep ascending, >= 0), layers [layer_begin, layer_end); then
+ * ctx_len = s + keep_len[i] and the row's pages behind ctx_len + reserve go back.
+ * rotate != 0: a key that moves by delta positions is re-rotated by R(delta)
+ * (Eq. 3), as when documents are relocated, rounded to bf16 once more: positions
+ * taken out of the middle of a context leave no gap.  rotate = 0 moves keys
+ * unchanged: drafted tokens already carry the position of their depth.
+ * keep: int32 [n][max_keep]; keep_len: int32 [n], 0 .. max_keep (0 keeps
+ * nothing); result int32 [n]: the row's new length.
+ * workspace: pic_page_compact_workspace_size(...) bytes (0 for max_keep <= 16;
+ * then it may be NULL), 256-byte aligned, contents do not matter.
+ * Three launches.  Positions are copied once, also where source and target
+ * ranges overlap: each CTA holds 16 rows on chip and stores them when the CTAs
+ * that read what it overwrites have done so.
+ * Device checks: rows, lengths (BAD_REQUEST), keep lists (BAD_POSITION),
+ * max_pages (BLOCK_TABLE_SHORT), page ids (BAD_PAGE), and every page a position
+ * moves into has this row as its only user (SHARED_PAGE).
+ */
+size_t pic_page_compact_workspace_size(const pic_geom_t *geom, int32_t n, int32_t max_keep);
+
+pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, const int32_t *row,
+                              const int32_t *start, const int32_t *keep, int32_t max_keep,
+                              const int32_t *keep_len, int32_t reserve, int32_t rotate,
+                              int32_t rows, int32_t *ctx_len, int32_t *block_table,
+                              int32_t max_pages, int64_t num_pages, int32_t *page_refs,
+                              void *k_cache, void *v_cache, int32_t layer_begin,
+                              int32_t layer_end, int32_t *result, void *workspace,
+                              size_t workspace_bytes, pic_stream_t stream);
+
+/*
+ * pic_page_free -- the listed rows give back their pages (one user less each)
+ * and become empty (-1 entries, ctx_len 0).  One launch.  Device checks: rows
+ * (BAD_REQUEST), page ids and pages without users (BAD_PAGE).
+ */
+pic_status_t pic_page_free(int32_t n, const int32_t *row, int32_t rows, int32_t *ctx_len,
+                           int32_t *block_table, int32_t max_pages, int64_t num_pages,
+                           int32_t *page_refs, pic_stream_t stream);
+
+/*
+ * pic_page_copy -- the K and V of whole pages, layers [layer_begin,
+ * layer_end): page src_page[i] of the source cache (src_pages pages a layer) to
+ * page dst_page[i] of the destination cache (dst_pages pages a layer), which
+ * may be the same cache: no page may then be both a source and a destination.
+ * Entries where both are -1 are skipped.  Any n >= 0.  One launch.  Device
+ * check: page ids (BAD_PAGE).
+ */
+pic_status_t pic_page_copy(const pic_geom_t *geom, int32_t n, const int32_t *src_page,
+                           const int32_t *dst_page, const void *k_src, const void *v_src,
+                           int64_t src_pages, void *k_dst, void *v_dst, int64_t dst_pages,
+                           int32_t layer_begin, int32_t layer_end, pic_stream_t stream);
 
 #ifdef __cplusplus
 } /* extern "C" */

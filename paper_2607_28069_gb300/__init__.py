@@ -25,6 +25,9 @@ __all__ = [
     "pic_prefill_num_splits", "pic_prefill_plan_splits", "pic_decode_num_splits",
     "pic_attend_decode_noalloc",
     "pic_attend_decode", "pic_decode_workspace_size", "pic_device_status", "PicError",
+    "pic_draft_workspace_size", "pic_attend_draft", "pic_verify_draft", "pic_page_reserve",
+    "pic_page_fork", "pic_page_compact_workspace_size", "pic_page_compact", "pic_page_free",
+    "pic_page_copy",
     "EXPORTED_SYMBOLS", "ROPE_HALF", "ROPE_INTERLEAVED",
 ]
 
@@ -45,12 +48,15 @@ EXPORTED_SYMBOLS = (
     "pic_append_inline",
     "pic_attend_prefill", "pic_attend_prefill_fused", "pic_decode_workspace_size", "pic_decode_num_splits",
     "pic_attend_decode", "pic_attend_decode_noalloc", "pic_copy_async", "pic_launch_probe",
-    "pic_wait_probe",
+    "pic_wait_probe", "pic_draft_workspace_size", "pic_attend_draft", "pic_verify_draft",
+    "pic_page_reserve", "pic_page_fork", "pic_page_compact_workspace_size", "pic_page_compact",
+    "pic_page_free", "pic_page_copy",
 )
 
 DEVICE_CODES = {
     0: "ok", 1: "bad doc id", 2: "bad doc length", 3: "bad request", 4: "context overflow",
-    5: "block table short", 6: "bad page", 7: "bad position", 8: "timeout",
+    5: "block table short", 6: "bad page", 7: "bad position", 8: "timeout", 9: "shared page",
+    10: "no free page",
 }
 
 
@@ -147,6 +153,17 @@ def load():
         "pic_decode_num_splits": (I32, [G, I32, I32, I32]),
         "pic_attend_decode": (I32, [G, I32, I32, P, P, P, P, I32, P, I32, I64, P, P, P, P, I32, I32,
                                     P, SZ, P]),
+        "pic_draft_workspace_size": (SZ, [G, I32, I32]),
+        "pic_attend_draft": (I32, [G, I32, I32, I32, P, P, P, P, P, P, P, I32, I64, P, P, P, P, P,
+                                   SZ, P]),
+        "pic_verify_draft": (I32, [I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P]),
+        "pic_page_reserve": (I32, [I32, P, I32, I32, P, P, I32, I64, P, P, P]),
+        "pic_page_fork": (I32, [G, I32, P, P, I32, I32, P, P, I32, I64, P, P, P, I32, I32, P, P]),
+        "pic_page_compact_workspace_size": (SZ, [G, I32, I32]),
+        "pic_page_compact": (I32, [G, I32, P, P, P, I32, P, I32, I32, I32, P, P, I32, I64, P, P, P,
+                                   I32, I32, P, P, SZ, P]),
+        "pic_page_free": (I32, [I32, P, I32, P, P, I32, I64, P, P]),
+        "pic_page_copy": (I32, [G, I32, P, P, P, P, I64, P, P, I64, I32, I32, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -416,3 +433,93 @@ def pic_attention_deviation(geom: Geometry, layer: int, inline_pos, inline_len, 
         sums, counts, stream)
     if st:
         _check(st, "pic_attention_deviation")
+
+
+# -- speculative decoding over the linked cache (see include/pic.h)
+def pic_draft_workspace_size(geom: Geometry, batch: int, max_draft: int) -> int:
+    g = geom._c()
+    return load().pic_draft_workspace_size(ctypes.byref(g), batch, max_draft)
+
+
+def pic_attend_draft(geom: Geometry, layer: int, q, k_new, v_new, ctx_len, draft_len, block_table,
+                     num_pages: int, k_cache, v_cache, out, parent=None, lse=None, workspace=None,
+                     stream=None):
+    """One layer of one step over drafted tokens: q [B][T][Hq][d], k_new and
+    v_new [B][T][Hkv][d] un-rotated, T <= 64, a tree by parent [B][T] (None: a
+    chain) behind ctx_len [B] cached positions; draft_len [B] tokens of each
+    request count.  Appends the keys and values at slots ctx_len + i and writes
+    out [B][T][Hq][d]."""
+    st = (_nat or _native()).attend_draft(
+        geom, layer, q, k_new, v_new, ctx_len, draft_len, parent, block_table, num_pages, k_cache,
+        v_cache, out, lse, workspace, stream)
+    if st:
+        _check(st, "pic_attend_draft")
+
+
+def pic_verify_draft(tokens, draft_len, target_prob, uniform, path, path_len, next_token,
+                     draft_prob=None, parent=None, stream=None):
+    """Which drafted tokens the target keeps and the token after them:
+    target_prob float32 [B][T][V], draft_prob [B][T - 1][V] for a sampled chain
+    or None (a tree by parent, or a chain); the last dimension contiguous, the
+    others of any stride.  Fills path [B][T], path_len [B], next_token [B]."""
+    st = (_nat or _native()).verify_draft(
+        tokens, draft_len, target_prob, uniform, path, path_len, next_token, draft_prob, parent,
+        stream)
+    if st:
+        _check(st, "pic_verify_draft")
+
+
+def pic_page_reserve(row, extra: int, ctx_len, block_table, num_pages: int, page_refs, result,
+                     stream=None):
+    """Pages for `extra` positions behind each listed row's ctx_len."""
+    st = (_nat or _native()).page_reserve(row, extra, ctx_len, block_table, num_pages, page_refs,
+                                          result, stream)
+    if st:
+        _check(st, "pic_page_reserve")
+
+
+def pic_page_fork(geom: Geometry, src_row, dst_row, ctx_len, block_table, num_pages: int, page_refs,
+                  k_cache, v_cache, result, reserve: int = 0, layer_begin: int = 0,
+                  layer_end: Optional[int] = None, stream=None):
+    """Each empty row dst_row[i] becomes a branch of row src_row[i]."""
+    st = (_nat or _native()).page_fork(
+        geom, src_row, dst_row, ctx_len, block_table, num_pages, page_refs, k_cache, v_cache,
+        result, reserve, layer_begin, geom.num_layers if layer_end is None else layer_end, stream)
+    if st:
+        _check(st, "pic_page_fork")
+
+
+def pic_page_compact_workspace_size(geom: Geometry, n: int, max_keep: int) -> int:
+    g = geom._c()
+    return load().pic_page_compact_workspace_size(ctypes.byref(g), n, max_keep)
+
+
+def pic_page_compact(geom: Geometry, row, keep, keep_len, ctx_len, block_table, num_pages: int,
+                     page_refs, k_cache, v_cache, result, start=None, reserve: int = 0,
+                     rotate: bool = False, workspace=None, layer_begin: int = 0,
+                     layer_end: Optional[int] = None, stream=None):
+    """Of each listed row's positions from start (None: its ctx_len) on, keep
+    those at start + keep[i][:keep_len[i]], moved together."""
+    st = (_nat or _native()).page_compact(
+        geom, row, keep, keep_len, ctx_len, block_table, num_pages, page_refs, k_cache, v_cache,
+        result, start, reserve, 1 if rotate else 0, layer_begin,
+        geom.num_layers if layer_end is None else layer_end, workspace, stream)
+    if st:
+        _check(st, "pic_page_compact")
+
+
+def pic_page_free(row, block_table, num_pages: int, page_refs, ctx_len, stream=None):
+    """The listed rows give back their pages and become empty."""
+    st = (_nat or _native()).page_free(row, ctx_len, block_table, num_pages, page_refs, stream)
+    if st:
+        _check(st, "pic_page_free")
+
+
+def pic_page_copy(geom: Geometry, src_page, dst_page, k_src, v_src, k_dst, v_dst,
+                  layer_begin: int = 0, layer_end: Optional[int] = None, stream=None):
+    """Whole pages from one cache to another (or to other pages of the same)."""
+    st = (_nat or _native()).page_copy(
+        geom, src_page, dst_page, k_src, v_src, k_dst, v_dst, layer_begin,
+        geom.num_layers if layer_end is None else layer_end, stream)
+    if st:
+        _check(st, "pic_page_copy")

@@ -613,6 +613,218 @@ PyObject *attention_deviation(PyObject *, PyObject *const *v, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------------ speculative decoding
+// A tensor of `ndim` dimensions whose last one is contiguous (the others may
+// have any stride): its data and strides.
+float *strided3(const View &w, const char *name, int64_t *strides) {
+  if (w.skip || w.dim() != 3) raise(PyExc_ValueError, "%s must have three dimensions%s", name);
+  if (!w.t->is_cuda()) raise(PyExc_ValueError, "%s must be a CUDA tensor%s", name);
+  if (w.t->scalar_type() != at::kFloat) raise(PyExc_ValueError, "%s must be torch.float32%s", name);
+  if (w.size(2) != 1 && w.t->stride(2) != 1)
+    raise(PyExc_ValueError, "%s must be contiguous in its last dimension%s", name);
+  strides[0] = w.t->stride(0);
+  strides[1] = w.t->stride(1);
+  return static_cast<float *>(w.data());
+}
+
+// A tensor argument with `n` elements in all.
+template <typename T>
+T *sized(Args &a, at::ScalarType dtype, const char *name, int64_t n, bool optional = false) {
+  const View w = view_of(a.next(), name);
+  T *p = static_cast<T *>(checked(w, dtype, name, optional));
+  if (w && w.numel() != n) raise(PyExc_ValueError, "%s has the wrong number of elements%s", name);
+  return p;
+}
+// A cache [layers][pages][Hkv][page][d] of the geometry; *pages gets its pages.
+void *cache_of(Args &a, const Geom &g, const char *name, int64_t *pages) {
+  const View w = view_of(a.next(), name);
+  void *p = checked(w, at::kBFloat16, name);
+  if (w.dim() != 5 || w.size(0) != g.g.num_layers || w.size(2) != g.g.num_kv_heads ||
+      w.size(3) != g.g.page_size || w.size(4) != g.g.head_dim || (*pages >= 0 && w.size(1) != *pages))
+    raise(PyExc_ValueError, "%s must be [num_layers][num_pages][num_kv_heads][page_size][head_dim]%s",
+          name);
+  *pages = w.size(1);
+  return p;
+}
+
+PyObject *attend_draft(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    Geom g(a.next());
+    const int32_t layer = a.i32();
+    const View qv = view_of(a.next(), "q");
+    const void *q = checked(qv, at::kBFloat16, "q");
+    if (qv.dim() != 4 || qv.size(2) != g.g.num_q_heads || qv.size(3) != g.g.head_dim)
+      raise(PyExc_ValueError, "%s must be [batch][max_draft][num_q_heads][head_dim]%s", "q");
+    const int64_t B = qv.size(0), T = qv.size(1), kvn = B * T * g.g.num_kv_heads * g.g.head_dim;
+    const void *kn = sized<void>(a, at::kBFloat16, "k_new", kvn);
+    const void *vn = sized<void>(a, at::kBFloat16, "v_new", kvn);
+    const int32_t *ctx = sized<int32_t>(a, at::kInt, "ctx_len", B);
+    const int32_t *len = sized<int32_t>(a, at::kInt, "draft_len", B);
+    const int32_t *parent = sized<int32_t>(a, at::kInt, "parent", B * T, true);
+    const View bt = view_of(a.next(), "block_table");
+    const int32_t *table = static_cast<int32_t *>(checked(bt, at::kInt, "block_table"));
+    const int64_t max_pages = second(bt, "block_table");
+    if (bt.size(0) != B) raise(PyExc_ValueError, "%s must have a row per request%s", "block_table");
+    int64_t num_pages = a.integer();
+    void *kc = cache_of(a, g, "k_cache", &num_pages), *vc = cache_of(a, g, "v_cache", &num_pages);
+    void *out = sized<void>(a, at::kBFloat16, "out", qv.numel());
+    float *lse = sized<float>(a, at::kFloat, "lse", B * T * g.g.num_q_heads, true);
+    const View wv = view_of(a.next(), "workspace");
+    void *ws = checked(wv, at::kByte, "workspace");
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_attend_draft(&g.g, layer, (int32_t)B, (int32_t)T, q, kn, vn, ctx, len, parent, table,
+                              (int32_t)max_pages, num_pages, kc, vc, out, lse, ws, (size_t)wv.numel(),
+                              s);
+    });
+  });
+}
+
+PyObject *verify_draft(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    const View tv = view_of(a.next(), "tokens");
+    const int32_t *tok = static_cast<int32_t *>(checked(tv, at::kInt, "tokens"));
+    need_2d(tv, "tokens");
+    const int64_t B = tv.size(0), T = tv.size(1);
+    const int32_t *len = sized<int32_t>(a, at::kInt, "draft_len", B);
+    int64_t ts[2], ds[2] = {0, 0};
+    const View pv = view_of(a.next(), "target_prob");
+    if (!pv) raise(PyExc_ValueError, "%s is required%s", "target_prob");
+    const float *target = strided3(pv, "target_prob", ts);
+    if (pv.size(0) != B || pv.size(1) != T)
+      raise(PyExc_ValueError, "%s must be [batch][max_draft][vocab]%s", "target_prob");
+    const float *u = sized<float>(a, at::kFloat, "uniform", B * T);
+    int32_t *path = sized<int32_t>(a, at::kInt, "path", B * T);
+    int32_t *path_len = sized<int32_t>(a, at::kInt, "path_len", B);
+    int32_t *next = sized<int32_t>(a, at::kInt, "next_token", B);
+    const View dv = view_of(a.next(), "draft_prob");
+    const float *draft = nullptr;
+    if (dv) {
+      draft = strided3(dv, "draft_prob", ds);
+      if (dv.size(0) != B || dv.size(1) != T - 1 || dv.size(2) != pv.size(2))
+        raise(PyExc_ValueError, "%s must be [batch][max_draft - 1][vocab]%s", "draft_prob");
+      if (T == 1) draft = nullptr;  // nothing was drafted
+    }
+    const int32_t *parent = sized<int32_t>(a, at::kInt, "parent", B * T, true);
+    if (dv && parent) raise(PyExc_ValueError, "%s needs a chain (no parent)%s", "draft_prob");
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_verify_draft((int32_t)B, (int32_t)T, (int32_t)pv.size(2), tok, parent, len, target,
+                              ts, draft, draft ? ds : nullptr, u, path, path_len, next, s);
+    });
+  });
+}
+
+// The block table and what belongs to it: [rows][max_pages], page counts.
+struct Table {
+  int32_t *ctx, *table, *refs;
+  int64_t rows, max_pages, num_pages;
+};
+Table table_of(Args &a) {  // ctx_len, block_table, num_pages, page_refs
+  Table t;
+  const View cv = view_of(a.next(), "ctx_len");
+  t.ctx = static_cast<int32_t *>(checked(cv, at::kInt, "ctx_len"));
+  const View bt = view_of(a.next(), "block_table");
+  t.table = static_cast<int32_t *>(checked(bt, at::kInt, "block_table"));
+  t.max_pages = second(bt, "block_table");
+  t.rows = bt.size(0);
+  if (cv.numel() != t.rows) raise(PyExc_ValueError, "%s must have an entry per row%s", "ctx_len");
+  t.num_pages = a.integer();
+  t.refs = sized<int32_t>(a, at::kInt, "page_refs", t.num_pages);
+  return t;
+}
+
+PyObject *page_reserve(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    const View rv = view_of(a.next(), "row");
+    const int32_t *row = static_cast<int32_t *>(checked(rv, at::kInt, "row"));
+    const int32_t extra = a.i32();
+    const Table t = table_of(a);
+    int32_t *res = sized<int32_t>(a, at::kInt, "result", rv.numel());
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_page_reserve((int32_t)rv.numel(), row, extra, (int32_t)t.rows, t.ctx, t.table,
+                              (int32_t)t.max_pages, t.num_pages, t.refs, res, s);
+    });
+  });
+}
+
+PyObject *page_fork(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    Geom g(a.next());
+    const View sv = view_of(a.next(), "src_row");
+    const int32_t *src = static_cast<int32_t *>(checked(sv, at::kInt, "src_row"));
+    const int32_t *dst = sized<int32_t>(a, at::kInt, "dst_row", sv.numel());
+    Table t = table_of(a);
+    void *kc = cache_of(a, g, "k_cache", &t.num_pages), *vc = cache_of(a, g, "v_cache", &t.num_pages);
+    int32_t *res = sized<int32_t>(a, at::kInt, "result", sv.numel());
+    const int32_t reserve = a.i32(), lb = a.i32(), le = a.i32();
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_page_fork(&g.g, (int32_t)sv.numel(), src, dst, reserve, (int32_t)t.rows, t.ctx,
+                           t.table, (int32_t)t.max_pages, t.num_pages, t.refs, kc, vc, lb, le, res, s);
+    });
+  });
+}
+
+PyObject *page_compact(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    Geom g(a.next());
+    const View rv = view_of(a.next(), "row");
+    const int32_t *row = static_cast<int32_t *>(checked(rv, at::kInt, "row"));
+    const int64_t m = rv.numel();
+    const View kv = view_of(a.next(), "keep");
+    const int32_t *keep = static_cast<int32_t *>(checked(kv, at::kInt, "keep"));
+    const int64_t max_keep = second(kv, "keep");
+    if (kv.size(0) != m) raise(PyExc_ValueError, "%s must have a list per row%s", "keep");
+    const int32_t *keep_len = sized<int32_t>(a, at::kInt, "keep_len", m);
+    Table t = table_of(a);
+    void *kc = cache_of(a, g, "k_cache", &t.num_pages), *vc = cache_of(a, g, "v_cache", &t.num_pages);
+    int32_t *res = sized<int32_t>(a, at::kInt, "result", m);
+    const int32_t *start = sized<int32_t>(a, at::kInt, "start", m, true);
+    const int32_t reserve = a.i32(), rotate = a.i32(), lb = a.i32(), le = a.i32();
+    const View wv = view_of(a.next(), "workspace");
+    void *ws = checked(wv, at::kByte, "workspace", true);
+    const size_t bytes = wv ? (size_t)wv.numel() : 0;
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_page_compact(&g.g, (int32_t)m, row, start, keep, (int32_t)max_keep, keep_len, reserve,
+                              rotate, (int32_t)t.rows, t.ctx, t.table, (int32_t)t.max_pages,
+                              t.num_pages, t.refs, kc, vc, lb, le, res, ws, bytes, s);
+    });
+  });
+}
+
+PyObject *page_free(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    const View rv = view_of(a.next(), "row");
+    const int32_t *row = static_cast<int32_t *>(checked(rv, at::kInt, "row"));
+    const Table t = table_of(a);
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_page_free((int32_t)rv.numel(), row, (int32_t)t.rows, t.ctx, t.table,
+                           (int32_t)t.max_pages, t.num_pages, t.refs, s);
+    });
+  });
+}
+
+PyObject *page_copy(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    Geom g(a.next());
+    const View sv = view_of(a.next(), "src_page");
+    const int32_t *src = static_cast<int32_t *>(checked(sv, at::kInt, "src_page"));
+    const int32_t *dst = sized<int32_t>(a, at::kInt, "dst_page", sv.numel());
+    int64_t sp = -1, dp = -1;
+    const void *ks = cache_of(a, g, "k_src", &sp), *vs = cache_of(a, g, "v_src", &sp);
+    void *kd = cache_of(a, g, "k_dst", &dp), *vd = cache_of(a, g, "v_dst", &dp);
+    const int32_t lb = a.i32(), le = a.i32();
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_page_copy(&g.g, (int32_t)sv.numel(), src, dst, ks, vs, sp, kd, vd, dp, lb, le, s);
+    });
+  });
+}
+
 #define FAST(name, fn) {name, (PyCFunction)(void (*)(void))(fn), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     FAST("compose", compose),
@@ -627,6 +839,13 @@ PyMethodDef methods[] = {
     FAST("copy_async", copy_async),
     FAST("copy_range", copy_range),
     FAST("attention_deviation", attention_deviation),
+    FAST("attend_draft", attend_draft),
+    FAST("verify_draft", verify_draft),
+    FAST("page_reserve", page_reserve),
+    FAST("page_fork", page_fork),
+    FAST("page_compact", page_compact),
+    FAST("page_free", page_free),
+    FAST("page_copy", page_copy),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pic_native", nullptr, -1, methods,

@@ -158,6 +158,22 @@ PIC_DEV float2 rope_cos_sin_fast(long long pos, double theta) {
   return make_float2(c, s);
 }
 
+// The angle as a fraction of a turn, in whole numbers: 2^64 times the turns per
+// position, so that pos * turn mod 2^64 is the reduced angle exactly (up to
+// theta / 2 pi's own rounding in fp64, 2^-53 of a turn per position) without
+// any fp64 work per angle, of which an SM does about two operations a clock.
+PIC_DEV uint64_t rope_turn(double theta) {
+  double t = theta * (1.0 / 6.283185307179586476925286766559);
+  t -= floor(t);
+  return (uint64_t)__double2ull_rz(t * 18446744073709551616.0);
+}
+PIC_DEV float2 rope_cos_sin_turn(int pos, uint64_t turn) {
+  const int32_t hi = (int32_t)(((uint64_t)(int64_t)pos * turn) >> 32);
+  float s, c;
+  sincospif((float)hi * 4.656612873077392578125e-10f, &s, &c);  // hi / 2^31 half turns
+  return make_float2(c, s);
+}
+
 // Frequency i of layer `layer`: the per-layer table when the geometry has
 // one, else the table shared by all layers.
 PIC_DEV double rope_theta(const RopeParams &rp, int layer, int i) {

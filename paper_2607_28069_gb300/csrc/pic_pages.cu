@@ -1,0 +1,767 @@
+// pic_page_reserve, pic_page_fork, pic_page_compact, pic_page_free and
+// pic_page_copy: the pages of a cache while its contexts branch, grow and
+// shrink.
+//
+// The state is the block table (which pages a row uses, in logical order) and
+// one count per page (how many rows use it; 0 = free).  There is no list of free
+// pages: an allocation scans the counts and takes the lowest free numbers in the
+// order of the call, so the result depends on the state alone and a page may be
+// given back by any number of CTAs in any order.
+//
+// All data movement is HBM-bound: each byte is read once and written once, in
+// 16-byte pieces with several loads of a thread in flight.
+#include <algorithm>
+
+#include "pic_internal.cuh"
+
+namespace pic {
+namespace pages {
+
+constexpr int kPage = 16;
+constexpr int kMaxRows = 4096;  // rows a call may list
+
+// Bounded spin on a flag that another CTA of this launch sets (ld.acquire).
+PIC_DEV int ld_acquire(const int32_t *p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+PIC_DEV bool wait_flag(const int32_t *flag, int32_t *status, int detail) {
+  if (ld_acquire(flag)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t i = 1;; ++i) {
+    if (ld_acquire(flag)) return true;
+    if ((i & 63u) == 0 && globaltimer_ns() - t0 > kWaitLimitNs) {
+      dev_fail(status, PIC_DEV_TIMEOUT, detail);
+      return false;
+    }
+  }
+}
+
+// ------------------------------------------------------------- allocation
+struct PlanParams {
+  int n, rows, max_pages, extra;
+  long long num_pages;
+  const int32_t *row, *src_row;  // src_row: fork
+  int32_t *ctx_len, *block_table, *page_refs, *result;
+  int32_t *status;
+};
+
+constexpr int kPlanThreads = 1024;
+
+// Exclusive prefix sum over the block; *total gets the sum.
+PIC_DEV int block_scan(int v, int *warp_sums, int *total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) warp_sums[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    int s = lane < kPlanThreads / 32 ? warp_sums[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += y;
+    }
+    warp_sums[lane] = s;
+  }
+  __syncthreads();
+  *total = warp_sums[kPlanThreads / 32 - 1];
+  const int before = warp ? warp_sums[warp - 1] : 0;
+  __syncthreads();  // warp_sums may be written again
+  return before + x - v;
+}
+
+// One CTA: what each listed row needs, then the free pages in ascending order,
+// the k-th of them to the row whose range of the needs' prefix sum holds k.
+template <bool kFork>
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
+  pdl_entry();
+  extern __shared__ int32_t sh[];
+  int32_t *first = sh, *col0 = sh + p.n + 1, *len_of = col0 + p.n;  // len_of: fork
+  __shared__ int warp_sums[32];
+  const int tid = threadIdx.x;
+  int carry = 0;
+  for (int j0 = 0; j0 < p.n; j0 += kPlanThreads) {
+    const int j = j0 + tid;
+    int need = 0, at = 0, res = -1, len = -1;
+    if (j < p.n) {
+      const int r = p.row[j];  // the row that gets the pages
+      const int a = kFork ? p.src_row[j] : r;
+      int code = PIC_DEV_OK;
+      if (r < 0 || r >= p.rows || a < 0 || a >= p.rows || (kFork && a == r)) {
+        code = PIC_DEV_BAD_REQUEST;
+      } else {
+        const int32_t *ta = p.block_table + (size_t)a * p.max_pages;
+        const int32_t *tr = p.block_table + (size_t)r * p.max_pages;
+        len = p.ctx_len[a];
+        const long long want = ((long long)len + p.extra + kPage - 1) / kPage;
+        if (len < 0 || (kFork && tr[0] >= 0)) {
+          code = PIC_DEV_BAD_REQUEST;
+        } else if (want > p.max_pages) {
+          code = PIC_DEV_BLOCK_TABLE_SHORT;
+        } else if constexpr (kFork) {
+          at = len / kPage;
+          need = (int)want - at;
+          res = len;
+          if (len % kPage && (ta[at] < 0 || ta[at] >= p.num_pages)) code = PIC_DEV_BAD_PAGE;
+        } else {
+          int lo = (len + kPage - 1) / kPage, hi = (int)want;  // the first entry without a page
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (tr[mid] >= 0) lo = mid + 1;
+            else hi = mid;
+          }
+          at = lo;
+          need = max(0, (int)want - lo);
+          res = (int)want;
+        }
+      }
+      if (code != PIC_DEV_OK) {
+        dev_fail(p.status, code, j);
+        need = 0, res = -1;
+      }
+    }
+    int total;
+    const int before = block_scan(need, warp_sums, &total);
+    if (j < p.n) {
+      first[j] = carry + before;
+      col0[j] = at;
+      if constexpr (kFork) len_of[j] = res;
+      else p.result[j] = res;
+    }
+    carry += total;
+  }
+  if (tid == 0) first[p.n] = carry;
+  __syncthreads();
+  const int want_all = carry;
+
+  int found = 0;
+  for (long long base = 0; base < p.num_pages && found < want_all; base += 4 * kPlanThreads) {
+    const long long pg = base + 4 * tid;
+    int32_t c[4];
+    if (pg + 3 < p.num_pages && (reinterpret_cast<uintptr_t>(p.page_refs) & 15) == 0) {
+      const int4 v = *reinterpret_cast<const int4 *>(p.page_refs + pg);
+      c[0] = v.x, c[1] = v.y, c[2] = v.z, c[3] = v.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = pg + i < p.num_pages ? p.page_refs[pg + i] : 1;
+    }
+    int mine = 0, total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine += c[i] == 0;
+    int k = found + block_scan(mine, warp_sums, &total);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c[i] == 0) {
+        if (k < want_all) {
+          int lo = 0, hi = p.n;  // the last row with first <= k
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first[mid] <= k) lo = mid;
+            else hi = mid;
+          }
+          p.block_table[(size_t)p.row[lo] * p.max_pages + col0[lo] + (k - first[lo])] = (int32_t)(pg + i);
+          p.page_refs[pg + i] = 1;
+        }
+        ++k;
+      }
+    found += total;
+  }
+  found = min(found, want_all);
+  __syncthreads();
+  // rows beyond the free pages are refused, what one of them got goes back
+  for (int j = tid; j < p.n; j += kPlanThreads) {
+    const bool served = first[j + 1] <= found || first[j + 1] == first[j];
+    if (!served) {
+      dev_fail(p.status, PIC_DEV_NO_FREE_PAGE, j);
+      int32_t *t = p.block_table + (size_t)p.row[j] * p.max_pages + col0[j];
+      for (int k = first[j]; k < found; ++k) {
+        p.page_refs[t[k - first[j]]] = 0;
+        t[k - first[j]] = -1;
+      }
+    }
+    if constexpr (kFork) {
+      const int res = served ? len_of[j] : -1;
+      p.result[j] = res;
+      if (res >= 0) p.ctx_len[p.row[j]] = res;
+    } else if (!served) {
+      p.result[j] = -1;
+    }
+  }
+}
+
+// ------------------------------------------------------------------- fork
+struct ForkParams {
+  int n, max_pages, hkv, piece_row, layers, table_blocks;  // piece_row: 16-byte pieces of a row
+  long long num_pages, layer_pieces;
+  const int32_t *src_row, *dst_row, *result;
+  int32_t *block_table, *page_refs;
+  uint4 *k, *v;  // at layer_begin
+  int32_t *status;
+};
+
+// After the plan: blocks [0, table_blocks) enter the shared pages into the
+// branches' rows and count their new users, one thread per entry; the others
+// copy the valid rows of each context's last page, one warp per (branch, layer,
+// kv head), K and V, up to 16 16-byte loads of a lane in flight.
+__global__ void __launch_bounds__(256) fork_kernel(ForkParams p) {
+  pdl_entry();
+  if ((int)blockIdx.x < p.table_blocks) {
+    const int per = (p.max_pages + 255) / 256;
+    const int j = (int)blockIdx.x / per, e = ((int)blockIdx.x % per) * 256 + (int)threadIdx.x;
+    const int len = p.result[j];
+    if (len < 0 || e >= len / kPage) return;
+    const int page = p.block_table[(size_t)p.src_row[j] * p.max_pages + e];
+    if (page < 0 || page >= p.num_pages) {
+      dev_fail(p.status, PIC_DEV_BAD_PAGE, j);
+      return;
+    }
+    atomicAdd(p.page_refs + page, 1);
+    p.block_table[(size_t)p.dst_row[j] * p.max_pages + e] = page;
+    return;
+  }
+  const int lane = threadIdx.x & 31;
+  const long long w = ((long long)blockIdx.x - p.table_blocks) * 8 + (threadIdx.x >> 5);
+  const int j = (int)(w / ((long long)p.layers * p.hkv));
+  if (j >= p.n) return;
+  const int len = p.result[j], full = len / kPage, rows = len % kPage;
+  if (len < 0 || rows == 0) return;
+  const int rem = (int)(w % ((long long)p.layers * p.hkv)), l = rem / p.hkv, h = rem % p.hkv;
+  const int from = p.block_table[(size_t)p.src_row[j] * p.max_pages + full];
+  const int to = p.block_table[(size_t)p.dst_row[j] * p.max_pages + full];
+  const int pieces = rows * p.piece_row;  // at most 16 * 16
+  const long long layer = (long long)l * p.layer_pieces;
+  const long long a = layer + ((long long)from * p.hkv + h) * kPage * p.piece_row;
+  const long long z = layer + ((long long)to * p.hkv + h) * kPage * p.piece_row;
+  uint4 x[8], y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (lane + 32 * i < pieces) {
+      x[i] = p.k[a + lane + 32 * i];
+      y[i] = p.v[a + lane + 32 * i];
+    }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (lane + 32 * i < pieces) {
+      p.k[z + lane + 32 * i] = x[i];
+      p.v[z + lane + 32 * i] = y[i];
+    }
+}
+
+// ------------------------------------------------------------------- free
+struct FreeParams {
+  int n, rows, max_pages;
+  long long num_pages;
+  const int32_t *row;
+  const int32_t *result;  // compact: the rows' new lengths (-1: refused); null: free
+  int reserve;
+  int32_t *ctx_len, *block_table, *page_refs, *status;
+};
+
+// One CTA per listed row: the entries from the cut on are taken out one by
+// one (an exchange, so that a page goes back once whatever the call lists) and
+// their pages lose a user.  A row's entries are contiguous: the first 256 without
+// any page end the walk.
+__global__ void __launch_bounds__(256) release_kernel(FreeParams p) {
+  pdl_entry();
+  const int j = blockIdx.x, r = p.row[j];
+  int cut = 0;
+  if (p.result) {
+    const int len = p.result[j];
+    if (len < 0) return;
+    cut = (int)min((long long)p.max_pages, ((long long)len + p.reserve + kPage - 1) / kPage);
+    if (threadIdx.x == 0) p.ctx_len[r] = len;
+  } else {
+    if (r < 0 || r >= p.rows) {
+      if (threadIdx.x == 0) dev_fail(p.status, PIC_DEV_BAD_REQUEST, j);
+      return;
+    }
+    if (threadIdx.x == 0) p.ctx_len[r] = 0;
+  }
+  int32_t *t = p.block_table + (size_t)r * p.max_pages;
+  for (int e0 = cut; e0 < p.max_pages; e0 += 256) {
+    const int e = e0 + (int)threadIdx.x;
+    const int page = e < p.max_pages ? atomicExch(t + e, -1) : -1;
+    if (page >= p.num_pages) {
+      dev_fail(p.status, PIC_DEV_BAD_PAGE, j);
+    } else if (page >= 0 && atomicSub(p.page_refs + page, 1) <= 0) {
+      atomicAdd(p.page_refs + page, 1);  // nobody used it
+      dev_fail(p.status, PIC_DEV_BAD_PAGE, j);
+    }
+    if (!__syncthreads_or(page >= 0)) break;
+  }
+}
+
+// ---------------------------------------------------------------- compact
+constexpr int kSeg = 16;      // kept positions per CTA
+constexpr int kUnits = 8;     // 32-byte units of a thread
+constexpr int kMoveThreads = 256;
+
+struct CompactParams {
+  int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, layers, layer_begin, rotate;
+  long long num_pages, layer_elems;
+  const int32_t *row, *start, *keep, *keep_len;
+  const int32_t *ctx_len, *block_table, *page_refs;
+  int32_t *result;
+  __nv_bfloat16 *k, *v;  // at layer_begin
+  int32_t *flags;        // [0] ticket, then [n][layers * hgroups][segs]: "reads done"; null: one segment
+  int32_t *status;
+};
+
+// One CTA per listed row: every check of its list, before anything moves; the
+// verdict goes to result.  Clears the row's flags.
+__global__ void __launch_bounds__(256) compact_check_kernel(CompactParams p) {
+  pdl_entry();
+  const int j = blockIdx.x, tid = threadIdx.x;
+  if (p.flags) {
+    const long long per = (long long)p.layers * p.hgroups * p.segs;
+    for (long long i = tid; i < per; i += 256) p.flags[1 + j * per + i] = 0;
+    if (j == 0 && tid == 0) p.flags[0] = 0;
+  }
+  const int r = p.row[j], m = p.keep_len[j];
+  int code = PIC_DEV_OK, s = 0;
+  if (r < 0 || r >= p.rows || m < 0 || m > p.max_keep) {
+    code = PIC_DEV_BAD_REQUEST;
+  } else {
+    s = p.start ? p.start[j] : p.ctx_len[r];
+    if (s < 0 || (long long)s + m > (long long)p.max_pages * kPage)
+      code = s < 0 ? PIC_DEV_BAD_REQUEST : PIC_DEV_BLOCK_TABLE_SHORT;
+  }
+  if (code == PIC_DEV_OK) {
+    const int32_t *t = p.block_table + (size_t)r * p.max_pages;
+    const int32_t *kp = p.keep + (size_t)j * p.max_keep;
+    for (int i = tid; i < m; i += 256) {
+      const int k = kp[i];
+      if (k < i || (i > 0 && kp[i - 1] >= k)) {  // ascending from >= 0 on: never below i
+        code = PIC_DEV_BAD_POSITION;
+        break;
+      }
+      const long long from = (long long)s + k, to = (long long)s + i;
+      if (from >= (long long)p.max_pages * kPage) {
+        code = PIC_DEV_BLOCK_TABLE_SHORT;
+        break;
+      }
+      const int a = t[from / kPage], z = t[to / kPage];
+      if (a < 0 || a >= p.num_pages || z < 0 || z >= p.num_pages) {
+        code = PIC_DEV_BAD_PAGE;
+        break;
+      }
+      if (k != i && p.page_refs[z] != 1) {
+        code = PIC_DEV_SHARED_PAGE;
+        break;
+      }
+    }
+  }
+  if (code != PIC_DEV_OK) dev_fail(p.status, code, j);
+  const bool bad = __syncthreads_or(code != PIC_DEV_OK);
+  if (tid == 0) p.result[j] = bad ? -1 : s + m;
+}
+
+// One CTA = 16 kept positions x a group of kv heads x a layer of one row: it
+// reads them all into registers, says so, waits for the CTAs whose sources lie
+// in what it overwrites, and stores.  keep is ascending, so those are CTAs of
+// earlier segments of the same (row, layer, head group) only; a CTA's segment
+// comes from a ticket, so they have started before it, and they read before they
+// wait: every wait ends.  Keys move by i - keep[i] positions and are re-rotated
+// by that, with cos/sin of the 16 moves formed once per CTA.
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads) compact_move_kernel(CompactParams p, RopeParams rp) {
+  constexpr int KC = D / 16;  // 8-pair chunks of a row
+  pdl_entry();
+  __shared__ float2 cs[kSeg][D / 2];
+  __shared__ int32_t k_of[kSeg];
+  __shared__ long long from_of[kSeg], to_of[kSeg];  // page * hkv * 16 + row
+  __shared__ int ticket;
+  const int tid = threadIdx.x;
+  long long at = blockIdx.x;
+  if (p.flags) {
+    if (tid == 0) ticket = atomicAdd(p.flags, 1);
+    __syncthreads();
+    at = ticket;
+  }
+  const int lh = (int)(at % (p.layers * p.hgroups));
+  at /= p.layers * p.hgroups;
+  const int j = (int)(at % p.n), seg = (int)(at / p.n);
+  const int layer = lh / p.hgroups, h0 = (lh % p.hgroups) * p.hgroup;
+  const int heads = min(p.hgroup, p.hkv - h0);
+  const int res = p.result[j];
+  if (res < 0) return;
+  const int m = p.keep_len[j], i0 = seg * kSeg, cnt = min(kSeg, m - i0);
+  if (cnt <= 0) return;
+  const int32_t *kp = p.keep + (size_t)j * p.max_keep;
+  if (tid < cnt) {
+    const int s = res - m, i = i0 + tid, k = kp[i];
+    const int32_t *t = p.block_table + (size_t)p.row[j] * p.max_pages;
+    k_of[tid] = k;
+    from_of[tid] = (long long)t[(s + k) / kPage] * p.hkv * kPage + (s + k) % kPage;
+    to_of[tid] = (long long)t[(s + i) / kPage] * p.hkv * kPage + (s + i) % kPage;
+  }
+  __syncthreads();
+
+  // ---- read: unit u = (position, K or V, head, chunk)
+  const long long lbase = (long long)layer * p.layer_elems;
+  const int units = cnt * 2 * heads * KC;
+  const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
+  uint4 a[kUnits], b[kUnits];
+#pragma unroll
+  for (int q = 0; q < kUnits; ++q) {
+    const int u = tid + q * kMoveThreads;
+    if (u < units) {
+      const int h = (u / KC) % heads, kv = (u / (KC * heads)) & 1, i = u / (KC * heads * 2);
+      if (k_of[i] != i0 + i) {
+        const __nv_bfloat16 *src =
+            (kv ? p.v : p.k) + lbase + (from_of[i] + (long long)(h0 + h) * kPage) * D;
+        a[q] = *reinterpret_cast<const uint4 *>(src + pc.off_a);
+        b[q] = *reinterpret_cast<const uint4 *>(src + pc.off_b);
+      }
+    }
+  }
+  if (p.rotate)
+    for (int e = tid; e < cnt * (D / 2); e += kMoveThreads) {
+      const int i = e / (D / 2), f = e % (D / 2);
+      cs[i][f] = rope_cos_sin_turn(i0 + i - k_of[i],
+                                   rope_turn(rope_theta(rp, p.layer_begin + layer, f)));
+    }
+  if (p.flags) {
+    int32_t *fl = p.flags + 1 + ((long long)j * p.layers * p.hgroups + lh) * p.segs;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) atomicExch(fl + seg, 1);
+    // segment s2 < seg reads up to keep[16 (s2 + 1) - 1], this one writes from i0 on
+    bool ok = true;
+    for (int s2 = seg - 1 - tid; ok && s2 >= 0 && kp[(s2 + 1) * kSeg - 1] >= i0; s2 -= kMoveThreads)
+      ok = wait_flag(fl + s2, p.status, j);
+    if (__syncthreads_or(!ok)) return;
+  } else {
+    __syncthreads();
+  }
+  // ---- store
+#pragma unroll
+  for (int q = 0; q < kUnits; ++q) {
+    const int u = tid + q * kMoveThreads;
+    if (u < units) {
+      const int h = (u / KC) % heads, kv = (u / (KC * heads)) & 1, i = u / (KC * heads * 2);
+      if (k_of[i] != i0 + i) {
+        __nv_bfloat16 *dst =
+            (kv ? p.v : p.k) + lbase + (to_of[i] + (long long)(h0 + h) * kPage) * D;
+        if (p.rotate && !kv) {
+          rotate_store(a[q], b[q], dst, pc, rp.style, &cs[i][8 * (tid % KC)]);
+        } else {
+          st_global16(dst + pc.off_a, a[q]);
+          st_global16(dst + pc.off_b, b[q]);
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------- copy
+struct CopyParams {
+  int n, layers, pieces_page;  // 2 KB pieces of a page of one layer
+  long long src_pages, dst_pages, total;  // total: pieces in all
+  const int32_t *src_page, *dst_page;
+  const uint4 *ks, *vs;
+  uint4 *kd, *vd;  // all at layer_begin
+  int32_t *status;
+};
+
+constexpr int kCopyPieces = 4;  // pieces of a warp (8 KB)
+
+// A page of a layer is contiguous: a warp moves four consecutive 2 KB pieces,
+// all 16 16-byte loads of a lane before its stores.
+__global__ void __launch_bounds__(256) copy_kernel(CopyParams p) {
+  pdl_entry();
+  const int lane = threadIdx.x & 31;
+  const long long w0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kCopyPieces;
+  uint4 x[kCopyPieces][4];
+  uint4 *to[kCopyPieces];
+#pragma unroll
+  for (int i = 0; i < kCopyPieces; ++i) {
+    to[i] = nullptr;
+    const long long w = w0 + i;
+    if (w >= p.total) continue;
+    const int piece = (int)(w % p.pieces_page);
+    const long long item = w / p.pieces_page;  // ((pair * layers) + layer) * 2 + kv
+    const int kv = (int)(item & 1), layer = (int)((item >> 1) % p.layers);
+    const int pair = (int)((item >> 1) / p.layers);
+    const int s = p.src_page[pair], d = p.dst_page[pair];
+    if (s < 0 || s >= p.src_pages || d < 0 || d >= p.dst_pages) {
+      if (piece == 0 && (item % (2 * p.layers)) == 0 && lane == 0 && !(s == -1 && d == -1))
+        dev_fail(p.status, PIC_DEV_BAD_PAGE, pair);
+      continue;
+    }
+    const long long from = (((long long)layer * p.src_pages + s) * p.pieces_page + piece) * 128;
+    const uint4 *src = (kv ? p.vs : p.ks) + from + lane;
+    to[i] = (kv ? p.vd : p.kd) +
+            (((long long)layer * p.dst_pages + d) * p.pieces_page + piece) * 128 + lane;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[i][q] = src[q * 32];
+  }
+#pragma unroll
+  for (int i = 0; i < kCopyPieces; ++i)
+    if (to[i])
+#pragma unroll
+      for (int q = 0; q < 4; ++q) st_global16(to[i] + q * 32, x[i][q]);
+}
+
+// ------------------------------------------------------------------- host
+static pic_status_t check_table(const char *who, int32_t n, const int32_t *row, int32_t rows,
+                                const int32_t *ctx_len, const int32_t *block_table,
+                                int32_t max_pages, int64_t num_pages, const int32_t *page_refs) {
+  if (n < 0 || n > kMaxRows)
+    return fail(n < 0 ? PIC_ERR_INVALID_ARG : PIC_ERR_UNSUPPORTED, "%s: %d rows (at most %d)", who,
+                n, kMaxRows);
+  if (rows <= 0 || max_pages <= 0 || num_pages <= 0)
+    return fail(PIC_ERR_INVALID_ARG, "%s: sizes must be positive", who);
+  if (num_pages > INT32_MAX || max_pages > INT32_MAX / kPage ||
+      (long long)n * max_pages > INT32_MAX)
+    return fail(PIC_ERR_UNSUPPORTED, "%s: page numbers or positions beyond 32 bits", who);
+  if (n && (!row || !ctx_len || !block_table || !page_refs))
+    return fail(PIC_ERR_INVALID_ARG, "%s: NULL tensor", who);
+  return PIC_OK;
+}
+
+static pic_status_t check_cache(const char *who, const pic_geom_t *geom, RopeParams *rp,
+                                const void *k, const void *v, int32_t layer_begin,
+                                int32_t layer_end) {
+  pic_status_t st = make_rope(geom, rp);
+  if (st != PIC_OK) return st;
+  if (layer_begin < 0 || layer_end > geom->num_layers || layer_begin > layer_end)
+    return fail(PIC_ERR_INVALID_ARG, "%s: layers [%d, %d) outside [0, %d)", who, layer_begin,
+                layer_end, geom->num_layers);
+  if (!k || !v) return fail(PIC_ERR_INVALID_ARG, "%s: NULL tensor", who);
+  if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15)
+    return fail(PIC_ERR_INVALID_ARG, "%s: bf16 tensors must be 16-byte aligned", who);
+  return PIC_OK;
+}
+
+static pic_status_t launched(const char *who, cudaError_t e) {
+  if (e == cudaSuccess) e = cudaGetLastError();
+  return e == cudaSuccess ? PIC_OK : cuda_fail(e, who);
+}
+
+template <bool kFork>
+static cudaError_t launch_plan(const PlanParams &pp, pic_stream_t stream) {
+  const size_t smem = (size_t)(pp.n + 1 + pp.n * (kFork ? 2 : 1)) * 4;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(plan_kernel<kFork>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_dependent(plan_kernel<kFork>, dim3(1), dim3(kPlanThreads), smem, stream, pp);
+}
+
+// Head groups of a compaction: as many heads as 16 positions of a CTA hold.
+static int heads_per_group(const pic_geom_t *g) {
+  return kMoveThreads * kUnits / (kSeg * 2 * (g->head_dim / 16));
+}
+static size_t flag_bytes(const pic_geom_t *g, int n, int max_keep, int layers) {
+  const int hg = heads_per_group(g);
+  const size_t groups = (size_t)(g->num_kv_heads + hg - 1) / hg;
+  const size_t segs = ((size_t)max_keep + kSeg - 1) / kSeg;
+  return segs <= 1 ? 0 : (1 + (size_t)n * layers * groups * segs) * 4;
+}
+
+}  // namespace pages
+}  // namespace pic
+
+extern "C" pic_status_t pic_page_reserve(int32_t n, const int32_t *row, int32_t extra, int32_t rows,
+                                         const int32_t *ctx_len, int32_t *block_table,
+                                         int32_t max_pages, int64_t num_pages, int32_t *page_refs,
+                                         int32_t *result, pic_stream_t stream) {
+  using namespace pic;
+  using namespace pic::pages;
+  static const char *who = "pic_page_reserve";
+  pic_status_t st = check_table(who, n, row, rows, ctx_len, block_table, max_pages, num_pages, page_refs);
+  if (st != PIC_OK) return st;
+  if (extra < 0) return fail(PIC_ERR_INVALID_ARG, "%s: extra %d is negative", who, extra);
+  if (n == 0) return PIC_OK;
+  if (!result) return fail(PIC_ERR_INVALID_ARG, "%s: NULL tensor", who);
+  PlanParams pp{n, rows, max_pages, extra, num_pages, row, nullptr, const_cast<int32_t *>(ctx_len),
+                block_table, page_refs, result, device_status_ptr()};
+  if (!pp.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
+  return launched(who, launch_plan<false>(pp, stream));
+}
+
+extern "C" pic_status_t pic_page_fork(const pic_geom_t *geom, int32_t n, const int32_t *src_row,
+                                      const int32_t *dst_row, int32_t reserve, int32_t rows,
+                                      int32_t *ctx_len, int32_t *block_table, int32_t max_pages,
+                                      int64_t num_pages, int32_t *page_refs, void *k_cache,
+                                      void *v_cache, int32_t layer_begin, int32_t layer_end,
+                                      int32_t *result, pic_stream_t stream) {
+  using namespace pic;
+  using namespace pic::pages;
+  static const char *who = "pic_page_fork";
+  RopeParams rp;
+  pic_status_t st = check_cache(who, geom, &rp, k_cache, v_cache, layer_begin, layer_end);
+  if (st == PIC_OK)
+    st = check_table(who, n, dst_row, rows, ctx_len, block_table, max_pages, num_pages, page_refs);
+  if (st != PIC_OK) return st;
+  if (reserve < 0) return fail(PIC_ERR_INVALID_ARG, "%s: reserve %d is negative", who, reserve);
+  if (n == 0) return PIC_OK;
+  if (!src_row || !result) return fail(PIC_ERR_INVALID_ARG, "%s: NULL tensor", who);
+  int32_t *status = device_status_ptr();
+  if (!status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
+  PlanParams pp{n, rows, max_pages, reserve, num_pages, dst_row, src_row, ctx_len, block_table,
+                page_refs, result, status};
+  cudaError_t e = launch_plan<true>(pp, stream);
+  if (e != cudaSuccess) return cuda_fail(e, who);
+  ForkParams fp;
+  fp.n = n;
+  fp.max_pages = max_pages;
+  fp.hkv = geom->num_kv_heads;
+  fp.piece_row = geom->head_dim * 2 / 16;
+  fp.layers = layer_end - layer_begin;
+  const long long table_blocks = (long long)n * ((max_pages + 255) / 256);
+  const long long copy_blocks = ((long long)n * fp.layers * fp.hkv + 7) / 8;
+  if (table_blocks + copy_blocks > INT32_MAX)
+    return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
+  fp.table_blocks = (int)table_blocks;
+  fp.num_pages = num_pages;
+  fp.layer_pieces = (long long)num_pages * fp.hkv * kPage * fp.piece_row;
+  fp.src_row = src_row;
+  fp.dst_row = dst_row;
+  fp.result = result;
+  fp.block_table = block_table;
+  fp.page_refs = page_refs;
+  fp.k = static_cast<uint4 *>(k_cache) + layer_begin * fp.layer_pieces;
+  fp.v = static_cast<uint4 *>(v_cache) + layer_begin * fp.layer_pieces;
+  fp.status = status;
+  return launched(who, launch_dependent(fork_kernel, dim3((unsigned)(table_blocks + copy_blocks)),
+                                        dim3(256), 0, stream, fp));
+}
+
+extern "C" size_t pic_page_compact_workspace_size(const pic_geom_t *geom, int32_t n,
+                                                  int32_t max_keep) {
+  if (!geom || n <= 0 || max_keep <= 0 || geom->num_layers <= 0 || geom->num_kv_heads <= 0 ||
+      (geom->head_dim != 64 && geom->head_dim != 128))
+    return 0;
+  return pic::pages::flag_bytes(geom, n, max_keep, geom->num_layers);
+}
+
+extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, const int32_t *row,
+                                         const int32_t *start, const int32_t *keep,
+                                         int32_t max_keep, const int32_t *keep_len,
+                                         int32_t reserve, int32_t rotate, int32_t rows,
+                                         int32_t *ctx_len, int32_t *block_table, int32_t max_pages,
+                                         int64_t num_pages, int32_t *page_refs, void *k_cache,
+                                         void *v_cache, int32_t layer_begin, int32_t layer_end,
+                                         int32_t *result, void *workspace, size_t workspace_bytes,
+                                         pic_stream_t stream) {
+  using namespace pic;
+  using namespace pic::pages;
+  static const char *who = "pic_page_compact";
+  RopeParams rp;
+  pic_status_t st = check_cache(who, geom, &rp, k_cache, v_cache, layer_begin, layer_end);
+  if (st == PIC_OK)
+    st = check_table(who, n, row, rows, ctx_len, block_table, max_pages, num_pages, page_refs);
+  if (st != PIC_OK) return st;
+  if (reserve < 0 || max_keep <= 0)
+    return fail(PIC_ERR_INVALID_ARG, "%s: reserve %d, max_keep %d", who, reserve, max_keep);
+  if (n == 0) return PIC_OK;
+  if (!keep || !keep_len || !result) return fail(PIC_ERR_INVALID_ARG, "%s: NULL tensor", who);
+  CompactParams cp;
+  cp.n = n;
+  cp.rows = rows;
+  cp.max_pages = max_pages;
+  cp.max_keep = max_keep;
+  cp.segs = (max_keep + kSeg - 1) / kSeg;
+  cp.hkv = geom->num_kv_heads;
+  cp.hgroup = std::min(heads_per_group(geom), cp.hkv);
+  cp.hgroups = (cp.hkv + cp.hgroup - 1) / cp.hgroup;
+  cp.layers = layer_end - layer_begin;
+  cp.layer_begin = layer_begin;
+  cp.rotate = rotate != 0;
+  cp.num_pages = num_pages;
+  cp.layer_elems = (long long)num_pages * cp.hkv * kPage * geom->head_dim;
+  cp.row = row;
+  cp.start = start;
+  cp.keep = keep;
+  cp.keep_len = keep_len;
+  cp.ctx_len = ctx_len;
+  cp.block_table = block_table;
+  cp.page_refs = page_refs;
+  cp.result = result;
+  cp.k = static_cast<__nv_bfloat16 *>(k_cache) + layer_begin * cp.layer_elems;
+  cp.v = static_cast<__nv_bfloat16 *>(v_cache) + layer_begin * cp.layer_elems;
+  cp.flags = nullptr;
+  const size_t bytes = flag_bytes(geom, n, max_keep, cp.layers);
+  if (bytes) {
+    if (!workspace || workspace_bytes < bytes || (reinterpret_cast<uintptr_t>(workspace) & 255))
+      return fail(PIC_ERR_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", who, bytes);
+    cp.flags = static_cast<int32_t *>(workspace);
+  }
+  const long long blocks = (long long)n * cp.layers * cp.hgroups * cp.segs;
+  if (blocks > INT32_MAX) return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
+  cp.status = device_status_ptr();
+  if (!cp.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
+  cudaError_t e = launch_dependent(compact_check_kernel, dim3(n), dim3(256), 0, stream, cp);
+  if (e == cudaSuccess && blocks > 0)
+    e = geom->head_dim == 128
+            ? launch_dependent(compact_move_kernel<128>, dim3((unsigned)blocks), dim3(kMoveThreads),
+                               0, stream, cp, rp)
+            : launch_dependent(compact_move_kernel<64>, dim3((unsigned)blocks), dim3(kMoveThreads),
+                               0, stream, cp, rp);
+  if (e != cudaSuccess) return cuda_fail(e, who);
+  FreeParams fp{n, rows, max_pages, num_pages, row, result, reserve, ctx_len, block_table, page_refs,
+                cp.status};
+  return launched(who, launch_dependent(release_kernel, dim3(n), dim3(256), 0, stream, fp));
+}
+
+extern "C" pic_status_t pic_page_free(int32_t n, const int32_t *row, int32_t rows, int32_t *ctx_len,
+                                      int32_t *block_table, int32_t max_pages, int64_t num_pages,
+                                      int32_t *page_refs, pic_stream_t stream) {
+  using namespace pic;
+  using namespace pic::pages;
+  static const char *who = "pic_page_free";
+  pic_status_t st = check_table(who, n, row, rows, ctx_len, block_table, max_pages, num_pages, page_refs);
+  if (st != PIC_OK || n == 0) return st;
+  FreeParams fp{n, rows, max_pages, num_pages, row, nullptr, 0, ctx_len, block_table, page_refs,
+                device_status_ptr()};
+  if (!fp.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
+  return launched(who, launch_dependent(release_kernel, dim3(n), dim3(256), 0, stream, fp));
+}
+
+extern "C" pic_status_t pic_page_copy(const pic_geom_t *geom, int32_t n, const int32_t *src_page,
+                                      const int32_t *dst_page, const void *k_src, const void *v_src,
+                                      int64_t src_pages, void *k_dst, void *v_dst,
+                                      int64_t dst_pages, int32_t layer_begin, int32_t layer_end,
+                                      pic_stream_t stream) {
+  using namespace pic;
+  using namespace pic::pages;
+  static const char *who = "pic_page_copy";
+  RopeParams rp;
+  pic_status_t st = check_cache(who, geom, &rp, k_src, v_src, layer_begin, layer_end);
+  if (st == PIC_OK) st = check_cache(who, geom, &rp, k_dst, v_dst, layer_begin, layer_end);
+  if (st != PIC_OK) return st;
+  if (n < 0 || src_pages <= 0 || dst_pages <= 0)
+    return fail(PIC_ERR_INVALID_ARG, "%s: n %d, pages must be positive", who, n);
+  if (n == 0 || layer_begin == layer_end) return PIC_OK;
+  if (!src_page || !dst_page) return fail(PIC_ERR_INVALID_ARG, "%s: NULL tensor", who);
+  CopyParams cp;
+  cp.n = n;
+  cp.layers = layer_end - layer_begin;
+  cp.pieces_page = geom->num_kv_heads * kPage * geom->head_dim * 2 / 2048;
+  cp.src_pages = src_pages;
+  cp.dst_pages = dst_pages;
+  cp.total = (long long)n * cp.layers * 2 * cp.pieces_page;
+  cp.src_page = src_page;
+  cp.dst_page = dst_page;
+  const long long so = (long long)layer_begin * src_pages * cp.pieces_page * 128;
+  const long long to = (long long)layer_begin * dst_pages * cp.pieces_page * 128;
+  cp.ks = static_cast<const uint4 *>(k_src) + so;
+  cp.vs = static_cast<const uint4 *>(v_src) + so;
+  cp.kd = static_cast<uint4 *>(k_dst) + to;
+  cp.vd = static_cast<uint4 *>(v_dst) + to;
+  cp.status = device_status_ptr();
+  if (!cp.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
+  const long long blocks = (cp.total + 8 * kCopyPieces - 1) / (8 * kCopyPieces);
+  if (blocks > INT32_MAX) return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
+  return launched(who, launch_dependent(copy_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, cp));
+}

@@ -1,0 +1,255 @@
+"""pic_attend_draft against a 64-bit softmax over the same bf16 cache, written from
+the formulas: chains and trees, one to 64 tokens, contexts that end at, before and
+behind page and tile edges (0 cached positions too), ragged batches with empty
+requests, GQA groups of 1 to 16 (up to 1024 query rows per kv head), both head
+dims and RoPE styles.  Slots and pages behind the drafts hold NaN.
+
+Bars: keys as in the parity tests (bf16 rounding of an fp32 rotation).  Outputs:
+the weights are rounded to bf16 (2^-9 of each), the output once more (2^-9 of it),
+and a query element now and then rounds the other way than in 64 bits; together
+under 1e-2 of a row, and of 1 + |o| per element.  lse: fp32 scores of bf16 queries,
+2e-3 as in the decode tests."""
+import numpy as np
+import pytest
+import torch
+
+from tests.helpers import attn_close, f64, kv_tolerance_ok
+
+pytestmark = pytest.mark.gpu
+
+
+def rope(x, pos, base, style):
+    d = x.shape[-1]
+    w = np.exp(1j * np.asarray(pos, np.float64)[:, None, None]
+               * base ** (-2.0 * np.arange(d // 2) / d))
+    if style == 0:
+        z = (x[..., :d // 2] + 1j * x[..., d // 2:]) * w
+        return np.concatenate([z.real, z.imag], -1)
+    z = (x[..., 0::2] + 1j * x[..., 1::2]) * w
+    return np.stack([z.real, z.imag], -1).reshape(x.shape)
+
+
+def bf16(x):
+    return torch.as_tensor(x).to(torch.bfloat16).double().numpy()
+
+
+def line_of(par, n):
+    """Ancestors of each token and the token itself."""
+    line = []
+    for i in range(n):
+        line.append((line[par[i]] if par[i] >= 0 else []) + [i])
+    return line
+
+
+def draw(heads, dim, style, ctx, draft, T, tree, layers=2, seed=0, q_scale=1.0, base=5e5):
+    import paper_2607_28069_gb300 as pic
+    hq, hkv = heads
+    B = len(ctx)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rng = np.random.default_rng(seed)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    pages = max(-(-(c + T) // 16) for c in ctx) + 1
+    num = B * pages + 2
+    bt = torch.as_tensor(rng.permutation(num)[:B * pages].reshape(B, pages), dtype=torch.int32)
+    kc, vc = rnd(layers, num, hkv, 16, dim), rnd(layers, num, hkv, 16, dim)
+    # everything that is no cached position of a request is NaN
+    used = torch.zeros((num, 16), dtype=torch.bool)
+    for b, c in enumerate(ctx):
+        t = torch.arange(c)
+        used[bt[b, t // 16].long(), t % 16] = True
+    for cache in (kc, vc):
+        cache.permute(1, 3, 0, 2, 4)[~used.cuda()] = float("nan")
+    par = np.full((B, T), -1, np.int64)
+    for i in range(1, T):
+        par[:, i] = np.maximum(0, i - 1 - rng.integers(0, 4, size=B)) if tree else i - 1
+    if tree and T > 4:
+        par[:, 4] = -1  # a second root
+    dev = lambda x: torch.as_tensor(np.asarray(x), dtype=torch.int32).cuda()  # noqa: E731
+    s = dict(geom=pic.Geometry(layers, hq, hkv, dim, base, rope_style=style), layer=layers - 1,
+             q=rnd(B, T, hq, dim) * q_scale, k=rnd(B, T, hkv, dim), v=rnd(B, T, hkv, dim),
+             ctx=dev(ctx), draft=dev(draft), bt=bt.cuda(), num=num, kc=kc, vc=vc,
+             out=torch.full((B, T, hq, dim), 7.0, dtype=torch.bfloat16, device="cuda"),
+             lse=torch.full((B, T, hq), 7.0, device="cuda"), parent=dev(par) if tree else None,
+             ws=torch.full((pic.pic_draft_workspace_size(pic.Geometry(layers, hq, hkv, dim, base), B,
+                                                         T),), 255, dtype=torch.uint8,
+                           device="cuda"), par=par, base=base, style=style)
+    return s
+
+
+def call(s, **kw):
+    import paper_2607_28069_gb300 as pic
+    a = dict(parent=s["parent"], lse=s["lse"], workspace=s["ws"])
+    a.update(kw)
+    pic.pic_attend_draft(s["geom"], s["layer"], s["q"], s["k"], s["v"], s["ctx"], s["draft"],
+                         s["bt"], s["num"], s["kc"], s["vc"], s["out"], **a)
+
+
+def check(s, ctx, draft, k_before, v_before):
+    hq, hkv = s["q"].shape[2], s["k"].shape[2]
+    d, G, lay = s["q"].shape[3], hq // hkv, s["layer"]
+    kc, vc, bt = s["kc"], s["vc"], s["bt"].cpu().numpy()
+    touched = torch.zeros(kc.shape[:2] + (16,), dtype=torch.bool)
+    for b, (c, n) in enumerate(zip(ctx, draft)):
+        assert bool((s["out"][b, n:] == 7).all()) and bool((s["lse"][b, n:] == 7).all())
+        if n == 0:
+            continue
+        line = line_of(s["par"][b], n)
+        pos = [c + len(x) - 1 for x in line]
+        t = np.arange(c + n)
+        page = bt[b][t // 16]
+        touched[lay, page[c:], t[c:] % 16] = True
+        K, V = f64(kc[lay])[page, :, t % 16], f64(vc[lay])[page, :, t % 16]
+        ok, worst = kv_tolerance_ok(K[c:], rope(f64(s["k"][b, :n]), pos, s["base"], s["style"]))
+        assert ok, (b, worst)
+        assert np.array_equal(V[c:], f64(s["v"][b, :n]))
+        qr = bf16(rope(f64(s["q"][b, :n]), pos, s["base"], s["style"]))
+        vis = np.zeros((n, c + n), bool)
+        vis[:, :c] = True
+        for i in range(n):
+            vis[i, [c + j for j in line[i]]] = True
+        for h in range(hq):
+            z = np.where(vis, qr[:, h] @ K[:, h // G].T / np.sqrt(d), -np.inf)
+            m = z.max(-1, keepdims=True)
+            w = np.exp(z - m)
+            l = w.sum(-1, keepdims=True)
+            ok, worst, rel = attn_close(f64(s["out"][b, :n, h]), w @ V[:, h // G] / l, abs_tol=1e-2,
+                                        row_rel=1e-2)
+            assert ok, (b, h, worst, rel)
+            assert np.abs(f64(s["lse"][b, :n, h]) - (m + np.log(l))[:, 0]).max() < 2e-3
+    # nothing else in the caches changed, bit for bit
+    for new, old in ((kc, k_before), (vc, v_before)):
+        same = (new.view(torch.int16) == old.view(torch.int16)).permute(0, 1, 3, 2, 4)
+        assert bool(same[~touched.cuda()].all())
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("heads,dim,style", [((4, 4), 128, 0), ((14, 2), 64, 1), ((32, 2), 128, 1),
+                                             ((7, 1), 128, 0), ((16, 1), 64, 0)])
+@pytest.mark.parametrize("T", [1, 5, 64])
+def test_draft_attention(cuda_lib, heads, dim, style, T, tree):
+    ctx = [0, 1, 15, 16, 127, 128, 129, 300, 64 * 16]
+    draft = [T, max(1, T - 1), T, 1, T, max(1, T // 2), T, 0, T]
+    s = draw(heads, dim, style, ctx, draft, T, tree, seed=T + dim)
+    before = s["kc"].clone(), s["vc"].clone()
+    call(s)
+    assert cuda_lib.pic_device_status() == (0, 0)
+    check(s, ctx, draft, *before)
+
+
+@pytest.mark.parametrize("heads,dim", [((8, 1), 128), ((8, 2), 64)])
+def test_long_contexts_split_over_many_ctas(cuda_lib, heads, dim):
+    """One long context (its tiles over all SMs, up to 152 partial states per
+    row) beside a short one, with scores that jump along the context."""
+    ctx, draft = [40001, 77], [9, 3]
+    s = draw(heads, dim, 0, ctx, draft, 9, True, layers=1, q_scale=4.0)
+    # later keys larger: the running maximum grows on the way
+    t = torch.arange(40001, device="cuda")
+    page = s["bt"][0].long()[t // 16]
+    s["kc"][0, page, :, t % 16] *= (1 + 3 * t / 40001)[:, None, None].bfloat16()
+    before = s["kc"].clone(), s["vc"].clone()
+    call(s)
+    assert cuda_lib.pic_device_status() == (0, 0)
+    check(s, ctx, draft, *before)
+
+
+def test_many_requests_and_repeated_calls(cuda_lib):
+    """More units than SMs, more requests than a warp; the same call twice gives
+    the same bits, on another stream too."""
+    rng = np.random.default_rng(3)
+    ctx, draft = rng.integers(0, 400, 70).tolist(), rng.integers(0, 5, 70).tolist()
+    s = draw((8, 4), 128, 0, ctx, draft, 4, True)
+    before = s["kc"].clone(), s["vc"].clone()
+    call(s)
+    check(s, ctx, draft, *before)
+    out, lse = s["out"].clone(), s["lse"].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call(s, stream=side)
+    side.synchronize()
+    assert torch.equal(out, s["out"]) and torch.equal(lse, s["lse"])
+    assert cuda_lib.pic_device_status() == (0, 0)
+
+
+def test_a_chain_is_decoding_token_by_token(cuda_lib):
+    """Drafting a chain gives what decoding its tokens one after the other gives."""
+    import paper_2607_28069_gb300 as pic
+    ctx, T = [200, 31], 4
+    s = draw((8, 2), 128, 0, ctx, [T, T], T, False)
+    kc, vc = s["kc"].clone(), s["vc"].clone()
+    call(s)
+    out = torch.empty((2, 8, 128), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(pic.pic_decode_workspace_size(s["geom"], 2, 256), dtype=torch.uint8,
+                     device="cuda")
+    for b in range(2):  # decode reads whole pages: no NaN behind the context there
+        for cache in (kc, vc):
+            t = torch.arange(ctx[b], s["bt"].shape[1] * 16, device="cuda")
+            cache.permute(1, 3, 0, 2, 4)[s["bt"][b].long()[t // 16], t % 16] = 0
+    for i in range(T):
+        pic.pic_attend_decode(s["geom"], 1, s["q"][:, i].contiguous(), s["k"][:, i].contiguous(),
+                              s["v"][:, i].contiguous(), s["ctx"], s["bt"], s["num"], kc, vc, out,
+                              256, workspace=ws, pos_offset=i)
+        ok, worst, rel = attn_close(f64(s["out"][:, i]), f64(out), abs_tol=1e-2, row_rel=1e-2)
+        assert ok, (i, worst, rel)
+    assert pic.pic_device_status() == (0, 0)
+
+
+def test_per_layer_frequencies(cuda_lib):
+    import paper_2607_28069_gb300 as pic
+    ctx, draft = [37, 500], [3, 6]
+    s = draw((8, 2), 128, 0, ctx, draft, 6, True, base=1e6)
+    i = torch.arange(64, dtype=torch.float64)
+    table = torch.stack([1e4 ** (-2 * i / 128), 1e6 ** (-2 * i / 128)]).cuda()
+    s["geom"] = pic.Geometry(2, 8, 2, 128, 77.0, layer_inv_freq=table)
+    before = s["kc"].clone(), s["vc"].clone()
+    call(s)
+    assert pic.pic_device_status() == (0, 0)
+    check(s, ctx, draft, *before)
+
+
+def test_device_checks(cuda_lib):
+    """A bad length, a table too short, a page outside the cache, a parent behind
+    its child: reported, and the other requests served."""
+    for name, code in (("length", 3), ("short", 5), ("page", 6), ("parent", 3)):
+        ctx, draft = [33, 20], [3, 3]
+        s = draw((4, 1), 64, 0, ctx, draft, 3, True)
+        if name == "length":
+            s["draft"][0] = 4
+        elif name == "short":
+            s["ctx"][0] = s["bt"].shape[1] * 16 - 2
+        elif name == "page":
+            s["bt"][0, 2] = s["num"]
+        else:
+            s["parent"][0, 1] = 2
+        before = s["kc"].clone(), s["vc"].clone()
+        call(s)
+        assert cuda_lib.pic_device_status() == (code, 0), name
+        if name in ("length", "short"):
+            assert bool((s["out"][0] == 7).all())
+            s2 = dict(s, out=s["out"][1:], lse=s["lse"][1:], q=s["q"][1:], k=s["k"][1:],
+                      v=s["v"][1:], bt=s["bt"][1:], par=s["par"][1:])
+            check(s2, ctx[1:], draft[1:], *before)
+
+
+def test_refusals(cuda_lib):
+    import paper_2607_28069_gb300 as pic
+    s = draw((4, 1), 64, 0, [16], [2], 2, False)
+    with pytest.raises(ValueError, match="k_new has the wrong number of elements"):
+        call(dict(s, k=s["k"][:, :1].contiguous()))
+    with pytest.raises(ValueError, match="k_cache must be"):
+        call(dict(s, kc=s["kc"][:1]))
+    with pytest.raises(ValueError, match="q must be contiguous"):
+        call(dict(s, q=s["q"].transpose(2, 3)))
+    with pytest.raises(ValueError, match="workspace is required"):
+        call(s, workspace=None)
+    with pytest.raises(pic.PicError, match="workspace needs") as e:
+        call(s, workspace=s["ws"][:1024])
+    assert e.value.status == 4
+    big = torch.zeros((1, 65, 4, 64), dtype=torch.bfloat16, device="cuda")
+    kv = torch.zeros((1, 65, 1, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(pic.PicError, match="max_draft 65") as e:
+        pic.pic_attend_draft(s["geom"], 0, big, kv, kv, s["ctx"], s["draft"], s["bt"], s["num"],
+                             s["kc"], s["vc"], big, workspace=s["ws"])
+    assert e.value.status == 2
+    s["layer"] = 2
+    with pytest.raises(pic.PicError, match="layer 2"):
+        call(s)
