@@ -707,9 +707,10 @@ pic_status_t pic_page_fork(const pic_geom_t *geom, int32_t n, const int32_t *src
  * nothing); result int32 [n]: the row's new length.
  * workspace: pic_page_compact_workspace_size(...) bytes (0 for max_keep <= 16;
  * then it may be NULL), 256-byte aligned, contents do not matter.
- * Three launches.  Positions are copied once, also where source and target
- * ranges overlap: each CTA holds 16 rows on chip and stores them when the CTAs
- * that read what it overwrites have done so.
+ * At least one layer.  Two launches (three for max_keep > 16).  Positions are
+ * copied once, also where source and target ranges overlap: each CTA holds 16
+ * rows on chip and stores them when the CTAs that read what it overwrites have
+ * done so.
  * Device checks: rows, lengths (BAD_REQUEST), keep lists (BAD_POSITION),
  * max_pages (BLOCK_TABLE_SHORT), page ids (BAD_PAGE), and every page a position
  * moves into has this row as its only user (SHARED_PAGE).

@@ -49,7 +49,9 @@ struct PlanParams {
 
 constexpr int kPlanThreads = 1024;
 
-// Exclusive prefix sum over the block; *total gets the sum.
+// Exclusive prefix sum over the block; *total gets the sum.  One barrier: every
+// warp adds up the warps' sums itself.  The caller alternates between two buffers
+// of 32, so that a buffer is written again only behind a later barrier.
 PIC_DEV int block_scan(int v, int *warp_sums, int *total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int x = v;
@@ -60,21 +62,17 @@ PIC_DEV int block_scan(int v, int *warp_sums, int *total) {
   }
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  if (warp == 0) {
-    int s = lane < kPlanThreads / 32 ? warp_sums[lane] : 0;
+  int s = warp_sums[lane];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, s, o);
-      if (lane >= o) s += y;
-    }
-    warp_sums[lane] = s;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
   }
-  __syncthreads();
-  *total = warp_sums[kPlanThreads / 32 - 1];
-  const int before = warp ? warp_sums[warp - 1] : 0;
-  __syncthreads();  // warp_sums may be written again
-  return before + x - v;
+  *total = __shfl_sync(0xffffffffu, s, 31);
+  const int before = __shfl_sync(0xffffffffu, s, max(warp - 1, 0));
+  return (warp ? before : 0) + x - v;
 }
+static_assert(kPlanThreads == 32 * 32, "a lane per warp sum");
 
 // One CTA: what each listed row needs, then the free pages in ascending order,
 // the k-th of them to the row whose range of the needs' prefix sum holds k.
@@ -83,9 +81,24 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
   pdl_entry();
   extern __shared__ int32_t sh[];
   int32_t *first = sh, *col0 = sh + p.n + 1, *len_of = col0 + p.n;  // len_of: fork
-  __shared__ int warp_sums[32];
+  __shared__ int warp_sums[2][32];
   const int tid = threadIdx.x;
-  int carry = 0;
+  int carry = 0, turn = 0;
+  // the counts of four pages; the first ones go out before the needs are known
+  const bool vec = (reinterpret_cast<uintptr_t>(p.page_refs) & 15) == 0;
+  auto counts = [&](long long pg) {
+    int4 v = make_int4(1, 1, 1, 1);
+    if (vec && pg + 3 < p.num_pages) {
+      v = *reinterpret_cast<const int4 *>(p.page_refs + pg);
+    } else {
+      if (pg < p.num_pages) v.x = p.page_refs[pg];
+      if (pg + 1 < p.num_pages) v.y = p.page_refs[pg + 1];
+      if (pg + 2 < p.num_pages) v.z = p.page_refs[pg + 2];
+      if (pg + 3 < p.num_pages) v.w = p.page_refs[pg + 3];
+    }
+    return v;
+  };
+  int4 ahead = counts(4 * tid);
   for (int j0 = 0; j0 < p.n; j0 += kPlanThreads) {
     const int j = j0 + tid;
     int need = 0, at = 0, res = -1, len = -1;
@@ -127,7 +140,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
       }
     }
     int total;
-    const int before = block_scan(need, warp_sums, &total);
+    const int before = block_scan(need, warp_sums[turn ^= 1], &total);
     if (j < p.n) {
       first[j] = carry + before;
       col0[j] = at;
@@ -143,18 +156,13 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
   int found = 0;
   for (long long base = 0; base < p.num_pages && found < want_all; base += 4 * kPlanThreads) {
     const long long pg = base + 4 * tid;
-    int32_t c[4];
-    if (pg + 3 < p.num_pages && (reinterpret_cast<uintptr_t>(p.page_refs) & 15) == 0) {
-      const int4 v = *reinterpret_cast<const int4 *>(p.page_refs + pg);
-      c[0] = v.x, c[1] = v.y, c[2] = v.z, c[3] = v.w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c[i] = pg + i < p.num_pages ? p.page_refs[pg + i] : 1;
-    }
+    const int4 v = ahead;
+    ahead = counts(pg + 4 * kPlanThreads);
+    const int32_t c[4] = {v.x, v.y, v.z, v.w};
     int mine = 0, total;
 #pragma unroll
     for (int i = 0; i < 4; ++i) mine += c[i] == 0;
-    int k = found + block_scan(mine, warp_sums, &total);
+    int k = found + block_scan(mine, warp_sums[turn ^= 1], &total);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (c[i] == 0) {
@@ -301,6 +309,7 @@ __global__ void __launch_bounds__(256) release_kernel(FreeParams p) {
 constexpr int kSeg = 16;      // kept positions per CTA
 constexpr int kUnits = 8;     // 32-byte units of a thread
 constexpr int kMoveThreads = 256;
+constexpr int kCheckThreads = 1024, kCheckDeep = 4;
 
 struct CompactParams {
   int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, layers, layer_begin, rotate;
@@ -309,153 +318,239 @@ struct CompactParams {
   const int32_t *ctx_len, *block_table, *page_refs;
   int32_t *result;
   __nv_bfloat16 *k, *v;  // at layer_begin
-  int32_t *flags;        // [0] ticket, then [n][layers * hgroups][segs]: "reads done"; null: one segment
+  // several segments (workspace): from and to slot of every kept position, per
+  // (row, segment) the first segment to wait for, a ticket, and per (row, layer and
+  // head group, segment) "reads done"
+  longlong2 *slot;       // [n][max_keep]
+  int32_t *wait_from;    // [n][segs]
+  int32_t *ticket, *flags;
   int32_t *status;
 };
 
-// One CTA per listed row: every check of its list, before anything moves; the
-// verdict goes to result.  Clears the row's flags.
-__global__ void __launch_bounds__(256) compact_check_kernel(CompactParams p) {
-  pdl_entry();
-  const int j = blockIdx.x, tid = threadIdx.x;
-  if (p.flags) {
-    const long long per = (long long)p.layers * p.hgroups * p.segs;
-    for (long long i = tid; i < per; i += 256) p.flags[1 + j * per + i] = 0;
-    if (j == 0 && tid == 0) p.flags[0] = 0;
-  }
+// The start of row j's window, or -1 with *code set.
+PIC_DEV int compact_start(const CompactParams &p, int j, int *code) {
   const int r = p.row[j], m = p.keep_len[j];
-  int code = PIC_DEV_OK, s = 0;
   if (r < 0 || r >= p.rows || m < 0 || m > p.max_keep) {
-    code = PIC_DEV_BAD_REQUEST;
-  } else {
-    s = p.start ? p.start[j] : p.ctx_len[r];
-    if (s < 0 || (long long)s + m > (long long)p.max_pages * kPage)
-      code = s < 0 ? PIC_DEV_BAD_REQUEST : PIC_DEV_BLOCK_TABLE_SHORT;
+    *code = PIC_DEV_BAD_REQUEST;
+    return -1;
   }
-  if (code == PIC_DEV_OK) {
-    const int32_t *t = p.block_table + (size_t)r * p.max_pages;
-    const int32_t *kp = p.keep + (size_t)j * p.max_keep;
-    for (int i = tid; i < m; i += 256) {
-      const int k = kp[i];
-      if (k < i || (i > 0 && kp[i - 1] >= k)) {  // ascending from >= 0 on: never below i
-        code = PIC_DEV_BAD_POSITION;
-        break;
-      }
-      const long long from = (long long)s + k, to = (long long)s + i;
-      if (from >= (long long)p.max_pages * kPage) {
-        code = PIC_DEV_BLOCK_TABLE_SHORT;
-        break;
-      }
-      const int a = t[from / kPage], z = t[to / kPage];
-      if (a < 0 || a >= p.num_pages || z < 0 || z >= p.num_pages) {
+  const int s = p.start ? p.start[j] : p.ctx_len[r];
+  if (s < 0 || (long long)s + m > (long long)p.max_pages * kPage) {
+    *code = s < 0 ? PIC_DEV_BAD_REQUEST : PIC_DEV_BLOCK_TABLE_SHORT;
+    return -1;
+  }
+  return s;
+}
+
+// kN entries of a keep list at once (i[q] < 0: none): their checks and their
+// slots, as page * 16 + row of the page.
+template <int kN>
+PIC_DEV int compact_entries(const CompactParams &p, int j, int s, const int *i, int *k,
+                            longlong2 *slot) {
+  const int32_t *t = p.block_table + (size_t)p.row[j] * p.max_pages;
+  const int32_t *kp = p.keep + (size_t)j * p.max_keep;
+  int before[kN], a[kN], z[kN], refs[kN], code = PIC_DEV_OK;
+#pragma unroll
+  for (int q = 0; q < kN; ++q) {
+    k[q] = i[q] >= 0 ? kp[i[q]] : 0;
+    before[q] = i[q] > 0 ? kp[i[q] - 1] : -1;
+  }
+#pragma unroll
+  for (int q = 0; q < kN; ++q) {
+    a[q] = z[q] = -1;
+    if (i[q] < 0) continue;
+    if (k[q] < i[q] || before[q] >= k[q]) {  // ascending from >= 0 on: never below i
+      code = PIC_DEV_BAD_POSITION;
+    } else if ((long long)s + k[q] >= (long long)p.max_pages * kPage) {
+      code = PIC_DEV_BLOCK_TABLE_SHORT;
+    } else {
+      a[q] = t[(s + k[q]) / kPage];
+      z[q] = t[(s + i[q]) / kPage];
+      if (a[q] < 0 || a[q] >= p.num_pages || z[q] < 0 || z[q] >= p.num_pages) {
         code = PIC_DEV_BAD_PAGE;
-        break;
-      }
-      if (k != i && p.page_refs[z] != 1) {
-        code = PIC_DEV_SHARED_PAGE;
-        break;
+        a[q] = z[q] = -1;
       }
     }
+  }
+#pragma unroll
+  for (int q = 0; q < kN; ++q) refs[q] = z[q] >= 0 && k[q] != i[q] ? p.page_refs[z[q]] : 1;
+#pragma unroll
+  for (int q = 0; q < kN; ++q) {
+    if (refs[q] != 1) code = PIC_DEV_SHARED_PAGE;
+    slot[q] = make_longlong2((long long)a[q] * kPage + (s + k[q]) % kPage,
+                             (long long)z[q] * kPage + (s + i[q]) % kPage);
+  }
+  return code;
+}
+
+// Lists of more than one segment, one CTA per listed row: every check before
+// anything moves (the verdict goes to result), the slots, the segments to wait
+// for, the flags cleared.  Four entries of a thread at a time, because an entry is
+// a chain of three loads: 9001 entries 33 us one at a time.
+__global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactParams p) {
+  pdl_entry();
+  const int j = blockIdx.x, tid = threadIdx.x;
+  const long long per = (long long)p.layers * p.hgroups * p.segs;
+  for (long long i = tid; i < per; i += kCheckThreads) p.flags[j * per + i] = 0;
+  if (j == 0 && tid == 0) *p.ticket = 0;
+  int code = PIC_DEV_OK;
+  const int s = compact_start(p, j, &code);
+  const int m = s >= 0 ? p.keep_len[j] : 0;
+  for (int i0 = tid; i0 < m && code == PIC_DEV_OK; i0 += kCheckThreads * kCheckDeep) {
+    int i[kCheckDeep], k[kCheckDeep];
+    longlong2 slot[kCheckDeep];
+#pragma unroll
+    for (int q = 0; q < kCheckDeep; ++q)
+      i[q] = i0 + q * kCheckThreads < m ? i0 + q * kCheckThreads : -1;
+    code = compact_entries<kCheckDeep>(p, j, s, i, k, slot);
+#pragma unroll
+    for (int q = 0; q < kCheckDeep; ++q)
+      if (i[q] >= 0) p.slot[(size_t)j * p.max_keep + i[q]] = slot[q];
   }
   if (code != PIC_DEV_OK) dev_fail(p.status, code, j);
   const bool bad = __syncthreads_or(code != PIC_DEV_OK);
   if (tid == 0) p.result[j] = bad ? -1 : s + m;
+  if (bad) return;
+  // segment s2 reads up to keep[16 (s2 + 1) - 1], segment seg writes from 16 seg on
+  const int32_t *kp = p.keep + (size_t)j * p.max_keep;
+  for (int seg = tid; seg < (m + kSeg - 1) / kSeg; seg += kCheckThreads) {
+    int lo = 0, hi = seg;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (kp[(mid + 1) * kSeg - 1] >= seg * kSeg) hi = mid;
+      else lo = mid + 1;
+    }
+    p.wait_from[(size_t)j * p.segs + seg] = lo;
+  }
 }
 
-// One CTA = 16 kept positions x a group of kv heads x a layer of one row: it
+// A CTA moves 16 kept positions x a group of kv heads x a layer of one row: it
 // reads them all into registers, says so, waits for the CTAs whose sources lie
 // in what it overwrites, and stores.  keep is ascending, so those are CTAs of
-// earlier segments of the same (row, layer, head group) only; a CTA's segment
-// comes from a ticket, so they have started before it, and they read before they
-// wait: every wait ends.  Keys move by i - keep[i] positions and are re-rotated
-// by that, with cos/sin of the 16 moves formed once per CTA.
-template <int D>
-__global__ void __launch_bounds__(kMoveThreads) compact_move_kernel(CompactParams p, RopeParams rp) {
+// earlier segments of the same (row, layer, head group) only; a segment comes from
+// a ticket, so they have started before it, and they read before they wait: every
+// wait ends.  Keys move by i - keep[i] positions and are re-rotated by that, with
+// cos/sin of the 16 moves formed once per CTA.
+// kLong: several segments, checked by compact_check_kernel, by CTAs that stay
+// and look up the next segment's positions while they wait.  Otherwise one
+// segment per row, and every CTA checks its list itself (16 entries), so the call
+// is a launch shorter.
+template <int D, bool kLong>
+__global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactParams p, RopeParams rp) {
   constexpr int KC = D / 16;  // 8-pair chunks of a row
   pdl_entry();
   __shared__ float2 cs[kSeg][D / 2];
-  __shared__ int32_t k_of[kSeg];
-  __shared__ long long from_of[kSeg], to_of[kSeg];  // page * hkv * 16 + row
-  __shared__ int ticket;
-  const int tid = threadIdx.x;
-  long long at = blockIdx.x;
-  if (p.flags) {
-    if (tid == 0) ticket = atomicAdd(p.flags, 1);
-    __syncthreads();
-    at = ticket;
-  }
-  const int lh = (int)(at % (p.layers * p.hgroups));
-  at /= p.layers * p.hgroups;
-  const int j = (int)(at % p.n), seg = (int)(at / p.n);
-  const int layer = lh / p.hgroups, h0 = (lh % p.hgroups) * p.hgroup;
-  const int heads = min(p.hgroup, p.hkv - h0);
-  const int res = p.result[j];
-  if (res < 0) return;
-  const int m = p.keep_len[j], i0 = seg * kSeg, cnt = min(kSeg, m - i0);
-  if (cnt <= 0) return;
-  const int32_t *kp = p.keep + (size_t)j * p.max_keep;
-  if (tid < cnt) {
-    const int s = res - m, i = i0 + tid, k = kp[i];
-    const int32_t *t = p.block_table + (size_t)p.row[j] * p.max_pages;
-    k_of[tid] = k;
-    from_of[tid] = (long long)t[(s + k) / kPage] * p.hkv * kPage + (s + k) % kPage;
-    to_of[tid] = (long long)t[(s + i) / kPage] * p.hkv * kPage + (s + i) % kPage;
-  }
-  __syncthreads();
-
-  // ---- read: unit u = (position, K or V, head, chunk)
-  const long long lbase = (long long)layer * p.layer_elems;
-  const int units = cnt * 2 * heads * KC;
+  __shared__ int32_t k_of[2][kSeg];
+  __shared__ longlong2 slot_of[2][kSeg];
+  __shared__ int next_at, next_cnt[2];
+  const int tid = threadIdx.x, lhs = p.layers * p.hgroups;
+  const long long all = (long long)lhs * p.n * p.segs;
   const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
-  uint4 a[kUnits], b[kUnits];
-#pragma unroll
-  for (int q = 0; q < kUnits; ++q) {
-    const int u = tid + q * kMoveThreads;
-    if (u < units) {
+
+  // the positions of item `at` into buffer `buf` (the count 0: nothing to move)
+  auto look_up = [&](long long at, int buf) {
+    const int j = (int)(at / lhs % p.n), seg = (int)(at / lhs / p.n);
+    if constexpr (kLong) {
+      const int res = p.result[j], m = p.keep_len[j];
+      if (tid < kSeg) {
+        const size_t i = (size_t)j * p.max_keep + min(seg * kSeg + tid, p.max_keep - 1);
+        k_of[buf][tid] = p.keep[i];
+        slot_of[buf][tid] = p.slot[i];
+      }
+      if (tid == 0) next_cnt[buf] = res < 0 ? 0 : max(0, min(kSeg, m - seg * kSeg));
+    } else if (tid < 32) {
+      int code = PIC_DEV_OK;
+      const int s = compact_start(p, j, &code), m = s >= 0 ? p.keep_len[j] : 0;
+      int i[1] = {tid < m ? tid : -1}, k[1];
+      longlong2 slot[1];
+      if (s >= 0) code = compact_entries<1>(p, j, s, i, k, slot);
+      const bool bad = __any_sync(0xffffffffu, code != PIC_DEV_OK);
+      if (at % lhs == 0) {  // one CTA of a row reports
+        if (code != PIC_DEV_OK && (tid == 0 || s >= 0)) dev_fail(p.status, code, j);
+        if (tid == 0) p.result[j] = bad ? -1 : s + m;
+      }
+      if (tid < kSeg && s >= 0) k_of[buf][tid] = k[0], slot_of[buf][tid] = slot[0];
+      if (tid == 0) next_cnt[buf] = bad ? 0 : m;
+    }
+  };
+
+  long long at = blockIdx.x;
+  if constexpr (kLong) {
+    if (tid == 0) next_at = atomicAdd(p.ticket, 1);
+    __syncthreads();
+    at = next_at;
+  }
+  int buf = 0;
+  if (at < all) look_up(at, 0);
+  __syncthreads();
+  while (at < all) {
+    const int lh = (int)(at % lhs), j = (int)(at / lhs % p.n), seg = (int)(at / lhs / p.n);
+    const int layer = lh / p.hgroups, h0 = (lh % p.hgroups) * p.hgroup;
+    const int heads = min(p.hgroup, p.hkv - h0), cnt = next_cnt[buf], i0 = seg * kSeg;
+    // ---- read: unit u = (position, K or V, head, chunk)
+    const long long lbase = (long long)layer * p.layer_elems;
+    const int units = cnt * 2 * heads * KC;
+    auto where = [&](int u, bool to) {  // the unit's 16 positions' vector of one head
       const int h = (u / KC) % heads, kv = (u / (KC * heads)) & 1, i = u / (KC * heads * 2);
-      if (k_of[i] != i0 + i) {
-        const __nv_bfloat16 *src =
-            (kv ? p.v : p.k) + lbase + (from_of[i] + (long long)(h0 + h) * kPage) * D;
+      const long long sl = to ? slot_of[buf][i].y : slot_of[buf][i].x;
+      return (kv ? p.v : p.k) + lbase +
+             (((sl / kPage) * p.hkv + h0 + h) * kPage + sl % kPage) * D;
+    };
+    uint4 a[kUnits], b[kUnits];
+#pragma unroll
+    for (int q = 0; q < kUnits; ++q) {
+      const int u = tid + q * kMoveThreads;
+      if (u < units && k_of[buf][u / (KC * heads * 2)] != i0 + u / (KC * heads * 2)) {
+        const __nv_bfloat16 *src = where(u, false);
         a[q] = *reinterpret_cast<const uint4 *>(src + pc.off_a);
         b[q] = *reinterpret_cast<const uint4 *>(src + pc.off_b);
       }
     }
-  }
-  if (p.rotate)
-    for (int e = tid; e < cnt * (D / 2); e += kMoveThreads) {
-      const int i = e / (D / 2), f = e % (D / 2);
-      cs[i][f] = rope_cos_sin_turn(i0 + i - k_of[i],
-                                   rope_turn(rope_theta(rp, p.layer_begin + layer, f)));
+    if (kLong && tid == 0) next_at = atomicAdd(p.ticket, 1);
+    if (p.rotate)
+      for (int e = tid; e < cnt * (D / 2); e += kMoveThreads) {
+        const int i = e / (D / 2), f = e % (D / 2);
+        cs[i][f] = rope_cos_sin_turn(i0 + i - k_of[buf][i],
+                                     rope_turn(rope_theta(rp, p.layer_begin + layer, f)));
+      }
+    if constexpr (kLong) {
+      int32_t *fl = p.flags + ((long long)j * lhs + lh) * p.segs;
+      __threadfence();
+      __syncthreads();
+      const long long after = next_at;
+      bool ok = true;
+      if (cnt > 0) {
+        if (tid == 0) atomicExch(fl + seg, 1);
+        const int lo = p.wait_from[(size_t)j * p.segs + seg];
+        if (after < all) look_up(after, buf ^ 1);
+        for (int s2 = seg - 1 - tid; ok && s2 >= lo; s2 -= kMoveThreads)
+          ok = wait_flag(fl + s2, p.status, j);
+      } else if (after < all) {
+        look_up(after, buf ^ 1);
+      }
+      if (__syncthreads_or(!ok)) return;
+      at = after;
+    } else {
+      __syncthreads();
+      at = all;
     }
-  if (p.flags) {
-    int32_t *fl = p.flags + 1 + ((long long)j * p.layers * p.hgroups + lh) * p.segs;
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) atomicExch(fl + seg, 1);
-    // segment s2 < seg reads up to keep[16 (s2 + 1) - 1], this one writes from i0 on
-    bool ok = true;
-    for (int s2 = seg - 1 - tid; ok && s2 >= 0 && kp[(s2 + 1) * kSeg - 1] >= i0; s2 -= kMoveThreads)
-      ok = wait_flag(fl + s2, p.status, j);
-    if (__syncthreads_or(!ok)) return;
-  } else {
-    __syncthreads();
-  }
-  // ---- store
+    // ---- store
 #pragma unroll
-  for (int q = 0; q < kUnits; ++q) {
-    const int u = tid + q * kMoveThreads;
-    if (u < units) {
-      const int h = (u / KC) % heads, kv = (u / (KC * heads)) & 1, i = u / (KC * heads * 2);
-      if (k_of[i] != i0 + i) {
-        __nv_bfloat16 *dst =
-            (kv ? p.v : p.k) + lbase + (to_of[i] + (long long)(h0 + h) * kPage) * D;
-        if (p.rotate && !kv) {
+    for (int q = 0; q < kUnits; ++q) {
+      const int u = tid + q * kMoveThreads, i = u / (KC * heads * 2);
+      if (u < units && k_of[buf][i] != i0 + i) {
+        __nv_bfloat16 *dst = const_cast<__nv_bfloat16 *>(where(u, true));
+        if (p.rotate && ((u / (KC * heads)) & 1) == 0) {
           rotate_store(a[q], b[q], dst, pc, rp.style, &cs[i][8 * (tid % KC)]);
         } else {
           st_global16(dst + pc.off_a, a[q]);
           st_global16(dst + pc.off_b, b[q]);
         }
       }
+    }
+    if constexpr (kLong) {
+      __syncthreads();  // cs and the buffer may be written again
+      buf ^= 1;
     }
   }
 }
@@ -561,11 +656,31 @@ static cudaError_t launch_plan(const PlanParams &pp, pic_stream_t stream) {
 static int heads_per_group(const pic_geom_t *g) {
   return kMoveThreads * kUnits / (kSeg * 2 * (g->head_dim / 16));
 }
-static size_t flag_bytes(const pic_geom_t *g, int n, int max_keep, int layers) {
+struct CompactSpace {  // byte offsets in the workspace
+  size_t wait, ticket, flags, total;
+};
+static CompactSpace compact_space(const pic_geom_t *g, int n, int max_keep, int layers) {
   const int hg = heads_per_group(g);
   const size_t groups = (size_t)(g->num_kv_heads + hg - 1) / hg;
   const size_t segs = ((size_t)max_keep + kSeg - 1) / kSeg;
-  return segs <= 1 ? 0 : (1 + (size_t)n * layers * groups * segs) * 4;
+  CompactSpace c;
+  c.wait = (size_t)n * max_keep * sizeof(longlong2);
+  c.ticket = c.wait + (size_t)n * segs * 4;
+  c.flags = c.ticket + 4;
+  c.total = segs <= 1 ? 0 : c.flags + (size_t)n * layers * groups * segs * 4;
+  return c;
+}
+
+template <int D>
+static cudaError_t launch_move(const CompactParams &cp, const RopeParams &rp, long long items,
+                               pic_stream_t stream) {
+  // two CTAs an SM hold 16 positions each: the long form's stay
+  if (cp.flags)
+    return launch_dependent(compact_move_kernel<D, true>,
+                            dim3((unsigned)std::min(items, 2LL * 152)), dim3(kMoveThreads), 0, stream,
+                            cp, rp);
+  return launch_dependent(compact_move_kernel<D, false>, dim3((unsigned)items), dim3(kMoveThreads), 0,
+                          stream, cp, rp);
 }
 
 }  // namespace pages
@@ -642,7 +757,7 @@ extern "C" size_t pic_page_compact_workspace_size(const pic_geom_t *geom, int32_
   if (!geom || n <= 0 || max_keep <= 0 || geom->num_layers <= 0 || geom->num_kv_heads <= 0 ||
       (geom->head_dim != 64 && geom->head_dim != 128))
     return 0;
-  return pic::pages::flag_bytes(geom, n, max_keep, geom->num_layers);
+  return pic::pages::compact_space(geom, n, max_keep, geom->num_layers).total;
 }
 
 extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, const int32_t *row,
@@ -690,24 +805,30 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
   cp.result = result;
   cp.k = static_cast<__nv_bfloat16 *>(k_cache) + layer_begin * cp.layer_elems;
   cp.v = static_cast<__nv_bfloat16 *>(v_cache) + layer_begin * cp.layer_elems;
-  cp.flags = nullptr;
-  const size_t bytes = flag_bytes(geom, n, max_keep, cp.layers);
-  if (bytes) {
-    if (!workspace || workspace_bytes < bytes || (reinterpret_cast<uintptr_t>(workspace) & 255))
-      return fail(PIC_ERR_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", who, bytes);
-    cp.flags = static_cast<int32_t *>(workspace);
+  cp.flags = cp.ticket = cp.wait_from = nullptr;
+  cp.slot = nullptr;
+  const CompactSpace cw = compact_space(geom, n, max_keep, cp.layers);
+  if (cw.total) {
+    if (!workspace || workspace_bytes < cw.total || (reinterpret_cast<uintptr_t>(workspace) & 255))
+      return fail(PIC_ERR_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", who, cw.total);
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    cp.slot = reinterpret_cast<longlong2 *>(ws);
+    cp.wait_from = reinterpret_cast<int32_t *>(ws + cw.wait);
+    cp.ticket = reinterpret_cast<int32_t *>(ws + cw.ticket);
+    cp.flags = reinterpret_cast<int32_t *>(ws + cw.flags);
   }
-  const long long blocks = (long long)n * cp.layers * cp.hgroups * cp.segs;
-  if (blocks > INT32_MAX) return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
+  const long long items = (long long)n * cp.layers * cp.hgroups * cp.segs;
+  if (items > INT32_MAX / 2)
+    return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
+  if (items == 0) return fail(PIC_ERR_INVALID_ARG, "%s: no layers", who);
   cp.status = device_status_ptr();
   if (!cp.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
-  cudaError_t e = launch_dependent(compact_check_kernel, dim3(n), dim3(256), 0, stream, cp);
-  if (e == cudaSuccess && blocks > 0)
-    e = geom->head_dim == 128
-            ? launch_dependent(compact_move_kernel<128>, dim3((unsigned)blocks), dim3(kMoveThreads),
-                               0, stream, cp, rp)
-            : launch_dependent(compact_move_kernel<64>, dim3((unsigned)blocks), dim3(kMoveThreads),
-                               0, stream, cp, rp);
+  cudaError_t e = cudaSuccess;
+  if (cp.flags)
+    e = launch_dependent(compact_check_kernel, dim3(n), dim3(kCheckThreads), 0, stream, cp);
+  if (e == cudaSuccess)
+    e = geom->head_dim == 128 ? launch_move<128>(cp, rp, items, stream)
+                              : launch_move<64>(cp, rp, items, stream);
   if (e != cudaSuccess) return cuda_fail(e, who);
   FreeParams fp{n, rows, max_pages, num_pages, row, result, reserve, ctx_len, block_table, page_refs,
                 cp.status};

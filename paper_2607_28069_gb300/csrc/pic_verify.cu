@@ -25,7 +25,7 @@ namespace verify {
 
 constexpr int kMaxDraft = 64;
 constexpr int kMaxVocab = 1 << 24;
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kCluster = 8;
 constexpr int kChunk = 1024;
 constexpr int kMaxChunks = kMaxVocab / kChunk / kCluster;  // of one CTA
@@ -40,106 +40,131 @@ struct Params {
 };
 
 struct Shared {
-  uint64_t chunk[kMaxChunks];
+  uint64_t chunk[kMaxChunks];   // sums of this CTA's chunks
+  uint64_t tile[32 * 33];       // the weights of the chunk that is searched
   uint64_t warp[kWarps];
-  uint64_t total;  // of this CTA
-  int32_t found;   // the token, written by the CTA that holds it
-  int32_t first_refused;
+  uint64_t totals[2][kCluster]; // every CTA's sum, written by that CTA (by turns)
+  int32_t found;                // the token, written by the CTA that holds it
+  int32_t refused;
 };
 
 // A weight as a whole number of 2^-36; NaN, negative: 0.
 PIC_DEV uint64_t weight(float p) {
   return (uint64_t)(fminf(fmaxf(p, 0.f), 1.f) * 68719476736.f);
 }
-PIC_DEV uint64_t ld_cluster64(uint32_t addr) {
-  uint64_t v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
-  return v;
+PIC_DEV void st_cluster64(uint32_t addr, uint64_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
-PIC_DEV int ld_cluster32(uint32_t addr) {
-  int v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+PIC_DEV void st_cluster32(uint32_t addr, int v) {
+  asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+PIC_DEV uint64_t scan64(uint64_t v) {  // inclusive prefix sum over the warp
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t y = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += y;
+  }
   return v;
 }
 
-// The weight of entry x of the row: of p, or of what p has more than q.
-PIC_DEV uint64_t entry(const float *p, const float *q, int x) {
-  const float a = __ldg(p + x);
-  return weight(q ? __fsub_rn(a, __ldg(q + x)) : a);
+// N entries of a row, 32 apart, as weights: of p, or of what p has more than q.
+// All loads go out before the first is used.
+template <int N, bool kBoth>
+PIC_DEV void load_weights(const float *p, const float *q, int x0, int vocab, uint64_t *w) {
+  float a[N], b[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int x = x0 + 32 * i;
+    a[i] = x < vocab ? __ldg(p + x) : 0.f;
+    if constexpr (kBoth) b[i] = x < vocab ? __ldg(q + x) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = weight(kBoth ? __fsub_rn(a[i], b[i]) : a[i]);
 }
 
-// One draw by the whole cluster; every thread gets the token (-1: no weight).
-PIC_DEV int draw(Shared &sh, const float *p, const float *q, int vocab, float u) {
+// The sum of one chunk (32 loads of a lane in flight), the same in every lane.
+template <bool kBoth>
+PIC_DEV uint64_t chunk_sum(const float *p, const float *q, int c, int vocab) {
+  constexpr int N = kBoth ? 16 : 32;
+  const int x0 = c * kChunk + (threadIdx.x & 31);
+  uint64_t s = 0, w[N];
+#pragma unroll 1
+  for (int i = 0; i < 32; i += N) {
+    load_weights<N, kBoth>(p, q, x0 + 32 * i, vocab, w);
+#pragma unroll
+    for (int k = 0; k < N; ++k) s += w[k];
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
+
+// One warp: the entry of chunk c where the running sum passes `left`.
+template <bool kBoth>
+PIC_DEV int search_chunk(Shared &sh, const float *p, const float *q, int c, int vocab, uint64_t left) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int i = 0; i < 32; i += 16) {
+    uint64_t w[16];
+    load_weights<16, kBoth>(p, q, c * kChunk + 32 * i + lane, vocab, w);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sh.tile[(i + k) * 33 + lane] = w[k];
+  }
+  __syncwarp();
+  uint64_t v = 0;  // lane l: entries 32 l .. 32 l + 31
+#pragma unroll
+  for (int k = 0; k < 32; ++k) v += sh.tile[lane * 33 + k];
+  uint64_t x = scan64(v);
+  const int row = __ffs(__ballot_sync(0xffffffffu, x > left)) - 1;
+  left -= __shfl_sync(0xffffffffu, x - v, row);
+  x = scan64(sh.tile[row * 33 + lane]);
+  return c * kChunk + row * 32 + __ffs(__ballot_sync(0xffffffffu, x > left)) - 1;
+}
+
+// One draw by the whole cluster.  Returns false where the row has no weight.
+// The token goes to every CTA's sh.found (kAll) or is written to *out by the CTA
+// that finds it.  turn: the draws of a kernel alternate between 0 and 1.
+template <bool kBoth, bool kAll>
+PIC_DEV bool draw(Shared &sh, int turn, const float *p, const float *q, int vocab, float u,
+                  int32_t *out) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t rank = cluster_rank();
+  const int rank = (int)cluster_rank();
   const int chunks = (vocab + kChunk - 1) / kChunk;
   const int c0 = (int)((long long)chunks * rank / kCluster);
   const int c1 = (int)((long long)chunks * (rank + 1) / kCluster);
   uint64_t mine = 0;
   for (int c = c0 + warp; c < c1; c += kWarps) {
-    uint64_t s = 0;
-    const int x0 = c * kChunk + lane;
-    if ((c + 1) * kChunk <= vocab) {
-      // every load of the chunk before the first sum
-      float a[32];
-#pragma unroll
-      for (int i = 0; i < 32; ++i) a[i] = __ldg(p + x0 + 32 * i);
-      if (q) {
-        float b[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) b[i] = __ldg(q + x0 + 32 * i);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) a[i] = __fsub_rn(a[i], b[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < 32; ++i) s += weight(a[i]);
-    } else {
-      for (int x = x0; x < vocab; x += 32) s += entry(p, q, x);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    const uint64_t s = chunk_sum<kBoth>(p, q, c, vocab);
     if (lane == 0) sh.chunk[c - c0] = s;
     mine += s;
   }
   if (lane == 0) sh.warp[warp] = mine;
   __syncthreads();
-  if (tid == 0) {
+  if (tid < kCluster) {  // this CTA's total to every CTA
     uint64_t s = 0;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) s += sh.warp[w];
-    sh.total = s;
+    st_cluster64(map_to_rank(smem_u32(&sh.totals[turn][rank]), tid), s);
   }
   cluster_sync_all();
-  uint64_t total = 0, before = 0, own = 0;
-  uint64_t t[kCluster];
+  uint64_t total = 0, t[kCluster];
 #pragma unroll
-  for (int c = 0; c < kCluster; ++c) t[c] = ld_cluster64(map_to_rank(smem_u32(&sh.total), c));
-#pragma unroll
-  for (int c = 0; c < kCluster; ++c) {
-    if (c < (int)rank) before += t[c];
-    if (c == (int)rank) own = t[c];
-    total += t[c];
-  }
+  for (int c = 0; c < kCluster; ++c) total += t[c] = sh.totals[turn][c];
   // floor(total * floor(2^24 u) / 2^24); u outside [0, 1) (NaN: 0)
   const uint64_t n = (uint64_t)fminf(fmaxf(u, 0.f) * 16777216.f, 16777215.f);
   const uint64_t at = (__umul64hi(total, n) << 40) | ((total * n) >> 24);
-  // the owner of the threshold
-  int owner = 0;
-  uint64_t run = 0;
+  uint64_t run = 0, left = 0;
+  bool owner = false;
 #pragma unroll
   for (int c = 0; c < kCluster; ++c) {
-    if (run <= at && at < run + t[c]) owner = c;
+    if (c == rank && run <= at && at < run + t[c]) owner = true, left = at - run;
     run += t[c];
   }
-  if (total != 0 && owner == (int)rank && warp == 0) {
-    uint64_t left = at - before;  // < own
+  if (owner && warp == 0) {
     int c = 0;
-    for (; c < c1 - c0; c += 32) {  // the chunk: 32 sums at a time
-      uint64_t v = c + lane < c1 - c0 ? sh.chunk[c + lane] : 0, x = v;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
+    for (;; c += 32) {  // the chunk: 32 sums at a time
+      const uint64_t v = c + lane < c1 - c0 ? sh.chunk[c + lane] : 0, x = scan64(v);
       const unsigned past = __ballot_sync(0xffffffffu, x > left);
       if (past) {
         const int l = __ffs(past) - 1;
@@ -149,108 +174,99 @@ PIC_DEV int draw(Shared &sh, const float *p, const float *q, int vocab, float u)
       }
       left -= __shfl_sync(0xffffffffu, x, 31);
     }
-    const int x0 = (c0 + c) * kChunk + lane * 32;  // 32 consecutive entries a lane
-    uint64_t v = 0;
-    for (int i = 0; i < 32; ++i)
-      if (x0 + i < vocab) v += entry(p, q, x0 + i);
-    uint64_t x = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint64_t y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    const unsigned past = __ballot_sync(0xffffffffu, x > left);
-    if (past && lane == __ffs(past) - 1) {
-      uint64_t run2 = x - v;
-      int i = 0;
-      for (; i < 31; ++i) {
-        run2 += entry(p, q, x0 + i);
-        if (run2 > left) break;
-      }
-      sh.found = x0 + i;
+    const int x = search_chunk<kBoth>(sh, p, q, c0 + c, vocab, left);
+    if constexpr (kAll) {
+      if (lane < kCluster) st_cluster32(map_to_rank(smem_u32(&sh.found), lane), x);
+    } else if (lane == 0) {
+      *out = x;
     }
   }
-  (void)own;
-  cluster_sync_all();
-  return total ? ld_cluster32(map_to_rank(smem_u32(&sh.found), owner)) : -1;
+  if constexpr (kAll) cluster_sync_all();
+  return total != 0;
 }
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 4)
     verify_kernel(Params p) {
   pdl_entry();
   extern __shared__ __align__(16) uint8_t smem[];
   Shared &sh = *reinterpret_cast<Shared *>(smem);
+  // every CTA of the cluster runs before another one writes to its shared memory
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31;
-  const uint32_t rank = cluster_rank();
   const int b = blockIdx.x / kCluster;
-  const bool writer = rank == 0 && tid < 32;  // a warp writes the request's outputs
-  int n = p.draft_len[b];
-  if (n < 0 || n > p.max_draft) {
-    if (writer && lane == 0) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
-    n = 0;
-  }
+  const bool writer = cluster_rank() == 0 && tid < 32;  // a warp writes the request's outputs
   int32_t *path = p.path + (size_t)b * p.max_draft;
   const float *target = p.target + b * p.tb;
   const float *u = p.uniform + (size_t)b * p.max_draft;
+  // lane's tokens lane and lane + 32: read before their number is known
   const int32_t *tok = p.tokens + (size_t)b * p.max_draft;
+  const int i0 = lane, i1 = lane + 32;
+  const int tok0 = i0 < p.max_draft ? tok[i0] : -1, tok1 = i1 < p.max_draft ? tok[i1] : -1;
+  int n = p.draft_len[b];
+  const bool bad = n < 0 || n > p.max_draft;
+  if (bad) {
+    if (writer && lane == 0) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
+    n = 0;
+  }
   int len = 0, next = -1;
   if (n > 0 && p.draft) {
     // ---- a chain of sampled tokens: all tests at once, the first refusal
     const float *draft = p.draft + b * p.db;
     if (tid < 32) {
-      int r = n;  // the first refused token
-      for (int i0 = 1; i0 < n && r == n; i0 += 32) {
-        const int i = i0 + lane;
-        bool ok = true;
-        if (i < n) {
-          const int x = tok[i];
-          ok = false;
-          if (x >= 0 && x < p.vocab)
-            ok = __fmul_rn(u[i - 1], __ldg(draft + (i - 1) * p.dt + x)) <
-                 __ldg(target + (i - 1) * p.tt + x);
-        }
-        const unsigned no = __ballot_sync(0xffffffffu, !ok);
-        if (no) r = i0 + __ffs(no) - 1;
-      }
-      if (lane == 0) sh.first_refused = r;
+      auto refused = [&](int i, int x) {
+        if (i < 1 || i >= n) return false;
+        if (x < 0 || x >= p.vocab) return true;
+        return !(__fmul_rn(u[i - 1], __ldg(draft + (i - 1) * p.dt + x)) <
+                 __ldg(target + (i - 1) * p.tt + x));
+      };
+      const bool r0 = refused(i0, tok0), r1 = refused(i1, tok1);
+      const unsigned m0 = __ballot_sync(0xffffffffu, r0), m1 = __ballot_sync(0xffffffffu, r1);
+      if (lane == 0) sh.refused = m0 ? __ffs(m0) - 1 : m1 ? __ffs(m1) + 31 : n;
     }
     __syncthreads();
-    const int r = sh.first_refused;
-    len = r;
-    const float *row = target + (r - 1) * p.tt;
-    if (r < n) next = draw(sh, row, draft + (r - 1) * p.dt, p.vocab, u[n - 1]);
-    if (r == n || next < 0) next = draw(sh, row, nullptr, p.vocab, u[n - 1]);
+    len = sh.refused;
     if (writer)
       for (int i = lane; i < p.max_draft; i += 32) path[i] = i < len ? i : -1;
-  } else if (n > 0) {
+    if (writer && lane == 0) p.path_len[b] = len;
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    const float *row = target + (len - 1) * p.tt;
+    const float un = u[n - 1];
+    if (len < n && draw<true, false>(sh, 0, row, draft + (len - 1) * p.dt, p.vocab, un, p.next + b))
+      return;
+    if (!draw<false, false>(sh, 1, row, nullptr, p.vocab, un, p.next + b) && writer && lane == 0)
+      p.next[b] = -1;
+    return;
+  }
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  if (n > 0) {
     // ---- the target's draws down a tree
-    const int32_t *par = p.parent ? p.parent + (size_t)b * p.max_draft : nullptr;
+    int par0 = i0 - 1, par1 = i1 - 1;
+    if (p.parent) {
+      const int32_t *par = p.parent + (size_t)b * p.max_draft;
+      par0 = i0 < p.max_draft ? par[i0] : -1;
+      par1 = i1 < p.max_draft ? par[i1] : -1;
+    }
     int at = 0;
     if (writer && lane == 0) path[0] = 0;
     for (len = 1;; ++len) {
-      next = draw(sh, target + at * p.tt, nullptr, p.vocab, u[len - 1]);
-      int child = -1;
-      for (int c0 = 0; c0 < n && child < 0; c0 += 32) {  // each warp alike
-        const int c = c0 + lane;
-        const bool hit = c < n && c > at && next >= 0 && tok[c] == next &&
-                         (par ? par[c] : c - 1) == at;
-        const unsigned m = __ballot_sync(0xffffffffu, hit);
-        if (m) child = c0 + __ffs(m) - 1;
-      }
-      if (child < 0) break;
-      at = child;
+      next = draw<false, true>(sh, len & 1, target + at * p.tt, nullptr, p.vocab, u[len - 1], nullptr)
+                 ? sh.found : -1;
+      // each warp alike: the first child that carries the token
+      const bool h0 = i0 < n && i0 > at && tok0 == next && par0 == at && next >= 0;
+      const bool h1 = i1 < n && i1 > at && tok1 == next && par1 == at && next >= 0;
+      const unsigned m0 = __ballot_sync(0xffffffffu, h0), m1 = __ballot_sync(0xffffffffu, h1);
+      if (!(m0 | m1)) break;
+      at = m0 ? __ffs(m0) - 1 : __ffs(m1) + 31;
       if (writer && lane == 0) path[len] = at;
     }
-    if (writer)
-      for (int i = len + lane; i < p.max_draft; i += 32) path[i] = -1;
-  } else if (writer) {
-    for (int i = lane; i < p.max_draft; i += 32) path[i] = -1;
   }
-  if (writer && lane == 0) {
-    p.path_len[b] = len;
-    p.next[b] = next;
+  if (writer) {
+    for (int i = len + lane; i < p.max_draft; i += 32) path[i] = -1;
+    if (lane == 0) {
+      p.path_len[b] = len;
+      p.next[b] = next;
+    }
   }
-  cluster_sync_all();  // the others may still read this CTA's shared memory
 }
 
 }  // namespace verify
