@@ -273,9 +273,10 @@ struct FreeParams {
 
 // One CTA per listed row: the entries from the cut on are taken out one by
 // one (an exchange, so that a page goes back once whatever the call lists) and
-// their pages lose a user.  A row's entries are contiguous: the first 256 without
-// any page end the walk.
-__global__ void __launch_bounds__(256) release_kernel(FreeParams p) {
+// their pages lose a user.  A row's entries are contiguous: the first kReleaseThreads
+// without any page end the walk.
+constexpr int kReleaseThreads = 512;
+__global__ void __launch_bounds__(kReleaseThreads) release_kernel(FreeParams p) {
   pdl_entry();
   const int j = blockIdx.x, r = p.row[j];
   int cut = 0;
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(256) release_kernel(FreeParams p) {
     if (threadIdx.x == 0) p.ctx_len[r] = 0;
   }
   int32_t *t = p.block_table + (size_t)r * p.max_pages;
-  for (int e0 = cut; e0 < p.max_pages; e0 += 256) {
+  for (int e0 = cut; e0 < p.max_pages; e0 += kReleaseThreads) {
     const int e = e0 + (int)threadIdx.x;
     const int page = e < p.max_pages ? atomicExch(t + e, -1) : -1;
     if (page >= p.num_pages) {
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(256) release_kernel(FreeParams p) {
 constexpr int kSeg = 16;      // kept positions per CTA
 constexpr int kUnits = 8;     // 32-byte units of a thread
 constexpr int kMoveThreads = 256;
-constexpr int kCheckThreads = 1024, kCheckDeep = 4;
+constexpr int kCheckThreads = 1024, kCheckDeep = 8;
 
 struct CompactParams {
   int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, layers, layer_begin, rotate;
@@ -385,8 +386,8 @@ PIC_DEV int compact_entries(const CompactParams &p, int j, int s, const int *i, 
 
 // Lists of more than one segment, one CTA per listed row: every check before
 // anything moves (the verdict goes to result), the slots, the segments to wait
-// for, the flags cleared.  Four entries of a thread at a time, because an entry is
-// a chain of three loads: 9001 entries 33 us one at a time.
+// for, the flags cleared.  Eight entries of a thread at a time, because an entry is
+// a chain of three loads: 9001 entries 33 us one at a time with 256 threads.
 __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactParams p) {
   pdl_entry();
   const int j = blockIdx.x, tid = threadIdx.x;
@@ -480,7 +481,9 @@ __global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactPa
     __syncthreads();
     at = next_at;
   }
-  int buf = 0;
+  int buf = 0, turn_layer = -1;
+  const int f = tid % (D / 2);  // the frequency this thread forms cos/sin of
+  uint64_t turn = 0;            // (fp64 work: once, not once per segment)
   if (at < all) look_up(at, 0);
   __syncthreads();
   while (at < all) {
@@ -489,30 +492,32 @@ __global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactPa
     const int heads = min(p.hgroup, p.hkv - h0), cnt = next_cnt[buf], i0 = seg * kSeg;
     // ---- read: unit u = (position, K or V, head, chunk)
     const long long lbase = (long long)layer * p.layer_elems;
-    const int units = cnt * 2 * heads * KC;
-    auto where = [&](int u, bool to) {  // the unit's 16 positions' vector of one head
-      const int h = (u / KC) % heads, kv = (u / (KC * heads)) & 1, i = u / (KC * heads * 2);
-      const long long sl = to ? slot_of[buf][i].y : slot_of[buf][i].x;
-      return (kv ? p.v : p.k) + lbase +
-             (((sl / kPage) * p.hkv + h0 + h) * kPage + sl % kPage) * D;
+    // (division by KC heads <= 64 as a product: exact for u < 2048)
+    const int per = KC * heads, units = cnt * 2 * per, magic = ((1 << 20) + per - 1) / per;
+    auto pair_of = [&](int u) { return (u * magic) >> 20; };  // 2 * position + (0 K, 1 V)
+    auto where = [&](int u, int w, bool to) {
+      const int h = h0 + (u - w * per) / KC;
+      const long long sl = to ? slot_of[buf][w >> 1].y : slot_of[buf][w >> 1].x;
+      return (w & 1 ? p.v : p.k) + lbase + (((sl >> 4) * p.hkv + h) * kPage + (sl & 15)) * D;
     };
     uint4 a[kUnits], b[kUnits];
 #pragma unroll
     for (int q = 0; q < kUnits; ++q) {
-      const int u = tid + q * kMoveThreads;
-      if (u < units && k_of[buf][u / (KC * heads * 2)] != i0 + u / (KC * heads * 2)) {
-        const __nv_bfloat16 *src = where(u, false);
+      const int u = tid + q * kMoveThreads, w = pair_of(u);
+      if (u < units && k_of[buf][w >> 1] != i0 + (w >> 1)) {
+        const __nv_bfloat16 *src = where(u, w, false);
         a[q] = *reinterpret_cast<const uint4 *>(src + pc.off_a);
         b[q] = *reinterpret_cast<const uint4 *>(src + pc.off_b);
       }
     }
     if (kLong && tid == 0) next_at = atomicAdd(p.ticket, 1);
-    if (p.rotate)
-      for (int e = tid; e < cnt * (D / 2); e += kMoveThreads) {
-        const int i = e / (D / 2), f = e % (D / 2);
-        cs[i][f] = rope_cos_sin_turn(i0 + i - k_of[buf][i],
-                                     rope_turn(rope_theta(rp, p.layer_begin + layer, f)));
-      }
+    if (p.rotate) {
+      if (layer != turn_layer && (turn_layer < 0 || rp.layer_theta))
+        turn = rope_turn(rope_theta(rp, p.layer_begin + layer, f));
+      turn_layer = layer;
+      for (int i = tid / (D / 2); i < cnt; i += kMoveThreads / (D / 2))
+        cs[i][f] = rope_cos_sin_turn(i0 + i - k_of[buf][i], turn);
+    }
     if constexpr (kLong) {
       int32_t *fl = p.flags + ((long long)j * lhs + lh) * p.segs;
       __threadfence();
@@ -537,10 +542,10 @@ __global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactPa
     // ---- store
 #pragma unroll
     for (int q = 0; q < kUnits; ++q) {
-      const int u = tid + q * kMoveThreads, i = u / (KC * heads * 2);
+      const int u = tid + q * kMoveThreads, w = pair_of(u), i = w >> 1;
       if (u < units && k_of[buf][i] != i0 + i) {
-        __nv_bfloat16 *dst = const_cast<__nv_bfloat16 *>(where(u, true));
-        if (p.rotate && ((u / (KC * heads)) & 1) == 0) {
+        __nv_bfloat16 *dst = where(u, w, true);
+        if (p.rotate && !(w & 1)) {
           rotate_store(a[q], b[q], dst, pc, rp.style, &cs[i][8 * (tid % KC)]);
         } else {
           st_global16(dst + pc.off_a, a[q]);
@@ -832,7 +837,7 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
   if (e != cudaSuccess) return cuda_fail(e, who);
   FreeParams fp{n, rows, max_pages, num_pages, row, result, reserve, ctx_len, block_table, page_refs,
                 cp.status};
-  return launched(who, launch_dependent(release_kernel, dim3(n), dim3(256), 0, stream, fp));
+  return launched(who, launch_dependent(release_kernel, dim3(n), dim3(kReleaseThreads), 0, stream, fp));
 }
 
 extern "C" pic_status_t pic_page_free(int32_t n, const int32_t *row, int32_t rows, int32_t *ctx_len,
@@ -846,7 +851,7 @@ extern "C" pic_status_t pic_page_free(int32_t n, const int32_t *row, int32_t row
   FreeParams fp{n, rows, max_pages, num_pages, row, nullptr, 0, ctx_len, block_table, page_refs,
                 device_status_ptr()};
   if (!fp.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
-  return launched(who, launch_dependent(release_kernel, dim3(n), dim3(256), 0, stream, fp));
+  return launched(who, launch_dependent(release_kernel, dim3(n), dim3(kReleaseThreads), 0, stream, fp));
 }
 
 extern "C" pic_status_t pic_page_copy(const pic_geom_t *geom, int32_t n, const int32_t *src_page,
