@@ -277,6 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tbase = *tmem_slot;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int detail = -2;
 
   Segments sg(p, (int)blockIdx.x, (int)gridDim.x);
@@ -571,7 +572,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       ++s;
     }
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {

@@ -237,11 +237,12 @@ __global__ void __launch_bounds__(256) fork_kernel(ForkParams p) {
   const long long w = ((long long)blockIdx.x - p.table_blocks) * 8 + (threadIdx.x >> 5);
   const int j = (int)(w / ((long long)p.layers * p.hkv));
   if (j >= p.n) return;
-  const int len = p.result[j], full = len / kPage, rows = len % kPage;
+  const int len = p.result[j], src = p.src_row[j], dst = p.dst_row[j];  // one round trip
+  const int full = len / kPage, rows = len % kPage;
   if (len < 0 || rows == 0) return;
   const int rem = (int)(w % ((long long)p.layers * p.hkv)), l = rem / p.hkv, h = rem % p.hkv;
-  const int from = p.block_table[(size_t)p.src_row[j] * p.max_pages + full];
-  const int to = p.block_table[(size_t)p.dst_row[j] * p.max_pages + full];
+  const int from = p.block_table[(size_t)src * p.max_pages + full];
+  const int to = p.block_table[(size_t)dst * p.max_pages + full];
   const int pieces = rows * p.piece_row;  // at most 16 * 16
   const long long layer = (long long)l * p.layer_pieces;
   const long long a = layer + ((long long)from * p.hkv + h) * kPage * p.piece_row;
@@ -412,16 +413,15 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
   const bool bad = __syncthreads_or(code != PIC_DEV_OK);
   if (tid == 0) p.result[j] = bad ? -1 : s + m;
   if (bad) return;
-  // segment s2 reads up to keep[16 (s2 + 1) - 1], segment seg writes from 16 seg on
+  // segment s2 reads up to its last keep entry, segment seg writes from 16 seg
+  // on: s2 is the first to wait for of the segments that begin behind s2 - 1's
+  // last source and not behind its own
   const int32_t *kp = p.keep + (size_t)j * p.max_keep;
-  for (int seg = tid; seg < (m + kSeg - 1) / kSeg; seg += kCheckThreads) {
-    int lo = 0, hi = seg;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (kp[(mid + 1) * kSeg - 1] >= seg * kSeg) hi = mid;
-      else lo = mid + 1;
-    }
-    p.wait_from[(size_t)j * p.segs + seg] = lo;
+  const int segs = (m + kSeg - 1) / kSeg;
+  for (int s2 = tid; s2 < segs; s2 += kCheckThreads) {
+    const int lo = s2 ? kp[s2 * kSeg - 1] / kSeg : -1;
+    const int hi = min(kp[min((s2 + 1) * kSeg, m) - 1] / kSeg, segs - 1);
+    for (int seg = lo + 1; seg <= hi; ++seg) p.wait_from[(size_t)j * p.segs + seg] = s2;
   }
 }
 
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactPa
   __shared__ float2 cs[kSeg][D / 2];
   __shared__ int32_t k_of[2][kSeg];
   __shared__ longlong2 slot_of[2][kSeg];
-  __shared__ int next_at, next_cnt[2];
+  __shared__ int next_at, next_cnt[2], next_lo[2];
   const int tid = threadIdx.x, lhs = p.layers * p.hgroups;
   const long long all = (long long)lhs * p.n * p.segs;
   const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
@@ -452,13 +452,19 @@ __global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactPa
   auto look_up = [&](long long at, int buf) {
     const int j = (int)(at / lhs % p.n), seg = (int)(at / lhs / p.n);
     if constexpr (kLong) {
-      const int res = p.result[j], m = p.keep_len[j];
-      if (tid < kSeg) {
-        const size_t i = (size_t)j * p.max_keep + min(seg * kSeg + tid, p.max_keep - 1);
-        k_of[buf][tid] = p.keep[i];
-        slot_of[buf][tid] = p.slot[i];
+      // the last 16 threads: their loads run beside the others' polls
+      const int t = tid - (kMoveThreads - kSeg);
+      if (t >= 0) {
+        const size_t i = (size_t)j * p.max_keep + min(seg * kSeg + t, p.max_keep - 1);
+        const int k = p.keep[i], res = p.result[j], m = p.keep_len[j];
+        const int lo = p.wait_from[(size_t)j * p.segs + seg];
+        slot_of[buf][t] = p.slot[i];
+        k_of[buf][t] = k;
+        if (t == 0) {
+          next_cnt[buf] = res < 0 ? 0 : max(0, min(kSeg, m - seg * kSeg));
+          next_lo[buf] = lo;
+        }
       }
-      if (tid == 0) next_cnt[buf] = res < 0 ? 0 : max(0, min(kSeg, m - seg * kSeg));
     } else if (tid < 32) {
       int code = PIC_DEV_OK;
       const int s = compact_start(p, j, &code), m = s >= 0 ? p.keep_len[j] : 0;
@@ -526,9 +532,8 @@ __global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactPa
       bool ok = true;
       if (cnt > 0) {
         if (tid == 0) atomicExch(fl + seg, 1);
-        const int lo = p.wait_from[(size_t)j * p.segs + seg];
         if (after < all) look_up(after, buf ^ 1);
-        for (int s2 = seg - 1 - tid; ok && s2 >= lo; s2 -= kMoveThreads)
+        for (int s2 = seg - 1 - tid; ok && s2 >= next_lo[buf]; s2 -= kMoveThreads)
           ok = wait_flag(fl + s2, p.status, j);
       } else if (after < all) {
         look_up(after, buf ^ 1);
