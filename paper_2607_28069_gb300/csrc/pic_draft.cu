@@ -12,12 +12,12 @@
 // Launches:
 //  1. draft_append_kernel: per token its depth and ancestor bits, the rotated
 //     key and the value into their slots, the rotated queries packed.
-//  2. draft_attn_kernel: one persistent CTA per SM.  All (request, kv head, row
-//     tile) units' key tiles form one sequence, unit after unit, of which every
-//     CTA takes an equal share (the lengths are only known on the device, and
-//     batches are ragged), so no SM waits for a longer request's.  A CTA's share
-//     is a run of segments, each a range of one unit's key tiles; a unit that
-//     lies within one CTA is finished there, the others leave partial states.
+//  2. draft_attn_kernel: one persistent CTA per SM.  All (request, kv head, pair of
+//     row tiles) units' key tiles form one sequence, unit after unit, of which
+//     every CTA takes an equal share (the lengths are only known on the device,
+//     and batches are ragged), so no SM waits for a longer request's.  A CTA's
+//     share is a run of segments, each a range of one unit's key tiles; a unit
+//     that lies within one CTA is finished there, the others leave partial states.
 //  3. draft_merge_kernel: log-sum-exp merge of those.
 #include <algorithm>
 
@@ -30,10 +30,17 @@ constexpr int BM = 128, BN = 128;  // rows of a tile, keys of a tile
 constexpr int kMaxDraft = 64;
 constexpr int kCtas = 152;         // one per SM
 constexpr int NSK = 3, NSV = 2;    // ring stages of K and V
-constexpr int NQB = 2;             // query tiles: the present segment's and the next one's
-constexpr int kThreads = 256;      // K producer, MMA, V producer, -, four softmax warps
+constexpr int NQB = 2;             // query tiles
+constexpr int kThreads = 384;      // K producer, MMA, V producer, ring, two softmax warpgroups
+constexpr int kRegLaunch = 168;    // 65536 / kThreads, whole eights
+constexpr int kRegControl = 88, kRegSoftmax = 208;
+static_assert(128 * kRegControl + 256 * kRegSoftmax <= kThreads * kRegLaunch,
+              "setmaxnreg split exceeds the registers the CTA is launched with");
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColO = 256;    // S at 0 and 128, O at 256 and 256 + D
+constexpr uint32_t kColO = 256;    // S_t at 128 t, O_t at 256 + D t
+// Named barriers (0: __syncthreads): P_t from warpgroup t to the MMA warp, the
+// ring warp's word to the MMA warp, the two warpgroups' exchange.
+constexpr int kNbP = 1, kNbRing = 3, kNbPair = 4;
 
 template <int D>
 struct Layout {
@@ -41,7 +48,8 @@ struct Layout {
   static constexpr int kQ = 0;
   static constexpr int kK = kQ + NQB * kTile;
   static constexpr int kV = kK + NSK * kTile;
-  static constexpr int kBar = kV + NSV * kTile;
+  static constexpr int kML = kV + NSV * kTile;  // float [2][BM]: the warpgroups' m, then l
+  static constexpr int kBar = kML + 2 * BM * 4;
   static constexpr int kAlloc = kBar + 256 + 1024;
 };
 
@@ -53,49 +61,114 @@ enum {
   B_VFULL = B_KEMPTY + NSK,
   B_VEMPTY = B_VFULL + NSV,
   B_VFIX = B_VEMPTY + NSV,   // per V stage: the rows behind the last draft are cleared
-  B_SFULL = B_VFIX + NSV,    // S(g) in buffer g % 2
-  B_P = B_SFULL + 2,         // P(g) in buffer g % 2
-  B_PV = B_P + 2,            // PV(g) done, g % 2
-  B_OEMPTY = B_PV + 2,       // O buffer read
-  B_END = B_OEMPTY + 2,
+  B_SFULL = B_VFIX + NSV,    // S_t
+  B_OEND = B_SFULL + 2,      // a segment's last PV of warpgroup t
+  B_ODONE = B_OEND + 2,      // a segment's O read by both warpgroups
+  B_END = B_ODONE + 1,
   B_COUNT = B_END + 1
 };
 static_assert(B_COUNT * 8 + 16 <= 256, "barrier area");
 
 struct Params {
-  int batch, max_draft, Hq, Hkv, G, r_pad, rt_max, max_pages, oob_row, layer;
+  int batch, max_draft, Hq, Hkv, G, r_pad, rp_max, max_pages, oob_row, layer;
   long long num_pages, layer_row0;
   const int32_t *ctx_len, *draft_len, *parent, *block_table;
   const __nv_bfloat16 *q, *k_new, *v_new;
   __nv_bfloat16 *k_cache, *v_cache;  // at the layer
   __nv_bfloat16 *qp;                 // workspace: packed rotated queries
   uint64_t *mask;                    // workspace: [batch][max_draft] ancestor bits
-  int2 *unit;                        // workspace: [batch][Hkv][rt_max] first and last CTA
-  float *part_o;                     // workspace: [2 kCtas][BM][D]
-  float2 *part_ml;                   // workspace: [2 kCtas][BM]
+  struct Share *share;               // workspace: [kCtas] each CTA's start
+  int2 *unit;                        // workspace: [batch][Hkv][rp_max] first and last CTA
+  float *part_o;                     // workspace: [kCtas][2][row tile of the pair][BM][D]
+  float2 *part_ml;                   // the same without [D]
   __nv_bfloat16 *out;
   float *lse;
   int32_t *status;
   float scale_log2;
 };
 
-// What a request brings: its key tiles and row tiles (0 for one left alone).
+// What a request brings: its key tiles, row tiles and pairs of row tiles (0 for
+// one left alone).
 struct Request {
-  int ctx, n, tiles, rt;
+  int ctx, n, tiles, rt, rp;
 };
-PIC_DEV Request request_of(const Params &p, int b) {
+PIC_DEV Request request_of(const Params &p, int ctx, int n) {
   Request r;
-  r.ctx = p.ctx_len[b];
-  r.n = p.draft_len[b];
+  r.ctx = ctx;
+  r.n = n;
   const bool ok = r.ctx >= 0 && r.n > 0 && r.n <= p.max_draft &&
                   (long long)r.ctx + r.n <= (long long)p.max_pages * 16;
   if (!ok) r.ctx = r.n = 0;
   r.tiles = ok ? (r.ctx + r.n + BN - 1) / BN : 0;
   r.rt = (r.n * p.G + BM - 1) / BM;
+  r.rp = (r.rt + 1) / 2;
   return r;
+}
+PIC_DEV Request request_of(const Params &p, int b) {
+  return request_of(p, p.ctx_len[b], p.draft_len[b]);
+}
+
+// A CTA's share of the batch's key tiles (of which there are `total`, dealt to
+// `ctas` CTAs): tiles [pos, end), the first of them in request b, whose first tile
+// is `base`.
+struct alignas(16) Share {
+  int total, ctas, pos, end, b, base, ctx, n;  // ctx, n: request b's
+};
+
+PIC_DEV int work_of(const Params &p, const Request &r) { return p.Hkv * r.rp * r.tiles; }
+
+// One warp: the shares of CTAs lane, lane + 32, ... in `grid` CTAs.  Every CTA
+// that takes part has a tile.
+PIC_DEV void deal_shares(const Params &p, int grid) {
+  const int lane = threadIdx.x & 31;
+  int total = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    int w = b0 + lane < p.batch ? work_of(p, request_of(p, b0 + lane)) : 0;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+    total += w;
+  }
+  const int ctas = min(grid, total);
+  constexpr int kPer = (kCtas + 31) / 32;
+  Share sh[kPer];
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int c = lane + 32 * q;
+    sh[q] = Share{total, ctas, 0, 0, 0, 0, 0, 0};
+    if (c < ctas) {
+      sh[q].pos = (int)((long long)total * c / ctas);
+      sh[q].end = (int)((long long)total * (c + 1) / ctas);
+    }
+  }
+  int base = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    const Request r = b0 + lane < p.batch ? request_of(p, b0 + lane) : Request{0, 0, 0, 0, 0};
+    const int w = work_of(p, r);
+    int x = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    // lane l's request holds tiles [base + x - w, base + x)
+    for (int l = 0; l < min(32, p.batch - b0); ++l) {
+      const int hi = base + __shfl_sync(0xffffffffu, x, l), lo = hi - __shfl_sync(0xffffffffu, w, l);
+      const int ctx = __shfl_sync(0xffffffffu, r.ctx, l), n = __shfl_sync(0xffffffffu, r.n, l);
+#pragma unroll
+      for (int q = 0; q < kPer; ++q)
+        if (sh[q].end > 0 && sh[q].pos >= lo && sh[q].pos < hi)
+          sh[q].b = b0 + l, sh[q].base = lo, sh[q].ctx = ctx, sh[q].n = n;
+    }
+    base += __shfl_sync(0xffffffffu, x, 31);
+  }
+#pragma unroll
+  for (int q = 0; q < kPer; ++q)
+    if (lane + 32 * q < grid) p.share[lane + 32 * q] = sh[q];
 }
 
 // ------------------------------------------------------------------ append
+// One CTA per token, and one more (blockIdx.x = max_draft of the first request)
+// that deals out the key tiles.
 template <int D>
 __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams rp) {
   constexpr int KC = D / 16;
@@ -103,6 +176,10 @@ __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams 
   __shared__ float2 cs[D / 2];
   __shared__ int32_t par[kMaxDraft];
   __shared__ int depth;
+  if ((int)blockIdx.x == p.max_draft) {
+    if (blockIdx.y == 0 && threadIdx.x < 32) deal_shares(p, kCtas);
+    return;
+  }
   const int b = blockIdx.y, i = blockIdx.x, tid = threadIdx.x;
   const int ctx = p.ctx_len[b], n = p.draft_len[b];
   const bool bad = ctx < 0 || n < 0 || n > p.max_draft;
@@ -167,83 +244,73 @@ __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams 
 // The segments of one CTA, walked by each role's warp for itself.
 struct Segments {
   const Params &p;
-  long long total, pos, end;  // key tiles of the batch, next tile, end of this CTA's share
-  long long base;             // first tile of request b
+  int total, pos, end;  // key tiles of the batch (the host keeps them below 2^31), next
+                        // tile, end of this CTA's share
+  int base;             // first tile of request b
   int b, cta, ctas;
   Request r;
   // the present segment
-  int hk, rt, kt0, n;
+  int hk, pair, kt0, n;
+  bool two;          // the pair has two row tiles
   bool first, last;  // holds the unit's first, last key tile
-  long long unit0;   // the unit's first tile
+  int unit0;         // the unit's first tile
 
-  PIC_DEV long long work(const Request &x) const { return (long long)p.Hkv * x.rt * x.tiles; }
-
-  PIC_DEV Segments(const Params &pp, int cta_, int grid) : p(pp), cta(cta_) {
-    const int lane = threadIdx.x & 31;
-    total = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-      long long w = b0 + lane < p.batch ? work(request_of(p, b0 + lane)) : 0;
-#pragma unroll
-      for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-      total += w;
-    }
-    // every CTA that takes part has a tile
-    ctas = (int)min((long long)grid, total);
-    base = pos = end = 0;
-    b = 0;
-    if (cta >= ctas) return;
-    pos = total * cta / ctas;
-    end = total * (cta + 1) / ctas;
-    // the request that holds tile `pos`
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-      long long w = b0 + lane < p.batch ? work(request_of(p, b0 + lane)) : 0, x = w;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      const unsigned past = __ballot_sync(0xffffffffu, base + x > pos);
-      if (past) {
-        const int l = __ffs(past) - 1;
-        b = b0 + l;
-        base += __shfl_sync(0xffffffffu, x - w, l);
-        break;
-      }
-      base += __shfl_sync(0xffffffffu, x, 31);
-    }
-    r = request_of(p, b);
+  PIC_DEV Segments(const Params &pp, int cta_) : p(pp), cta(cta_) {
+    const int4 *q = reinterpret_cast<const int4 *>(p.share + cta);
+    const int4 x = q[0], y = q[1];
+    total = x.x, ctas = x.y, pos = x.z, end = x.w;
+    b = y.x, base = y.y;
+    r = request_of(p, y.z, y.w);
   }
   PIC_DEV bool next() {
     if (pos >= end) return false;
-    while (pos - base >= work(r)) {
-      base += work(r);
+    while (pos - base >= work_of(p, r)) {
+      base += work_of(p, r);
       r = request_of(p, ++b);
     }
-    const int u = (int)((pos - base) / r.tiles);
-    unit0 = base + (long long)u * r.tiles;
-    kt0 = (int)(pos - unit0);
-    n = (int)min((long long)(r.tiles - kt0), end - pos);
-    hk = u / r.rt;
-    rt = u % r.rt;
+    const int u = (pos - base) / r.tiles;
+    unit0 = base + u * r.tiles;
+    kt0 = pos - unit0;
+    n = min(r.tiles - kt0, end - pos);
+    hk = u / r.rp;
+    pair = u % r.rp;
+    two = 2 * pair + 1 < r.rt;
     first = kt0 == 0;
     last = kt0 + n == r.tiles;
     pos += n;
     return true;
   }
   // the CTA whose share holds tile t
-  PIC_DEV int owner(long long t) const { return (int)(((t + 1) * ctas - 1) / total); }
-  // the partial slot of the present segment: a CTA has at most one segment
-  // that ends a unit begun elsewhere or lies inside one (0), and one that begins
-  // a unit and leaves its end to others (1)
-  PIC_DEV int slot() const { return 2 * cta + (first ? 1 : 0); }
+  PIC_DEV int owner(int t) const { return (int)(((long long)(t + 1) * ctas - 1) / total); }
+  // the partial slot of row tile t of the present segment: a CTA has at most
+  // one segment that ends a unit begun elsewhere or lies inside one (0), and one
+  // that begins a unit and leaves its end to others (1)
+  PIC_DEV int slot(int t) const { return (2 * cta + (first ? 1 : 0)) * 2 + t; }
+  // key tiles of warpgroup t (see draft_attn_kernel)
+  PIC_DEV int count(int t) const { return two ? n : (n + 1 - t) / 2; }
 };
 
 // --------------------------------------------------------------- attention
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
-    draft_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
-                      const __grid_constant__ CUtensorMap tm_k,
-                      const __grid_constant__ CUtensorMap tm_v, Params p) {
+// Two softmax warpgroups, one query row per thread, each with its scores S_t and
+// its accumulator O_t in TMEM.  Where a unit has two row tiles, warpgroup t takes
+// row tile t, and both read every key tile; with one row tile, warpgroup t takes
+// the key tiles of parity t, and the two states are joined at the segment's end
+// (each warpgroup half of the columns).  Either way one warpgroup's softmax runs
+// beside the other's MMAs.  MMA order, for t = 0, 1, 0, ...: PV_t of warpgroup t's
+// tile before, QK_t of its next one, across segments.  MMAs complete in order, so
+// S_t full means that PV_t has finished and O_t may be rescaled; O_t is only
+// rescaled when a row's maximum grew by more than 2^8.
+//
+// Waits: the MMA warp meets the ring warp (which waits for K, V, Q and the
+// accumulators on its behalf) and the softmax warps on named barriers only.  These
+// have no limit, so after a wait that ran out every role still walks all segments
+// and meets each barrier; the MMA warp then issues nothing but its commits.
+// The body is one function per group of warps (kSoftmax: the two softmax
+// warpgroups, else the four control warps), entered right after the group's
+// setmaxnreg, so that no value lives across the reallocation.
+template <int D, bool kSoftmax>
+PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
+                             const CUtensorMap &tm_v, const Params &p) {
   using L = Layout<D>;
   constexpr int PANELS = D / 64;
   constexpr uint32_t IDESC_QK = idesc_bf16(BM, BN, false, false);
@@ -262,8 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < B_COUNT; ++i)
-      mbar_init(bar(i), (i == B_P || i == B_P + 1 || i == B_OEMPTY || i == B_OEMPTY + 1) ? 4 : 1);
+    for (int i = 0; i < B_COUNT; ++i) mbar_init(bar(i), i == B_ODONE ? 8 : 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -280,199 +346,44 @@ __global__ void __launch_bounds__(kThreads, 1)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int detail = -2;
 
-  Segments sg(p, (int)blockIdx.x, (int)gridDim.x);
-  if (warp == 0 || warp == 2) {
-    // ===================================================== TMA producers
-    // Warp 0 the query tile of each segment and K, warp 2 V.  Lane l < 8
-    // moves page l of a tile as one box.
-    const bool is_k = warp == 0;
-    const int nst = is_k ? NSK : NSV;
-    const int b_full = is_k ? B_KFULL : B_VFULL, b_empty = is_k ? B_KEMPTY : B_VEMPTY;
-    const uint32_t ring = sbase + (is_k ? L::kK : L::kV);
-    const CUtensorMap *tmap = is_k ? &tm_k : &tm_v;
-    int g = 0, s = 0;   // tiles and segments issued
-    bool ok = true;
-    while (ok && sg.next()) {
-      if (is_k) {
-        if (s >= NQB)
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(B_QEMPTY + s % NQB), (s / NQB - 1) & 1,
-                                                 abort_flag, p.status, detail));
-        if (!ok) break;
-        if (lane == 0) {
-          mbar_expect_tx(bar(B_QFULL + s % NQB), L::kTile);
-          const int row = (sg.b * p.Hkv + sg.hk) * p.r_pad + sg.rt * BM;
-#pragma unroll
-          for (int pn = 0; pn < PANELS; ++pn)
-            tma_load_2d(sbase + L::kQ + (s % NQB) * L::kTile + pn * BM * 128, &tm_q, pn * 64, row,
-                        bar(B_QFULL + s % NQB));
-        }
-        __syncwarp();
-      }
-      ++s;
-      const int32_t *bt = p.block_table + (size_t)sg.b * p.max_pages;
-      const int keys = sg.r.ctx + sg.r.n;
-      for (int j = 0; j < sg.n; ++j, ++g) {
-        const int st = g % nst, kt = sg.kt0 + j;
-        int y = p.oob_row;  // zeros
-        const int pidx = kt * 8 + lane;
-        if (lane < 8 && (long long)pidx * 16 < keys && pidx < p.max_pages) {
-          const int page = bt[pidx];
-          if (page >= 0 && page < p.num_pages)
-            y = (int)(p.layer_row0 + ((long long)page * p.Hkv + sg.hk) * 16);
-          else if (is_k)
-            dev_fail(p.status, PIC_DEV_BAD_PAGE, sg.b);
-        }
-        if (g >= nst) {
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(b_empty + st), (g / nst - 1) & 1, abort_flag,
-                                                 p.status, detail));
-          if (!ok) break;
-        }
-        if (lane == 0) mbar_expect_tx(bar(b_full + st), L::kTile);
-        __syncwarp();
-        if (lane < 8) {
-          const uint32_t dst = ring + st * L::kTile + lane * kPageBytes;
-          if constexpr (PANELS == 2)
-            tma_load_4d(dst, tmap, 0, 0, 0, y >> 3, bar(b_full + st));
-          else
-            tma_load_2d(dst, tmap, 0, y, bar(b_full + st));
-        }
-        if (!is_k && kt != sg.r.tiles - 1) {
-          if (lane == 0) mbar_arrive(bar(B_VFIX + st));
-        } else if (!is_k) {
-          // Rows behind the last draft may hold anything, and a weight of zero
-          // does not silence an infinity: they are cleared before PV reads them
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(b_full + st), (g / nst) & 1, abort_flag,
-                                                 p.status, detail));
-          if (!ok) {
-            ++g;
-            break;
-          }
-          const int r0 = keys - kt * BN, r1 = (r0 + 15) & ~15;  // the rest of its page
-          constexpr int CH = D / 8;
-          for (int e = lane; e < (r1 - r0) * CH; e += 32) {
-            const int row = r0 + e / CH, ch = e % CH, rr = row & 15;
-            const uint32_t off =
-                PANELS == 2 ? (uint32_t)((rr >> 3) * 2048 + (ch >> 3) * 1024 + (rr & 7) * 128 +
-                                         (((ch & 7) ^ (rr & 7)) << 4))
-                            : (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4));
-            sts128(ring + st * L::kTile + (row >> 4) * kPageBytes + off, make_uint4(0, 0, 0, 0));
-          }
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(B_VFIX + st));
-        }
-      }
-    }
-    // what was issued lands before the CTA exits
-    if (lane == 0) {
-      for (int j = max(0, g - nst); j < g; ++j)
-        mbar_wait_no_flag(bar(b_full + j % nst), (j / nst) & 1, p.status, detail, kWaitLimitNs);
-      if (is_k)
-        for (int j = max(0, s - NQB); j < s; ++j)
-          mbar_wait_no_flag(bar(B_QFULL + j % NQB), (j / NQB) & 1, p.status, detail, kWaitLimitNs);
-    }
-  } else if (warp == 1) {
-    // ===================================================== MMA issuer
-    // The tiles of all segments in one sequence g: QK(g + 1) is issued before
-    // PV(g), so the scores of the next tile are there when a softmax ends.
-    const uint32_t el = elect_one();
-    const uint32_t ub = __shfl_sync(0xffffffffu, tbase, 0);
-    const MatDesc dQ = sdesc_sw128(sbase + L::kQ, 16, 1024);
-    const MatDesc dK = sdesc_sw128(sbase + L::kK, 16, kGroupStride);
-    const MatDesc dV = sdesc_sw128(sbase + L::kV, kPanelOff, kGroupStride);
-    bool ok = true;
-    auto wait = [&](int i, uint32_t parity) {
-      if (ok)
-        ok = __all_sync(0xffffffffu, mbar_wait(bar(i), parity, abort_flag, p.status, detail));
-      return ok;
-    };
-    // the tile whose QK was issued last waits for its PV
-    int g = 0, s = 0;
-    bool have = false, pv_first = false, pv_lasttile = false;
-    int pv_s = 0;
-    auto pv = [&](int gg) {
-      const int st = gg % NSV, ob = pv_s & 1;
-      wait(B_VFULL + st, (gg / NSV) & 1);
-      if (pv_lasttile) wait(B_VFIX + st, (gg / NSV) & 1);
-      if (pv_first && pv_s >= 2) wait(B_OEMPTY + ob, (pv_s / 2 - 1) & 1);
-      wait(B_P + (gg & 1), (gg >> 1) & 1);
-      if (!ok) return;
-      tc_fence_after();
-      const uint32_t tO = ub + kColO + ob * D, tP = ub + (gg & 1) * 128;
-      const MatDesc dv = dV.at(st * L::kTile);
-#pragma unroll
-      for (int kk = 0; kk < BN / 16; ++kk)
-        mma_ts(tO, tP + kk * 8, dv.at(kk * kPageBytes), IDESC_PV, !(pv_first && kk == 0), el);
-      mma_commit(bar(B_VEMPTY + st), el);
-      mma_commit(bar(B_PV + (gg & 1)), el);
-    };
-    while (ok && sg.next()) {
-      wait(B_QFULL + s % NQB, (s / NQB) & 1);
-      for (int j = 0; ok && j < sg.n; ++j, ++g) {
-        const int st = g % NSK;
-        if (!wait(B_KFULL + st, (g / NSK) & 1)) break;
-        tc_fence_after();
-        const uint32_t tS = ub + (g & 1) * 128;
-        const MatDesc dq = dQ.at((s % NQB) * L::kTile), dk = dK.at(st * L::kTile);
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-          mma_ss(tS, dq.at((kk >> 2) * (BM * 128) + (kk & 3) * 32),
-                 dk.at((kk >> 2) * kPanelOff + (kk & 3) * 32), IDESC_QK, kk > 0, el);
-        mma_commit(bar(B_KEMPTY + st), el);
-        if (j == sg.n - 1) mma_commit(bar(B_QEMPTY + s % NQB), el);
-        mma_commit(bar(B_SFULL + (g & 1)), el);
-        if (have) pv(g - 1);
-        have = true;
-        pv_first = j == 0;
-        pv_lasttile = sg.kt0 + j == sg.r.tiles - 1;
-        pv_s = s;
-      }
-      ++s;
-    }
-    if (ok && have) pv(g - 1);
-    mma_commit(bar(B_END), el);
-    if (lane == 0) mbar_wait_no_flag(bar(B_END), 0, p.status, detail, 4 * kWaitLimitNs);
-    __syncwarp();
-  } else if (warp >= 4) {
+  Segments sg(p, (int)blockIdx.x);
+  if constexpr (kSoftmax) {
     // ===================================================== softmax
-    // One thread per row; tile g's scores from TMEM, the exponentials back as
-    // bf16 over them.  O is rescaled only when a row's maximum grew by more than
-    // 2^8; sums and O stay within fp32 (exponents up to 2^8, P in bf16).
-    const int wq = warp & 3, row = wq * 32 + lane;
+    const int t = (warp - 4) >> 2, wq = warp & 3, row = wq * 32 + lane;
     const uint32_t tl = tbase + ((uint32_t)(wq * 32) << 16);
-    int g = 0, s = 0;
+    const uint32_t tS = tl + t * 128, tO = tl + kColO + t * D;
+    float *ml_s = reinterpret_cast<float *>(smem + L::kML);
+    int nS = 0, nEnd = 0;  // tiles and segments of this warpgroup
     bool ok = true;
+    // The MMA warp commits every S_t and every segment's end, also after an abort
     auto wait = [&](int i, uint32_t parity) {
-      if (ok)
-        ok = __all_sync(0xffffffffu, mbar_wait(bar(i), parity, abort_flag, p.status, detail));
-      return ok;
+      const bool was = ok;
+      ok = mbar_wait_while(ok, bar(i), parity, p.status, detail, 4 * kWaitLimitNs);
+      if (was && !ok) *abort_flag = 1;
     };
-    while (ok && sg.next()) {
-      const int ob = s & 1;
-      const uint32_t tO = tl + kColO + ob * D;
-      const int rr = sg.rt * BM + row;
-      const bool valid = rr < sg.r.n * p.G;
-      const int tok = valid ? rr / p.G : 0, head = sg.hk * p.G + (valid ? rr % p.G : 0);
-      const uint64_t mask = valid ? p.mask[(size_t)sg.b * p.max_draft + tok] : 0;
+    while (sg.next()) {
+      const int n = sg.count(t);
+      // this thread's row: token rr / G, query head hk G + rr % G
+      auto row_of = [&]() { return (2 * sg.pair + (sg.two ? t : 0)) * BM + row; };
       if (sg.first && threadIdx.x == 128)
-        p.unit[((size_t)sg.b * p.Hkv + sg.hk) * p.rt_max + sg.rt] =
+        p.unit[((size_t)sg.b * p.Hkv + sg.hk) * p.rp_max + sg.pair] =
             make_int2((int)blockIdx.x, sg.owner(sg.unit0 + sg.r.tiles - 1));
       float m_used = -INFINITY, l = 0.f;
-      for (int j = 0; j < sg.n; ++j, ++g) {
-        if (!wait(B_SFULL + (g & 1), (g >> 1) & 1)) break;
-        // PV(g - 2) is done (its commit precedes that of S(g)); waited for all the
-        // same, so that this barrier is never more than one phase ahead of its waiter
-        if (g >= 2 && !wait(B_PV + (g & 1), ((g >> 1) - 1) & 1)) break;
+      for (int i = 0; i < n; ++i, ++nS) {
+        const int kt = sg.kt0 + (sg.two ? i : 2 * i + t);
+        wait(B_SFULL + t, nS & 1);
         tc_fence_after();
-        const uint32_t tS = tl + (g & 1) * 128;
         float x[BN];
 #pragma unroll
         for (int c = 0; c < BN / 32; ++c) tmem_ld32(tS + c * 32, reinterpret_cast<uint32_t *>(x + c * 32));
         tmem_wait_ld();
-        const int off = (sg.kt0 + j) * BN - sg.r.ctx;  // key c of the tile is draft off + c
+        const int off = kt * BN - sg.r.ctx;  // key c of the tile is draft off + c
         if (off > -BN) {
           // its visible keys as 128 bits: all below the context's end, then the
           // ancestors' bits
+          const int rr = row_of();
+          const uint64_t mask =
+              rr < sg.r.n * p.G ? p.mask[(size_t)sg.b * p.max_draft + rr / p.G] : 0;
           uint32_t w[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
@@ -489,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < BN; c += 8)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) mx[i] = max3f(mx[i], x[c + 2 * i], x[c + 2 * i + 1]);
+          for (int q = 0; q < 4; ++q) mx[q] = max3f(mx[q], x[c + 2 * q], x[c + 2 * q + 1]);
         const float m_new = fmaxf(m_used, max3f(mx[0], mx[1], fmaxf(mx[2], mx[3])) * p.scale_log2);
         const bool resc = m_new > m_used + 8.f;
         float alpha = 1.f;
@@ -497,9 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           alpha = ex2(m_used - m_new);
           m_used = m_new;
         }
-        if (j > 0 && __any_sync(0xffffffffu, resc)) {
-          if (!wait(B_PV + ((g - 1) & 1), ((g - 1) >> 1) & 1)) break;  // PV(g - 1) has finished
-          tc_fence_after();
+        if (i > 0 && __any_sync(0xffffffffu, resc)) {
 #pragma unroll 1
           for (int c = 0; c < D / 16; ++c) {
             float o[16];
@@ -532,28 +441,65 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_P + (g & 1)));
+        named_bar_arrive(kNbP + t, 128 + 32);
       }
-      if (!ok) break;
-      // ---- the segment's last PV, then its rows
-      if (!wait(B_PV + ((g - 1) & 1), ((g - 1) >> 1) & 1)) break;
-      tc_fence_after();
-      const bool whole = sg.first && sg.last;
-      const size_t o_row = (((size_t)sg.b * p.max_draft + tok) * p.Hq + head);
-      const size_t p_row = (size_t)sg.slot() * BM + row;
+      // ---- the segment's rows: after its last PV, o = w_0 O_0 + w_1 O_1 (with one
+      // row tile), or O_t alone
+      if (n > 0) {
+        wait(B_OEND + t, nEnd & 1);
+        ++nEnd;
+        tc_fence_after();
+      }
+      float M = m_used, w0 = 1.f, w1 = 0.f;
+      if (!sg.two) {  // m, then l through one array of shared memory
+        auto exchange = [&](float v) {
+          ml_s[t * BM + row] = v;
+          named_bar_sync(kNbPair, 256);
+          const float other = ml_s[(t ^ 1) * BM + row];
+          named_bar_sync(kNbPair, 256);
+          return other;
+        };
+        tc_fence_before();
+        const float mo = exchange(m_used), lo = exchange(l);
+        tc_fence_after();
+        M = fmaxf(m_used, mo);
+        const float wt = m_used == -INFINITY ? 0.f : ex2(m_used - M);
+        const float wo = mo == -INFINITY ? 0.f : ex2(mo - M);
+        l = t ? fmaf(lo, wo, l * wt) : fmaf(l, wt, lo * wo);  // l_0 w_0 + l_1 w_1 in both
+        w0 = t ? wo : wt;
+        w1 = t ? wt : wo;
+      }
+      const int rr = row_of();
+      const bool valid = rr < sg.r.n * p.G;
+      const bool store = valid && ok && !*abort_flag, whole = sg.first && sg.last;
+      const size_t o_row = ((size_t)sg.b * p.max_draft + rr / p.G) * p.Hq + sg.hk * p.G + rr % p.G;
+      const size_t p_row = (size_t)sg.slot(sg.two ? t : 0) * BM + row;
       const float inv = l > 0.f ? 1.f / l : 0.f;
+      const int c_begin = sg.two ? 0 : t * (D / 64), c_end = sg.two ? D / 32 : (t + 1) * (D / 64);
+      const uint32_t tA = sg.two ? tO : tl + kColO;
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
+      for (int c = c_begin; c < c_end; ++c) {
         float o[32];
-        tmem_ld32(tO + c * 32, reinterpret_cast<uint32_t *>(o));
+        tmem_ld32(tA + c * 32, reinterpret_cast<uint32_t *>(o));
         tmem_wait_ld();
+        if (!sg.two) {
+#pragma unroll
+          for (int q = 0; q < 32; ++q) o[q] *= w0;
+          if (sg.n > 1) {  // (with one tile O_1 was never written)
+            float o1[32];
+            tmem_ld32(tA + D + c * 32, reinterpret_cast<uint32_t *>(o1));
+            tmem_wait_ld();
+#pragma unroll
+            for (int q = 0; q < 32; ++q) o[q] = fmaf(o1[q], w1, o[q]);
+          }
+        }
         if (whole) {
 #pragma unroll
           for (int q = 0; q < 32; ++q) o[q] *= inv;
-          if (valid)
+          if (store)
 #pragma unroll
             for (int q = 0; q < 4; ++q) st_global16(p.out + o_row * D + c * 32 + q * 8, pack8(o + q * 8));
-        } else if (valid) {
+        } else if (store) {
 #pragma unroll
           for (int q = 0; q < 8; ++q)
             *reinterpret_cast<float4 *>(p.part_o + p_row * D + c * 32 + q * 4) =
@@ -562,15 +508,221 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_OEMPTY + ob));
-      if (whole) {
-        if (valid && p.lse)
-          p.lse[o_row] = l > 0.f ? (m_used + __log2f(l)) * 0.69314718055994531f : -INFINITY;
-      } else if (valid) {
-        p.part_ml[p_row] = make_float2(l > 0.f ? m_used : -INFINITY, l);
+      if (lane == 0) mbar_arrive(bar(B_ODONE));
+      if (store && (sg.two || t == 0)) {
+        if (!whole)
+          p.part_ml[p_row] = make_float2(l > 0.f ? M : -INFINITY, l);
+        else if (p.lse)
+          p.lse[o_row] = l > 0.f ? (M + __log2f(l)) * 0.69314718055994531f : -INFINITY;
       }
+    }
+  } else if (warp == 0 || warp == 2) {
+    // ===================================================== TMA producers
+    // Warp 0 the query tiles of each segment and K, warp 2 V.  Lane l < 8
+    // moves page l of a tile as one box.
+    const bool is_k = warp == 0;
+    const int nst = is_k ? NSK : NSV;
+    const int b_full = is_k ? B_KFULL : B_VFULL, b_empty = is_k ? B_KEMPTY : B_VEMPTY;
+    const uint32_t ring = sbase + (is_k ? L::kK : L::kV);
+    const CUtensorMap *tmap = is_k ? &tm_k : &tm_v;
+    int g = 0, nq = 0;  // key and query tiles issued
+    bool ok = true;
+    auto wait = [&](int i, uint32_t parity) {
+      if (ok)
+        ok = __all_sync(0xffffffffu, mbar_wait(bar(i), parity, abort_flag, p.status, detail));
+      return ok;
+    };
+    while (ok && sg.next()) {
+      const int32_t *bt = p.block_table + (size_t)sg.b * p.max_pages;
+      const int keys = sg.r.ctx + sg.r.n;
+      auto page_row = [&](int kt) {  // lanes 0..7: the row of page `lane` of tile kt
+        int y = p.oob_row;  // zeros
+        const int pidx = kt * 8 + lane;
+        if (lane < 8 && (long long)pidx * 16 < keys && pidx < p.max_pages) {
+          const int page = bt[pidx];
+          if (page >= 0 && page < p.num_pages)
+            y = (int)(p.layer_row0 + ((long long)page * p.Hkv + sg.hk) * 16);
+          else if (is_k)
+            dev_fail(p.status, PIC_DEV_BAD_PAGE, sg.b);
+        }
+        return y;
+      };
+      int y_next = page_row(sg.kt0);
+      if (is_k)
+        for (int t = 0; t <= (sg.two ? 1 : 0); ++t, ++nq) {
+          const int qb = nq % NQB;
+          if (nq >= NQB && !wait(B_QEMPTY + qb, (nq / NQB - 1) & 1)) break;
+          if (lane == 0) {
+            mbar_expect_tx(bar(B_QFULL + qb), L::kTile);
+            const int row = (sg.b * p.Hkv + sg.hk) * p.r_pad + (2 * sg.pair + t) * BM;
+#pragma unroll
+            for (int pn = 0; pn < PANELS; ++pn)
+              tma_load_2d(sbase + L::kQ + qb * L::kTile + pn * BM * 128, &tm_q, pn * 64, row,
+                          bar(B_QFULL + qb));
+          }
+          __syncwarp();
+        }
+      for (int j = 0; ok && j < sg.n; ++j) {
+        const int st = g % nst, kt = sg.kt0 + j, y = y_next;
+        if (j + 1 < sg.n) y_next = page_row(kt + 1);
+        if (g >= nst && !wait(b_empty + st, (g / nst - 1) & 1)) break;
+        if (lane == 0) mbar_expect_tx(bar(b_full + st), L::kTile);
+        __syncwarp();
+        if (lane < 8) {
+          const uint32_t dst = ring + st * L::kTile + lane * kPageBytes;
+          if constexpr (PANELS == 2)
+            tma_load_4d(dst, tmap, 0, 0, 0, y >> 3, bar(b_full + st));
+          else
+            tma_load_2d(dst, tmap, 0, y, bar(b_full + st));
+        }
+        ++g;
+        if (is_k) continue;
+        if (kt == sg.r.tiles - 1) {
+          // Rows behind the last draft may hold anything, and a weight of zero
+          // does not silence an infinity: they are cleared before PV reads them
+          if (!wait(b_full + st, ((g - 1) / nst) & 1)) break;
+          const int r0 = keys - kt * BN, r1 = (r0 + 15) & ~15;  // the rest of its page
+          constexpr int CH = D / 8;
+          for (int e = lane; e < (r1 - r0) * CH; e += 32) {
+            const int row = r0 + e / CH, ch = e % CH, rr = row & 15;
+            const uint32_t off =
+                PANELS == 2 ? (uint32_t)((rr >> 3) * 2048 + (ch >> 3) * 1024 + (rr & 7) * 128 +
+                                         (((ch & 7) ^ (rr & 7)) << 4))
+                            : (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4));
+            sts128(ring + st * L::kTile + (row >> 4) * kPageBytes + off, make_uint4(0, 0, 0, 0));
+          }
+          fence_proxy_async();
+          __syncwarp();
+        }
+        if (lane == 0) mbar_arrive(bar(B_VFIX + st));
+      }
+    }
+    // what was issued lands before the CTA exits
+    if (lane == 0) {
+      for (int j = max(0, g - nst); j < g; ++j)
+        mbar_wait_no_flag(bar(b_full + j % nst), (j / nst) & 1, p.status, detail, kWaitLimitNs);
+      if (is_k)
+        for (int j = max(0, nq - NQB); j < nq; ++j)
+          mbar_wait_no_flag(bar(B_QFULL + j % NQB), (j / NQB) & 1, p.status, detail, kWaitLimitNs);
+    }
+  } else if (warp == 1) {
+    // ===================================================== MMA issuer
+    const uint32_t el = elect_one();
+    const uint32_t ub = __shfl_sync(0xffffffffu, tbase, 0);
+    const MatDesc dQ = sdesc_sw128(sbase + L::kQ, 16, 1024);
+    const MatDesc dK = sdesc_sw128(sbase + L::kK, 16, kGroupStride);
+    const MatDesc dV = sdesc_sw128(sbase + L::kV, kPanelOff, kGroupStride);
+    // the tile of warpgroup t whose QK was issued last and whose PV comes next
+    int pv_g[2] = {-1, -1};
+    bool pv_first[2] = {}, pv_end[2] = {}, pv_free[2] = {};  // its segment's first, last of this warpgroup; V free behind it
+    auto pv = [&](int t, bool go) {
+      named_bar_sync(kNbP + t, 128 + 32);  // P_t
+      tc_fence_after();
+      const int st = pv_g[t] % NSV;
+      const uint32_t tO = ub + kColO + t * D, tP = ub + t * 128;
+      const MatDesc dv = dV.at(st * L::kTile);
+      if (go)
+#pragma unroll
+        for (int kk = 0; kk < BN / 16; ++kk)
+          mma_ts(tO, tP + kk * 8, dv.at(kk * kPageBytes), IDESC_PV, !(pv_first[t] && kk == 0), el);
+      if (pv_free[t]) mma_commit(bar(B_VEMPTY + st), el);
+      if (pv_end[t]) mma_commit(bar(B_OEND + t), el);
+    };
+    int g0 = 0, q0 = 0;  // key and query tiles of the segments before
+    while (sg.next()) {
+      const int macros = sg.count(0);
+      for (int m = 0; m < macros; ++m)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bool cur = m < sg.count(t);
+          if (!cur && pv_g[t] < 0) continue;
+          const bool go = !named_bar_or(kNbRing, 64, false);
+          tc_fence_after();
+          if (pv_g[t] >= 0) pv(t, go);
+          pv_g[t] = -1;
+          if (!cur) continue;
+          const int j = sg.two ? m : 2 * m + t, g = g0 + j, st = g % NSK;
+          const int qb = (q0 + (sg.two ? t : 0)) % NQB;
+          const uint32_t tS = ub + t * 128;
+          const MatDesc dq = dQ.at(qb * L::kTile), dk = dK.at(st * L::kTile);
+          if (go)
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              mma_ss(tS, dq.at((kk >> 2) * (BM * 128) + (kk & 3) * 32),
+                     dk.at((kk >> 2) * kPanelOff + (kk & 3) * 32), IDESC_QK, kk > 0, el);
+          mma_commit(bar(B_SFULL + t), el);
+          if (!sg.two || t == 1) mma_commit(bar(B_KEMPTY + st), el);
+          if (j == sg.n - 1) mma_commit(bar(B_QEMPTY + qb), el);
+          pv_g[t] = g;
+          pv_first[t] = m == 0;
+          pv_end[t] = m == sg.count(t) - 1;
+          pv_free[t] = !sg.two || t == 1;
+        }
+      g0 += sg.n;
+      q0 += sg.two ? 2 : 1;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if (pv_g[t] >= 0) {
+        const bool go = !named_bar_or(kNbRing, 64, false);
+        tc_fence_after();
+        pv(t, go);
+      }
+    mma_commit(bar(B_END), el);
+    if (lane == 0) mbar_wait_no_flag(bar(B_END), 0, p.status, detail, 4 * kWaitLimitNs);
+    __syncwarp();
+  } else if (warp == 3) {
+    // ===================================================== ring warp
+    // The MMA warp's waits, in its order.
+    bool ok = true;
+    auto wait = [&](int i, uint32_t parity) {
+      if (ok) ok = mbar_wait(bar(i), parity, abort_flag, p.status, detail);
+    };
+    auto meet = [&]() {
+      ok = __all_sync(0xffffffffu, ok);
+      named_bar_or(kNbRing, 64, !ok);
+    };
+    int pv_g[2] = {-1, -1}, pv_s[2] = {};  // pv_s: its segment where it is the first of it, else 0
+    bool pv_fix[2] = {};
+    auto wait_pv = [&](int t) {
+      const int st = pv_g[t] % NSV;
+      wait(B_VFULL + st, (pv_g[t] / NSV) & 1);
+      if (pv_fix[t]) wait(B_VFIX + st, (pv_g[t] / NSV) & 1);
+      if (pv_s[t] > 0) wait(B_ODONE, (pv_s[t] - 1) & 1);
+    };
+    int g0 = 0, q0 = 0, s = 0;
+    while (sg.next()) {
+      const int macros = sg.count(0);
+      for (int m = 0; m < macros; ++m)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bool cur = m < sg.count(t);
+          if (!cur && pv_g[t] < 0) continue;
+          if (pv_g[t] >= 0) wait_pv(t);
+          pv_g[t] = -1;
+          if (cur) {
+            const int j = sg.two ? m : 2 * m + t, g = g0 + j;
+            if (m == 0) {
+              const int q = q0 + (sg.two ? t : 0);
+              wait(B_QFULL + q % NQB, (q / NQB) & 1);
+            }
+            wait(B_KFULL + g % NSK, (g / NSK) & 1);
+            pv_g[t] = g;
+            pv_s[t] = m == 0 ? s : 0;
+            pv_fix[t] = sg.kt0 + j == sg.r.tiles - 1;
+          }
+          meet();
+        }
+      g0 += sg.n;
+      q0 += sg.two ? 2 : 1;
       ++s;
     }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if (pv_g[t] >= 0) {
+        wait_pv(t);
+        meet();
+      }
   }
   tc_fence_before();
   __syncthreads();
@@ -580,78 +732,137 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    draft_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
+                      const __grid_constant__ CUtensorMap tm_k,
+                      const __grid_constant__ CUtensorMap tm_v, Params p) {
+  if (threadIdx.x < 128) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegControl));
+    draft_attn_body<D, false>(tm_q, tm_k, tm_v, p);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegSoftmax));
+    draft_attn_body<D, true>(tm_q, tm_k, tm_v, p);
+  }
+}
+
 // ------------------------------------------------------------------- merge
 // o = sum_c w_c O_c / sum_c w_c l_c, w_c = 2^(m_c - M), over the CTAs that hold
-// key tiles of a row's unit: one CTA per (token, query head), its four warps
-// over the partials, combined in shared memory in a fixed order.
-template <int D>
+// key tiles of a row's unit.  kWarps warps per (token, query head), each with its
+// share of the partials: the (m, l) pairs of all of them first (a lane per
+// partial), then the O rows, eight loads in flight; the warps' sums are combined in
+// shared memory in a fixed order.  One warp per row where there are many rows, four
+// where a unit may be split over many CTAs (76 partials of two units by one load
+// after the other had cost 11 of 27.5 us).
+template <int D, int kWarps>
 __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
-  constexpr int CPL = D / 32;
+  constexpr int CPL = D / 32, kRows = 4 / kWarps, U = 8;
   __shared__ float acc_s[4][D], m_s[4], l_s[4];
+  __shared__ float2 w_s[4][(kCtas + kWarps - 1) / kWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z;
+  const int h = blockIdx.x * kRows + warp / kWarps, i = blockIdx.y, b = blockIdx.z;
   const Request r = request_of(p, b);
-  if (i >= r.n) return;
-  const int hk = h / p.G, rr = i * p.G + h % p.G, rt = rr / BM, row = rr % BM;
-  const int2 u = p.unit[((size_t)b * p.Hkv + hk) * p.rt_max + rt];
+  if (i >= r.n || h >= p.Hq) return;  // (kWarps = 4: the whole CTA)
+  const int hk = h / p.G, rr = i * p.G + h % p.G, rt = rr / BM, row = rr % BM, pair = rt / 2;
+  const int2 u = p.unit[((size_t)b * p.Hkv + hk) * p.rp_max + pair];
   if (u.x == u.y) return;  // finished by its CTA
-  float m = -INFINITY, l = 0.f, acc[CPL];
-#pragma unroll
-  for (int q = 0; q < CPL; ++q) acc[q] = 0.f;
-  for (int c = u.x + warp; c <= u.y; c += 4) {
-    const size_t pr = (size_t)(2 * c + (c == u.x ? 1 : 0)) * BM + row;
-    const float2 ml = p.part_ml[pr];
-    float v[CPL];
-#pragma unroll
-    for (int q = 0; q < CPL; ++q) v[q] = p.part_o[pr * D + q * 32 + lane];
-    if (ml.y <= 0.f) continue;
-    const float mn = fmaxf(m, ml.x), wa = m == -INFINITY ? 0.f : ex2(m - mn), wb = ex2(ml.x - mn);
-    l = l * wa + ml.y * wb;
-#pragma unroll
-    for (int q = 0; q < CPL; ++q) acc[q] = acc[q] * wa + v[q] * wb;
-    m = mn;
+  const int parts = u.y - u.x + 1, t = 2 * pair + 1 < r.rt ? rt & 1 : 0;
+  // partial c is the one of CTA u.x + c; this warp's are c = w0, w0 + kWarps, ...
+  const int w0 = warp % kWarps, mine = (parts - w0 + kWarps - 1) / kWarps;
+  auto part_row = [&](int c) {
+    c = c * kWarps + w0;
+    return (size_t)((2 * (u.x + c) + (c == 0 ? 1 : 0)) * 2 + t) * BM + row;
+  };
+  float M = -INFINITY;
+  for (int c = lane; c < mine; c += 32) {
+    const float2 ml = p.part_ml[part_row(c)];
+    w_s[warp][c] = ml;
+    M = fmaxf(M, ml.x);
   }
 #pragma unroll
-  for (int q = 0; q < CPL; ++q) acc_s[warp][q * 32 + lane] = acc[q];
-  if (lane == 0) m_s[warp] = m, l_s[warp] = l;
-  __syncthreads();
-  const float M = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3]));
-  float L = 0.f, w[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    w[c] = m_s[c] == -INFINITY ? 0.f : ex2(m_s[c] - M);
-    L = fmaf(w[c], l_s[c], L);
+  for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  float l = 0.f, acc[CPL];
+  for (int c = lane; c < mine; c += 32) {
+    const float2 ml = w_s[warp][c];
+    const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
+    l = fmaf(w, ml.y, l);
+    w_s[warp][c].x = w;
   }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  __syncwarp();
+#pragma unroll
+  for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
+#pragma unroll 1
+  for (int c0 = 0; c0 < mine; c0 += U) {
+    float v[U][CPL];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float *src = p.part_o + part_row(min(c0 + k, mine - 1)) * D + lane * CPL;
+      if constexpr (CPL == 4) {
+        const float4 f = *reinterpret_cast<const float4 *>(src);
+        v[k][0] = f.x, v[k][1] = f.y, v[k][2] = f.z, v[k][3] = f.w;
+      } else {
+        const float2 f = *reinterpret_cast<const float2 *>(src);
+        v[k][0] = f.x, v[k][1] = f.y;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float wk = c0 + k < mine ? w_s[warp][c0 + k].x : 0.f;
+      if (wk != 0.f)  // 0: past the end, or no key of the part was visible
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wk, v[k][e], acc[e]);
+    }
+  }
   const size_t o_row = ((size_t)b * p.max_draft + i) * p.Hq + h;
-  for (int e = threadIdx.x; e < D; e += 128) {
-    float a = 0.f;
+  if constexpr (kWarps == 4) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) a = fmaf(w[c], acc_s[c][e], a);
-    p.out[o_row * D + e] = __float2bfloat16_rn(a * inv);
+    for (int e = 0; e < CPL; ++e) acc_s[warp][lane * CPL + e] = acc[e];
+    if (lane == 0) m_s[warp] = M, l_s[warp] = l;
+    __syncthreads();
+    if (warp) return;
+    const float mw[4] = {m_s[0], m_s[1], m_s[2], m_s[3]};
+    M = fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3]));
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float wc = mw[c] == -INFINITY ? 0.f : ex2(mw[c] - M);
+      l = fmaf(wc, l_s[c], l);
+#pragma unroll
+      for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wc, acc_s[c][lane * CPL + e], acc[e]);
+    }
   }
-  if (threadIdx.x == 0 && p.lse)
-    p.lse[o_row] = L > 0.f ? (M + __log2f(L)) * 0.69314718055994531f : -INFINITY;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  __nv_bfloat162 *dst = reinterpret_cast<__nv_bfloat162 *>(p.out + o_row * D + lane * CPL);
+#pragma unroll
+  for (int e = 0; e < CPL; e += 2) dst[e / 2] = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
+  if (lane == 0 && p.lse)
+    p.lse[o_row] = l > 0.f ? (M + __log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
 // -------------------------------------------------------------------- host
 struct Plan {
-  int r_pad, rt_max;
-  size_t q_bytes, mask_bytes, unit_bytes, o_bytes, ml_bytes, total;
+  int r_pad, rp_max;
+  size_t q_bytes, mask_bytes, share_bytes, unit_bytes, o_bytes, ml_bytes, total;
 };
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
   Plan pl;
   const int G = g->num_q_heads / g->num_kv_heads;
-  pl.rt_max = (int)(((long long)max_draft * G + BM - 1) / BM);
-  pl.r_pad = pl.rt_max * BM;
+  const int rt_max = (int)(((long long)max_draft * G + BM - 1) / BM);
+  pl.rp_max = (rt_max + 1) / 2;
+  pl.r_pad = rt_max * BM;
   pl.q_bytes = align256((size_t)batch * g->num_kv_heads * pl.r_pad * g->head_dim * 2);
   pl.mask_bytes = align256((size_t)batch * max_draft * 8);
-  pl.unit_bytes = align256((size_t)batch * g->num_kv_heads * pl.rt_max * sizeof(int2));
-  pl.o_bytes = align256((size_t)2 * kCtas * BM * g->head_dim * 4);
-  pl.ml_bytes = align256((size_t)2 * kCtas * BM * sizeof(float2));
-  pl.total = pl.q_bytes + pl.mask_bytes + pl.unit_bytes + pl.o_bytes + pl.ml_bytes;
+  pl.share_bytes = align256(kCtas * sizeof(Share));
+  pl.unit_bytes = align256((size_t)batch * g->num_kv_heads * pl.rp_max * sizeof(int2));
+  pl.o_bytes = align256((size_t)4 * kCtas * BM * g->head_dim * 4);
+  pl.ml_bytes = align256((size_t)4 * kCtas * BM * sizeof(float2));
+  pl.total = pl.q_bytes + pl.mask_bytes + pl.share_bytes + pl.unit_bytes + pl.o_bytes + pl.ml_bytes;
   return pl;
 }
 
@@ -662,12 +873,24 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tk, const CU
                                        cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        Layout<D>::kAlloc);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(draft_append_kernel<D>, dim3(p.max_draft, p.batch), dim3(128), 0, stream, p, rp);
+  // the setmaxnreg split needs the registers the kernel was built to launch with:
+  // with fewer the softmax warpgroups would wait for them for ever
+  static const bool built = [] {
+    cudaFuncAttributes at;
+    return cudaFuncGetAttributes(&at, draft_attn_kernel<D>) == cudaSuccess &&
+           at.numRegs >= kRegLaunch;
+  }();
+  if (!built) return cudaErrorInvalidConfiguration;
+  e = launch_dependent(draft_append_kernel<D>, dim3(p.max_draft + 1, p.batch), dim3(128), 0, stream, p, rp);
   if (e != cudaSuccess) return e;
   e = launch_dependent(draft_attn_kernel<D>, dim3(kCtas), dim3(kThreads), Layout<D>::kAlloc, stream,
                        tq, tk, tv, p);
   if (e != cudaSuccess) return e;
-  return launch_dependent(draft_merge_kernel<D>, dim3(p.Hq, p.max_draft, p.batch), dim3(128), 0,
+  // a unit is split over about 152 / (batch Hkv) CTAs or more
+  if ((long long)p.batch * p.Hkv >= 16)
+    return launch_dependent(draft_merge_kernel<D, 1>, dim3((p.Hq + 3) / 4, p.max_draft, p.batch),
+                            dim3(128), 0, stream, p);
+  return launch_dependent(draft_merge_kernel<D, 4>, dim3(p.Hq, p.max_draft, p.batch), dim3(128), 0,
                           stream, p);
 }
 
@@ -712,7 +935,8 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   const int D = geom->head_dim, Hkv = geom->num_kv_heads;
   const long long rows_total = (long long)geom->num_layers * num_pages * Hkv * 16;
   const Plan pl = plan(geom, batch, max_draft);
-  if (rows_total + 16 >= INT32_MAX || (long long)batch * Hkv * pl.r_pad >= INT32_MAX)
+  if (rows_total + 16 >= INT32_MAX || (long long)batch * Hkv * pl.r_pad >= INT32_MAX ||
+      (double)batch * Hkv * pl.rp_max * (max_pages / 8 + 1) >= INT32_MAX)
     return fail(PIC_ERR_UNSUPPORTED, "%s: cache or queries have more than 2^31 rows", who);
   if (batch > 65535) return fail(PIC_ERR_UNSUPPORTED, "%s: grid too large", who);
   if (!workspace || workspace_bytes < pl.total || (reinterpret_cast<uintptr_t>(workspace) & 255))
@@ -725,7 +949,7 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   p.Hkv = Hkv;
   p.G = p.Hq / Hkv;
   p.r_pad = pl.r_pad;
-  p.rt_max = pl.rt_max;
+  p.rp_max = pl.rp_max;
   p.max_pages = max_pages;
   p.oob_row = (int)((rows_total + 15) / 16 * 16);
   p.layer = layer;
@@ -746,6 +970,8 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   ws += pl.q_bytes;
   p.mask = reinterpret_cast<uint64_t *>(ws);
   ws += pl.mask_bytes;
+  p.share = reinterpret_cast<Share *>(ws);
+  ws += pl.share_bytes;
   p.unit = reinterpret_cast<int2 *>(ws);
   ws += pl.unit_bytes;
   p.part_o = reinterpret_cast<float *>(ws);
