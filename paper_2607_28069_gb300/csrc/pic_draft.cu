@@ -87,6 +87,12 @@ struct Params {
   float scale_log2;
 };
 
+PIC_DEV void st_global32(void *p, const float *f) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]),
+               "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7])
+               : "memory");
+}
+
 // What a request brings: its key tiles, row tiles and pairs of row tiles (0 for
 // one left alone).
 struct Request {
@@ -113,6 +119,7 @@ PIC_DEV Request request_of(const Params &p, int b) {
 // is `base`.
 struct alignas(16) Share {
   int total, ctas, pos, end, b, base, ctx, n;  // ctx, n: request b's
+  int unit0, hk, pair, tiles;                  // of the unit of tile pos
 };
 
 PIC_DEV int work_of(const Params &p, const Request &r) { return p.Hkv * r.rp * r.tiles; }
@@ -134,7 +141,7 @@ PIC_DEV void deal_shares(const Params &p, int grid) {
 #pragma unroll
   for (int q = 0; q < kPer; ++q) {
     const int c = lane + 32 * q;
-    sh[q] = Share{total, ctas, 0, 0, 0, 0, 0, 0};
+    sh[q] = Share{total, ctas, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     if (c < ctas) {
       sh[q].pos = (int)((long long)total * c / ctas);
       sh[q].end = (int)((long long)total * (c + 1) / ctas);
@@ -162,8 +169,17 @@ PIC_DEV void deal_shares(const Params &p, int grid) {
     base += __shfl_sync(0xffffffffu, x, 31);
   }
 #pragma unroll
-  for (int q = 0; q < kPer; ++q)
+  for (int q = 0; q < kPer; ++q) {
+    const Request r = request_of(p, sh[q].ctx, sh[q].n);
+    if (r.tiles > 0) {
+      const int u = (sh[q].pos - sh[q].base) / r.tiles;
+      sh[q].tiles = r.tiles;
+      sh[q].unit0 = sh[q].base + u * r.tiles;
+      sh[q].hk = u / r.rp;
+      sh[q].pair = u % r.rp;
+    }
     if (lane + 32 * q < grid) p.share[lane + 32 * q] = sh[q];
+  }
 }
 
 // ------------------------------------------------------------------ append
@@ -257,23 +273,26 @@ struct Segments {
 
   PIC_DEV Segments(const Params &pp, int cta_) : p(pp), cta(cta_) {
     const int4 *q = reinterpret_cast<const int4 *>(p.share + cta);
-    const int4 x = q[0], y = q[1];
+    const int4 x = q[0], y = q[1], z = q[2];
     total = x.x, ctas = x.y, pos = x.z, end = x.w;
     b = y.x, base = y.y;
     r = request_of(p, y.z, y.w);
+    unit0 = z.x, hk = z.y, pair = z.z;  // the first segment's unit
   }
   PIC_DEV bool next() {
     if (pos >= end) return false;
-    while (pos - base >= work_of(p, r)) {
-      base += work_of(p, r);
-      r = request_of(p, ++b);
+    if (pos >= unit0 + r.tiles) {  // a unit behind the first segment's
+      while (pos - base >= work_of(p, r)) {
+        base += work_of(p, r);
+        r = request_of(p, ++b);
+      }
+      const int u = (pos - base) / r.tiles;
+      unit0 = base + u * r.tiles;
+      hk = u / r.rp;
+      pair = u % r.rp;
     }
-    const int u = (pos - base) / r.tiles;
-    unit0 = base + u * r.tiles;
     kt0 = pos - unit0;
     n = min(r.tiles - kt0, end - pos);
-    hk = u / r.rp;
-    pair = u % r.rp;
     two = 2 * pair + 1 < r.rt;
     first = kt0 == 0;
     last = kt0 + n == r.tiles;
@@ -373,35 +392,57 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
         const int kt = sg.kt0 + (sg.two ? i : 2 * i + t);
         wait(B_SFULL + t, nS & 1);
         tc_fence_after();
-        float x[BN];
-#pragma unroll
-        for (int c = 0; c < BN / 32; ++c) tmem_ld32(tS + c * 32, reinterpret_cast<uint32_t *>(x + c * 32));
-        tmem_wait_ld();
+        // The scores are read twice, 32 columns at a time, once for the maximum and
+        // once for the exponentials: the loops stay short, and short code counts
+        // for more than the second read, because each call begins with cold
+        // instruction caches (with a row's 128 scores in registers and everything
+        // unrolled, a request of 4k keys spent half of its 12600 cycles on that).
+        float x0[32], x1[32];
+        auto load = [&](float *x, int c) { tmem_ld32(tS + c * 32, reinterpret_cast<uint32_t *>(x)); };
+        auto chunks = [&](auto &&work) {  // work(x, c), the next chunk on its way meanwhile
+          load(x0, 0);
+          tmem_wait_ld();
+#pragma unroll 1
+          for (int c = 0; c < BN / 32; c += 2) {
+            load(x1, c + 1);
+            work(x0, c);
+            tmem_wait_ld();
+            if (c + 2 < BN / 32) load(x0, c + 2);
+            work(x1, c + 1);
+            tmem_wait_ld();
+          }
+        };
         const int off = kt * BN - sg.r.ctx;  // key c of the tile is draft off + c
         if (off > -BN) {
-          // its visible keys as 128 bits: all below the context's end, then the
-          // ancestors' bits
+          // hide what the row does not see: of a chunk's keys as 32 bits, those below
+          // the context's end are visible, then the ancestors' bits
           const int rr = row_of();
           const uint64_t mask =
               rr < sg.r.n * p.G ? p.mask[(size_t)sg.b * p.max_draft + rr / p.G] : 0;
-          uint32_t w[4];
+#pragma unroll 1
+          for (int c = 0; c < BN / 32; ++c) {
+            const int o = off + 32 * c;  // draft of the chunk's first key
+            if (o <= -32) continue;
+            const uint32_t w = o >= 64 ? 0u : o >= 0 ? (uint32_t)(mask >> o)
+                               : (0xffffffffu >> (32 + o)) | ((uint32_t)mask << -o);
+            load(x0, c);
+            tmem_wait_ld();
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int o = off + 32 * q;  // draft of bit 0 of the word
-            w[q] = o >= 64 ? 0u : o >= 0 ? (uint32_t)(mask >> o)
-                 : o <= -32 ? 0xffffffffu
-                            : (0xffffffffu >> (32 + o)) | ((uint32_t)mask << -o);
+            for (int q = 0; q < 32; ++q)
+              if (!((w >> q) & 1u)) x0[q] = -INFINITY;
+            tmem_st32(tS + c * 32, reinterpret_cast<uint32_t *>(x0));
           }
-#pragma unroll
-          for (int c = 0; c < BN; ++c)
-            if (!((w[c >> 5] >> (c & 31)) & 1u)) x[c] = -INFINITY;
+          tmem_wait_st();
         }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float mx[2] = {-INFINITY, -INFINITY};
+        chunks([&](const float *x, int) {
 #pragma unroll
-        for (int c = 0; c < BN; c += 8)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) mx[q] = max3f(mx[q], x[c + 2 * q], x[c + 2 * q + 1]);
-        const float m_new = fmaxf(m_used, max3f(mx[0], mx[1], fmaxf(mx[2], mx[3])) * p.scale_log2);
+          for (int q = 0; q < 32; q += 4) {
+            mx[0] = max3f(mx[0], x[q], x[q + 1]);
+            mx[1] = max3f(mx[1], x[q + 2], x[q + 3]);
+          }
+        });
+        const float m_new = fmaxf(m_used, fmaxf(mx[0], mx[1]) * p.scale_log2);
         const bool resc = m_new > m_used + 8.f;
         float alpha = 1.f;
         if (resc) {
@@ -421,22 +462,22 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
         }
         const float mref = m_used == -INFINITY ? 0.f : m_used;
         const uint64_t sc2 = f2pack(p.scale_log2, p.scale_log2), nm2 = f2pack(-mref, -mref);
-        uint64_t acc[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int c0 = 0; c0 < BN; c0 += 32) {
+        uint64_t acc[2] = {0, 0};
+        // P of chunk c over columns 16 c .. 16 c + 15, whose scores have been read
+        chunks([&](const float *x, int c) {
           uint32_t pk[16];
 #pragma unroll
           for (int q = 0; q < 16; ++q) {
-            const uint64_t e = exp2_mufu2(fma2(f2pack(x[c0 + 2 * q], x[c0 + 2 * q + 1]), sc2, nm2));
-            acc[q & 3] = add2(acc[q & 3], e);
+            const uint64_t e = exp2_mufu2(fma2(f2pack(x[2 * q], x[2 * q + 1]), sc2, nm2));
+            acc[q & 1] = add2(acc[q & 1], e);
             float e0, e1;
             f2unpack(e, e0, e1);
             pk[q] = pack2(e0, e1);
           }
-          tmem_st16(tS + c0 / 2, pk);
-        }
+          tmem_st16(tS + c * 16, pk);
+        });
         float l0, l1;
-        f2unpack(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), l0, l1);
+        f2unpack(add2(acc[0], acc[1]), l0, l1);
         l = fmaf(l, alpha, l0 + l1);
         tmem_wait_st();
         tc_fence_before();
@@ -500,10 +541,10 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
 #pragma unroll
             for (int q = 0; q < 4; ++q) st_global16(p.out + o_row * D + c * 32 + q * 8, pack8(o + q * 8));
         } else if (store) {
+          // 32 bytes at a time: a lane's row is its own, so each store of 16 would
+          // be half a sector
 #pragma unroll
-          for (int q = 0; q < 8; ++q)
-            *reinterpret_cast<float4 *>(p.part_o + p_row * D + c * 32 + q * 4) =
-                make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+          for (int q = 0; q < 32; q += 8) st_global32(p.part_o + p_row * D + c * 32 + q, o + q);
         }
       }
       tc_fence_before();
