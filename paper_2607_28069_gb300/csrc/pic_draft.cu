@@ -78,7 +78,7 @@ struct Params {
   __nv_bfloat16 *qp;                 // workspace: packed rotated queries
   uint64_t *mask;                    // workspace: [batch][max_draft] ancestor bits
   struct Share *share;               // workspace: [kCtas] each CTA's start
-  int2 *unit;                        // workspace: [batch][Hkv][rp_max] first and last CTA
+  int32_t *base;                     // workspace: [batch] each request's first key tile
   float *part_o;                     // workspace: [kCtas][2][row tile of the pair][BM][D]
   float2 *part_ml;                   // the same without [D]
   __nv_bfloat16 *out;
@@ -124,28 +124,35 @@ struct alignas(16) Share {
 
 PIC_DEV int work_of(const Params &p, const Request &r) { return p.Hkv * r.rp * r.tiles; }
 
-// One warp: the shares of CTAs lane, lane + 32, ... in `grid` CTAs.  Every CTA
-// that takes part has a tile.
-PIC_DEV void deal_shares(const Params &p, int grid) {
-  const int lane = threadIdx.x & 31;
-  int total = 0;
+PIC_DEV int mul_div(int a, int b, int c) {  // a * b / c, all >= 0
+  const unsigned long long x = (unsigned long long)a * b;
+  return x < (1ull << 32) ? (int)((unsigned)x / (unsigned)c) : (int)(x / (unsigned)c);
+}
+// The CTA whose share holds tile t.
+PIC_DEV int owner_of(int t, int total, int ctas) {
+  const unsigned long long x = (unsigned long long)(t + 1) * ctas - 1;
+  return x < (1ull << 32) ? (int)((unsigned)x / (unsigned)total) : (int)(x / (unsigned)total);
+}
+
+// One CTA of 128 threads: the shares of CTAs tid and tid + 128 of kCtas (every CTA
+// that takes part has a tile), and every request's first tile.
+PIC_DEV void deal_shares(const Params &p) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  int total = 0;  // every warp for itself
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
     int w = b0 + lane < p.batch ? work_of(p, request_of(p, b0 + lane)) : 0;
 #pragma unroll
     for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
     total += w;
   }
-  const int ctas = min(grid, total);
-  constexpr int kPer = (kCtas + 31) / 32;
-  Share sh[kPer];
+  const int ctas = min(kCtas, total);
+  static_assert(kCtas <= 256, "two shares a thread");
+  int pos[2], end[2], at[2] = {-1, -1}, base_of[2], ctx_of[2], n_of[2];
 #pragma unroll
-  for (int q = 0; q < kPer; ++q) {
-    const int c = lane + 32 * q;
-    sh[q] = Share{total, ctas, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-    if (c < ctas) {
-      sh[q].pos = (int)((long long)total * c / ctas);
-      sh[q].end = (int)((long long)total * (c + 1) / ctas);
-    }
+  for (int q = 0; q < 2; ++q) {
+    const int c = tid + 128 * q;
+    pos[q] = end[q] = base_of[q] = ctx_of[q] = n_of[q] = 0;
+    if (c < ctas) pos[q] = mul_div(total, c, ctas), end[q] = mul_div(total, c + 1, ctas);
   }
   int base = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
@@ -157,28 +164,32 @@ PIC_DEV void deal_shares(const Params &p, int grid) {
       const int y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
     }
+    if (tid < 32 && b0 + lane < p.batch) p.base[b0 + lane] = base + x - w;
     // lane l's request holds tiles [base + x - w, base + x)
+#pragma unroll 1
     for (int l = 0; l < min(32, p.batch - b0); ++l) {
       const int hi = base + __shfl_sync(0xffffffffu, x, l), lo = hi - __shfl_sync(0xffffffffu, w, l);
       const int ctx = __shfl_sync(0xffffffffu, r.ctx, l), n = __shfl_sync(0xffffffffu, r.n, l);
 #pragma unroll
-      for (int q = 0; q < kPer; ++q)
-        if (sh[q].end > 0 && sh[q].pos >= lo && sh[q].pos < hi)
-          sh[q].b = b0 + l, sh[q].base = lo, sh[q].ctx = ctx, sh[q].n = n;
+      for (int q = 0; q < 2; ++q)
+        if (end[q] > 0 && pos[q] >= lo && pos[q] < hi)
+          at[q] = b0 + l, base_of[q] = lo, ctx_of[q] = ctx, n_of[q] = n;
     }
     base += __shfl_sync(0xffffffffu, x, 31);
   }
 #pragma unroll
-  for (int q = 0; q < kPer; ++q) {
-    const Request r = request_of(p, sh[q].ctx, sh[q].n);
+  for (int q = 0; q < 2; ++q) {
+    if (tid + 128 * q >= kCtas) continue;
+    Share sh{total, ctas, pos[q], end[q], at[q], base_of[q], ctx_of[q], n_of[q], 0, 0, 0, 0};
+    const Request r = request_of(p, sh.ctx, sh.n);
     if (r.tiles > 0) {
-      const int u = (sh[q].pos - sh[q].base) / r.tiles;
-      sh[q].tiles = r.tiles;
-      sh[q].unit0 = sh[q].base + u * r.tiles;
-      sh[q].hk = u / r.rp;
-      sh[q].pair = u % r.rp;
+      const int u = (sh.pos - sh.base) / r.tiles;
+      sh.tiles = r.tiles;
+      sh.unit0 = sh.base + u * r.tiles;
+      sh.hk = u / r.rp;
+      sh.pair = u - sh.hk * r.rp;
     }
-    if (lane + 32 * q < grid) p.share[lane + 32 * q] = sh[q];
+    p.share[tid + 128 * q] = sh;
   }
 }
 
@@ -193,10 +204,36 @@ __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams 
   __shared__ int32_t par[kMaxDraft];
   __shared__ int depth;
   if ((int)blockIdx.x == p.max_draft) {
-    if (blockIdx.y == 0 && threadIdx.x < 32) deal_shares(p, kCtas);
+    if (blockIdx.y == 0) deal_shares(p);
     return;
   }
   const int b = blockIdx.y, i = blockIdx.x, tid = threadIdx.x;
+  const size_t tok = (size_t)b * p.max_draft + i;
+  // The token's projections go out before anything is known of its request:
+  // chunk (8 pairs) u of the query heads, then of the key heads, two a thread (for
+  // more the loop below goes on), and the value pieces.
+  const int units = (p.Hq + p.Hkv) * KC;
+  auto source = [&](int u) {
+    const int h = u / KC;
+    return h < p.Hq ? p.q + (tok * p.Hq + h) * D : p.k_new + (tok * p.Hkv + h - p.Hq) * D;
+  };
+  const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
+  constexpr int kAhead = 3;
+  uint4 qa[kAhead], qb[kAhead], vn = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a) {
+    qa[a] = qb[a] = make_uint4(0, 0, 0, 0);
+    if (tid + 128 * a < units) {
+      const __nv_bfloat16 *src = source(tid + 128 * a);
+      qa[a] = ld_stream(src + pc.off_a);
+      qb[a] = ld_stream(src + pc.off_b);
+    }
+  }
+  const int pieces = p.Hkv * (D / 8);
+  const __nv_bfloat16 *v_src = p.v_new + tok * p.Hkv * D;
+  if (tid < pieces) vn = ld_stream(v_src + tid * 8);
+  if (tid < p.max_draft) par[tid] = p.parent ? p.parent[(size_t)b * p.max_draft + tid] : tid - 1;
+  const uint64_t turn = tid < D / 2 ? rope_turn(rope_theta(rp, p.layer, tid)) : 0;
   const int ctx = p.ctx_len[b], n = p.draft_len[b];
   const bool bad = ctx < 0 || n < 0 || n > p.max_draft;
   if (bad || (long long)ctx + n > (long long)p.max_pages * 16) {
@@ -205,54 +242,55 @@ __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams 
     return;
   }
   if (i >= n) return;
-  if (tid < n) {
-    int q = tid - 1;
-    if (p.parent) {
-      q = p.parent[(size_t)b * p.max_draft + tid];
-      if (q < -1 || q >= tid) {
-        if (tid == i) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
-        q = -1;
-      }
-    }
-    par[tid] = q;
-  }
+  const int slot = ctx + i;
+  int page = p.block_table[(size_t)b * p.max_pages + slot / 16];
   __syncthreads();
   if (tid == 0) {
     uint64_t m = 1ull << i;
-    int d = 0;
-    for (int q = par[i]; q >= 0; q = par[q]) m |= 1ull << q, ++d;
-    p.mask[(size_t)b * p.max_draft + i] = m;
-    depth = d;
-  }
-  __syncthreads();
-  const int pos = ctx + depth, slot = ctx + i;
-  if (tid < D / 2) cs[tid] = rope_cos_sin_turn(pos, rope_turn(rope_theta(rp, p.layer, tid)));
-  int page = p.block_table[(size_t)b * p.max_pages + slot / 16];
-  if (page < 0 || page >= p.num_pages) {
-    if (tid == 0) dev_fail(p.status, PIC_DEV_BAD_PAGE, b);
-    page = -1;
-  }
-  __syncthreads();
-  const size_t tok = (size_t)b * p.max_draft + i;
-  for (int u = tid; u < (p.Hq + p.Hkv) * KC; u += 128) {
-    const int h = u / KC, c = u % KC;
-    if (h < p.Hq) {
-      const int hk = h / p.G, g = h % p.G;
-      rotate_chunk(p.q + (tok * p.Hq + h) * D,
-                   p.qp + ((size_t)(b * p.Hkv + hk) * p.r_pad + i * p.G + g) * D, c, D / 2, rp.style,
-                   cs + 8 * c, true);
-    } else if (page >= 0) {
-      const int hk = h - p.Hq;
-      rotate_chunk(p.k_new + (tok * p.Hkv + hk) * D,
-                   p.k_cache + (((size_t)page * p.Hkv + hk) * 16 + slot % 16) * D, c, D / 2, rp.style,
-                   cs + 8 * c, true);
+    int d = 0, q = i;
+    for (;;) {
+      const int up = par[q];
+      if (up < -1 || up >= q) {
+        if (q == i) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
+        break;
+      }
+      if (up < 0) break;
+      q = up;
+      m |= 1ull << q, ++d;
     }
+    p.mask[tok] = m;
+    depth = d;
+    if (page < 0 || page >= p.num_pages) dev_fail(p.status, PIC_DEV_BAD_PAGE, b);
+  }
+  if (page >= p.num_pages) page = -1;
+  __syncthreads();
+  if (tid < D / 2) cs[tid] = rope_cos_sin_turn(ctx + depth, turn);
+  __syncthreads();
+  auto store = [&](int u, uint4 a, uint4 c) {
+    const int h = u / KC, hk = h < p.Hq ? h / p.G : h - p.Hq;
+    __nv_bfloat16 *dst;
+    if (h < p.Hq)
+      dst = p.qp + ((size_t)(b * p.Hkv + hk) * p.r_pad + i * p.G + h - hk * p.G) * D;
+    else if (page >= 0)
+      dst = p.k_cache + (((size_t)page * p.Hkv + hk) * 16 + slot % 16) * D;
+    else
+      return;
+    rotate_store(a, c, dst, pc, rp.style, cs + 8 * (tid % KC));
+  };
+  // (128 is a multiple of KC: a thread's chunk of a row is always the same)
+#pragma unroll
+  for (int a = 0; a < kAhead; ++a)
+    if (tid + 128 * a < units) store(tid + 128 * a, qa[a], qb[a]);
+#pragma unroll 1
+  for (int u = tid + 128 * kAhead; u < units; u += 128) {
+    const __nv_bfloat16 *src = source(u);
+    store(u, ld_stream(src + pc.off_a), ld_stream(src + pc.off_b));
   }
   if (page >= 0)
-    for (int u = tid; u < p.Hkv * (D / 8); u += 128) {
+    for (int u = tid; u < pieces; u += 128) {
       const int hk = u / (D / 8), c = u % (D / 8);
       st_global16(p.v_cache + (((size_t)page * p.Hkv + hk) * 16 + slot % 16) * D + c * 8,
-                  ld_stream(p.v_new + (tok * p.Hkv + hk) * D + c * 8));
+                  u == tid ? vn : ld_stream(v_src + u * 8));
     }
 }
 
@@ -260,10 +298,10 @@ __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams 
 // The segments of one CTA, walked by each role's warp for itself.
 struct Segments {
   const Params &p;
-  int total, pos, end;  // key tiles of the batch (the host keeps them below 2^31), next
-                        // tile, end of this CTA's share
+  int pos, end;         // next key tile (the host keeps them below 2^31), end of this
+                        // CTA's share
   int base;             // first tile of request b
-  int b, cta, ctas;
+  int b, cta;
   Request r;
   // the present segment
   int hk, pair, kt0, n;
@@ -274,7 +312,7 @@ struct Segments {
   PIC_DEV Segments(const Params &pp, int cta_) : p(pp), cta(cta_) {
     const int4 *q = reinterpret_cast<const int4 *>(p.share + cta);
     const int4 x = q[0], y = q[1], z = q[2];
-    total = x.x, ctas = x.y, pos = x.z, end = x.w;
+    pos = x.z, end = x.w;
     b = y.x, base = y.y;
     r = request_of(p, y.z, y.w);
     unit0 = z.x, hk = z.y, pair = z.z;  // the first segment's unit
@@ -299,8 +337,6 @@ struct Segments {
     pos += n;
     return true;
   }
-  // the CTA whose share holds tile t
-  PIC_DEV int owner(int t) const { return (int)(((long long)(t + 1) * ctas - 1) / total); }
   // the partial slot of row tile t of the present segment: a CTA has at most
   // one segment that ends a unit begun elsewhere or lies inside one (0), and one
   // that begins a unit and leaves its end to others (1)
@@ -384,9 +420,6 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
       const int n = sg.count(t);
       // this thread's row: token rr / G, query head hk G + rr % G
       auto row_of = [&]() { return (2 * sg.pair + (sg.two ? t : 0)) * BM + row; };
-      if (sg.first && threadIdx.x == 128)
-        p.unit[((size_t)sg.b * p.Hkv + sg.hk) * p.rp_max + sg.pair] =
-            make_int2((int)blockIdx.x, sg.owner(sg.unit0 + sg.r.tiles - 1));
       float m_used = -INFINITY, l = 0.f;
       for (int i = 0; i < n; ++i, ++nS) {
         const int kt = sg.kt0 + (sg.two ? i : 2 * i + t);
@@ -806,7 +839,9 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   const Request r = request_of(p, b);
   if (i >= r.n || h >= p.Hq) return;  // (kWarps = 4: the whole CTA)
   const int hk = h / p.G, rr = i * p.G + h % p.G, rt = rr / BM, row = rr % BM, pair = rt / 2;
-  const int2 u = p.unit[((size_t)b * p.Hkv + hk) * p.rp_max + pair];
+  const int total = p.share[0].total, ctas = p.share[0].ctas;
+  const int t0 = p.base[b] + (hk * r.rp + pair) * r.tiles;
+  const int2 u = make_int2(owner_of(t0, total, ctas), owner_of(t0 + r.tiles - 1, total, ctas));
   if (u.x == u.y) return;  // finished by its CTA
   const int parts = u.y - u.x + 1, t = 2 * pair + 1 < r.rt ? rt & 1 : 0;
   // partial c is the one of CTA u.x + c; this warp's are c = w0, w0 + kWarps, ...
@@ -888,7 +923,7 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
 // -------------------------------------------------------------------- host
 struct Plan {
   int r_pad, rp_max;
-  size_t q_bytes, mask_bytes, share_bytes, unit_bytes, o_bytes, ml_bytes, total;
+  size_t q_bytes, mask_bytes, share_bytes, base_bytes, o_bytes, ml_bytes, total;
 };
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
@@ -900,10 +935,10 @@ inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
   pl.q_bytes = align256((size_t)batch * g->num_kv_heads * pl.r_pad * g->head_dim * 2);
   pl.mask_bytes = align256((size_t)batch * max_draft * 8);
   pl.share_bytes = align256(kCtas * sizeof(Share));
-  pl.unit_bytes = align256((size_t)batch * g->num_kv_heads * pl.rp_max * sizeof(int2));
+  pl.base_bytes = align256((size_t)batch * 4);
   pl.o_bytes = align256((size_t)4 * kCtas * BM * g->head_dim * 4);
   pl.ml_bytes = align256((size_t)4 * kCtas * BM * sizeof(float2));
-  pl.total = pl.q_bytes + pl.mask_bytes + pl.share_bytes + pl.unit_bytes + pl.o_bytes + pl.ml_bytes;
+  pl.total = pl.q_bytes + pl.mask_bytes + pl.share_bytes + pl.base_bytes + pl.o_bytes + pl.ml_bytes;
   return pl;
 }
 
@@ -1013,8 +1048,8 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   ws += pl.mask_bytes;
   p.share = reinterpret_cast<Share *>(ws);
   ws += pl.share_bytes;
-  p.unit = reinterpret_cast<int2 *>(ws);
-  ws += pl.unit_bytes;
+  p.base = reinterpret_cast<int32_t *>(ws);
+  ws += pl.base_bytes;
   p.part_o = reinterpret_cast<float *>(ws);
   ws += pl.o_bytes;
   p.part_ml = reinterpret_cast<float2 *>(ws);
