@@ -78,6 +78,7 @@ struct Params {
   __nv_bfloat16 *qp;                 // workspace: packed rotated queries
   uint64_t *mask;                    // workspace: [batch][max_draft] ancestor bits
   struct Share *share;               // workspace: [kCtas] each CTA's start
+  int32_t *rows;                     // workspace: [kCtas][32] K/V rows of its first 32 pages
   int32_t *base;                     // workspace: [batch] each request's first key tile
   float *part_o;                     // workspace: [kCtas][2][row tile of the pair][BM][D]
   float2 *part_ml;                   // the same without [D]
@@ -134,26 +135,31 @@ PIC_DEV int owner_of(int t, int total, int ctas) {
   return x < (1ull << 32) ? (int)((unsigned)x / (unsigned)total) : (int)(x / (unsigned)total);
 }
 
-// One CTA of 128 threads: the shares of CTAs tid and tid + 128 of kCtas (every CTA
-// that takes part has a tile), and every request's first tile.
-PIC_DEV void deal_shares(const Params &p) {
-  const int tid = threadIdx.x, lane = tid & 31;
-  int total = 0;  // every warp for itself
+// The K/V row (of the whole cache) of page pidx of request b's kv head hk; zeros
+// are read for a page past the last key or outside the cache.
+PIC_DEV int page_row(const Params &p, int page, int pidx, int keys, int hk) {
+  if ((long long)pidx * 16 >= keys || page < 0 || page >= p.num_pages) return p.oob_row;
+  return (int)(p.layer_row0 + ((long long)page * p.Hkv + hk) * 16);
+}
+
+// The shares of CTAs first .. first + 3 (every CTA that takes part has a tile), by
+// one warp, lane l < 4 for CTA first + l; the warp of CTA 0 also notes every
+// request's first tile.
+constexpr int kDealt = 4;
+PIC_DEV void deal_shares(const Params &p, int first) {
+  const int lane = threadIdx.x & 31, c = first + lane;
+  int total = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
     int w = b0 + lane < p.batch ? work_of(p, request_of(p, b0 + lane)) : 0;
 #pragma unroll
     for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
     total += w;
   }
-  const int ctas = min(kCtas, total);
-  static_assert(kCtas <= 256, "two shares a thread");
-  int pos[2], end[2], at[2] = {-1, -1}, base_of[2], ctx_of[2], n_of[2];
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int c = tid + 128 * q;
-    pos[q] = end[q] = base_of[q] = ctx_of[q] = n_of[q] = 0;
-    if (c < ctas) pos[q] = mul_div(total, c, ctas), end[q] = mul_div(total, c + 1, ctas);
-  }
+  // two key tiles at least, one for each softmax warpgroup: half as many tiles a CTA
+  // are no faster and leave twice the partials to merge
+  const int ctas = min(kCtas, (total + 1) / 2);
+  Share sh{total, ctas, 0, 0, -1, 0, 0, 0, 0, 0, 0, 0};
+  if (lane < kDealt && c < ctas) sh.pos = mul_div(total, c, ctas), sh.end = mul_div(total, c + 1, ctas);
   int base = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
     const Request r = b0 + lane < p.batch ? request_of(p, b0 + lane) : Request{0, 0, 0, 0, 0};
@@ -164,38 +170,57 @@ PIC_DEV void deal_shares(const Params &p) {
       const int y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
     }
-    if (tid < 32 && b0 + lane < p.batch) p.base[b0 + lane] = base + x - w;
-    // lane l's request holds tiles [base + x - w, base + x)
-#pragma unroll 1
-    for (int l = 0; l < min(32, p.batch - b0); ++l) {
-      const int hi = base + __shfl_sync(0xffffffffu, x, l), lo = hi - __shfl_sync(0xffffffffu, w, l);
-      const int ctx = __shfl_sync(0xffffffffu, r.ctx, l), n = __shfl_sync(0xffffffffu, r.n, l);
+    if (first == 0 && b0 + lane < p.batch) p.base[b0 + lane] = base + x - w;
+    // lane l's request holds tiles [base + x - w, base + x): the one of tile pos
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
-        if (end[q] > 0 && pos[q] >= lo && pos[q] < hi)
-          at[q] = b0 + l, base_of[q] = lo, ctx_of[q] = ctx, n_of[q] = n;
+    for (int k = 0; k < kDealt; ++k) {
+      const int pos = __shfl_sync(0xffffffffu, sh.pos, k), end = __shfl_sync(0xffffffffu, sh.end, k);
+      const unsigned in = __ballot_sync(0xffffffffu, end > 0 && pos >= base + x - w && pos < base + x);
+      if (in) {
+        const int l = __ffs(in) - 1;
+        const int lo = base + __shfl_sync(0xffffffffu, x - w, l);
+        const int ctx = __shfl_sync(0xffffffffu, r.ctx, l), n = __shfl_sync(0xffffffffu, r.n, l);
+        if (lane == k) sh.b = b0 + l, sh.base = lo, sh.ctx = ctx, sh.n = n;
+      }
     }
     base += __shfl_sync(0xffffffffu, x, 31);
   }
+  const Request r = request_of(p, sh.ctx, sh.n);
+  if (r.tiles > 0) {
+    const int u = (sh.pos - sh.base) / r.tiles;
+    sh.tiles = r.tiles;
+    sh.unit0 = sh.base + u * r.tiles;
+    sh.hk = u / r.rp;
+    sh.pair = u - sh.hk * r.rp;
+  }
+  if (lane < kDealt && c < kCtas) p.share[c] = sh;
+  // the rows of each CTA's first 32 pages: its producers then start from one round
+  // trip
+  int page[kDealt], pidx[kDealt], keys[kDealt], hk[kDealt];
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    if (tid + 128 * q >= kCtas) continue;
-    Share sh{total, ctas, pos[q], end[q], at[q], base_of[q], ctx_of[q], n_of[q], 0, 0, 0, 0};
-    const Request r = request_of(p, sh.ctx, sh.n);
-    if (r.tiles > 0) {
-      const int u = (sh.pos - sh.base) / r.tiles;
-      sh.tiles = r.tiles;
-      sh.unit0 = sh.base + u * r.tiles;
-      sh.hk = u / r.rp;
-      sh.pair = u - sh.hk * r.rp;
-    }
-    p.share[tid + 128 * q] = sh;
+  for (int k = 0; k < kDealt; ++k) {
+    const int b = __shfl_sync(0xffffffffu, sh.b, k);
+    pidx[k] = __shfl_sync(0xffffffffu, sh.pos - sh.unit0, k) * 8 + lane;
+    keys[k] = __shfl_sync(0xffffffffu, sh.ctx + sh.n, k);
+    hk[k] = __shfl_sync(0xffffffffu, sh.hk, k);
+    page[k] = -1;
+    if (b >= 0 && (long long)pidx[k] * 16 < keys[k])
+      page[k] = p.block_table[(size_t)b * p.max_pages + pidx[k]];
+  }
+#pragma unroll
+  for (int k = 0; k < kDealt; ++k) {
+    const int b = __shfl_sync(0xffffffffu, sh.b, k);
+    if (b >= 0 && (long long)pidx[k] * 16 < keys[k] && (page[k] < 0 || page[k] >= p.num_pages))
+      dev_fail(p.status, PIC_DEV_BAD_PAGE, b);
+    if (first + k < kCtas)
+      p.rows[(first + k) * 32 + lane] = page_row(p, page[k], pidx[k], keys[k], hk[k]);
   }
 }
 
 // ------------------------------------------------------------------ append
-// One CTA per token, and one more (blockIdx.x = max_draft of the first request)
-// that deals out the key tiles.
+// One CTA per token, and behind the first request's kDealers that deal out the
+// key tiles.
+constexpr int kDealers = (kCtas + 4 * kDealt - 1) / (4 * kDealt);
 template <int D>
 __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams rp) {
   constexpr int KC = D / 16;
@@ -203,11 +228,13 @@ __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams 
   __shared__ float2 cs[D / 2];
   __shared__ int32_t par[kMaxDraft];
   __shared__ int depth;
-  if ((int)blockIdx.x == p.max_draft) {
-    if (blockIdx.y == 0) deal_shares(p);
+  // (the dealers first: theirs is the longer chain)
+  if (blockIdx.x < kDealers) {
+    deal_shares(p, ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 5)) * kDealt);
     return;
   }
-  const int b = blockIdx.y, i = blockIdx.x, tid = threadIdx.x;
+  const int item = (int)blockIdx.x - kDealers, tid = threadIdx.x;
+  const int b = item / p.max_draft, i = item % p.max_draft;
   const size_t tok = (size_t)b * p.max_draft + i;
   // The token's projections go out before anything is known of its request:
   // chunk (8 pairs) u of the query heads, then of the key heads, two a thread (for
@@ -600,6 +627,8 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
     const uint32_t ring = sbase + (is_k ? L::kK : L::kV);
     const CUtensorMap *tmap = is_k ? &tm_k : &tm_v;
     int g = 0, nq = 0;  // key and query tiles issued
+    const int rows_first = p.rows[blockIdx.x * 32 + lane];
+    bool at_start = true;  // in the share's first segment
     bool ok = true;
     auto wait = [&](int i, uint32_t parity) {
       if (ok)
@@ -607,21 +636,7 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
       return ok;
     };
     while (ok && sg.next()) {
-      const int32_t *bt = p.block_table + (size_t)sg.b * p.max_pages;
       const int keys = sg.r.ctx + sg.r.n;
-      auto page_row = [&](int kt) {  // lanes 0..7: the row of page `lane` of tile kt
-        int y = p.oob_row;  // zeros
-        const int pidx = kt * 8 + lane;
-        if (lane < 8 && (long long)pidx * 16 < keys && pidx < p.max_pages) {
-          const int page = bt[pidx];
-          if (page >= 0 && page < p.num_pages)
-            y = (int)(p.layer_row0 + ((long long)page * p.Hkv + sg.hk) * 16);
-          else if (is_k)
-            dev_fail(p.status, PIC_DEV_BAD_PAGE, sg.b);
-        }
-        return y;
-      };
-      int y_next = page_row(sg.kt0);
       if (is_k)
         for (int t = 0; t <= (sg.two ? 1 : 0); ++t, ++nq) {
           const int qb = nq % NQB;
@@ -636,9 +651,25 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
           }
           __syncwarp();
         }
+      // The block-table entries of four tiles at a time, a lane per page, read four
+      // tiles ahead of their use.
+      const int32_t *bt = p.block_table + (size_t)sg.b * p.max_pages;
+      auto entry = [&](int j) {  // of page `lane` of the four tiles from tile j on
+        const int pidx = (sg.kt0 + j) * 8 + lane;
+        return j < sg.n && (long long)pidx * 16 < keys ? bt[pidx] : -1;
+      };
+      int next = -1, y4 = rows_first;
+      if (!at_start) next = entry(0);
       for (int j = 0; ok && j < sg.n; ++j) {
-        const int st = g % nst, kt = sg.kt0 + j, y = y_next;
-        if (j + 1 < sg.n) y_next = page_row(kt + 1);
+        const int st = g % nst, kt = sg.kt0 + j;
+        if ((j & 3) == 0 && (j > 0 || !at_start)) {
+          const int pidx = kt * 8 + lane;
+          if (is_k && (long long)pidx * 16 < keys && j + lane / 8 < sg.n &&
+              (next < 0 || next >= p.num_pages))
+            dev_fail(p.status, PIC_DEV_BAD_PAGE, sg.b);
+          y4 = page_row(p, next, pidx, keys, sg.hk);
+        }
+        const int y = __shfl_sync(0xffffffffu, y4, (j & 3) * 8 + (lane & 7));
         if (g >= nst && !wait(b_empty + st, (g / nst - 1) & 1)) break;
         if (lane == 0) mbar_expect_tx(bar(b_full + st), L::kTile);
         __syncwarp();
@@ -649,6 +680,7 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
           else
             tma_load_2d(dst, tmap, 0, y, bar(b_full + st));
         }
+        if ((j & 3) == 0) next = entry(j + 4);
         ++g;
         if (is_k) continue;
         if (kt == sg.r.tiles - 1) {
@@ -670,6 +702,7 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
         }
         if (lane == 0) mbar_arrive(bar(B_VFIX + st));
       }
+      at_start = false;
     }
     // what was issued lands before the CTA exits
     if (lane == 0) {
@@ -923,7 +956,7 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
 // -------------------------------------------------------------------- host
 struct Plan {
   int r_pad, rp_max;
-  size_t q_bytes, mask_bytes, share_bytes, base_bytes, o_bytes, ml_bytes, total;
+  size_t q_bytes, mask_bytes, share_bytes, rows_bytes, base_bytes, o_bytes, ml_bytes, total;
 };
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
@@ -935,10 +968,11 @@ inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
   pl.q_bytes = align256((size_t)batch * g->num_kv_heads * pl.r_pad * g->head_dim * 2);
   pl.mask_bytes = align256((size_t)batch * max_draft * 8);
   pl.share_bytes = align256(kCtas * sizeof(Share));
+  pl.rows_bytes = align256(kCtas * 32 * 4);
   pl.base_bytes = align256((size_t)batch * 4);
   pl.o_bytes = align256((size_t)4 * kCtas * BM * g->head_dim * 4);
   pl.ml_bytes = align256((size_t)4 * kCtas * BM * sizeof(float2));
-  pl.total = pl.q_bytes + pl.mask_bytes + pl.share_bytes + pl.base_bytes + pl.o_bytes + pl.ml_bytes;
+  pl.total = pl.q_bytes + pl.mask_bytes + pl.share_bytes + pl.rows_bytes + pl.base_bytes + pl.o_bytes + pl.ml_bytes;
   return pl;
 }
 
@@ -957,7 +991,8 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tk, const CU
            at.numRegs >= kRegLaunch;
   }();
   if (!built) return cudaErrorInvalidConfiguration;
-  e = launch_dependent(draft_append_kernel<D>, dim3(p.max_draft + 1, p.batch), dim3(128), 0, stream, p, rp);
+  e = launch_dependent(draft_append_kernel<D>, dim3(kDealers + p.max_draft * p.batch), dim3(128), 0, stream, p,
+                       rp);
   if (e != cudaSuccess) return e;
   e = launch_dependent(draft_attn_kernel<D>, dim3(kCtas), dim3(kThreads), Layout<D>::kAlloc, stream,
                        tq, tk, tv, p);
@@ -1048,6 +1083,8 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   ws += pl.mask_bytes;
   p.share = reinterpret_cast<Share *>(ws);
   ws += pl.share_bytes;
+  p.rows = reinterpret_cast<int32_t *>(ws);
+  ws += pl.rows_bytes;
   p.base = reinterpret_cast<int32_t *>(ws);
   ws += pl.base_bytes;
   p.part_o = reinterpret_cast<float *>(ws);

@@ -230,6 +230,22 @@ def test_device_checks(cuda_lib):
             check(s2, ctx[1:], draft[1:], *before)
 
 
+@pytest.mark.parametrize("ctx,at", [(100, 1), (100, 5), (9000, 300), (9000, 556)])
+def test_a_bad_page_in_the_context_reads_as_zeros(cuda_lib, ctx, at):
+    """Anywhere in a CTA's share: reported, and its keys and values count as zeros."""
+    s = draw((4, 1), 64, 0, [ctx, 40], [2, 2], 2, False, layers=1)
+    good = s["bt"][0, at].item()
+    s["kc"][0, good], s["vc"][0, good] = 0, 0
+    call(s)
+    assert cuda_lib.pic_device_status() == (0, 0)
+    out, lse = s["out"].clone(), s["lse"].clone()
+    for bad in (-1, s["num"], 2 ** 31 - 1):
+        s["bt"][0, at] = bad
+        call(s)
+        assert cuda_lib.pic_device_status() == (6, 0)
+        assert torch.equal(s["out"], out) and torch.equal(s["lse"], lse)
+
+
 def test_refusals(cuda_lib):
     import paper_2607_28069_gb300 as pic
     s = draw((4, 1), 64, 0, [16], [2], 2, False)
