@@ -70,7 +70,7 @@ enum {
 static_assert(B_COUNT * 8 + 16 <= 256, "barrier area");
 
 struct Params {
-  int batch, max_draft, Hq, Hkv, G, r_pad, rp_max, max_pages, oob_row, layer;
+  int batch, max_draft, Hq, Hkv, G, r_pad, max_pages, oob_row, layer;
   long long num_pages, layer_row0;
   const int32_t *ctx_len, *draft_len, *parent, *block_table;
   const __nv_bfloat16 *q, *k_new, *v_new;
@@ -94,10 +94,9 @@ PIC_DEV void st_global32(void *p, const float *f) {
                : "memory");
 }
 
-// What a request brings: its key tiles, row tiles and pairs of row tiles (0 for
-// one left alone).
+// What a request brings: its key tiles and row tiles (0 for one left alone).
 struct Request {
-  int ctx, n, tiles, rt, rp;
+  int ctx, n, tiles, rt;
 };
 PIC_DEV Request request_of(const Params &p, int ctx, int n) {
   Request r;
@@ -108,28 +107,41 @@ PIC_DEV Request request_of(const Params &p, int ctx, int n) {
   if (!ok) r.ctx = r.n = 0;
   r.tiles = ok ? (r.ctx + r.n + BN - 1) / BN : 0;
   r.rt = (r.n * p.G + BM - 1) / BM;
-  r.rp = (r.rt + 1) / 2;
   return r;
 }
 PIC_DEV Request request_of(const Params &p, int b) {
   return request_of(p, p.ctx_len[b], p.draft_len[b]);
 }
 
-// A CTA's share of the batch's key tiles (of which there are `total`, dealt to
-// `ctas` CTAs): tiles [pos, end), the first of them in request b, whose first tile
-// is `base`.
+// The work is counted in steps, a row tile times a key tile: a unit of two row tiles
+// has 2 `tiles` of them, two for each key tile, one of one row tile `tiles`; the
+// pairs of a kv head come first.  (Two row tiles take nearly twice the time of one
+// unless HBM sets the pace.)  A key tile belongs to the CTA whose share holds its
+// last step.
+//
+// A CTA's share of the batch's `total` steps, which are dealt to `ctas` CTAs: steps
+// [pos, end), the first of them in request b, whose first step is `base`, and
+// there in the unit of (hk, pair) that begins at unit0.
 struct alignas(16) Share {
   int total, ctas, pos, end, b, base, ctx, n;  // ctx, n: request b's
-  int unit0, hk, pair, tiles;                  // of the unit of tile pos
+  int unit0, hk, pair, pad;
 };
 
-PIC_DEV int work_of(const Params &p, const Request &r) { return p.Hkv * r.rp * r.tiles; }
+PIC_DEV int work_of(const Params &p, const Request &r) { return p.Hkv * r.rt * r.tiles; }
+
+// The unit of step pos of request r, whose first step is base.
+PIC_DEV void unit_of(const Request &r, int base, int pos, int *unit0, int *hk, int *pair) {
+  const int per = r.rt * r.tiles;  // of a kv head
+  *hk = (pos - base) / per;
+  *pair = (pos - base - *hk * per) / (2 * r.tiles);
+  *unit0 = base + *hk * per + *pair * 2 * r.tiles;
+}
 
 PIC_DEV int mul_div(int a, int b, int c) {  // a * b / c, all >= 0
   const unsigned long long x = (unsigned long long)a * b;
   return x < (1ull << 32) ? (int)((unsigned)x / (unsigned)c) : (int)(x / (unsigned)c);
 }
-// The CTA whose share holds tile t.
+// The CTA whose share holds step t.
 PIC_DEV int owner_of(int t, int total, int ctas) {
   const unsigned long long x = (unsigned long long)(t + 1) * ctas - 1;
   return x < (1ull << 32) ? (int)((unsigned)x / (unsigned)total) : (int)(x / (unsigned)total);
@@ -155,14 +167,14 @@ PIC_DEV void deal_shares(const Params &p, int first) {
     for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
     total += w;
   }
-  // two key tiles at least, one for each softmax warpgroup: half as many tiles a CTA
-  // are no faster and leave twice the partials to merge
-  const int ctas = min(kCtas, (total + 1) / 2);
+  // two steps at least, one for each softmax warpgroup: half as many are no faster
+  // and leave twice the partials to merge
+  const int ctas = min(kCtas, max(1, total / 2));
   Share sh{total, ctas, 0, 0, -1, 0, 0, 0, 0, 0, 0, 0};
-  if (lane < kDealt && c < ctas) sh.pos = mul_div(total, c, ctas), sh.end = mul_div(total, c + 1, ctas);
+  if (lane < kDealt && c < ctas && total > 0) sh.pos = mul_div(total, c, ctas), sh.end = mul_div(total, c + 1, ctas);
   int base = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
-    const Request r = b0 + lane < p.batch ? request_of(p, b0 + lane) : Request{0, 0, 0, 0, 0};
+    const Request r = b0 + lane < p.batch ? request_of(p, b0 + lane) : Request{0, 0, 0, 0};
     const int w = work_of(p, r);
     int x = w;
 #pragma unroll
@@ -171,7 +183,7 @@ PIC_DEV void deal_shares(const Params &p, int first) {
       if (lane >= o) x += y;
     }
     if (first == 0 && b0 + lane < p.batch) p.base[b0 + lane] = base + x - w;
-    // lane l's request holds tiles [base + x - w, base + x): the one of tile pos
+    // lane l's request holds steps [base + x - w, base + x): the one of step pos
 #pragma unroll
     for (int k = 0; k < kDealt; ++k) {
       const int pos = __shfl_sync(0xffffffffu, sh.pos, k), end = __shfl_sync(0xffffffffu, sh.end, k);
@@ -186,12 +198,10 @@ PIC_DEV void deal_shares(const Params &p, int first) {
     base += __shfl_sync(0xffffffffu, x, 31);
   }
   const Request r = request_of(p, sh.ctx, sh.n);
+  int kt0 = 0;
   if (r.tiles > 0) {
-    const int u = (sh.pos - sh.base) / r.tiles;
-    sh.tiles = r.tiles;
-    sh.unit0 = sh.base + u * r.tiles;
-    sh.hk = u / r.rp;
-    sh.pair = u - sh.hk * r.rp;
+    unit_of(r, sh.base, sh.pos, &sh.unit0, &sh.hk, &sh.pair);
+    kt0 = (sh.pos - sh.unit0) >> (2 * sh.pair + 1 < r.rt ? 1 : 0);
   }
   if (lane < kDealt && c < kCtas) p.share[c] = sh;
   // the rows of each CTA's first 32 pages: its producers then start from one round
@@ -200,7 +210,7 @@ PIC_DEV void deal_shares(const Params &p, int first) {
 #pragma unroll
   for (int k = 0; k < kDealt; ++k) {
     const int b = __shfl_sync(0xffffffffu, sh.b, k);
-    pidx[k] = __shfl_sync(0xffffffffu, sh.pos - sh.unit0, k) * 8 + lane;
+    pidx[k] = __shfl_sync(0xffffffffu, kt0, k) * 8 + lane;
     keys[k] = __shfl_sync(0xffffffffu, sh.ctx + sh.n, k);
     hk[k] = __shfl_sync(0xffffffffu, sh.hk, k);
     page[k] = -1;
@@ -325,16 +335,15 @@ __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams 
 // The segments of one CTA, walked by each role's warp for itself.
 struct Segments {
   const Params &p;
-  int pos, end;         // next key tile (the host keeps them below 2^31), end of this
-                        // CTA's share
-  int base;             // first tile of request b
+  int pos, end;         // next step (the host keeps them below 2^31), end of this CTA's share
+  int base;             // first step of request b
   int b, cta;
   Request r;
   // the present segment
   int hk, pair, kt0, n;
   bool two;          // the pair has two row tiles
   bool first, last;  // holds the unit's first, last key tile
-  int unit0;         // the unit's first tile
+  int unit0;         // the unit's first step
 
   PIC_DEV Segments(const Params &pp, int cta_) : p(pp), cta(cta_) {
     const int4 *q = reinterpret_cast<const int4 *>(p.share + cta);
@@ -343,25 +352,25 @@ struct Segments {
     b = y.x, base = y.y;
     r = request_of(p, y.z, y.w);
     unit0 = z.x, hk = z.y, pair = z.z;  // the first segment's unit
+    two = 2 * pair + 1 < r.rt;
   }
   PIC_DEV bool next() {
     if (pos >= end) return false;
-    if (pos >= unit0 + r.tiles) {  // a unit behind the first segment's
+    if (pos >= unit0 + (r.tiles << (two ? 1 : 0))) {  // a unit behind the first segment's
       while (pos - base >= work_of(p, r)) {
         base += work_of(p, r);
         r = request_of(p, ++b);
       }
-      const int u = (pos - base) / r.tiles;
-      unit0 = base + u * r.tiles;
-      hk = u / r.rp;
-      pair = u % r.rp;
+      unit_of(r, base, pos, &unit0, &hk, &pair);
+      two = 2 * pair + 1 < r.rt;
     }
-    kt0 = pos - unit0;
-    n = min(r.tiles - kt0, end - pos);
-    two = 2 * pair + 1 < r.rt;
+    const int shift = two ? 1 : 0;
+    kt0 = (pos - unit0) >> shift;
+    n = min(r.tiles, (end - unit0) >> shift) - kt0;
+    if (n <= 0) return false;  // half a key tile of the next CTA's
     first = kt0 == 0;
     last = kt0 + n == r.tiles;
-    pos += n;
+    pos = last ? unit0 + (r.tiles << shift) : end;
     return true;
   }
   // the partial slot of row tile t of the present segment: a CTA has at most
@@ -873,8 +882,9 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   if (i >= r.n || h >= p.Hq) return;  // (kWarps = 4: the whole CTA)
   const int hk = h / p.G, rr = i * p.G + h % p.G, rt = rr / BM, row = rr % BM, pair = rt / 2;
   const int total = p.share[0].total, ctas = p.share[0].ctas;
-  const int t0 = p.base[b] + (hk * r.rp + pair) * r.tiles;
-  const int2 u = make_int2(owner_of(t0, total, ctas), owner_of(t0 + r.tiles - 1, total, ctas));
+  const int step = 2 * pair + 1 < r.rt ? 2 : 1, t0 = p.base[b] + (hk * r.rt + pair * 2) * r.tiles;
+  const int2 u = make_int2(owner_of(t0 + step - 1, total, ctas),
+                           owner_of(t0 + step * r.tiles - 1, total, ctas));
   if (u.x == u.y) return;  // finished by its CTA
   const int parts = u.y - u.x + 1, t = 2 * pair + 1 < r.rt ? rt & 1 : 0;
   // partial c is the one of CTA u.x + c; this warp's are c = w0, w0 + kWarps, ...
@@ -955,7 +965,7 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
 
 // -------------------------------------------------------------------- host
 struct Plan {
-  int r_pad, rp_max;
+  int r_pad;
   size_t q_bytes, mask_bytes, share_bytes, rows_bytes, base_bytes, o_bytes, ml_bytes, total;
 };
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -963,7 +973,6 @@ inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
   Plan pl;
   const int G = g->num_q_heads / g->num_kv_heads;
   const int rt_max = (int)(((long long)max_draft * G + BM - 1) / BM);
-  pl.rp_max = (rt_max + 1) / 2;
   pl.r_pad = rt_max * BM;
   pl.q_bytes = align256((size_t)batch * g->num_kv_heads * pl.r_pad * g->head_dim * 2);
   pl.mask_bytes = align256((size_t)batch * max_draft * 8);
@@ -1047,7 +1056,7 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   const long long rows_total = (long long)geom->num_layers * num_pages * Hkv * 16;
   const Plan pl = plan(geom, batch, max_draft);
   if (rows_total + 16 >= INT32_MAX || (long long)batch * Hkv * pl.r_pad >= INT32_MAX ||
-      (double)batch * Hkv * pl.rp_max * (max_pages / 8 + 1) >= INT32_MAX)
+      (double)batch * Hkv * (pl.r_pad / BM) * (max_pages / 8 + 1) >= INT32_MAX)
     return fail(PIC_ERR_UNSUPPORTED, "%s: cache or queries have more than 2^31 rows", who);
   if (batch > 65535) return fail(PIC_ERR_UNSUPPORTED, "%s: grid too large", who);
   if (!workspace || workspace_bytes < pl.total || (reinterpret_cast<uintptr_t>(workspace) & 255))
@@ -1060,7 +1069,6 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   p.Hkv = Hkv;
   p.G = p.Hq / Hkv;
   p.r_pad = pl.r_pad;
-  p.rp_max = pl.rp_max;
   p.max_pages = max_pages;
   p.oob_row = (int)((rows_total + 15) / 16 * 16);
   p.layer = layer;
