@@ -309,9 +309,10 @@ __global__ void __launch_bounds__(kReleaseThreads) release_kernel(FreeParams p) 
 
 // ---------------------------------------------------------------- compact
 constexpr int kSeg = 16;      // kept positions per CTA
-constexpr int kUnits = 8;     // 32-byte units of a thread
+constexpr int kUnits = 4;     // 32-byte units of a thread
+constexpr int kMoveCtas = 4;  // of an SM
 constexpr int kMoveThreads = 256;
-constexpr int kCheckThreads = 1024, kCheckDeep = 8;
+constexpr int kCheckThreads = 1024;  // kept positions of a checking CTA
 
 struct CompactParams {
   int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, layers, layer_begin, rotate;
@@ -325,6 +326,8 @@ struct CompactParams {
   // head group, segment) "reads done"
   longlong2 *slot;       // [n][max_keep]
   int32_t *wait_from;    // [n][segs]
+  int32_t *bad;          // [n][checks]: a checking CTA found a fault
+  int checks;
   int32_t *ticket, *flags;
   int32_t *status;
 };
@@ -344,81 +347,52 @@ PIC_DEV int compact_start(const CompactParams &p, int j, int *code) {
   return s;
 }
 
-// kN entries of a keep list at once (i[q] < 0: none): their checks and their
-// slots, as page * 16 + row of the page.
-template <int kN>
-PIC_DEV int compact_entries(const CompactParams &p, int j, int s, const int *i, int *k,
-                            longlong2 *slot) {
+// Entry i of a keep list: its checks and its slots, as page * 16 + row of the page.
+PIC_DEV int compact_entry(const CompactParams &p, int j, int s, int i, int *k_out,
+                          longlong2 *slot) {
   const int32_t *t = p.block_table + (size_t)p.row[j] * p.max_pages;
   const int32_t *kp = p.keep + (size_t)j * p.max_keep;
-  int before[kN], a[kN], z[kN], refs[kN], code = PIC_DEV_OK;
-#pragma unroll
-  for (int q = 0; q < kN; ++q) {
-    k[q] = i[q] >= 0 ? kp[i[q]] : 0;
-    before[q] = i[q] > 0 ? kp[i[q] - 1] : -1;
-  }
-#pragma unroll
-  for (int q = 0; q < kN; ++q) {
-    a[q] = z[q] = -1;
-    if (i[q] < 0) continue;
-    if (k[q] < i[q] || before[q] >= k[q]) {  // ascending from >= 0 on: never below i
-      code = PIC_DEV_BAD_POSITION;
-    } else if ((long long)s + k[q] >= (long long)p.max_pages * kPage) {
-      code = PIC_DEV_BLOCK_TABLE_SHORT;
-    } else {
-      a[q] = t[(s + k[q]) / kPage];
-      z[q] = t[(s + i[q]) / kPage];
-      if (a[q] < 0 || a[q] >= p.num_pages || z[q] < 0 || z[q] >= p.num_pages) {
-        code = PIC_DEV_BAD_PAGE;
-        a[q] = z[q] = -1;
-      }
-    }
-  }
-#pragma unroll
-  for (int q = 0; q < kN; ++q) refs[q] = z[q] >= 0 && k[q] != i[q] ? p.page_refs[z[q]] : 1;
-#pragma unroll
-  for (int q = 0; q < kN; ++q) {
-    if (refs[q] != 1) code = PIC_DEV_SHARED_PAGE;
-    slot[q] = make_longlong2((long long)a[q] * kPage + (s + k[q]) % kPage,
-                             (long long)z[q] * kPage + (s + i[q]) % kPage);
-  }
-  return code;
+  const int k = kp[i], before = i > 0 ? kp[i - 1] : -1;
+  if (k < i || before >= k) return PIC_DEV_BAD_POSITION;  // ascending from >= 0 on: never below i
+  if ((long long)s + k >= (long long)p.max_pages * kPage) return PIC_DEV_BLOCK_TABLE_SHORT;
+  const int a = t[(s + k) / kPage], z = t[(s + i) / kPage];
+  if (a < 0 || a >= p.num_pages || z < 0 || z >= p.num_pages) return PIC_DEV_BAD_PAGE;
+  if (k != i && p.page_refs[z] != 1) return PIC_DEV_SHARED_PAGE;
+  *k_out = k;
+  *slot = make_longlong2((long long)a * kPage + (s + k) % kPage, (long long)z * kPage + (s + i) % kPage);
+  return PIC_DEV_OK;
 }
 
-// Lists of more than one segment, one CTA per listed row: every check before
-// anything moves (the verdict goes to result), the slots, the segments to wait
-// for, the flags cleared.  Eight entries of a thread at a time, because an entry is
-// a chain of three loads: 9001 entries 33 us one at a time with 256 threads.
+// Lists of more than one segment, one CTA per 1024 entries of a listed row: every
+// check before anything moves, the slots, the segments to wait for, the flags
+// cleared.  (One CTA for a list of 9001 entries took 15 us: an entry is a chain of
+// three loads.)
 __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactParams p) {
   pdl_entry();
-  const int j = blockIdx.x, tid = threadIdx.x;
+  const int j = blockIdx.y, tid = threadIdx.x, i0 = blockIdx.x * kCheckThreads;
   const long long per = (long long)p.layers * p.hgroups * p.segs;
-  for (long long i = tid; i < per; i += kCheckThreads) p.flags[j * per + i] = 0;
-  if (j == 0 && tid == 0) *p.ticket = 0;
+  for (long long i = i0 + tid; i < per; i += (long long)p.checks * kCheckThreads)
+    p.flags[j * per + i] = 0;
+  if (j == 0 && i0 == 0 && tid == 0) *p.ticket = 0;
   int code = PIC_DEV_OK;
   const int s = compact_start(p, j, &code);
   const int m = s >= 0 ? p.keep_len[j] : 0;
-  for (int i0 = tid; i0 < m && code == PIC_DEV_OK; i0 += kCheckThreads * kCheckDeep) {
-    int i[kCheckDeep], k[kCheckDeep];
-    longlong2 slot[kCheckDeep];
-#pragma unroll
-    for (int q = 0; q < kCheckDeep; ++q)
-      i[q] = i0 + q * kCheckThreads < m ? i0 + q * kCheckThreads : -1;
-    code = compact_entries<kCheckDeep>(p, j, s, i, k, slot);
-#pragma unroll
-    for (int q = 0; q < kCheckDeep; ++q)
-      if (i[q] >= 0) p.slot[(size_t)j * p.max_keep + i[q]] = slot[q];
+  if (i0 + tid < m) {
+    int k;
+    longlong2 slot;
+    code = compact_entry(p, j, s, i0 + tid, &k, &slot);
+    if (code == PIC_DEV_OK) p.slot[(size_t)j * p.max_keep + i0 + tid] = slot;
   }
-  if (code != PIC_DEV_OK) dev_fail(p.status, code, j);
+  if (code != PIC_DEV_OK && (s >= 0 || (tid == 0 && i0 == 0))) dev_fail(p.status, code, j);
   const bool bad = __syncthreads_or(code != PIC_DEV_OK);
-  if (tid == 0) p.result[j] = bad ? -1 : s + m;
+  if (tid == 0) p.bad[j * p.checks + blockIdx.x] = bad;
   if (bad) return;
   // segment s2 reads up to its last keep entry, segment seg writes from 16 seg
   // on: s2 is the first to wait for of the segments that begin behind s2 - 1's
   // last source and not behind its own
   const int32_t *kp = p.keep + (size_t)j * p.max_keep;
-  const int segs = (m + kSeg - 1) / kSeg;
-  for (int s2 = tid; s2 < segs; s2 += kCheckThreads) {
+  const int segs = (m + kSeg - 1) / kSeg, s2 = i0 / kSeg + tid;
+  if (tid < kCheckThreads / kSeg && s2 < segs) {
     const int lo = s2 ? kp[s2 * kSeg - 1] / kSeg : -1;
     const int hi = min(kp[min((s2 + 1) * kSeg, m) - 1] / kSeg, segs - 1);
     for (int seg = lo + 1; seg <= hi; ++seg) p.wait_from[(size_t)j * p.segs + seg] = s2;
@@ -437,7 +411,7 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
 // segment per row, and every CTA checks its list itself (16 entries), so the call
 // is a launch shorter.
 template <int D, bool kLong>
-__global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactParams p, RopeParams rp) {
+__global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(CompactParams p, RopeParams rp) {
   constexpr int KC = D / 16;  // 8-pair chunks of a row
   pdl_entry();
   __shared__ float2 cs[kSeg][D / 2];
@@ -456,27 +430,34 @@ __global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactPa
       const int t = tid - (kMoveThreads - kSeg);
       if (t >= 0) {
         const size_t i = (size_t)j * p.max_keep + min(seg * kSeg + t, p.max_keep - 1);
-        const int k = p.keep[i], res = p.result[j], m = p.keep_len[j];
+        bool bad = false;
+        for (int c = t; c < p.checks; c += kSeg) bad |= p.bad[j * p.checks + c] != 0;
+        bad = __any_sync(0xffffu << (32 - kSeg), bad);
+        const int k = p.keep[i], m = p.keep_len[j];
         const int lo = p.wait_from[(size_t)j * p.segs + seg];
         slot_of[buf][t] = p.slot[i];
         k_of[buf][t] = k;
         if (t == 0) {
-          next_cnt[buf] = res < 0 ? 0 : max(0, min(kSeg, m - seg * kSeg));
+          next_cnt[buf] = bad ? 0 : max(0, min(kSeg, m - seg * kSeg));
           next_lo[buf] = lo;
+          if (at % lhs == 0 && seg == 0) {  // one CTA of a row reports
+            int code;
+            p.result[j] = bad ? -1 : compact_start(p, j, &code) + m;
+          }
         }
       }
     } else if (tid < 32) {
       int code = PIC_DEV_OK;
       const int s = compact_start(p, j, &code), m = s >= 0 ? p.keep_len[j] : 0;
-      int i[1] = {tid < m ? tid : -1}, k[1];
-      longlong2 slot[1];
-      if (s >= 0) code = compact_entries<1>(p, j, s, i, k, slot);
+      int k = 0;
+      longlong2 slot = make_longlong2(0, 0);
+      if (tid < m) code = compact_entry(p, j, s, tid, &k, &slot);
       const bool bad = __any_sync(0xffffffffu, code != PIC_DEV_OK);
       if (at % lhs == 0) {  // one CTA of a row reports
         if (code != PIC_DEV_OK && (tid == 0 || s >= 0)) dev_fail(p.status, code, j);
         if (tid == 0) p.result[j] = bad ? -1 : s + m;
       }
-      if (tid < kSeg && s >= 0) k_of[buf][tid] = k[0], slot_of[buf][tid] = slot[0];
+      if (tid < kSeg) k_of[buf][tid] = k, slot_of[buf][tid] = slot;
       if (tid == 0) next_cnt[buf] = bad ? 0 : m;
     }
   };
@@ -526,12 +507,16 @@ __global__ void __launch_bounds__(kMoveThreads, 2) compact_move_kernel(CompactPa
     }
     if constexpr (kLong) {
       int32_t *fl = p.flags + ((long long)j * lhs + lh) * p.segs;
-      __threadfence();
+      // every thread's loads are done at the barrier; thread 0's fence orders them,
+      // and not only its own, before the flag
       __syncthreads();
       const long long after = next_at;
       bool ok = true;
       if (cnt > 0) {
-        if (tid == 0) atomicExch(fl + seg, 1);
+        if (tid == 0) {
+          __threadfence();
+          atomicExch(fl + seg, 1);
+        }
         if (after < all) look_up(after, buf ^ 1);
         for (int s2 = seg - 1 - tid; ok && s2 >= next_lo[buf]; s2 -= kMoveThreads)
           ok = wait_flag(fl + s2, p.status, j);
@@ -667,15 +652,17 @@ static int heads_per_group(const pic_geom_t *g) {
   return kMoveThreads * kUnits / (kSeg * 2 * (g->head_dim / 16));
 }
 struct CompactSpace {  // byte offsets in the workspace
-  size_t wait, ticket, flags, total;
+  size_t wait, bad, ticket, flags, total;
 };
+static int compact_checks(int max_keep) { return (max_keep + kCheckThreads - 1) / kCheckThreads; }
 static CompactSpace compact_space(const pic_geom_t *g, int n, int max_keep, int layers) {
   const int hg = heads_per_group(g);
   const size_t groups = (size_t)(g->num_kv_heads + hg - 1) / hg;
   const size_t segs = ((size_t)max_keep + kSeg - 1) / kSeg;
   CompactSpace c;
   c.wait = (size_t)n * max_keep * sizeof(longlong2);
-  c.ticket = c.wait + (size_t)n * segs * 4;
+  c.bad = c.wait + (size_t)n * segs * 4;
+  c.ticket = c.bad + (size_t)n * compact_checks(max_keep) * 4;
   c.flags = c.ticket + 4;
   c.total = segs <= 1 ? 0 : c.flags + (size_t)n * layers * groups * segs * 4;
   return c;
@@ -684,10 +671,10 @@ static CompactSpace compact_space(const pic_geom_t *g, int n, int max_keep, int 
 template <int D>
 static cudaError_t launch_move(const CompactParams &cp, const RopeParams &rp, long long items,
                                pic_stream_t stream) {
-  // two CTAs an SM hold 16 positions each: the long form's stay
+  // the long form's CTAs stay
   if (cp.flags)
     return launch_dependent(compact_move_kernel<D, true>,
-                            dim3((unsigned)std::min(items, 2LL * 152)), dim3(kMoveThreads), 0, stream,
+                            dim3((unsigned)std::min(items, kMoveCtas * 152LL)), dim3(kMoveThreads), 0, stream,
                             cp, rp);
   return launch_dependent(compact_move_kernel<D, false>, dim3((unsigned)items), dim3(kMoveThreads), 0,
                           stream, cp, rp);
@@ -815,7 +802,8 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
   cp.result = result;
   cp.k = static_cast<__nv_bfloat16 *>(k_cache) + layer_begin * cp.layer_elems;
   cp.v = static_cast<__nv_bfloat16 *>(v_cache) + layer_begin * cp.layer_elems;
-  cp.flags = cp.ticket = cp.wait_from = nullptr;
+  cp.flags = cp.ticket = cp.wait_from = cp.bad = nullptr;
+  cp.checks = compact_checks(max_keep);
   cp.slot = nullptr;
   const CompactSpace cw = compact_space(geom, n, max_keep, cp.layers);
   if (cw.total) {
@@ -824,6 +812,7 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     cp.slot = reinterpret_cast<longlong2 *>(ws);
     cp.wait_from = reinterpret_cast<int32_t *>(ws + cw.wait);
+    cp.bad = reinterpret_cast<int32_t *>(ws + cw.bad);
     cp.ticket = reinterpret_cast<int32_t *>(ws + cw.ticket);
     cp.flags = reinterpret_cast<int32_t *>(ws + cw.flags);
   }
@@ -835,7 +824,7 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
   if (!cp.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
   cudaError_t e = cudaSuccess;
   if (cp.flags)
-    e = launch_dependent(compact_check_kernel, dim3(n), dim3(kCheckThreads), 0, stream, cp);
+    e = launch_dependent(compact_check_kernel, dim3(cp.checks, n), dim3(kCheckThreads), 0, stream, cp);
   if (e == cudaSuccess)
     e = geom->head_dim == 128 ? launch_move<128>(cp, rp, items, stream)
                               : launch_move<64>(cp, rp, items, stream);
