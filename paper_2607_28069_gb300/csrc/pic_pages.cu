@@ -322,10 +322,10 @@ struct CompactParams {
   int32_t *result;
   __nv_bfloat16 *k, *v;  // at layer_begin
   // several segments (workspace): from and to slot of every kept position, per
-  // (row, segment) the first segment to wait for, a ticket, and per (row, layer and
+  // (row, segment) the first and last segment to wait for, a ticket, and per (row, layer and
   // head group, segment) "reads done"
   longlong2 *slot;       // [n][max_keep]
-  int32_t *wait_from;    // [n][segs]
+  int2 *wait;            // [n][segs]
   int32_t *bad;          // [n][checks]: a checking CTA found a fault
   int checks;
   int32_t *ticket, *flags;
@@ -387,21 +387,27 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
   const bool bad = __syncthreads_or(code != PIC_DEV_OK);
   if (tid == 0) p.bad[j * p.checks + blockIdx.x] = bad;
   if (bad) return;
-  // segment s2 reads up to its last keep entry, segment seg writes from 16 seg
-  // on: s2 is the first to wait for of the segments that begin behind s2 - 1's
-  // last source and not behind its own
+  // Segment s2 reads positions keep[16 s2] .. its last entry, segment seg writes
+  // 16 seg .. 16 seg + 15: the ones to wait for are the first s2 that reads as far as
+  // 16 seg to the last that begins at or below 16 seg + 15.  Each s2 notes itself as
+  // the first for the segments from behind s2 - 1's last source to its own, and as
+  // the last for those from its first source to ahead of s2 + 1's.
   const int32_t *kp = p.keep + (size_t)j * p.max_keep;
   const int segs = (m + kSeg - 1) / kSeg, s2 = i0 / kSeg + tid;
   if (tid < kCheckThreads / kSeg && s2 < segs) {
+    int2 *w = p.wait + (size_t)j * p.segs;
+    const int begin = kp[s2 * kSeg] / kSeg;
+    const int end = min(s2 + 1 < segs ? kp[(s2 + 1) * kSeg] / kSeg : segs, segs);
     const int lo = s2 ? kp[s2 * kSeg - 1] / kSeg : -1;
     const int hi = min(kp[min((s2 + 1) * kSeg, m) - 1] / kSeg, segs - 1);
-    for (int seg = lo + 1; seg <= hi; ++seg) p.wait_from[(size_t)j * p.segs + seg] = s2;
+    for (int seg = s2 ? begin : 0; seg < end; ++seg) w[seg].y = seg < begin ? -1 : s2;
+    for (int seg = lo + 1; seg <= hi; ++seg) w[seg].x = s2;
   }
 }
 
 // A CTA moves 16 kept positions x a group of kv heads x a layer of one row: it
 // reads them all into registers, says so, waits for the CTAs whose sources lie
-// in what it overwrites, and stores.  keep is ascending, so those are CTAs of
+// in what it overwrites (few, and long past where much was left out), and stores.  keep is ascending, so those are CTAs of
 // earlier segments of the same (row, layer, head group) only; a segment comes from
 // a ticket, so they have started before it, and they read before they wait: every
 // wait ends.  Keys move by i - keep[i] positions and are re-rotated by that, with
@@ -417,7 +423,8 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
   __shared__ float2 cs[kSeg][D / 2];
   __shared__ int32_t k_of[2][kSeg];
   __shared__ longlong2 slot_of[2][kSeg];
-  __shared__ int next_at, next_cnt[2], next_lo[2];
+  __shared__ int next_at, next_cnt[2];
+  __shared__ int2 next_wait[2];
   const int tid = threadIdx.x, lhs = p.layers * p.hgroups;
   const long long all = (long long)lhs * p.n * p.segs;
   const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
@@ -434,12 +441,12 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
         for (int c = t; c < p.checks; c += kSeg) bad |= p.bad[j * p.checks + c] != 0;
         bad = __any_sync(0xffffu << (32 - kSeg), bad);
         const int k = p.keep[i], m = p.keep_len[j];
-        const int lo = p.wait_from[(size_t)j * p.segs + seg];
+        const int2 wait = p.wait[(size_t)j * p.segs + seg];
         slot_of[buf][t] = p.slot[i];
         k_of[buf][t] = k;
         if (t == 0) {
           next_cnt[buf] = bad ? 0 : max(0, min(kSeg, m - seg * kSeg));
-          next_lo[buf] = lo;
+          next_wait[buf] = make_int2(wait.x, min(wait.y, seg - 1));
           if (at % lhs == 0 && seg == 0) {  // one CTA of a row reports
             int code;
             p.result[j] = bad ? -1 : compact_start(p, j, &code) + m;
@@ -518,7 +525,7 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
           atomicExch(fl + seg, 1);
         }
         if (after < all) look_up(after, buf ^ 1);
-        for (int s2 = seg - 1 - tid; ok && s2 >= next_lo[buf]; s2 -= kMoveThreads)
+        for (int s2 = next_wait[buf].x + tid; ok && s2 <= next_wait[buf].y; s2 += kMoveThreads)
           ok = wait_flag(fl + s2, p.status, j);
       } else if (after < all) {
         look_up(after, buf ^ 1);
@@ -661,7 +668,7 @@ static CompactSpace compact_space(const pic_geom_t *g, int n, int max_keep, int 
   const size_t segs = ((size_t)max_keep + kSeg - 1) / kSeg;
   CompactSpace c;
   c.wait = (size_t)n * max_keep * sizeof(longlong2);
-  c.bad = c.wait + (size_t)n * segs * 4;
+  c.bad = c.wait + (size_t)n * segs * sizeof(int2);
   c.ticket = c.bad + (size_t)n * compact_checks(max_keep) * 4;
   c.flags = c.ticket + 4;
   c.total = segs <= 1 ? 0 : c.flags + (size_t)n * layers * groups * segs * 4;
@@ -802,7 +809,8 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
   cp.result = result;
   cp.k = static_cast<__nv_bfloat16 *>(k_cache) + layer_begin * cp.layer_elems;
   cp.v = static_cast<__nv_bfloat16 *>(v_cache) + layer_begin * cp.layer_elems;
-  cp.flags = cp.ticket = cp.wait_from = cp.bad = nullptr;
+  cp.flags = cp.ticket = cp.bad = nullptr;
+  cp.wait = nullptr;
   cp.checks = compact_checks(max_keep);
   cp.slot = nullptr;
   const CompactSpace cw = compact_space(geom, n, max_keep, cp.layers);
@@ -811,7 +819,7 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
       return fail(PIC_ERR_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", who, cw.total);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     cp.slot = reinterpret_cast<longlong2 *>(ws);
-    cp.wait_from = reinterpret_cast<int32_t *>(ws + cw.wait);
+    cp.wait = reinterpret_cast<int2 *>(ws + cw.wait);
     cp.bad = reinterpret_cast<int32_t *>(ws + cw.bad);
     cp.ticket = reinterpret_cast<int32_t *>(ws + cw.ticket);
     cp.flags = reinterpret_cast<int32_t *>(ws + cw.flags);
