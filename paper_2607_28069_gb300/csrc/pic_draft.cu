@@ -32,10 +32,6 @@ constexpr int kCtas = 152;         // one per SM
 constexpr int NSK = 3, NSV = 2;    // ring stages of K and V
 constexpr int NQB = 2;             // query tiles
 constexpr int kThreads = 384;      // K producer, MMA, V producer, ring, two softmax warpgroups
-constexpr int kRegLaunch = 168;    // 65536 / kThreads, whole eights
-constexpr int kRegControl = 88, kRegSoftmax = 208;
-static_assert(128 * kRegControl + 256 * kRegSoftmax <= kThreads * kRegLaunch,
-              "setmaxnreg split exceeds the registers the CTA is launched with");
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;    // S_t at 128 t, O_t at 256 + D t
 // Named barriers (0: __syncthreads): P_t from warpgroup t to the MMA warp, the
@@ -396,12 +392,11 @@ struct Segments {
 // accumulators on its behalf) and the softmax warps on named barriers only.  These
 // have no limit, so after a wait that ran out every role still walks all segments
 // and meets each barrier; the MMA warp then issues nothing but its commits.
-// The body is one function per group of warps (kSoftmax: the two softmax
-// warpgroups, else the four control warps), entered right after the group's
-// setmaxnreg, so that no value lives across the reallocation.
-template <int D, bool kSoftmax>
-PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
-                             const CUtensorMap &tm_v, const Params &p) {
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    draft_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
+                      const __grid_constant__ CUtensorMap tm_k,
+                      const __grid_constant__ CUtensorMap tm_v, Params p) {
   using L = Layout<D>;
   constexpr int PANELS = D / 64;
   constexpr uint32_t IDESC_QK = idesc_bf16(BM, BN, false, false);
@@ -438,7 +433,7 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
   const int detail = -2;
 
   Segments sg(p, (int)blockIdx.x);
-  if constexpr (kSoftmax) {
+  if (warp >= 4) {
     // ===================================================== softmax
     const int t = (warp - 4) >> 2, wq = warp & 3, row = wq * 32 + lane;
     const uint32_t tl = tbase + ((uint32_t)(wq * 32) << 16);
@@ -848,20 +843,6 @@ PIC_DEV void draft_attn_body(const CUtensorMap &tm_q, const CUtensorMap &tm_k,
   }
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
-    draft_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
-                      const __grid_constant__ CUtensorMap tm_k,
-                      const __grid_constant__ CUtensorMap tm_v, Params p) {
-  if (threadIdx.x < 128) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegControl));
-    draft_attn_body<D, false>(tm_q, tm_k, tm_v, p);
-  } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegSoftmax));
-    draft_attn_body<D, true>(tm_q, tm_k, tm_v, p);
-  }
-}
-
 // ------------------------------------------------------------------- merge
 // o = sum_c w_c O_c / sum_c w_c l_c, w_c = 2^(m_c - M), over the CTAs that hold
 // key tiles of a row's unit.  kWarps warps per (token, query head), each with its
@@ -992,14 +973,6 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tk, const CU
                                        cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        Layout<D>::kAlloc);
   if (e != cudaSuccess) return e;
-  // the setmaxnreg split needs the registers the kernel was built to launch with:
-  // with fewer the softmax warpgroups would wait for them for ever
-  static const bool built = [] {
-    cudaFuncAttributes at;
-    return cudaFuncGetAttributes(&at, draft_attn_kernel<D>) == cudaSuccess &&
-           at.numRegs >= kRegLaunch;
-  }();
-  if (!built) return cudaErrorInvalidConfiguration;
   e = launch_dependent(draft_append_kernel<D>, dim3(kDealers + p.max_draft * p.batch), dim3(128), 0, stream, p,
                        rp);
   if (e != cudaSuccess) return e;

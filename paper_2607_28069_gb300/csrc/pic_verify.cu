@@ -26,9 +26,11 @@ namespace verify {
 constexpr int kMaxDraft = 64;
 constexpr int kMaxVocab = 1 << 24;
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kCluster = 8;
 constexpr int kChunk = 1024;
-constexpr int kMaxChunks = kMaxVocab / kChunk / kCluster;  // of one CTA
+// Requests up to which a cluster has 16 CTAs instead of 8 (us, vocabulary 2^17, 8 and
+// 16 CTAs): chain of 8, 4 requests 5.9 and 4.2, 12 6.0 and 5.1, 16 6.0 and 7.4, 64 12.1
+// and 22.3; tree of 8, 12 requests 11.1 and 9.6, 24 15.4 and 16.4.
+constexpr int kWideBatch = 12;
 
 struct Params {
   int max_draft, vocab;
@@ -39,8 +41,9 @@ struct Params {
   int32_t *status;
 };
 
+template <int kCluster>
 struct Shared {
-  uint64_t chunk[kMaxChunks];   // sums of this CTA's chunks
+  uint64_t chunk[kMaxVocab / kChunk / kCluster];  // sums of this CTA's chunks
   uint64_t tile[32 * 33];       // the weights of the chunk that is searched
   uint64_t warp[kWarps];
   uint64_t totals[2][kCluster]; // every CTA's sum, written by that CTA (by turns)
@@ -100,65 +103,72 @@ PIC_DEV void load_entries(const float *p, const float *q, int x0, int vocab, flo
     for (int i = 0; i < N; ++i) a[i] = __fsub_rn(a[i], b[i]);
 }
 
-// The sum of one chunk (32 loads of a lane in flight), the same in every lane.
-template <bool kBoth>
-PIC_DEV uint64_t chunk_sum(const float *p, const float *q, int c, int vocab) {
-  constexpr int N = kBoth ? 16 : 32;
+// A chunk in pieces of N entries a lane (lane l's are l, 32 + l, ...), each given
+// to work(a, i), i the number of its first entry.
+template <int N, bool kBoth, typename F>
+PIC_DEV void walk_chunk(const float *p, const float *q, int c, int vocab, float *a, F &&work) {
   const int x0 = c * kChunk + (threadIdx.x & 31);
-  Weights w;
 #pragma unroll 1
   for (int i = 0; i < 32; i += N) {
-    float a[N];
     load_entries<N, kBoth>(p, q, x0 + 32 * i, vocab, a);
-#pragma unroll
-    for (int k = 0; k < N; ++k) w.add(a[k]);
+    work(a, i);
   }
-  uint64_t s = w.sum(32);
+}
+PIC_DEV uint64_t warp_sum(uint64_t s) {  // the same in every lane
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return s;
 }
-
-// One warp: the entry of chunk c where the running sum passes `left`.
-template <bool kBoth>
-PIC_DEV int search_chunk(Shared &sh, const float *p, const float *q, int c, int vocab, uint64_t left) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll 1
-  for (int i = 0; i < 32; i += 16) {
-    float a[16];
-    load_entries<16, kBoth>(p, q, c * kChunk + 32 * i + lane, vocab, a);
+// N of a chunk's entries into the search's tile, which is then searched by one
+// warp: the entry of chunk c where the running sum passes `left`.
+template <int N>
+PIC_DEV void fill_tile(uint64_t *tile, const float *a, int i) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      Weights w;
-      w.add(a[k]);
-      sh.tile[(i + k) * 33 + lane] = w.sum(1);
-    }
+  for (int k = 0; k < N; ++k) {
+    Weights w;
+    w.add(a[k]);
+    tile[(i + k) * 33 + (threadIdx.x & 31)] = w.sum(1);
   }
+}
+PIC_DEV int search_tile(const uint64_t *tile, int c, uint64_t left) {
+  const int lane = threadIdx.x & 31;
   __syncwarp();
   uint64_t v = 0;  // lane l: entries 32 l .. 32 l + 31
-#pragma unroll
-  for (int k = 0; k < 32; ++k) v += sh.tile[lane * 33 + k];
+#pragma unroll 8
+  for (int k = 0; k < 32; ++k) v += tile[lane * 33 + k];
   uint64_t x = scan64(v);
   const int row = __ffs(__ballot_sync(0xffffffffu, x > left)) - 1;
   left -= __shfl_sync(0xffffffffu, x - v, row);
-  x = scan64(sh.tile[row * 33 + lane]);
+  x = scan64(tile[row * 33 + lane]);
   return c * kChunk + row * 32 + __ffs(__ballot_sync(0xffffffffu, x > left)) - 1;
 }
 
 // One draw by the whole cluster.  Returns false where the row has no weight.
 // The token goes to every CTA's sh.found (kAll) or is written to *out by the CTA
 // that finds it.  turn: the draws of a kernel alternate between 0 and 1.
-template <bool kBoth, bool kAll>
-PIC_DEV bool draw(Shared &sh, int turn, const float *p, const float *q, int vocab, float u,
+template <int kCluster, bool kBoth, bool kAll>
+PIC_DEV bool draw(Shared<kCluster> &sh, int turn, const float *p, const float *q, int vocab, float u,
                   int32_t *out) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)cluster_rank();
   const int chunks = (vocab + kChunk - 1) / kChunk;
   const int c0 = (int)((long long)chunks * rank / kCluster);
   const int c1 = (int)((long long)chunks * (rank + 1) / kCluster);
+  // A wide cluster's warps keep their chunk's entries, which are then searched
+  // without another read where a warp has a single chunk; a narrow one has the
+  // registers for four CTAs an SM instead.
+  constexpr bool kKeep = kCluster == 16;
+  constexpr int N = kKeep || !kBoth ? 32 : 16;
   uint64_t mine = 0;
+  float a[N];
+#pragma unroll 1
   for (int c = c0 + warp; c < c1; c += kWarps) {
-    const uint64_t s = chunk_sum<kBoth>(p, q, c, vocab);
+    Weights w;
+    walk_chunk<N, kBoth>(p, q, c, vocab, a, [&](const float *v, int) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) w.add(v[k]);
+    });
+    const uint64_t s = warp_sum(w.sum(32));
     if (lane == 0) sh.chunk[c - c0] = s;
     mine += s;
   }
@@ -171,48 +181,57 @@ PIC_DEV bool draw(Shared &sh, int turn, const float *p, const float *q, int voca
     st_cluster64(map_to_rank(smem_u32(&sh.totals[turn][rank]), tid), s);
   }
   cluster_sync_all();
-  uint64_t total = 0, t[kCluster];
+  uint64_t total = 0, before = 0, own = 0;
 #pragma unroll
-  for (int c = 0; c < kCluster; ++c) total += t[c] = sh.totals[turn][c];
+  for (int c = 0; c < kCluster; ++c) {
+    const uint64_t t = sh.totals[turn][c];
+    if (c < rank) before += t;
+    if (c == rank) own = t;
+    total += t;
+  }
   // floor(total * floor(2^24 u) / 2^24); u outside [0, 1) (NaN: 0)
   const uint64_t n = (uint64_t)fminf(fmaxf(u, 0.f) * 16777216.f, 16777215.f);
   const uint64_t at = (__umul64hi(total, n) << 40) | ((total * n) >> 24);
-  uint64_t run = 0, left = 0;
-  bool owner = false;
-#pragma unroll
-  for (int c = 0; c < kCluster; ++c) {
-    if (c == rank && run <= at && at < run + t[c]) owner = true, left = at - run;
-    run += t[c];
-  }
-  if (owner && warp == 0) {
-    int c = 0;
-    for (;; c += 32) {  // the chunk: 32 sums at a time
-      const uint64_t v = c + lane < c1 - c0 ? sh.chunk[c + lane] : 0, x = scan64(v);
-      const unsigned past = __ballot_sync(0xffffffffu, x > left);
-      if (past) {
-        const int l = __ffs(past) - 1;
-        left -= __shfl_sync(0xffffffffu, x - v, l);
-        c += l;
-        break;
+  if (before <= at && at < before + own) {  // this CTA holds the threshold
+    uint64_t left = at - before;
+    const bool single = kKeep && c1 - c0 <= kWarps;  // a chunk a warp
+    int c = -1;  // the chunk, where this warp has to search it
+    if (single || warp == 0) {
+      for (int i = 0;; i += 32) {  // 32 sums at a time
+        const uint64_t v = i + lane < c1 - c0 ? sh.chunk[i + lane] : 0, x = scan64(v);
+        const unsigned past = __ballot_sync(0xffffffffu, x > left);
+        if (past) {
+          const int l = __ffs(past) - 1;
+          left -= __shfl_sync(0xffffffffu, x - v, l);
+          c = c0 + i + l;
+          break;
+        }
+        left -= __shfl_sync(0xffffffffu, x, 31);
       }
-      left -= __shfl_sync(0xffffffffu, x, 31);
+      if (single && c != c0 + warp) c = -1;
     }
-    const int x = search_chunk<kBoth>(sh, p, q, c0 + c, vocab, left);
-    if constexpr (kAll) {
-      if (lane < kCluster) st_cluster32(map_to_rank(smem_u32(&sh.found), lane), x);
-    } else if (lane == 0) {
-      *out = x;
+    if (c >= 0) {
+      if (single)
+        fill_tile<N>(sh.tile, a, 0);
+      else
+        walk_chunk<N, kBoth>(p, q, c, vocab, a, [&](const float *v, int i) { fill_tile<N>(sh.tile, v, i); });
+      const int x = search_tile(sh.tile, c, left);
+      if constexpr (kAll) {
+        if (lane < kCluster) st_cluster32(map_to_rank(smem_u32(&sh.found), lane), x);
+      } else if (lane == 0) {
+        *out = x;
+      }
     }
   }
   if constexpr (kAll) cluster_sync_all();
   return total != 0;
 }
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 4)
-    verify_kernel(Params p) {
+template <int kCluster>
+__global__ void __launch_bounds__(kThreads, kCluster == 16 ? 2 : 4) verify_kernel(Params p) {
   pdl_entry();
   extern __shared__ __align__(16) uint8_t smem[];
-  Shared &sh = *reinterpret_cast<Shared *>(smem);
+  Shared<kCluster> &sh = *reinterpret_cast<Shared<kCluster> *>(smem);
   // every CTA of the cluster runs before another one writes to its shared memory
   asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31;
@@ -254,9 +273,9 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 4)
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     const float *row = target + (len - 1) * p.tt;
     const float un = u[n - 1];
-    if (len < n && draw<true, false>(sh, 0, row, draft + (len - 1) * p.dt, p.vocab, un, p.next + b))
+    if (len < n && draw<kCluster, true, false>(sh, 0, row, draft + (len - 1) * p.dt, p.vocab, un, p.next + b))
       return;
-    if (!draw<false, false>(sh, 1, row, nullptr, p.vocab, un, p.next + b) && writer && lane == 0)
+    if (!draw<kCluster, false, false>(sh, 1, row, nullptr, p.vocab, un, p.next + b) && writer && lane == 0)
       p.next[b] = -1;
     return;
   }
@@ -272,7 +291,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 4)
     int at = 0;
     if (writer && lane == 0) path[0] = 0;
     for (len = 1;; ++len) {
-      next = draw<false, true>(sh, len & 1, target + at * p.tt, nullptr, p.vocab, u[len - 1], nullptr)
+      next = draw<kCluster, false, true>(sh, len & 1, target + at * p.tt, nullptr, p.vocab, u[len - 1], nullptr)
                  ? sh.found : -1;
       // each warp alike: the first child that carries the token
       const bool h0 = i0 < n && i0 > at && tok0 == next && par0 == at && next >= 0;
@@ -292,6 +311,17 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 4)
   }
 }
 
+template <int kCluster>
+static cudaError_t launch(const Params &p, int batch, cudaStream_t stream) {
+  if (kCluster > 8) {
+    const cudaError_t e = cudaFuncSetAttribute(verify_kernel<kCluster>,
+                                               cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_dependent_cluster(verify_kernel<kCluster>, dim3((unsigned)(batch * kCluster)),
+                                  dim3(kThreads), sizeof(Shared<kCluster>), stream, kCluster, p);
+}
+
 }  // namespace verify
 }  // namespace pic
 
@@ -307,7 +337,7 @@ extern "C" pic_status_t pic_verify_draft(int32_t batch, int32_t max_draft, int32
   static const char *who = "pic_verify_draft";
   if (batch <= 0 || max_draft <= 0 || vocab <= 0)
     return fail(PIC_ERR_INVALID_ARG, "%s: sizes must be positive", who);
-  if (max_draft > kMaxDraft || vocab > kMaxVocab || batch > INT32_MAX / kCluster)
+  if (max_draft > kMaxDraft || vocab > kMaxVocab || batch > INT32_MAX / 16)
     return fail(PIC_ERR_UNSUPPORTED, "%s: max_draft %d (at most %d), vocab %d (at most %d)", who,
                 max_draft, kMaxDraft, vocab, kMaxVocab);
   if (!tokens || !draft_len || !target_prob || !target_stride || !uniform || !path || !path_len ||
@@ -322,8 +352,7 @@ extern "C" pic_status_t pic_verify_draft(int32_t batch, int32_t max_draft, int32
            target_stride[0], target_stride[1], draft_prob ? draft_stride[0] : 0,
            draft_prob ? draft_stride[1] : 0, path, path_len, next_token, device_status_ptr()};
   if (!p.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
-  cudaError_t e = launch_dependent(verify_kernel, dim3((unsigned)(batch * kCluster)), dim3(kThreads),
-                                   sizeof(Shared), stream, p);
+  cudaError_t e = batch <= kWideBatch ? launch<16>(p, batch, stream) : launch<8>(p, batch, stream);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? PIC_OK : cuda_fail(e, who);
 }
