@@ -8,10 +8,12 @@ from __future__ import annotations
 
 import torch
 
-from . import (Geometry, _check, _native, pic_append_inline, pic_attend_decode, pic_attend_prefill,
-               pic_attend_prefill_fused, pic_compose, pic_copy_async, pic_decode_workspace_size,
-               pic_link, pic_prefill_fused_workspace_size, pic_prefill_plan_splits, pic_relocate,
-               pic_relocate_mapped)
+from . import (Geometry, _check, _native, pic_append_inline, pic_attend_decode, pic_attend_draft,
+               pic_attend_prefill, pic_attend_prefill_fused, pic_compose, pic_copy_async,
+               pic_decode_workspace_size, pic_draft_workspace_size, pic_link, pic_page_compact,
+               pic_page_compact_workspace_size, pic_page_fork, pic_page_free, pic_page_reserve,
+               pic_prefill_fused_workspace_size, pic_prefill_plan_splits, pic_relocate,
+               pic_relocate_mapped, pic_verify_draft)
 from .workloads import Workload
 
 
@@ -341,3 +343,92 @@ class CacheHitPath:
     def decode_pass(self, step: int):
         for layer in range(self.wl.spec.layers):
             self.decode(step, layer)
+
+
+class DraftDecoder:
+    """Speculative decoding over the contexts that a CacheHitPath has linked.
+
+    Rows 0 .. B - 1 are the path's requests as its prefill left them; further rows
+    are empty until ``fork`` makes them branches.  Every row's pages come from the
+    path's cache, whose pages beyond the requests' own (a workload with a larger
+    ``num_pages``, or decode steps it does not take) are the free ones.  One step:
+
+    * ``begin`` -- room for max_draft tokens behind every row in use;
+    * ``attend`` per layer -- the drafts' keys and values appended, their attention
+      in ``out[layer]`` (rows without drafts: draft_len 0);
+    * ``accept`` -- with the target's probabilities of the drafts: the accepted
+      path (``path``, ``path_len``), the token after it (``next_token``), the
+      accepted tokens' keys and values moved together, ctx_len advanced.
+
+    All device work, no synchronisation: a step can be captured in a CUDA graph.
+    """
+
+    def __init__(self, path: CacheHitPath, max_draft: int, rows: int | None = None,
+                 max_new: int = 256):
+        wl, dev = path.wl, path.k_cache.device
+        self.path, self.geom, self.max_draft = path, path.geom, max_draft
+        self.num_pages = wl.num_pages
+        B, have = wl.block_table.shape
+        self.rows = max(B, rows or B)
+        page = wl.spec.page_size
+        max_pages = max(have, -(-(path.max_ctx + max_new + max_draft) // page))
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.block_table = torch.full((self.rows, max_pages), -1, **i32)
+        self.block_table[:B, :have] = wl.block_table
+        self.ctx_len = torch.zeros(self.rows, **i32)
+        self.ctx_len[:B] = path.ctx_len
+        used = wl.block_table[wl.block_table >= 0].long()
+        self.page_refs = torch.bincount(used, minlength=self.num_pages).to(torch.int32)
+        self.all_rows = torch.arange(self.rows, **i32)
+        self._use(range(B))
+        self.result = torch.empty(self.rows, **i32)
+        self.path_idx = torch.empty((self.rows, max_draft), **i32)
+        self.path_len = torch.empty(self.rows, **i32)
+        self.next_token = torch.empty(self.rows, **i32)
+        g = self.geom
+        self.out = torch.empty((g.num_layers, self.rows, max_draft, g.num_q_heads, g.head_dim),
+                               dtype=torch.bfloat16, device=dev)
+        self.ws = torch.empty(pic_draft_workspace_size(g, self.rows, max_draft), dtype=torch.uint8,
+                              device=dev)
+        self.ws_compact = torch.empty(pic_page_compact_workspace_size(g, self.rows, max_draft),
+                                      dtype=torch.uint8, device=dev)
+
+    def _use(self, rows):
+        self.in_use = sorted(rows)
+        self._active = self._rows(self.in_use)
+
+    def _rows(self, rows):
+        return torch.tensor(list(rows), dtype=torch.int32, device=self.block_table.device)
+
+    def begin(self):
+        pic_page_reserve(self._active, self.max_draft, self.ctx_len, self.block_table,
+                         self.num_pages, self.page_refs, self.result[:len(self.in_use)])
+
+    def attend(self, layer: int, q, k, v, draft_len, parent=None, lse=None):
+        """Drafts of one layer: q [rows][max_draft][Hq][d], k and v
+        [rows][max_draft][Hkv][d] un-rotated (or tuples, as everywhere)."""
+        pic_attend_draft(self.geom, layer, q, k, v, self.ctx_len, draft_len, self.block_table,
+                         self.num_pages, self.path.k_cache, self.path.v_cache, (self.out, layer),
+                         parent=parent, lse=lse, workspace=self.ws)
+
+    def accept(self, tokens, draft_len, target_prob, uniform, draft_prob=None, parent=None):
+        pic_verify_draft(tokens, draft_len, target_prob, uniform, self.path_idx, self.path_len,
+                         self.next_token, draft_prob=draft_prob, parent=parent)
+        pic_page_compact(self.geom, self.all_rows, self.path_idx, self.path_len, self.ctx_len,
+                         self.block_table, self.num_pages, self.page_refs, self.path.k_cache,
+                         self.path.v_cache, self.result, reserve=self.max_draft,
+                         workspace=self.ws_compact)
+
+    def fork(self, src, dst):
+        """Rows dst (not in use) become branches of rows src: two lists of row numbers."""
+        if len(src) != len(dst) or set(dst) & set(self.in_use) or len(set(dst)) < len(dst):
+            raise ValueError("fork: every branch needs a row of its own that is not in use")
+        pic_page_fork(self.geom, self._rows(src), self._rows(dst), self.ctx_len, self.block_table,
+                      self.num_pages, self.page_refs, self.path.k_cache, self.path.v_cache,
+                      self.result[:len(dst)], reserve=self.max_draft)
+        self._use(self.in_use + list(dst))
+
+    def release(self, rows):
+        """The listed rows end: their pages go back."""
+        pic_page_free(self._rows(rows), self.block_table, self.num_pages, self.page_refs, self.ctx_len)
+        self._use(set(self.in_use) - set(rows))
