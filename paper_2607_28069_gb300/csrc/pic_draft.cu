@@ -120,7 +120,7 @@ PIC_DEV Request request_of(const Params &p, int b) {
 // there in the unit of (hk, pair) that begins at unit0.
 struct alignas(16) Share {
   int total, ctas, pos, end, b, base, ctx, n;  // ctx, n: request b's
-  int unit0, hk, pair, pad;
+  int unit0, hk, pair, per;                    // per: total / ctas
 };
 
 PIC_DEV int work_of(const Params &p, const Request &r) { return p.Hkv * r.rt * r.tiles; }
@@ -133,15 +133,22 @@ PIC_DEV void unit_of(const Request &r, int base, int pos, int *unit0, int *hk, i
   *unit0 = base + *hk * per + *pair * 2 * r.tiles;
 }
 
-PIC_DEV int mul_div(int a, int b, int c) {  // a * b / c, all >= 0
-  const unsigned long long x = (unsigned long long)a * b;
-  return x < (1ull << 32) ? (int)((unsigned)x / (unsigned)c) : (int)(x / (unsigned)c);
-}
-// The CTA whose share holds step t.
-PIC_DEV int owner_of(int t, int total, int ctas) {
-  const unsigned long long x = (unsigned long long)(t + 1) * ctas - 1;
-  return x < (1ull << 32) ? (int)((unsigned)x / (unsigned)total) : (int)(x / (unsigned)total);
-}
+// The first step of CTA c's share, floor(total c / ctas), without a 64-bit product
+// or a division: total = q ctas + r, and r c < 2^15 leaves (r c + 1/2) / ctas at least
+// 1 / 304 away from a whole number, far more than its rounding.
+struct Deal {
+  int ctas, q, r;
+  float inv;
+  PIC_DEV Deal(int total, int n, int quotient) : ctas(n), q(quotient), r(total - q * n), inv(1.f / (float)max(n, 1)) {}
+  PIC_DEV int first(int c) const { return q * c + (int)(((float)(r * c) + 0.5f) * inv); }
+  // The CTA whose share holds step t: a rounded estimate, then exact.
+  PIC_DEV int owner(int t, int total) const {
+    int c = min(ctas - 1, (int)((float)(t + 1) * (float)ctas / (float)total));
+    while (first(c) > t) --c;
+    while (first(c + 1) <= t) ++c;
+    return c;
+  }
+};
 
 // The K/V row (of the whole cache) of page pidx of request b's kv head hk; zeros
 // are read for a page past the last key or outside the cache.
@@ -166,8 +173,9 @@ PIC_DEV void deal_shares(const Params &p, int first) {
   // two steps at least, one for each softmax warpgroup: half as many are no faster
   // and leave twice the partials to merge
   const int ctas = min(kCtas, max(1, total / 2));
-  Share sh{total, ctas, 0, 0, -1, 0, 0, 0, 0, 0, 0, 0};
-  if (lane < kDealt && c < ctas && total > 0) sh.pos = mul_div(total, c, ctas), sh.end = mul_div(total, c + 1, ctas);
+  Share sh{total, ctas, 0, 0, -1, 0, 0, 0, 0, 0, 0, total / ctas};
+  const Deal deal(total, ctas, total / ctas);
+  if (lane < kDealt && c < ctas && total > 0) sh.pos = deal.first(c), sh.end = deal.first(c + 1);
   int base = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
     const Request r = b0 + lane < p.batch ? request_of(p, b0 + lane) : Request{0, 0, 0, 0};
@@ -224,44 +232,42 @@ PIC_DEV void deal_shares(const Params &p, int first) {
 }
 
 // ------------------------------------------------------------------ append
-// One CTA per token, and behind the first request's kDealers that deal out the
-// key tiles.
-constexpr int kDealers = (kCtas + 4 * kDealt - 1) / (4 * kDealt);
+// One CTA per token, behind `dealers` CTAs that deal out the work.  A thread takes
+// a chunk (8 pairs) of a query or key head, and a value piece: the host gives the
+// CTAs as many threads as there are chunks, up to kAppendMax.  One place in the code
+// rotates, because a call starts with cold instruction caches (three chunks a
+// thread, their rotations unrolled, took 4.6 us instead of @A us for 32/8 heads).
+constexpr int kAppendMax = 512;
 template <int D>
-__global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams rp) {
+__global__ void __launch_bounds__(kAppendMax) draft_append_kernel(Params p, RopeParams rp, int dealers) {
   constexpr int KC = D / 16;
   pdl_entry();
   __shared__ float2 cs[D / 2];
   __shared__ int32_t par[kMaxDraft];
   __shared__ int depth;
   // (the dealers first: theirs is the longer chain)
-  if (blockIdx.x < kDealers) {
-    deal_shares(p, ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 5)) * kDealt);
+  const int tid = threadIdx.x, threads = blockDim.x;
+  if ((int)blockIdx.x < dealers) {
+    deal_shares(p, ((int)blockIdx.x * (threads >> 5) + (tid >> 5)) * kDealt);
     return;
   }
-  const int item = (int)blockIdx.x - kDealers, tid = threadIdx.x;
+  const int item = (int)blockIdx.x - dealers;
   const int b = item / p.max_draft, i = item % p.max_draft;
   const size_t tok = (size_t)b * p.max_draft + i;
-  // The token's projections go out before anything is known of its request:
-  // chunk (8 pairs) u of the query heads, then of the key heads, two a thread (for
-  // more the loop below goes on), and the value pieces.
+  // The token's projections go out before anything is known of its request
   const int units = (p.Hq + p.Hkv) * KC;
-  auto source = [&](int u) {
-    const int h = u / KC;
-    return h < p.Hq ? p.q + (tok * p.Hq + h) * D : p.k_new + (tok * p.Hkv + h - p.Hq) * D;
-  };
+  // (the CTA's threads are a multiple of KC: a thread's chunk of a row is always the
+  // same)
   const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
-  constexpr int kAhead = 3;
-  uint4 qa[kAhead], qb[kAhead], vn = make_uint4(0, 0, 0, 0);
-#pragma unroll
-  for (int a = 0; a < kAhead; ++a) {
-    qa[a] = qb[a] = make_uint4(0, 0, 0, 0);
-    if (tid + 128 * a < units) {
-      const __nv_bfloat16 *src = source(tid + 128 * a);
-      qa[a] = ld_stream(src + pc.off_a);
-      qb[a] = ld_stream(src + pc.off_b);
-    }
-  }
+  uint4 qa = make_uint4(0, 0, 0, 0), qb = qa, vn = qa;
+  auto load = [&](int u) {
+    const int h = u / KC;
+    const __nv_bfloat16 *src =
+        h < p.Hq ? p.q + (tok * p.Hq + h) * D : p.k_new + (tok * p.Hkv + h - p.Hq) * D;
+    qa = ld_stream(src + pc.off_a);
+    qb = ld_stream(src + pc.off_b);
+  };
+  if (tid < units) load(tid);
   const int pieces = p.Hkv * (D / 8);
   const __nv_bfloat16 *v_src = p.v_new + tok * p.Hkv * D;
   if (tid < pieces) vn = ld_stream(v_src + tid * 8);
@@ -299,28 +305,20 @@ __global__ void __launch_bounds__(128) draft_append_kernel(Params p, RopeParams 
   __syncthreads();
   if (tid < D / 2) cs[tid] = rope_cos_sin_turn(ctx + depth, turn);
   __syncthreads();
-  auto store = [&](int u, uint4 a, uint4 c) {
+#pragma unroll 1
+  for (int u = tid; u < units; u += threads) {
+    if (u != tid) load(u);
     const int h = u / KC, hk = h < p.Hq ? h / p.G : h - p.Hq;
-    __nv_bfloat16 *dst;
+    __nv_bfloat16 *dst = nullptr;
     if (h < p.Hq)
       dst = p.qp + ((size_t)(b * p.Hkv + hk) * p.r_pad + i * p.G + h - hk * p.G) * D;
     else if (page >= 0)
       dst = p.k_cache + (((size_t)page * p.Hkv + hk) * 16 + slot % 16) * D;
-    else
-      return;
-    rotate_store(a, c, dst, pc, rp.style, cs + 8 * (tid % KC));
-  };
-  // (128 is a multiple of KC: a thread's chunk of a row is always the same)
-#pragma unroll
-  for (int a = 0; a < kAhead; ++a)
-    if (tid + 128 * a < units) store(tid + 128 * a, qa[a], qb[a]);
-#pragma unroll 1
-  for (int u = tid + 128 * kAhead; u < units; u += 128) {
-    const __nv_bfloat16 *src = source(u);
-    store(u, ld_stream(src + pc.off_a), ld_stream(src + pc.off_b));
+    if (dst) rotate_store(qa, qb, dst, pc, rp.style, cs + 8 * (tid % KC));
   }
   if (page >= 0)
-    for (int u = tid; u < pieces; u += 128) {
+#pragma unroll 1
+    for (int u = tid; u < pieces; u += threads) {
       const int hk = u / (D / 8), c = u % (D / 8);
       st_global16(p.v_cache + (((size_t)page * p.Hkv + hk) * 16 + slot % 16) * D + c * 8,
                   u == tid ? vn : ld_stream(v_src + u * 8));
@@ -862,10 +860,10 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   const Request r = request_of(p, b);
   if (i >= r.n || h >= p.Hq) return;  // (kWarps = 4: the whole CTA)
   const int hk = h / p.G, rr = i * p.G + h % p.G, rt = rr / BM, row = rr % BM, pair = rt / 2;
-  const int total = p.share[0].total, ctas = p.share[0].ctas;
+  const int total = p.share[0].total;
   const int step = 2 * pair + 1 < r.rt ? 2 : 1, t0 = p.base[b] + (hk * r.rt + pair * 2) * r.tiles;
-  const int2 u = make_int2(owner_of(t0 + step - 1, total, ctas),
-                           owner_of(t0 + step * r.tiles - 1, total, ctas));
+  const Deal deal(total, p.share[0].ctas, p.share[0].per);
+  const int2 u = make_int2(deal.owner(t0 + step - 1, total), deal.owner(t0 + step * r.tiles - 1, total));
   if (u.x == u.y) return;  // finished by its CTA
   const int parts = u.y - u.x + 1, t = 2 * pair + 1 < r.rt ? rt & 1 : 0;
   // partial c is the one of CTA u.x + c; this warp's are c = w0, w0 + kWarps, ...
@@ -874,7 +872,22 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
     c = c * kWarps + w0;
     return (size_t)((2 * (u.x + c) + (c == 0 ? 1 : 0)) * 2 + t) * BM + row;
   };
-  float M = -INFINITY;
+  float v[U][CPL], M = -INFINITY, l = 0.f, acc[CPL];
+  auto load = [&](int c0) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float *src = p.part_o + part_row(min(c0 + k, mine - 1)) * D + lane * CPL;
+      if constexpr (CPL == 4) {
+        const float4 f = *reinterpret_cast<const float4 *>(src);
+        v[k][0] = f.x, v[k][1] = f.y, v[k][2] = f.z, v[k][3] = f.w;
+      } else {
+        const float2 f = *reinterpret_cast<const float2 *>(src);
+        v[k][0] = f.x, v[k][1] = f.y;
+      }
+    }
+  };
+  if (mine > 0) load(0);  // beside the (m, l) pairs
+#pragma unroll 1
   for (int c = lane; c < mine; c += 32) {
     const float2 ml = p.part_ml[part_row(c)];
     w_s[warp][c] = ml;
@@ -882,7 +895,7 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  float l = 0.f, acc[CPL];
+#pragma unroll 1
   for (int c = lane; c < mine; c += 32) {
     const float2 ml = w_s[warp][c];
     const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
@@ -896,18 +909,7 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
 #pragma unroll 1
   for (int c0 = 0; c0 < mine; c0 += U) {
-    float v[U][CPL];
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const float *src = p.part_o + part_row(min(c0 + k, mine - 1)) * D + lane * CPL;
-      if constexpr (CPL == 4) {
-        const float4 f = *reinterpret_cast<const float4 *>(src);
-        v[k][0] = f.x, v[k][1] = f.y, v[k][2] = f.z, v[k][3] = f.w;
-      } else {
-        const float2 f = *reinterpret_cast<const float2 *>(src);
-        v[k][0] = f.x, v[k][1] = f.y;
-      }
-    }
+    if (c0) load(c0);
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const float wk = c0 + k < mine ? w_s[warp][c0 + k].x : 0.f;
@@ -973,8 +975,10 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tk, const CU
                                        cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        Layout<D>::kAlloc);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(draft_append_kernel<D>, dim3(kDealers + p.max_draft * p.batch), dim3(128), 0, stream, p,
-                       rp);
+  const int threads = std::min(kAppendMax, std::max(128, ((p.Hq + p.Hkv) * (D / 16) + 31) / 32 * 32));
+  const int dealers = (kCtas + threads / 32 * kDealt - 1) / (threads / 32 * kDealt);
+  e = launch_dependent(draft_append_kernel<D>, dim3(dealers + p.max_draft * p.batch), dim3(threads), 0,
+                       stream, p, rp, dealers);
   if (e != cudaSuccess) return e;
   e = launch_dependent(draft_attn_kernel<D>, dim3(kCtas), dim3(kThreads), Layout<D>::kAlloc, stream,
                        tq, tk, tv, p);
