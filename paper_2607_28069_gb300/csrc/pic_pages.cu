@@ -124,6 +124,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
           if (len % kPage && (ta[at] < 0 || ta[at] >= p.num_pages)) code = PIC_DEV_BAD_PAGE;
         } else {
           int lo = (len + kPage - 1) / kPage, hi = (int)want;  // the first entry without a page
+          if (lo < hi) {  // mostly all or none are there
+            const bool none = tr[lo] < 0, all = tr[hi - 1] >= 0;
+            if (none) hi = lo;
+            else if (all) lo = hi;
+          }
           while (lo < hi) {
             const int mid = (lo + hi) >> 1;
             if (tr[mid] >= 0) lo = mid + 1;
@@ -312,6 +317,7 @@ constexpr int kSeg = 16;      // kept positions per CTA
 constexpr int kUnits = 4;     // 32-byte units of a thread
 constexpr int kMoveCtas = 4;  // of an SM
 constexpr int kMoveThreads = 256;
+static_assert(kSeg == 16, "half a warp looks a segment's positions up");
 constexpr int kCheckThreads = 1024;  // kept positions of a checking CTA
 
 struct CompactParams {
