@@ -705,9 +705,9 @@ pic_status_t pic_page_fork(const pic_geom_t *geom, int32_t n, const int32_t *src
  * unchanged: drafted tokens already carry the position of their depth.
  * keep: int32 [n][max_keep]; keep_len: int32 [n], 0 .. max_keep (0 keeps
  * nothing); result int32 [n]: the row's new length.
- * workspace: pic_page_compact_workspace_size(...) bytes (0 for max_keep <= 16;
+ * workspace: pic_page_compact_workspace_size(...) bytes (0 for max_keep <= 64;
  * then it may be NULL), 256-byte aligned, contents do not matter.
- * At least one layer.  Two launches (three for max_keep > 16).  Positions are
+ * At least one layer.  Two launches (three for max_keep > 64).  Positions are
  * copied once, also where source and target ranges overlap: each CTA holds 16
  * rows on chip and stores them when the CTAs that read what it overwrites have
  * done so.

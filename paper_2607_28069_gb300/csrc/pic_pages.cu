@@ -313,7 +313,8 @@ __global__ void __launch_bounds__(kReleaseThreads) release_kernel(FreeParams p) 
 }
 
 // ---------------------------------------------------------------- compact
-constexpr int kSeg = 16;      // kept positions per CTA
+constexpr int kSeg = 16;      // kept positions that a CTA holds at once
+constexpr int kShort = 64;    // longest list that one CTA per (row, layer, heads) works off
 constexpr int kUnits = 4;     // 32-byte units of a thread
 constexpr int kMoveCtas = 4;  // of an SM
 constexpr int kMoveThreads = 256;
@@ -327,7 +328,7 @@ struct CompactParams {
   const int32_t *ctx_len, *block_table, *page_refs;
   int32_t *result;
   __nv_bfloat16 *k, *v;  // at layer_begin
-  // several segments (workspace): from and to slot of every kept position, per
+  // lists beyond kShort (workspace): from and to slot of every kept position, per
   // (row, segment) the first and last segment to wait for, a ticket, and per (row, layer and
   // head group, segment) "reads done"
   longlong2 *slot;       // [n][max_keep]
@@ -369,7 +370,7 @@ PIC_DEV int compact_entry(const CompactParams &p, int j, int s, int i, int *k_ou
   return PIC_DEV_OK;
 }
 
-// Lists of more than one segment, one CTA per 1024 entries of a listed row: every
+// Lists beyond kShort, one CTA per 1024 entries of a listed row: every
 // check before anything moves, the slots, the segments to wait for, the flags
 // cleared.  (One CTA for a list of 9001 entries took 15 us: an entry is a chain of
 // three loads.)
@@ -418,26 +419,29 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
 // a ticket, so they have started before it, and they read before they wait: every
 // wait ends.  Keys move by i - keep[i] positions and are re-rotated by that, with
 // cos/sin of the 16 moves formed once per CTA.
-// kLong: several segments, checked by compact_check_kernel, by CTAs that stay
-// and look up the next segment's positions while they wait.  Otherwise one
-// segment per row, and every CTA checks its list itself (16 entries), so the call
-// is a launch shorter.
+// kLong: lists checked by compact_check_kernel, moved by CTAs that stay and look up
+// the next segment's positions while they wait.  Otherwise (windows of drafts: up
+// to kShort entries, mostly few of them kept) a CTA takes all segments of a (row,
+// layer, head group) in turn, which needs no flags -- a segment's targets lie below
+// the next one's sources -- and checks the list itself, so the call is a launch
+// shorter.
 template <int D, bool kLong>
 __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(CompactParams p, RopeParams rp) {
   constexpr int KC = D / 16;  // 8-pair chunks of a row
   pdl_entry();
   __shared__ float2 cs[kSeg][D / 2];
-  __shared__ int32_t k_of[2][kSeg];
-  __shared__ longlong2 slot_of[2][kSeg];
+  constexpr int kBufs = kLong ? 2 : kShort / kSeg;
+  __shared__ int32_t k_of[kBufs][kSeg];
+  __shared__ longlong2 slot_of[kBufs][kSeg];
   __shared__ int next_at, next_cnt[2];
   __shared__ int2 next_wait[2];
   const int tid = threadIdx.x, lhs = p.layers * p.hgroups;
-  const long long all = (long long)lhs * p.n * p.segs;
+  const int all = lhs * p.n * (kLong ? p.segs : 1);  // (the host keeps it below 2^30)
   const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
 
   // the positions of item `at` into buffer `buf` (the count 0: nothing to move)
-  auto look_up = [&](long long at, int buf) {
-    const int j = (int)(at / lhs % p.n), seg = (int)(at / lhs / p.n);
+  auto look_up = [&](int at, int buf) {
+    const int j = at / lhs % p.n, seg = at / lhs / p.n;
     if constexpr (kLong) {
       // the last 16 threads: their loads run beside the others' polls
       const int t = tid - (kMoveThreads - kSeg);
@@ -459,23 +463,26 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
           }
         }
       }
-    } else if (tid < 32) {
+    } else {  // the whole list
       int code = PIC_DEV_OK;
       const int s = compact_start(p, j, &code), m = s >= 0 ? p.keep_len[j] : 0;
-      int k = 0;
-      longlong2 slot = make_longlong2(0, 0);
-      if (tid < m) code = compact_entry(p, j, s, tid, &k, &slot);
-      const bool bad = __any_sync(0xffffffffu, code != PIC_DEV_OK);
+      if (tid < m) {
+        int k = 0;
+        longlong2 slot = make_longlong2(0, 0);
+        code = compact_entry(p, j, s, tid, &k, &slot);
+        k_of[tid / kSeg][tid % kSeg] = k;
+        slot_of[tid / kSeg][tid % kSeg] = slot;
+      }
+      const bool bad = __syncthreads_or(code != PIC_DEV_OK);
       if (at % lhs == 0) {  // one CTA of a row reports
         if (code != PIC_DEV_OK && (tid == 0 || s >= 0)) dev_fail(p.status, code, j);
         if (tid == 0) p.result[j] = bad ? -1 : s + m;
       }
-      if (tid < kSeg) k_of[buf][tid] = k, slot_of[buf][tid] = slot;
-      if (tid == 0) next_cnt[buf] = bad ? 0 : m;
+      if (tid == 0) next_cnt[0] = bad ? 0 : m;
     }
   };
 
-  long long at = blockIdx.x;
+  int at = blockIdx.x;
   if constexpr (kLong) {
     if (tid == 0) next_at = atomicAdd(p.ticket, 1);
     __syncthreads();
@@ -486,10 +493,13 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
   uint64_t turn = 0;            // (fp64 work: once, not once per segment)
   if (at < all) look_up(at, 0);
   __syncthreads();
-  while (at < all) {
-    const int lh = (int)(at % lhs), j = (int)(at / lhs % p.n), seg = (int)(at / lhs / p.n);
+  const int len = kLong ? 0 : next_cnt[0];  // of the whole list
+  while (at < all && (kLong || buf * kSeg < len)) {
+    const int lh = at % lhs, j = at / lhs % p.n;
+    const int seg = kLong ? at / lhs / p.n : buf;
     const int layer = lh / p.hgroups, h0 = (lh % p.hgroups) * p.hgroup;
-    const int heads = min(p.hgroup, p.hkv - h0), cnt = next_cnt[buf], i0 = seg * kSeg;
+    const int heads = min(p.hgroup, p.hkv - h0), i0 = seg * kSeg;
+    const int cnt = kLong ? next_cnt[buf] : min(kSeg, len - i0);
     // ---- read: unit u = (position, K or V, head, chunk)
     const long long lbase = (long long)layer * p.layer_elems;
     // (division by KC heads <= 64 as a product: exact for u < 2048)
@@ -523,7 +533,7 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
       // every thread's loads are done at the barrier; thread 0's fence orders them,
       // and not only its own, before the flag
       __syncthreads();
-      const long long after = next_at;
+      const int after = next_at;
       bool ok = true;
       if (cnt > 0) {
         if (tid == 0) {
@@ -540,7 +550,6 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
       at = after;
     } else {
       __syncthreads();
-      at = all;
     }
     // ---- store
 #pragma unroll
@@ -556,10 +565,8 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
         }
       }
     }
-    if constexpr (kLong) {
-      __syncthreads();  // cs and the buffer may be written again
-      buf ^= 1;
-    }
+    if (kLong || (buf + 1) * kSeg < len) __syncthreads();  // cs and the buffer may be written again
+    buf = kLong ? buf ^ 1 : buf + 1;
   }
 }
 
@@ -677,7 +684,7 @@ static CompactSpace compact_space(const pic_geom_t *g, int n, int max_keep, int 
   c.bad = c.wait + (size_t)n * segs * sizeof(int2);
   c.ticket = c.bad + (size_t)n * compact_checks(max_keep) * 4;
   c.flags = c.ticket + 4;
-  c.total = segs <= 1 ? 0 : c.flags + (size_t)n * layers * groups * segs * 4;
+  c.total = max_keep <= kShort ? 0 : c.flags + (size_t)n * layers * groups * segs * 4;
   return c;
 }
 
@@ -830,7 +837,7 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
     cp.ticket = reinterpret_cast<int32_t *>(ws + cw.ticket);
     cp.flags = reinterpret_cast<int32_t *>(ws + cw.flags);
   }
-  const long long items = (long long)n * cp.layers * cp.hgroups * cp.segs;
+  const long long items = (long long)n * cp.layers * cp.hgroups * (cp.flags ? cp.segs : 1);
   if (items > INT32_MAX / 2)
     return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
   if (items == 0) return fail(PIC_ERR_INVALID_ARG, "%s: no layers", who);

@@ -267,6 +267,9 @@ def test_compact(cuda_lib, dim, hkv, style, rotate):
     m.check()
     m.compact([2], [list(range(90, 120))], start=[0], rotate=rotate, layers=(1, 2))
     m.check()
+    for n in (16, 17, 32, 33, 63, 64, 65, 80, 81):  # one to five segments, both forms' limits
+        m.compact([3], [[0] + list(range(n // 2, n // 2 + n - 1))], start=[100], reserve=300, rotate=rotate)
+        m.check()
 
 
 def test_compact_many_rows_at_once(cuda_lib):
@@ -365,7 +368,7 @@ def test_refusals_on_the_host(cuda_lib):
     with pytest.raises(m.pic.PicError, match="4097 rows"):
         m.pic.pic_page_free(m.i32([0] * 4097), m.dbt, 10, m.drefs, m.dctx)
     with pytest.raises(m.pic.PicError, match="workspace needs") as e:
-        m.pic.pic_page_compact(m.geom, m.i32([0]), m.i32([[0] * 17]), m.i32([1]), m.dctx, m.dbt, 10,
+        m.pic.pic_page_compact(m.geom, m.i32([0]), m.i32([[0] * 65]), m.i32([1]), m.dctx, m.dbt, 10,
                                m.drefs, m.dk, m.dv, res)
     assert e.value.status == 4
     with pytest.raises(m.pic.PicError, match=r"layers \[1, 3\)"):

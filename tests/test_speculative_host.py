@@ -101,12 +101,12 @@ def test_pages(lib):
 
     for kw, status, text in ((dict(max_keep=0), 1, "max_keep 0"), (dict(reserve=-1), 1, "reserve -1"),
                              (dict(keep=NULL), 1, "NULL"), (dict(le=0), 1, "no layers"),
-                             (dict(max_keep=17), 4, "workspace needs"),
-                             (dict(max_keep=17, ws=ctypes.c_void_p(264), ws_bytes=1 << 30), 4, "256-aligned")):
+                             (dict(max_keep=65), 4, "workspace needs"),
+                             (dict(max_keep=65, ws=ctypes.c_void_p(264), ws_bytes=1 << 30), 4, "256-aligned")):
         assert compact(**kw) == status and text in error(), (kw, error())
     assert compact(n=0) == 0
-    assert pic.pic_page_compact_workspace_size(geom(), 3, 16) == 0
-    assert pic.pic_page_compact_workspace_size(geom(), 3, 17) >= 3 * 17 * 16 + 3 * 2 * 2 * 2 * 4
+    assert pic.pic_page_compact_workspace_size(geom(), 3, 64) == 0
+    assert pic.pic_page_compact_workspace_size(geom(), 3, 65) >= 3 * 65 * 16 + 3 * 2 * 2 * 5 * 4
 
     def copy(n=1, src=FAKE, sp=9, dp=9, lb=0, le=2):
         return lib.pic_page_copy(g, n, src, FAKE, FAKE, FAKE, sp, FAKE, FAKE, dp, lb, le, NULL)
