@@ -75,7 +75,7 @@ struct Params {
   uint64_t *mask;                    // workspace: [batch][max_draft] ancestor bits
   struct Share *share;               // workspace: [kCtas] each CTA's start
   int32_t *rows;                     // workspace: [kCtas][32] K/V rows of its first 32 pages
-  int32_t *base;                     // workspace: [batch] each request's first key tile
+  int4 *req;                         // workspace: [batch] first step, ctx_len, draft_len as dealt
   float *part_o;                     // workspace: [kCtas][2][row tile of the pair][BM][D]
   float2 *part_ml;                   // the same without [D]
   __nv_bfloat16 *out;
@@ -159,7 +159,8 @@ PIC_DEV int page_row(const Params &p, int page, int pidx, int keys, int hk) {
 
 // The shares of CTAs first .. first + 3 (every CTA that takes part has a tile), by
 // one warp, lane l < 4 for CTA first + l; the warp of CTA 0 also notes every
-// request's first tile.
+// request's first step and lengths, from which the later kernels work: all roles of
+// a CTA have to walk the same segments, whatever is written to ctx_len meanwhile.
 constexpr int kDealt = 4;
 PIC_DEV void deal_shares(const Params &p, int first) {
   const int lane = threadIdx.x & 31, c = first + lane;
@@ -186,7 +187,7 @@ PIC_DEV void deal_shares(const Params &p, int first) {
       const int y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
     }
-    if (first == 0 && b0 + lane < p.batch) p.base[b0 + lane] = base + x - w;
+    if (first == 0 && b0 + lane < p.batch) p.req[b0 + lane] = make_int4(base + x - w, r.ctx, r.n, 0);
     // lane l's request holds steps [base + x - w, base + x): the one of step pos
 #pragma unroll
     for (int k = 0; k < kDealt; ++k) {
@@ -236,7 +237,7 @@ PIC_DEV void deal_shares(const Params &p, int first) {
 // a chunk (8 pairs) of a query or key head, and a value piece: the host gives the
 // CTAs as many threads as there are chunks, up to kAppendMax.  One place in the code
 // rotates, because a call starts with cold instruction caches (three chunks a
-// thread, their rotations unrolled, took 4.6 us instead of @A us for 32/8 heads).
+// thread, their rotations unrolled, took 5.3 us instead of 4.9, 16 x 16 tokens).
 constexpr int kAppendMax = 512;
 template <int D>
 __global__ void __launch_bounds__(kAppendMax) draft_append_kernel(Params p, RopeParams rp, int dealers) {
@@ -352,8 +353,13 @@ struct Segments {
     if (pos >= end) return false;
     if (pos >= unit0 + (r.tiles << (two ? 1 : 0))) {  // a unit behind the first segment's
       while (pos - base >= work_of(p, r)) {
-        base += work_of(p, r);
-        r = request_of(p, ++b);
+        if (++b >= p.batch) {
+          pos = end;
+          return false;
+        }
+        const int4 x = p.req[b];
+        base = x.x;
+        r = request_of(p, x.y, x.z);
       }
       unit_of(r, base, pos, &unit0, &hk, &pair);
       two = 2 * pair + 1 < r.rt;
@@ -857,11 +863,12 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int h = blockIdx.x * kRows + warp / kWarps, i = blockIdx.y, b = blockIdx.z;
-  const Request r = request_of(p, b);
+  const int4 rq = p.req[b];
+  const Request r = request_of(p, rq.y, rq.z);
   if (i >= r.n || h >= p.Hq) return;  // (kWarps = 4: the whole CTA)
   const int hk = h / p.G, rr = i * p.G + h % p.G, rt = rr / BM, row = rr % BM, pair = rt / 2;
   const int total = p.share[0].total;
-  const int step = 2 * pair + 1 < r.rt ? 2 : 1, t0 = p.base[b] + (hk * r.rt + pair * 2) * r.tiles;
+  const int step = 2 * pair + 1 < r.rt ? 2 : 1, t0 = rq.x + (hk * r.rt + pair * 2) * r.tiles;
   const Deal deal(total, p.share[0].ctas, p.share[0].per);
   const int2 u = make_int2(deal.owner(t0 + step - 1, total), deal.owner(t0 + step * r.tiles - 1, total));
   if (u.x == u.y) return;  // finished by its CTA
@@ -949,7 +956,7 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
 // -------------------------------------------------------------------- host
 struct Plan {
   int r_pad;
-  size_t q_bytes, mask_bytes, share_bytes, rows_bytes, base_bytes, o_bytes, ml_bytes, total;
+  size_t q_bytes, mask_bytes, share_bytes, rows_bytes, req_bytes, o_bytes, ml_bytes, total;
 };
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
@@ -961,10 +968,10 @@ inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
   pl.mask_bytes = align256((size_t)batch * max_draft * 8);
   pl.share_bytes = align256(kCtas * sizeof(Share));
   pl.rows_bytes = align256(kCtas * 32 * 4);
-  pl.base_bytes = align256((size_t)batch * 4);
+  pl.req_bytes = align256((size_t)batch * sizeof(int4));
   pl.o_bytes = align256((size_t)4 * kCtas * BM * g->head_dim * 4);
   pl.ml_bytes = align256((size_t)4 * kCtas * BM * sizeof(float2));
-  pl.total = pl.q_bytes + pl.mask_bytes + pl.share_bytes + pl.rows_bytes + pl.base_bytes + pl.o_bytes + pl.ml_bytes;
+  pl.total = pl.q_bytes + pl.mask_bytes + pl.share_bytes + pl.rows_bytes + pl.req_bytes + pl.o_bytes + pl.ml_bytes;
   return pl;
 }
 
@@ -1070,8 +1077,8 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   ws += pl.share_bytes;
   p.rows = reinterpret_cast<int32_t *>(ws);
   ws += pl.rows_bytes;
-  p.base = reinterpret_cast<int32_t *>(ws);
-  ws += pl.base_bytes;
+  p.req = reinterpret_cast<int4 *>(ws);
+  ws += pl.req_bytes;
   p.part_o = reinterpret_cast<float *>(ws);
   ws += pl.o_bytes;
   p.part_ml = reinterpret_cast<float2 *>(ws);

@@ -352,7 +352,11 @@ extern "C" pic_status_t pic_verify_draft(int32_t batch, int32_t max_draft, int32
            target_stride[0], target_stride[1], draft_prob ? draft_stride[0] : 0,
            draft_prob ? draft_stride[1] : 0, path, path_len, next_token, device_status_ptr()};
   if (!p.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
-  cudaError_t e = batch <= kWideBatch ? launch<16>(p, batch, stream) : launch<8>(p, batch, stream);
+  cudaError_t e = batch <= kWideBatch ? launch<16>(p, batch, stream) : cudaErrorInvalidClusterSize;
+  if (e != cudaSuccess) {  // (also where the device places no cluster of 16)
+    cudaGetLastError();
+    e = launch<8>(p, batch, stream);
+  }
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? PIC_OK : cuda_fail(e, who);
 }
