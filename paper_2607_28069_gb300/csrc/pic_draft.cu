@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool store = valid && ok && !*abort_flag, whole = sg.first && sg.last;
       const size_t o_row = ((size_t)sg.b * p.max_draft + rr / p.G) * p.Hq + sg.hk * p.G + rr % p.G;
       const size_t p_row = (size_t)sg.slot(sg.two ? t : 0) * BM + row;
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
       const int c_begin = sg.two ? 0 : t * (D / 64), c_end = sg.two ? D / 32 : (t + 1) * (D / 64);
       const uint32_t tA = sg.two ? tO : tl + kColO;
 #pragma unroll 1
@@ -620,9 +620,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) mbar_arrive(bar(B_ODONE));
       if (store && (sg.two || t == 0)) {
         if (!whole)
-          p.part_ml[p_row] = make_float2(l > 0.f ? M : -INFINITY, l);
+          p.part_ml[p_row] = make_float2(l == 0.f ? -INFINITY : M, l);
         else if (p.lse)
-          p.lse[o_row] = l > 0.f ? (M + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+          p.lse[o_row] = l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994531f;
       }
     }
   } else if (warp == 0 || warp == 2) {
@@ -945,12 +945,12 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
       for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wc, acc_s[c][lane * CPL + e], acc[e]);
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
   __nv_bfloat162 *dst = reinterpret_cast<__nv_bfloat162 *>(p.out + o_row * D + lane * CPL);
 #pragma unroll
   for (int e = 0; e < CPL; e += 2) dst[e / 2] = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
   if (lane == 0 && p.lse)
-    p.lse[o_row] = l > 0.f ? (M + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+    p.lse[o_row] = l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994531f;
 }
 
 // -------------------------------------------------------------------- host
@@ -1042,7 +1042,8 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   if (rows_total + 16 >= INT32_MAX || (long long)batch * Hkv * pl.r_pad >= INT32_MAX ||
       (double)batch * Hkv * (pl.r_pad / BM) * (max_pages / 8 + 1) >= INT32_MAX)
     return fail(PIC_ERR_UNSUPPORTED, "%s: cache or queries have more than 2^31 rows", who);
-  if (batch > 65535) return fail(PIC_ERR_UNSUPPORTED, "%s: grid too large", who);
+  if (batch > 65535 || max_pages > INT32_MAX / 16 - 16)
+    return fail(PIC_ERR_UNSUPPORTED, "%s: batch %d, max_pages %d", who, batch, max_pages);
   if (!workspace || workspace_bytes < pl.total || (reinterpret_cast<uintptr_t>(workspace) & 255))
     return fail(PIC_ERR_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", who, pl.total);
 

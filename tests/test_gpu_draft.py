@@ -269,3 +269,17 @@ def test_refusals(cuda_lib):
     s["layer"] = 2
     with pytest.raises(pic.PicError, match="layer 2"):
         call(s)
+
+
+@pytest.mark.parametrize("ctx,at", [(100, 3), (9000, 4801)])
+def test_a_nan_in_a_visible_key_shows(cuda_lib, ctx, at):
+    """In the rows that see it, whether or not their keys are split over CTAs, and in no
+    other row."""
+    s = draw((4, 2), 64, 0, [ctx, 40], [3, 2], 3, False, layers=1)
+    s["kc"][0, s["bt"][0, at // 16].long(), 1, at % 16, 5] = float("nan")
+    call(s)
+    bad = torch.zeros((2, 3, 4), dtype=torch.bool)
+    bad[0, :, 2:] = True
+    assert torch.equal(torch.isnan(s["lse"]).cpu(), bad)
+    nan = torch.isnan(s["out"]).cpu()
+    assert torch.equal(nan.any(-1), bad) and torch.equal(nan.all(-1), bad)
