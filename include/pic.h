@@ -684,7 +684,9 @@ pic_status_t pic_page_reserve(int32_t n, const int32_t *row, int32_t extra, int3
  * branch's ctx_len is set.  So both can append without touching each other.
  * result int32 [n]: the branch's length.  Two launches.
  * Device checks: rows, an empty destination, lengths (BAD_REQUEST), max_pages
- * (BLOCK_TABLE_SHORT), page ids (BAD_PAGE), free pages (NO_FREE_PAGE).
+ * (BLOCK_TABLE_SHORT), free pages (NO_FREE_PAGE), the last, partly filled page's id
+ * (BAD_PAGE); a full page's bad id is reported (BAD_PAGE) and not entered: the
+ * branch is made without it.
  */
 pic_status_t pic_page_fork(const pic_geom_t *geom, int32_t n, const int32_t *src_row,
                            const int32_t *dst_row, int32_t reserve, int32_t rows,

@@ -48,6 +48,11 @@ struct PlanParams {
 };
 
 constexpr int kPlanThreads = 1024;
+// A large pool's first pages are mostly all in use: kSkip loads of a thread pass over
+// 32768 of them by one barrier.  16 rows x 4 pages (us, without and with, the calls'
+// other work included): the first 130000 of 140000 pages in use 24 and 13, 950000 of
+// 10^6 142 and 33; with 20000 pages or fewer the loop's code would cost 0.1 to 0.2.
+constexpr int kSkip = 8, kSkipped = 4 * kSkip * kPlanThreads;
 
 // Exclusive prefix sum over the block; *total gets the sum.  One barrier: every
 // warp adds up the warps' sums itself.  The caller alternates between two buffers
@@ -76,7 +81,8 @@ static_assert(kPlanThreads == 32 * 32, "a lane per warp sum");
 
 // One CTA: what each listed row needs, then the free pages in ascending order,
 // the k-th of them to the row whose range of the needs' prefix sum holds k.
-template <bool kFork>
+// kLarge: pools of kSkipped pages or more.
+template <bool kFork, bool kLarge>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
   pdl_entry();
   extern __shared__ int32_t sh[];
@@ -159,30 +165,39 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
   const int want_all = carry;
 
   int found = 0;
-  for (long long base = 0; base < p.num_pages && found < want_all; base += 4 * kPlanThreads) {
+  long long base = 0;
+  if constexpr (kLarge) {
+    for (; vec && want_all > 0 && base + kSkipped <= p.num_pages; base += kSkipped) {
+      int4 v[kSkip];
+#pragma unroll
+      for (int q = 0; q < kSkip; ++q)
+        v[q] = *reinterpret_cast<const int4 *>(p.page_refs + base + 4 * (q * kPlanThreads + tid));
+      bool any = false;
+#pragma unroll
+      for (int q = 0; q < kSkip; ++q) any |= v[q].x == 0 || v[q].y == 0 || v[q].z == 0 || v[q].w == 0;
+      if (__syncthreads_or(any)) break;
+    }
+    if (base > 0) ahead = counts(base + 4 * tid);
+  }
+  for (; base < p.num_pages && found < want_all; base += 4 * kPlanThreads) {
     const long long pg = base + 4 * tid;
     const int4 v = ahead;
     ahead = counts(pg + 4 * kPlanThreads);
-    const int32_t c[4] = {v.x, v.y, v.z, v.w};
-    int mine = 0, total;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) mine += c[i] == 0;
-    int k = found + block_scan(mine, warp_sums[turn ^= 1], &total);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (c[i] == 0) {
-        if (k < want_all) {
-          int lo = 0, hi = p.n;  // the last row with first <= k
-          while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (first[mid] <= k) lo = mid;
-            else hi = mid;
-          }
-          p.block_table[(size_t)p.row[lo] * p.max_pages + col0[lo] + (k - first[lo])] = (int32_t)(pg + i);
-          p.page_refs[pg + i] = 1;
-        }
-        ++k;
+    // a bit per page of the thread's
+    unsigned free_pages = (v.x == 0) | (v.y == 0) << 1 | (v.z == 0) << 2 | (v.w == 0) << 3;
+    int total;
+    int k = found + block_scan(__popc(free_pages), warp_sums[turn ^= 1], &total);
+    for (; free_pages && k < want_all; free_pages &= free_pages - 1, ++k) {
+      const int i = __ffs(free_pages) - 1;
+      int lo = 0, hi = p.n;  // the last row with first <= k
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= k) lo = mid;
+        else hi = mid;
       }
+      p.block_table[(size_t)p.row[lo] * p.max_pages + col0[lo] + (k - first[lo])] = (int32_t)(pg + i);
+      p.page_refs[pg + i] = 1;
+    }
     found += total;
   }
   found = min(found, want_all);
@@ -655,16 +670,21 @@ static pic_status_t launched(const char *who, cudaError_t e) {
   return e == cudaSuccess ? PIC_OK : cuda_fail(e, who);
 }
 
-template <bool kFork>
+template <bool kFork, bool kLarge>
 static cudaError_t launch_plan(const PlanParams &pp, pic_stream_t stream) {
   const size_t smem = (size_t)(pp.n + 1 + pp.n * (kFork ? 2 : 1)) * 4;
   if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(plan_kernel<kFork>,
+    const cudaError_t e = cudaFuncSetAttribute(plan_kernel<kFork, kLarge>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                (int)smem);
     if (e != cudaSuccess) return e;
   }
-  return launch_dependent(plan_kernel<kFork>, dim3(1), dim3(kPlanThreads), smem, stream, pp);
+  return launch_dependent(plan_kernel<kFork, kLarge>, dim3(1), dim3(kPlanThreads), smem, stream, pp);
+}
+template <bool kFork>
+static cudaError_t launch_plan(const PlanParams &pp, pic_stream_t stream) {
+  return pp.num_pages >= kSkipped ? launch_plan<kFork, true>(pp, stream)
+                                  : launch_plan<kFork, false>(pp, stream);
 }
 
 // Head groups of a compaction: as many heads as 16 positions of a CTA hold.
@@ -738,6 +758,11 @@ extern "C" pic_status_t pic_page_fork(const pic_geom_t *geom, int32_t n, const i
   if (reserve < 0) return fail(PIC_ERR_INVALID_ARG, "%s: reserve %d is negative", who, reserve);
   if (n == 0) return PIC_OK;
   if (!src_row || !result) return fail(PIC_ERR_INVALID_ARG, "%s: NULL tensor", who);
+  const int layers = layer_end - layer_begin, hkv = geom->num_kv_heads;
+  const long long table_blocks = (long long)n * ((max_pages + 255) / 256);
+  const long long copy_blocks = ((long long)n * layers * hkv + 7) / 8;
+  if (table_blocks + copy_blocks > INT32_MAX)
+    return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
   int32_t *status = device_status_ptr();
   if (!status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
   PlanParams pp{n, rows, max_pages, reserve, num_pages, dst_row, src_row, ctx_len, block_table,
@@ -747,13 +772,9 @@ extern "C" pic_status_t pic_page_fork(const pic_geom_t *geom, int32_t n, const i
   ForkParams fp;
   fp.n = n;
   fp.max_pages = max_pages;
-  fp.hkv = geom->num_kv_heads;
+  fp.hkv = hkv;
   fp.piece_row = geom->head_dim * 2 / 16;
-  fp.layers = layer_end - layer_begin;
-  const long long table_blocks = (long long)n * ((max_pages + 255) / 256);
-  const long long copy_blocks = ((long long)n * fp.layers * fp.hkv + 7) / 8;
-  if (table_blocks + copy_blocks > INT32_MAX)
-    return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
+  fp.layers = layers;
   fp.table_blocks = (int)table_blocks;
   fp.num_pages = num_pages;
   fp.layer_pieces = (long long)num_pages * fp.hkv * kPage * fp.piece_row;

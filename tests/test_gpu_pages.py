@@ -375,3 +375,29 @@ def test_refusals_on_the_host(cuda_lib):
         m.pic.pic_page_copy(m.geom, m.i32([0]), m.i32([1]), m.dk, m.dv, m.dk, m.dv, 1, 3)
     with pytest.raises(ValueError, match="k_dst must be"):
         m.pic.pic_page_copy(m.geom, m.i32([0]), m.i32([1]), m.dk, m.dv, m.dk[:1], m.dv[:1])
+
+
+@pytest.mark.parametrize("pages,used", [(32767, 32700), (32768, 32760), (70000, 65530), (140000, 131072)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_large_pools(cuda_lib, pages, used, shift):
+    """Free pages near the end, and a few scattered ones where `shift` leaves the counts
+    unaligned too."""
+    import paper_2607_28069_gb300 as pic
+    refs = torch.ones(pages + shift, dtype=torch.int32, device="cuda")[shift:]
+    refs[used:] = 0
+    refs[used + 1:used + 4] = 7
+    if shift:
+        refs[used // 2] = 0
+    free = torch.nonzero(refs == 0)[:8, 0].tolist()  # may be fewer than are asked for
+    dev = lambda x: torch.as_tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+    bt, ctx = dev([[-1] * 8, [5, 6, 7] + [-1] * 5, [-1] * 8]), dev([0, 33, 0])
+    row, res, want = dev([2, 1, 0]), dev([9] * 3), refs.clone()
+    pic.pic_page_reserve(row, 40, ctx, bt, pages, refs, res)
+    exp = [[-1] * 8, [5, 6, 7] + free[3:5] + [-1] * 3, free[:3] + [-1] * 5]
+    if len(free) == 8:
+        exp[0] = free[5:] + [-1] * 5
+    assert cuda_lib.pic_device_status() == ((0, 0) if len(free) == 8 else (10, 2))
+    assert res.tolist() == [3, 5, 3 if len(free) == 8 else -1]
+    assert bt.tolist() == exp
+    want[torch.as_tensor(free[:8 if len(free) == 8 else 5], device="cuda")] = 1
+    assert torch.equal(refs, want)
