@@ -344,15 +344,17 @@ static_assert(kSeg == 16, "half a warp looks a segment's positions up");
 constexpr int kCheckThreads = 1024;  // kept positions of a checking CTA
 
 struct CompactParams {
-  int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, layers, layer_begin, rotate;
+  int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, layers, layer_begin, rotate, dim;
   long long num_pages, layer_elems;
   const int32_t *row, *start, *keep, *keep_len;
   const int32_t *ctx_len, *block_table, *page_refs;
   int32_t *result;
   __nv_bfloat16 *k, *v;  // at layer_begin
-  // lists beyond kShort (workspace): from and to slot of every kept position, per
-  // (row, segment) the first and last segment to wait for, a ticket, and per (row, layer and
-  // head group, segment) "reads done"
+  // lists beyond kShort (workspace): from and to row of every kept position (elements
+  // from the layer's begin to head 0's; as page and row, with the products at each use,
+  // 9001 of 15001 positions took 72.0 us instead of 70.7), per (row, segment) the first
+  // and last segment to wait for, a ticket, and per (row, layer and head group, segment)
+  // "reads done"
   longlong2 *slot;       // [n][max_keep]
   int2 *wait;            // [n][segs]
   int32_t *bad;          // [n][checks]: a checking CTA found a fault
@@ -410,7 +412,9 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
     int k;
     longlong2 slot;
     code = compact_entry(p, j, s, i0 + tid, &k, &slot);
-    if (code == PIC_DEV_OK) p.slot[(size_t)j * p.max_keep + i0 + tid] = slot;
+    auto elem = [&](long long sl) { return (sl / kPage * p.hkv * kPage + sl % kPage) * p.dim; };
+    if (code == PIC_DEV_OK)
+      p.slot[(size_t)j * p.max_keep + i0 + tid] = make_longlong2(elem(slot.x), elem(slot.y));
   }
   if (code != PIC_DEV_OK && (s >= 0 || (tid == 0 && i0 == 0))) dev_fail(p.status, code, j);
   const bool bad = __syncthreads_or(code != PIC_DEV_OK);
@@ -447,9 +451,9 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
 // layer, head group) in turn, which needs no flags -- a segment's targets lie below
 // the next one's sources -- and checks the list itself, so the call is a launch
 // shorter.
-// Measured: 9001 of 15001 positions, 8 heads, 4 layers, 60 us (295 MB read and
-// written: 4.9 TB/s; 52 us without the rotation).  A row of a head is 256 bytes, and
-// reads and writes of that size alternate.  8 rows that keep 5 of 16, 32 layers: 5.5
+// Measured: 9001 of 15001 positions, 8 heads, 4 layers, 59 us (295 MB read and
+// written: 5.0 TB/s; 54 without the rotation).  A row of a head is 256 bytes, and reads
+// and writes of that size alternate.  8 rows that keep 5 of 16, 32 layers: 5.5
 // us, latency.
 template <int D, bool kLong>
 __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(CompactParams p, RopeParams rp) {
@@ -534,7 +538,8 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
     auto where = [&](int u, int w, bool to) {
       const int h = h0 + (u - w * per) / KC;
       const long long sl = to ? slot_of[buf][w >> 1].y : slot_of[buf][w >> 1].x;
-      return (w & 1 ? p.v : p.k) + lbase + (((sl >> 4) * p.hkv + h) * kPage + (sl & 15)) * D;
+      return (w & 1 ? p.v : p.k) + lbase +
+             (kLong ? sl + h * (kPage * D) : (((sl >> 4) * p.hkv + h) * kPage + (sl & 15)) * D);
     };
     uint4 a[kUnits], b[kUnits];
 #pragma unroll
@@ -844,6 +849,7 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
   cp.layer_begin = layer_begin;
   cp.rotate = rotate != 0;
   cp.num_pages = num_pages;
+  cp.dim = geom->head_dim;
   cp.layer_elems = (long long)num_pages * cp.hkv * kPage * geom->head_dim;
   cp.row = row;
   cp.start = start;
