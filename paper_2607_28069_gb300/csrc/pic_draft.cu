@@ -22,8 +22,9 @@
 //
 // Measured, whole calls: 4 requests of 139k keys, 32 rows of each of 8 kv heads, 330
 // us (2.29 GB: 6.92 TB/s; a plain copy runs at 6.79); 16 of 33k, 112 rows of 4 kv
-// heads, 169 us (6.4 TB/s); 4 of 16k, 64 tokens of 32 heads, 69 us, where the softmax
-// of a tile sets the pace; one of 4288 keys 14.6 us, three dependent launches.
+// heads, 169 us (6.4 TB/s); 4 of 16k, 256 rows of 8 kv heads, 69 us, 39 of them the
+// keys' and values' time at the copy rate, the rest the launches around it and 23 MB of
+// partial states; one of 4288 keys 14.6 us, three dependent launches.
 #include <algorithm>
 
 #include "pic_internal.cuh"
@@ -404,10 +405,13 @@ struct Segments {
 // (most of that the output's own rounding; 0.0034 to 0.0038 and 0.0033 to 0.0036 with
 // queries scaled by 2).
 //
-// Bound by HBM up to about 128 rows: 322 us for 4 x 139k keys (7.1 TB/s), 162 us cold
-// for 16 x 33k (6.65 TB/s, DRAM 84% busy, tensor pipe 37%).  With more rows bound by
-// the softmax of a tile, and for short contexts by set-up, first tiles and the
-// epilogue (7.2 us with two key tiles in all).
+// Bound by HBM up to 256 rows of a kv head: 322 us for 4 x 139k keys (7.1 TB/s), 162 us cold
+// for 16 x 33k (6.65 TB/s, DRAM 84% busy, tensor pipe 37%).  With 512 rows a key tile of
+// two row tiles takes about 2750 cycles where its MMAs need 2080; for short contexts
+// set-up, first tiles and the epilogue count (7.2 us with two key tiles in all).
+// Against the short loops below: all scores of a row in registers were 6% slower; half
+// of them kept from the maximum for the exponentials, or no maximum after the first
+// tile, 1% faster at best and up to 9% slower in short calls.
 //
 // Waits: the MMA warp meets the ring warp (which waits for K, V, Q and the
 // accumulators on its behalf) and the softmax warps on named barriers only.  These
