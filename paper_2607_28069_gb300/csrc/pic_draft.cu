@@ -246,12 +246,45 @@ PIC_DEV void deal_shares(const Params &p, int first) {
 // place in the code rotates, because a call starts with cold instruction caches (three chunks a
 // thread, their rotations unrolled, took 5.3 us instead of 4.9, 16 x 16 tokens).
 constexpr int kAppendMax = 512;
+
+// Token i and its ancestors as bits, by one warp whose lanes hold the parents of
+// tokens lane and lane + 32: each round doubles the ancestors that a token knows.
+// (A walk up took 1.7 us for a line of 64.)  A parent that is none is read as -1.
+PIC_DEV uint64_t ancestors(const Params &p, const int (&parent)[2], int b, int i) {
+  const int lane = threadIdx.x & 31;
+  uint64_t m[2];
+  int up[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int q = lane + 32 * k;
+    const bool bad = parent[k] < -1 || parent[k] >= q;
+    if (bad && q == i) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
+    m[k] = 1ull << q;
+    up[k] = bad ? -1 : parent[k];
+  }
+  while (__any_sync(0xffffffffu, up[0] >= 0 || up[1] >= 0)) {
+    uint64_t nm[2];
+    int nu[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int from = up[k] & 31;
+      const uint64_t m0 = __shfl_sync(0xffffffffu, m[0], from), m1 = __shfl_sync(0xffffffffu, m[1], from);
+      const int u0 = __shfl_sync(0xffffffffu, up[0], from), u1 = __shfl_sync(0xffffffffu, up[1], from);
+      nm[k] = up[k] < 0 ? m[k] : m[k] | (up[k] < 32 ? m0 : m1);
+      nu[k] = up[k] < 0 ? -1 : up[k] < 32 ? u0 : u1;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) m[k] = nm[k], up[k] = nu[k];
+  }
+  const uint64_t m0 = __shfl_sync(0xffffffffu, m[0], i & 31), m1 = __shfl_sync(0xffffffffu, m[1], i & 31);
+  return i < 32 ? m0 : m1;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kAppendMax) draft_append_kernel(Params p, RopeParams rp, int dealers) {
   constexpr int KC = D / 16;
   pdl_entry();
   __shared__ float2 cs[D / 2];
-  __shared__ int32_t par[kMaxDraft];
   __shared__ int depth;
   // (the dealers first: theirs is the longer chain)
   const int tid = threadIdx.x, threads = blockDim.x;
@@ -279,7 +312,11 @@ __global__ void __launch_bounds__(kAppendMax) draft_append_kernel(Params p, Rope
   const int pieces = p.Hkv * (D / 8);
   const __nv_bfloat16 *v_src = p.v_new + tok * p.Hkv * D;
   if (tid < pieces) vn = ld_stream(v_src + tid * 8);
-  if (tid < p.max_draft) par[tid] = p.parent ? p.parent[(size_t)b * p.max_draft + tid] : tid - 1;
+  int up[2] = {-1, -1};  // warp 0: the parents of tokens tid and tid + 32
+  if (p.parent && tid < 32)
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (tid + 32 * k < p.max_draft) up[k] = p.parent[(size_t)b * p.max_draft + tid + 32 * k];
   const uint64_t turn = tid < D / 2 ? rope_turn(rope_theta(rp, p.layer, tid)) : 0;
   const int ctx = p.ctx_len[b], n = p.draft_len[b];
   const bool bad = ctx < 0 || n < 0 || n > p.max_draft;
@@ -291,23 +328,14 @@ __global__ void __launch_bounds__(kAppendMax) draft_append_kernel(Params p, Rope
   if (i >= n) return;
   const int slot = ctx + i;
   int page = p.block_table[(size_t)b * p.max_pages + slot / 16];
-  __syncthreads();
-  if (tid == 0) {
-    uint64_t m = 1ull << i;
-    int d = 0, q = i;
-    for (;;) {
-      const int up = par[q];
-      if (up < -1 || up >= q) {
-        if (q == i) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
-        break;
-      }
-      if (up < 0) break;
-      q = up;
-      m |= 1ull << q, ++d;
+  if (tid < 32) {
+    uint64_t line = ~0ull >> (63 - i);  // token i and its ancestors
+    if (p.parent) line = ancestors(p, up, b, i);
+    if (tid == 0) {
+      p.mask[tok] = line;
+      depth = __popcll(line) - 1;
+      if (page < 0 || page >= p.num_pages) dev_fail(p.status, PIC_DEV_BAD_PAGE, b);
     }
-    p.mask[tok] = m;
-    depth = d;
-    if (page < 0 || page >= p.num_pages) dev_fail(p.status, PIC_DEV_BAD_PAGE, b);
   }
   if (page >= p.num_pages) page = -1;
   __syncthreads();
