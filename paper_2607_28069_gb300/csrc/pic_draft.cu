@@ -170,9 +170,11 @@ PIC_DEV int page_row(const Params &p, int page, int pidx, int keys, int hk) {
 constexpr int kDealt = 4;
 PIC_DEV void deal_shares(const Params &p, int first) {
   const int lane = threadIdx.x & 31, c = first + lane;
+  auto request = [&](int b) { return b < p.batch ? request_of(p, b) : Request{0, 0, 0, 0}; };
+  const Request first32 = request(lane);  // mostly all of them: read once
   int total = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
-    int w = b0 + lane < p.batch ? work_of(p, request_of(p, b0 + lane)) : 0;
+    int w = work_of(p, b0 ? request(b0 + lane) : first32);
 #pragma unroll
     for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
     total += w;
@@ -185,7 +187,7 @@ PIC_DEV void deal_shares(const Params &p, int first) {
   if (lane < kDealt && c < ctas && total > 0) sh.pos = deal.first(c), sh.end = deal.first(c + 1);
   int base = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 32) {
-    const Request r = b0 + lane < p.batch ? request_of(p, b0 + lane) : Request{0, 0, 0, 0};
+    const Request r = b0 ? request(b0 + lane) : first32;
     const int w = work_of(p, r);
     int x = w;
 #pragma unroll
