@@ -916,13 +916,13 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int h = blockIdx.x * kRows + warp / kWarps, i = blockIdx.y, b = blockIdx.z;
-  const int4 rq = p.req[b];
+  const int4 rq = p.req[b];  // one round trip with the deal's figures
+  const int total = p.share[0].total;
+  const Deal deal(total, p.share[0].ctas, p.share[0].per);
   const Request r = request_of(p, rq.y, rq.z);
   if (i >= r.n || h >= p.Hq) return;  // (kWarps = 4: the whole CTA)
   const int hk = h / p.G, rr = i * p.G + h % p.G, rt = rr / BM, row = rr % BM, pair = rt / 2;
-  const int total = p.share[0].total;
   const int step = 2 * pair + 1 < r.rt ? 2 : 1, t0 = rq.x + (hk * r.rt + pair * 2) * r.tiles;
-  const Deal deal(total, p.share[0].ctas, p.share[0].per);
   const int2 u = make_int2(deal.owner(t0 + step - 1, total), deal.owner(t0 + step * r.tiles - 1, total));
   if (u.x == u.y) return;  // finished by its CTA
   const int parts = u.y - u.x + 1, t = 2 * pair + 1 < r.rt ? rt & 1 : 0;
