@@ -641,8 +641,9 @@ pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, int32_t bat
  *   counts; 0 for a request without tokens); next_token int32 [batch].  path and
  *   path_len are the keep list of pic_page_compact.
  * vocab <= 2^24.  A drafted token outside [0, vocab) is never accepted, a parent
- * not below its child never followed.  One launch, no workspace.  Device check:
- * draft_len (PIC_DEV_BAD_REQUEST, the request is treated as empty).
+ * not below its child never followed.  One launch (two for small trees, whose
+ * tokens are all drawn at once), no workspace.  Device check: draft_len
+ * (PIC_DEV_BAD_REQUEST, the request is treated as empty).
  */
 pic_status_t pic_verify_draft(int32_t batch, int32_t max_draft, int32_t vocab,
                               const int32_t *tokens, const int32_t *parent,

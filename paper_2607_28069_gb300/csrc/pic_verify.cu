@@ -17,11 +17,13 @@
 // through distributed shared memory, and the CTA that holds the threshold finds
 // its chunk and searches that one's entries, which a wide cluster's warps still hold
 // in registers and a narrow one's read again.
+// Small trees: every token's draw at once, a cluster each, whether the walk gets there
+// or not (the random number of a token depends on its depth alone), then the walk.
 //
 // Measured: 64 chains of 8 over 2^17 entries, one row or two of each read, 12.1 us
-// (67 MB at least: 5.5 TB/s), bound by HBM and the single wave of 512 CTAs; one
-// tree over 50001 entries 3.9 us for one level and 2.5 for each further one, a chain of
-// the row's loads, two cluster barriers and the search.
+// (67 MB at least: 5.5 TB/s), bound by HBM and the single wave of 512 CTAs.  A tree level by
+// level: 3.9 us for the first and 2.5 for each further one, a chain of the row's loads,
+// two cluster barriers and the search; at once, 16 tokens over 50001 entries, 5.6 us.
 #include <algorithm>
 
 #include "pic_internal.cuh"
@@ -37,6 +39,12 @@ constexpr int kChunk = 1024;
 // 16 CTAs): chain of 8, 4 requests 5.9 and 4.2, 12 6.0 and 5.1, 16 6.0 and 7.4, 64 12.1
 // and 22.3; tree of 8, 12 requests 11.1 and 9.6, 24 15.4 and 16.4.
 constexpr int kWideBatch = 12;
+// Trees whose tokens are all drawn at once (us of the call, level by level and at once;
+// random trees, two levels on average): 1 request x 16 tokens x 50001 entries 5.8 and
+// 5.4, 4 x 16 10.4 and 6.8, 8 x 16 12.8 and 11.1, 16 x 16 (256 draws) 11.6 and 17.0; x
+// 131072 entries 4 x 8 8.4 and 6.8, 8 x 8 (2^23 in all) 10.9 and 9.7, 4 x 16 9.7 and 10.5.
+constexpr int kNodes = 152;
+constexpr long long kNodeEntries = 1 << 23;
 
 struct Params {
   int max_draft, vocab;
@@ -55,6 +63,7 @@ struct Shared {
   uint64_t totals[2][kCluster]; // every CTA's sum, written by that CTA (by turns)
   int32_t found;                // the token, written by the CTA that holds it
   int32_t refused;
+  int32_t parent[kMaxDraft];    // nodes_kernel
 };
 
 // A weight as a whole number of 2^-36, trunc(2^36 p) for p clamped to [0, 1]
@@ -151,9 +160,10 @@ PIC_DEV int search_tile(const uint64_t *tile, int c, uint64_t left) {
 
 // One draw by the whole cluster.  Returns false where the row has no weight.
 // The token goes to every CTA's sh.found (kAll) or is written to *out by the CTA
-// that finds it.  turn: the draws of a kernel alternate between 0 and 1.
-template <int kCluster, bool kBoth, bool kAll>
-PIC_DEV bool draw(Shared<kCluster> &sh, int turn, const float *p, const float *q, int vocab, float u,
+// that finds it.  turn: the draws of a kernel alternate between 0 and 1.  number():
+// the random number, asked for behind a barrier.
+template <int kCluster, bool kBoth, bool kAll, typename F>
+PIC_DEV bool draw(Shared<kCluster> &sh, int turn, const float *p, const float *q, int vocab, F &&number,
                   int32_t *out) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = (int)cluster_rank();
@@ -196,7 +206,7 @@ PIC_DEV bool draw(Shared<kCluster> &sh, int turn, const float *p, const float *q
     total += t;
   }
   // floor(total * floor(2^24 u) / 2^24); u outside [0, 1) (NaN: 0)
-  const uint64_t n = (uint64_t)fminf(fmaxf(u, 0.f) * 16777216.f, 16777215.f);
+  const uint64_t n = (uint64_t)fminf(fmaxf(number(), 0.f) * 16777216.f, 16777215.f);
   const uint64_t at = (__umul64hi(total, n) << 40) | ((total * n) >> 24);
   if (before <= at && at < before + own) {  // this CTA holds the threshold
     uint64_t left = at - before;
@@ -231,6 +241,16 @@ PIC_DEV bool draw(Shared<kCluster> &sh, int turn, const float *p, const float *q
   }
   if constexpr (kAll) cluster_sync_all();
   return total != 0;
+}
+
+// The first child of token `at` that carries the token `next`, or -1, by a warp whose lanes
+// hold tokens and parents lane and lane + 32.
+PIC_DEV int child_of(int at, int next, int n, int tok0, int tok1, int par0, int par1) {
+  const int i0 = threadIdx.x & 31, i1 = i0 + 32;
+  const bool h0 = i0 < n && i0 > at && tok0 == next && par0 == at && next >= 0;
+  const bool h1 = i1 < n && i1 > at && tok1 == next && par1 == at && next >= 0;
+  const unsigned m0 = __ballot_sync(0xffffffffu, h0), m1 = __ballot_sync(0xffffffffu, h1);
+  return m0 ? __ffs(m0) - 1 : m1 ? __ffs(m1) + 31 : -1;
 }
 
 template <int kCluster>
@@ -278,7 +298,8 @@ __global__ void __launch_bounds__(kThreads, kCluster == 16 ? 2 : 4) verify_kerne
     if (writer && lane == 0) p.path_len[b] = len;
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     const float *row = target + (len - 1) * p.tt;
-    const float un = u[n - 1];
+    const float last = u[n - 1];
+    auto un = [&]() { return last; };
     if (len < n && draw<kCluster, true, false>(sh, 0, row, draft + (len - 1) * p.dt, p.vocab, un, p.next + b))
       return;
     if (!draw<kCluster, false, false>(sh, 1, row, nullptr, p.vocab, un, p.next + b) && writer && lane == 0)
@@ -297,14 +318,13 @@ __global__ void __launch_bounds__(kThreads, kCluster == 16 ? 2 : 4) verify_kerne
     int at = 0;
     if (writer && lane == 0) path[0] = 0;
     for (len = 1;; ++len) {
-      next = draw<kCluster, false, true>(sh, len & 1, target + at * p.tt, nullptr, p.vocab, u[len - 1], nullptr)
+      const float ul = u[len - 1];
+      next = draw<kCluster, false, true>(sh, len & 1, target + at * p.tt, nullptr, p.vocab, [&]() { return ul; },
+                                         nullptr)
                  ? sh.found : -1;
-      // each warp alike: the first child that carries the token
-      const bool h0 = i0 < n && i0 > at && tok0 == next && par0 == at && next >= 0;
-      const bool h1 = i1 < n && i1 > at && tok1 == next && par1 == at && next >= 0;
-      const unsigned m0 = __ballot_sync(0xffffffffu, h0), m1 = __ballot_sync(0xffffffffu, h1);
-      if (!(m0 | m1)) break;
-      at = m0 ? __ffs(m0) - 1 : __ffs(m1) + 31;
+      const int child = child_of(at, next, n, tok0, tok1, par0, par1);  // each warp alike
+      if (child < 0) break;
+      at = child;
       if (writer && lane == 0) path[len] = at;
     }
   }
@@ -317,15 +337,92 @@ __global__ void __launch_bounds__(kThreads, kCluster == 16 ? 2 : 4) verify_kerne
   }
 }
 
+// Small trees: the target's draw at every token at once, a cluster each, then (walk_kernel)
+// the way down as look-ups.  The draws are left in `path`.  A level after the other costs
+// 2.5 us each, this 4.7 to 7 in all.
 template <int kCluster>
-static cudaError_t launch(const Params &p, int batch, cudaStream_t stream) {
+__global__ void __launch_bounds__(kThreads, kCluster == 16 ? 2 : 4) nodes_kernel(Params p) {
+  pdl_entry();
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared<kCluster> &sh = *reinterpret_cast<Shared<kCluster> *>(smem);
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  const int tid = threadIdx.x;
+  const int item = blockIdx.x / kCluster, b = item / p.max_draft, i = item % p.max_draft;
+  const int n = p.draft_len[b];
+  if (p.parent && tid < p.max_draft) sh.parent[tid] = p.parent[(size_t)b * p.max_draft + tid];
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  if (i >= n || n > p.max_draft) return;
+  // its depth below token 0 (one that is not below token 0 is never visited)
+  auto number = [&]() {
+    int d = 0;
+    for (int q = i; q > 0; ++d) {
+      const int up = p.parent ? sh.parent[q] : q - 1;
+      if (up < 0 || up >= q) break;
+      q = up;
+    }
+    return p.uniform[(size_t)b * p.max_draft + d];
+  };
+  int32_t *out = p.path + (size_t)b * p.max_draft + i;
+  if (!draw<kCluster, false, false>(sh, 0, p.target + b * p.tb + i * p.tt, nullptr, p.vocab, number, out) &&
+      cluster_rank() == 0 && tid == 0)
+    *out = -1;
+}
+
+__global__ void __launch_bounds__(kThreads) walk_kernel(Params p, int batch) {  // a warp per request
+  pdl_entry();
+  const int b = blockIdx.x * kWarps + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (b >= batch) return;
+  const size_t row = (size_t)b * p.max_draft;
+  int tok[2], par[2], drawn[2], path[2] = {-1, -1};
+  int n = p.draft_len[b];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = lane + 32 * k;
+    const bool in = i < p.max_draft;
+    tok[k] = in ? p.tokens[row + i] : -1;
+    par[k] = !p.parent ? i - 1 : in ? p.parent[row + i] : -1;
+    drawn[k] = in ? p.path[row + i] : -1;
+  }
+  if (n < 0 || n > p.max_draft) {
+    if (lane == 0) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
+    n = 0;
+  }
+  int len = 0, next = -1;
+  for (int at = n > 0 ? 0 : -1; at >= 0;) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (len == lane + 32 * k) path[k] = at;
+    ++len;
+    const int d0 = __shfl_sync(0xffffffffu, drawn[0], at & 31), d1 = __shfl_sync(0xffffffffu, drawn[1], at & 31);
+    next = at < 32 ? d0 : d1;
+    at = child_of(at, next, n, tok[0], tok[1], par[0], par[1]);
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (lane + 32 * k < p.max_draft) p.path[row + lane + 32 * k] = path[k];
+  if (lane == 0) {
+    p.path_len[b] = len;
+    p.next[b] = next;
+  }
+}
+
+template <int kCluster>
+static cudaError_t launch(void (*kernel)(Params), const Params &p, int clusters, cudaStream_t stream) {
   if (kCluster > 8) {
-    const cudaError_t e = cudaFuncSetAttribute(verify_kernel<kCluster>,
-                                               cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
   }
-  return launch_dependent_cluster(verify_kernel<kCluster>, dim3((unsigned)(batch * kCluster)),
-                                  dim3(kThreads), sizeof(Shared<kCluster>), stream, kCluster, p);
+  return launch_dependent_cluster(kernel, dim3((unsigned)(clusters * kCluster)), dim3(kThreads),
+                                  sizeof(Shared<kCluster>), stream, kCluster, p);
+}
+// Wide clusters for few (also not where the device places none), else narrow ones.
+static cudaError_t launch(void (*wide)(Params), void (*narrow)(Params), const Params &p, int clusters,
+                          cudaStream_t stream) {
+  if (clusters <= kWideBatch) {
+    if (launch<16>(wide, p, clusters, stream) == cudaSuccess) return cudaSuccess;
+    cudaGetLastError();
+  }
+  return launch<8>(narrow, p, clusters, stream);
 }
 
 }  // namespace verify
@@ -358,10 +455,17 @@ extern "C" pic_status_t pic_verify_draft(int32_t batch, int32_t max_draft, int32
            target_stride[0], target_stride[1], draft_prob ? draft_stride[0] : 0,
            draft_prob ? draft_stride[1] : 0, path, path_len, next_token, device_status_ptr()};
   if (!p.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
-  cudaError_t e = batch <= kWideBatch ? launch<16>(p, batch, stream) : cudaErrorInvalidClusterSize;
-  if (e != cudaSuccess) {  // (also where the device places no cluster of 16)
-    cudaGetLastError();
-    e = launch<8>(p, batch, stream);
+  cudaError_t e;
+  // The draws of all tokens at once read more rows, but not one after the other: taken
+  // where their clusters are two waves at most and the rows of all tokens a few
+  // microseconds' reading.
+  const long long nodes = (long long)batch * max_draft;
+  if (!draft_prob && max_draft > 1 && nodes <= kNodes && nodes * vocab < kNodeEntries) {
+    e = launch(nodes_kernel<16>, nodes_kernel<8>, p, (int)nodes, stream);
+    if (e == cudaSuccess)
+      e = launch_dependent(walk_kernel, dim3((batch + kWarps - 1) / kWarps), dim3(kThreads), 0, stream, p, batch);
+  } else {
+    e = launch(verify_kernel<16>, verify_kernel<8>, p, batch, stream);
   }
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? PIC_OK : cuda_fail(e, who);

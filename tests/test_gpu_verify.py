@@ -177,3 +177,38 @@ def test_refusals(cuda_lib):
         run([[0, 0]], [2], p.double(), u)
     with pytest.raises(pic.PicError, match="max_draft 65"):
         run([[0] * 65], [2], torch.ones((1, 65, 4), device="cuda"), torch.zeros((1, 65), device="cuda"))
+
+
+@pytest.mark.parametrize("B", [1, 2, 5])  # 64 and 128 draws at once, 320 level by level
+@pytest.mark.parametrize("tree", [False, True])
+def test_deep_trees_in_both_forms(cuda_lib, B, tree):
+    """Lines of up to 64 accepted tokens, branches, tokens that hang on none or on one that
+    is not below them, a row without weight, and lengths that are refused."""
+    rng = np.random.default_rng(10 * B + tree)
+    T, V = 64, 1500
+    p = probs(rng, B, T, V)
+    u = rng.random((B, T)).astype(np.float32)
+    parent = np.tile(np.arange(T) - 1, (B, 1))
+    if tree:
+        parent[:, 5::5] -= 1  # every fifth token is a leaf, the line goes on beside it
+        parent[:, 44], parent[:, 49], parent[:, 54] = 44, -1, 99
+    lens = [T, T - 7, 0, -1, T][:B]
+    tokens = rng.integers(0, V, (B, T))
+    for b in range(B):  # every token is the target's own draw behind its parent
+        depth = [0] * T
+        for i in range(1, T):
+            if 0 <= parent[b, i] < i:
+                depth[i] = depth[parent[b, i]] + 1
+                tokens[b, i] = draw(weights(p[b, parent[b, i]]), u[b, depth[i] - 1])
+                if tree and i % 5 == 4 and i < 59:
+                    tokens[b, i] = (tokens[b, i] + 1) % V  # a leaf that is not taken
+        p[b, T - 10 + b] = 0
+    got = run(tokens, lens, p, u, None, parent if tree else None)
+    seen = 0
+    for b in range(B):
+        n = lens[b] if 0 <= lens[b] <= T else 0
+        want = rule(tokens[b].tolist(), n, p[b], u[b], None, parent[b].tolist() if tree else None)
+        assert (got[0][b], got[1][b], got[2][b]) == want, b
+        seen = max(seen, want[1])
+    assert seen > (40 if tree else 50)
+    assert cuda_lib.pic_device_status() == ((3, 3) if B == 5 else (0, 0))
