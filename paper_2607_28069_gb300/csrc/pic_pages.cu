@@ -344,7 +344,7 @@ static_assert(kSeg == 16, "half a warp looks a segment's positions up");
 constexpr int kCheckThreads = 1024;  // kept positions of a checking CTA
 
 struct CompactParams {
-  int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, layers, layer_begin, rotate, dim;
+  int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, lgroup, lhs, layers, layer_begin, rotate, dim;
   long long num_pages, layer_elems;
   const int32_t *row, *start, *keep, *keep_len;
   const int32_t *ctx_len, *block_table, *page_refs;
@@ -401,7 +401,7 @@ PIC_DEV int compact_entry(const CompactParams &p, int j, int s, int i, int *k_ou
 __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactParams p) {
   pdl_entry();
   const int j = blockIdx.y, tid = threadIdx.x, i0 = blockIdx.x * kCheckThreads;
-  const long long per = (long long)p.layers * p.hgroups * p.segs;
+  const long long per = (long long)p.lhs * p.segs;
   for (long long i = i0 + tid; i < per; i += (long long)p.checks * kCheckThreads)
     p.flags[j * per + i] = 0;
   if (j == 0 && i0 == 0 && tid == 0) *p.ticket = 0;
@@ -438,155 +438,104 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
   }
 }
 
-// A CTA moves 16 kept positions x a group of kv heads x a layer of one row: it
-// reads them all into registers, says so, waits for the CTAs whose sources lie
-// in what it overwrites (few, and long past where much was left out), and stores.
-// keep is ascending, so those are CTAs of earlier segments of the same (row, layer,
-// head group) only; a segment comes from a ticket, so they have started before it,
-// and they read before they wait: every wait ends.  Keys move by i - keep[i] positions and are re-rotated by that, with
-// cos/sin of the 16 moves formed once per CTA.
-// kLong: lists checked by compact_check_kernel, moved by CTAs that stay and look up
-// the next segment's positions while they wait.  Otherwise (windows of drafts: up
-// to kShort entries, mostly few of them kept) a CTA takes all segments of a (row,
-// layer, head group) in turn, which needs no flags -- a segment's targets lie below
-// the next one's sources -- and checks the list itself, so the call is a launch
-// shorter.
-// Measured: 9001 of 15001 positions, 8 heads, 4 layers, 59 us (295 MB read and
-// written: 5.0 TB/s; 54 without the rotation).  A row of a head is 256 bytes, and reads
-// and writes of that size alternate.  8 rows that keep 5 of 16, 32 layers: 5.5
-// us, latency.
-template <int D, bool kLong>
-__global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(CompactParams p, RopeParams rp) {
-  constexpr int KC = D / 16;  // 8-pair chunks of a row
+// A CTA moves 16 kept positions x a group of kv heads (and layers) of one row: it
+// reads them all on chip, says so, waits for the CTAs whose sources lie in what it
+// overwrites (few, and long past where much was left out), and stores.  keep is
+// ascending, so those are CTAs of earlier segments of the same (row, group) only; a
+// segment comes from a ticket, so they have started before it, and they read before
+// they wait: every wait ends.  Keys move by i - keep[i] positions and are re-rotated by
+// that, with cos/sin formed once per CTA.
+// Long lists (compact_move_kernel) are checked by compact_check_kernel, and moved by
+// CTAs that stay and look up the next segment's positions while they wait.  Short ones
+// (compact_short_kernel: windows of drafts, up to kShort entries, mostly few of them
+// kept) are worked off by a CTA per (row, layer, head group), which needs no flags -- a
+// segment's targets lie below the next one's sources -- and checks the list itself,
+// so the call is a launch shorter.
+// Measured: 9001 of 15001 positions, 8 heads, 4 layers, 57 us (295 MB read and
+// written: 5.2 TB/s; 53 without the rotation): a row of a head is 256 bytes, reads and
+// writes of that size alternate, and issue slots are over half busy with addresses and
+// rotations.  The short form: 8 rows that keep 5 of 16, 32 layers, 5.5 us, latency.
+
+// The units of a segment of group lh (heads, with kLayers of several layers): unit u =
+// (position, K or V, row of the group, chunk), thread tid's are tid, tid + kMoveThreads, ...
+template <int D, bool kLayers>
+struct Units {
+  static constexpr int KC = D / 16;  // 8-pair chunks of a row
+  int layer, h0, heads, per, count, magic, head_magic;  // per: units of a position's K or V
+  long long base;
+  PIC_DEV Units(const CompactParams &p, int lh, int positions) {
+    layer = lh / p.hgroups * (kLayers ? p.lgroup : 1);
+    h0 = (lh % p.hgroups) * p.hgroup;
+    heads = min(p.hgroup, p.hkv - h0);
+    per = KC * heads * (kLayers ? min(p.lgroup, p.layers - layer) : 1);
+    count = positions * 2 * per;
+    // (division by per <= 32 as a product: exact for u < 1024; by heads: for 8 of them)
+    magic = ((1 << 20) + per - 1) / per;
+    head_magic = (256 + heads - 1) / heads;
+    base = (long long)layer * p.layer_elems;
+  }
+  PIC_DEV int pair_of(int u) const { return (u * magic) >> 20; }  // 2 * position + (0 K, 1 V)
+  PIC_DEV int head_of(int u, int w) const { return h0 + (u - w * per) / KC; }  // without kLayers
+  // unit u's row in its (position, K or V) w, from the position's row of layer 0, head 0
+  PIC_DEV long long row_of(const CompactParams &p, int u, int w) const {
+    const int g = (u - w * per) / KC, l = kLayers ? (g * head_magic) >> 8 : 0;
+    return base + l * p.layer_elems + (h0 + g - l * heads) * (kPage * D);
+  }
+};
+
+// Short lists: a CTA takes all segments of a (row, layer, head group) in turn.
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_short_kernel(CompactParams p, RopeParams rp) {
+  constexpr int KC = D / 16;
   pdl_entry();
   __shared__ float2 cs[kSeg][D / 2];
-  constexpr int kBufs = kLong ? 2 : kShort / kSeg;
-  __shared__ int32_t k_of[kBufs][kSeg];
-  __shared__ longlong2 slot_of[kBufs][kSeg];
-  __shared__ int next_at, next_cnt[2];
-  __shared__ int2 next_wait[2];
-  const int tid = threadIdx.x, lhs = p.layers * p.hgroups;
-  const int all = lhs * p.n * (kLong ? p.segs : 1);  // (the host keeps it below 2^30)
+  __shared__ int32_t k_of[kShort / kSeg][kSeg];
+  __shared__ longlong2 slot_of[kShort / kSeg][kSeg];
+  const int tid = threadIdx.x, lhs = p.lhs;
+  const int lh = blockIdx.x % lhs, j = blockIdx.x / lhs;
   const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
-
-  // the positions of item `at` into buffer `buf` (the count 0: nothing to move)
-  auto look_up = [&](int at, int buf) {
-    const int j = at / lhs % p.n, seg = at / lhs / p.n;
-    if constexpr (kLong) {
-      // the last 16 threads: their loads run beside the others' polls
-      const int t = tid - (kMoveThreads - kSeg);
-      if (t >= 0) {
-        const size_t i = (size_t)j * p.max_keep + min(seg * kSeg + t, p.max_keep - 1);
-        bool bad = false;
-        for (int c = t; c < p.checks; c += kSeg) bad |= p.bad[j * p.checks + c] != 0;
-        bad = __any_sync(0xffffu << (32 - kSeg), bad);
-        const int k = p.keep[i], m = p.keep_len[j];
-        const int2 wait = p.wait[(size_t)j * p.segs + seg];
-        slot_of[buf][t] = p.slot[i];
-        k_of[buf][t] = k;
-        if (t == 0) {
-          next_cnt[buf] = bad ? 0 : max(0, min(kSeg, m - seg * kSeg));
-          next_wait[buf] = make_int2(wait.x, min(wait.y, seg - 1));
-          if (at % lhs == 0 && seg == 0) {  // one CTA of a row reports
-            int code;
-            p.result[j] = bad ? -1 : compact_start(p, j, &code) + m;
-          }
-        }
-      }
-    } else {  // the whole list
-      int code = PIC_DEV_OK;
-      const int s = compact_start(p, j, &code), m = s >= 0 ? p.keep_len[j] : 0;
-      if (tid < m) {
-        int k = 0;
-        longlong2 slot = make_longlong2(0, 0);
-        code = compact_entry(p, j, s, tid, &k, &slot);
-        k_of[tid / kSeg][tid % kSeg] = k;
-        slot_of[tid / kSeg][tid % kSeg] = slot;
-      }
-      const bool bad = __syncthreads_or(code != PIC_DEV_OK);
-      if (at % lhs == 0) {  // one CTA of a row reports
-        if (code != PIC_DEV_OK && (tid == 0 || s >= 0)) dev_fail(p.status, code, j);
-        if (tid == 0) p.result[j] = bad ? -1 : s + m;
-      }
-      if (tid == 0) next_cnt[0] = bad ? 0 : m;
-    }
-  };
-
-  int at = blockIdx.x;
-  if constexpr (kLong) {
-    if (tid == 0) next_at = atomicAdd(p.ticket, 1);
-    __syncthreads();
-    at = next_at;
+  int code = PIC_DEV_OK;
+  const int s = compact_start(p, j, &code), m = s >= 0 ? p.keep_len[j] : 0;
+  if (tid < m) {
+    int k = 0;
+    longlong2 slot = make_longlong2(0, 0);
+    code = compact_entry(p, j, s, tid, &k, &slot);
+    k_of[tid / kSeg][tid % kSeg] = k;
+    slot_of[tid / kSeg][tid % kSeg] = slot;
   }
-  int buf = 0, turn_layer = -1;
+  const bool bad = __syncthreads_or(code != PIC_DEV_OK);
+  if (lh == 0) {  // one CTA of a row reports
+    if (code != PIC_DEV_OK && (tid == 0 || s >= 0)) dev_fail(p.status, code, j);
+    if (tid == 0) p.result[j] = bad ? -1 : s + m;
+  }
+  if (bad) return;
   const int f = tid % (D / 2);  // the frequency this thread forms cos/sin of
-  uint64_t turn = 0;            // (fp64 work: once, not once per segment)
-  if (at < all) look_up(at, 0);
-  __syncthreads();
-  const int len = kLong ? 0 : next_cnt[0];  // of the whole list
-  while (at < all && (kLong || buf * kSeg < len)) {
-    const int lh = at % lhs, j = at / lhs % p.n;
-    const int seg = kLong ? at / lhs / p.n : buf;
-    const int layer = lh / p.hgroups, h0 = (lh % p.hgroups) * p.hgroup;
-    const int heads = min(p.hgroup, p.hkv - h0), i0 = seg * kSeg;
-    const int cnt = kLong ? next_cnt[buf] : min(kSeg, len - i0);
-    // ---- read: unit u = (position, K or V, head, chunk)
-    const long long lbase = (long long)layer * p.layer_elems;
-    // (division by KC heads <= 64 as a product: exact for u < 2048)
-    const int per = KC * heads, units = cnt * 2 * per, magic = ((1 << 20) + per - 1) / per;
-    auto pair_of = [&](int u) { return (u * magic) >> 20; };  // 2 * position + (0 K, 1 V)
+  const uint64_t turn = p.rotate ? rope_turn(rope_theta(rp, p.layer_begin + lh / p.hgroups, f)) : 0;
+  for (int seg = 0; seg * kSeg < m; ++seg) {
+    const int i0 = seg * kSeg, cnt = min(kSeg, m - i0);
+    const Units<D, false> un(p, lh, cnt);
     auto where = [&](int u, int w, bool to) {
-      const int h = h0 + (u - w * per) / KC;
-      const long long sl = to ? slot_of[buf][w >> 1].y : slot_of[buf][w >> 1].x;
-      return (w & 1 ? p.v : p.k) + lbase +
-             (kLong ? sl + h * (kPage * D) : (((sl >> 4) * p.hkv + h) * kPage + (sl & 15)) * D);
+      const long long sl = to ? slot_of[seg][w >> 1].y : slot_of[seg][w >> 1].x;
+      return (w & 1 ? p.v : p.k) + un.base + (((sl >> 4) * p.hkv + un.head_of(u, w)) * kPage + (sl & 15)) * D;
     };
     uint4 a[kUnits], b[kUnits];
 #pragma unroll
     for (int q = 0; q < kUnits; ++q) {
-      const int u = tid + q * kMoveThreads, w = pair_of(u);
-      if (u < units && k_of[buf][w >> 1] != i0 + (w >> 1)) {
+      const int u = tid + q * kMoveThreads, w = un.pair_of(u);
+      if (u < un.count && k_of[seg][w >> 1] != i0 + (w >> 1)) {
         const __nv_bfloat16 *src = where(u, w, false);
         a[q] = *reinterpret_cast<const uint4 *>(src + pc.off_a);
         b[q] = *reinterpret_cast<const uint4 *>(src + pc.off_b);
       }
     }
-    if (kLong && tid == 0) next_at = atomicAdd(p.ticket, 1);
-    if (p.rotate) {
-      if (layer != turn_layer && (turn_layer < 0 || rp.layer_theta))
-        turn = rope_turn(rope_theta(rp, p.layer_begin + layer, f));
-      turn_layer = layer;
+    if (p.rotate)
       for (int i = tid / (D / 2); i < cnt; i += kMoveThreads / (D / 2))
-        cs[i][f] = rope_cos_sin_turn(i0 + i - k_of[buf][i], turn);
-    }
-    if constexpr (kLong) {
-      int32_t *fl = p.flags + ((long long)j * lhs + lh) * p.segs;
-      // every thread's loads are done at the barrier; thread 0's fence orders them,
-      // and not only its own, before the flag
-      __syncthreads();
-      const int after = next_at;
-      bool ok = true;
-      if (cnt > 0) {
-        if (tid == 0) {
-          __threadfence();
-          atomicExch(fl + seg, 1);
-        }
-        if (after < all) look_up(after, buf ^ 1);
-        for (int s2 = next_wait[buf].x + tid; ok && s2 <= next_wait[buf].y; s2 += kMoveThreads)
-          ok = wait_flag(fl + s2, p.status, j);
-      } else if (after < all) {
-        look_up(after, buf ^ 1);
-      }
-      if (__syncthreads_or(!ok)) return;
-      at = after;
-    } else {
-      __syncthreads();
-    }
-    // ---- store
+        cs[i][f] = rope_cos_sin_turn(i0 + i - k_of[seg][i], turn);
+    __syncthreads();  // all are read: the targets lie below the next segment's sources
 #pragma unroll
     for (int q = 0; q < kUnits; ++q) {
-      const int u = tid + q * kMoveThreads, w = pair_of(u), i = w >> 1;
-      if (u < units && k_of[buf][i] != i0 + i) {
+      const int u = tid + q * kMoveThreads, w = un.pair_of(u), i = w >> 1;
+      if (u < un.count && k_of[seg][i] != i0 + i) {
         __nv_bfloat16 *dst = where(u, w, true);
         if (p.rotate && !(w & 1)) {
           rotate_store(a[q], b[q], dst, pc, rp.style, &cs[i][8 * (tid % KC)]);
@@ -596,8 +545,144 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_move_kernel(C
         }
       }
     }
-    if (kLong || (buf + 1) * kSeg < len) __syncthreads();  // cs and the buffer may be written again
-    buf = kLong ? buf ^ 1 : buf + 1;
+    if (i0 + kSeg < m) __syncthreads();  // cs may be written again
+  }
+}
+
+// Long lists.  A thread's units wait in its own part of shared memory, so that it keeps
+// the registers for addresses and rotations (in registers 70.3 us for the call above,
+// now 68.9; two buffers, the next segment's rows on their way during the stores, leave
+// three CTAs an SM: 72.2, and 57 instead of 51 with 2 heads of 64).
+constexpr int kLongCtas = 4;  // of an SM
+constexpr int kHeldBytes = kUnits * 2 * kMoveThreads * 16;
+PIC_DEV void cp_async16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+PIC_DEV void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// kLayers: several layers of narrow rows a CTA (lgroup; 2 rows of 32 layers x 2 heads of
+// 64, 1500 of 3000 positions, 51.6 and 31.1 us).
+template <int D, bool kLayers>
+__global__ void __launch_bounds__(kMoveThreads, kLongCtas) compact_move_kernel(CompactParams p, RopeParams rp) {
+  constexpr int KC = D / 16;
+  pdl_entry();
+  extern __shared__ __align__(16) uint4 held[];  // [kUnits][a, b][thread]: a thread's own units
+  __shared__ float2 cs[kSeg][D / 2];
+  __shared__ int32_t k_of[2][kSeg];
+  __shared__ longlong2 slot_of[2][kSeg];
+  __shared__ int next_at, cnt_of[2];
+  __shared__ int2 wait_of[2];
+  const int tid = threadIdx.x, lhs = p.lhs;
+  const int all = lhs * p.n * p.segs;  // (the host keeps it below 2^30)
+  const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
+
+  // the positions of item `at` into buffer `buf` (the count 0: nothing to move), by
+  // the last 16 threads: their loads run beside the others' polls
+  auto look_up = [&](int at, int buf) {
+    const int j = at / lhs % p.n, seg = at / lhs / p.n;
+    const int t = tid - (kMoveThreads - kSeg);
+    if (t >= 0) {
+      const size_t i = (size_t)j * p.max_keep + min(seg * kSeg + t, p.max_keep - 1);
+      bool bad = false;
+      for (int c = t; c < p.checks; c += kSeg) bad |= p.bad[j * p.checks + c] != 0;
+      bad = __any_sync(0xffffu << (32 - kSeg), bad);
+      const int k = p.keep[i], m = p.keep_len[j];
+      const int2 wait = p.wait[(size_t)j * p.segs + seg];
+      slot_of[buf][t] = p.slot[i];
+      k_of[buf][t] = k;
+      if (t == 0) {
+        cnt_of[buf] = bad ? 0 : max(0, min(kSeg, m - seg * kSeg));
+        wait_of[buf] = make_int2(wait.x, min(wait.y, seg - 1));
+        if (at % lhs == 0 && seg == 0) {  // one CTA of a row reports
+          int code;
+          p.result[j] = bad ? -1 : compact_start(p, j, &code) + m;
+        }
+      }
+    }
+  };
+  auto held_at = [&](int q) { return 2 * q * kMoveThreads + tid; };
+  auto row_of = [&](const Units<D, kLayers> &un, int u, int w, long long sl) {
+    return (w & 1 ? p.v : p.k) + un.row_of(p, u, w) + sl;
+  };
+  auto read = [&](int at, int buf) {
+    const int i0 = at / lhs / p.n * kSeg;
+    const Units<D, kLayers> un(p, at % lhs, cnt_of[buf]);
+#pragma unroll
+    for (int q = 0; q < kUnits; ++q) {
+      const int u = tid + q * kMoveThreads, w = un.pair_of(u);
+      if (u < un.count && k_of[buf][w >> 1] != i0 + (w >> 1)) {
+        const __nv_bfloat16 *src = row_of(un, u, w, slot_of[buf][w >> 1].x);
+        const uint32_t dst = smem_u32(held + held_at(q));
+        cp_async16(dst, src + pc.off_a);
+        cp_async16(dst + kMoveThreads * 16, src + pc.off_b);
+      }
+    }
+  };
+
+  if (tid == 0) next_at = atomicAdd(p.ticket, 1);
+  __syncthreads();
+  int at = next_at, buf = 0, turn_layer = -1;
+  const int f = tid % (D / 2);  // the frequency this thread forms cos/sin of
+  uint64_t turn = 0;            // (fp64 work: once, not once per segment)
+  if (at < all) look_up(at, 0);
+  __syncthreads();
+  if (at < all) read(at, 0);
+  while (at < all) {
+    const int lh = at % lhs, j = at / lhs % p.n, seg = at / lhs / p.n, i0 = seg * kSeg;
+    const int cnt = cnt_of[buf];
+    const Units<D, kLayers> un(p, lh, cnt);
+    if (tid == 0) next_at = atomicAdd(p.ticket, 1);
+    unsigned runs = 0;
+    if (p.rotate) {
+      // positions of a run that stayed together move alike: cos/sin for its first only
+      const int i = tid & 31;
+      runs = __ballot_sync(0xffffffffu, i < cnt && (i == 0 || k_of[buf][i] != k_of[buf][i - 1] + 1));
+      if (un.layer != turn_layer && (turn_layer < 0 || rp.layer_theta))
+        turn = rope_turn(rope_theta(rp, p.layer_begin + un.layer, f));
+      turn_layer = un.layer;
+      unsigned left = runs;
+      auto drop = [&](int n) {
+        for (int k = 0; k < n; ++k) left &= left - 1;
+      };
+      for (drop(tid / (D / 2)); left; drop(kMoveThreads / (D / 2))) {
+        const int r = __ffs(left) - 1;
+        cs[r][f] = rope_cos_sin_turn(i0 + r - k_of[buf][r], turn);
+      }
+    }
+    cp_async_wait();
+    int32_t *fl = p.flags + ((long long)j * lhs + lh) * p.segs;
+    // every thread's loads are done at the barrier; thread 0's fence orders them,
+    // and not only its own, before the flag
+    __syncthreads();
+    const int after = next_at;
+    bool ok = true;
+    if (cnt > 0 && tid == 0) {
+      __threadfence();
+      atomicExch(fl + seg, 1);
+    }
+    if (after < all) look_up(after, buf ^ 1);
+    if (cnt > 0)
+      for (int s2 = wait_of[buf].x + tid; ok && s2 <= wait_of[buf].y; s2 += kMoveThreads)
+        ok = wait_flag(fl + s2, p.status, j);
+    if (__syncthreads_or(!ok)) return;
+#pragma unroll
+    for (int q = 0; q < kUnits; ++q) {
+      const int u = tid + q * kMoveThreads, w = un.pair_of(u), i = w >> 1;
+      if (u < un.count && k_of[buf][i] != i0 + i) {
+        const uint4 a = held[held_at(q)], b = held[held_at(q) + kMoveThreads];
+        __nv_bfloat16 *dst = row_of(un, u, w, slot_of[buf][i].y);
+        if (p.rotate && !(w & 1)) {
+          rotate_store(a, b, dst, pc, rp.style, &cs[31 - __clz(runs & ((2u << i) - 1))][8 * (tid % KC)]);
+        } else {
+          st_global16(dst + pc.off_a, a);
+          st_global16(dst + pc.off_b, b);
+        }
+      }
+    }
+    if (after < all) read(after, buf ^ 1);
+    __syncthreads();  // cs and the buffer may be written again
+    at = after;
+    buf ^= 1;
   }
 }
 
@@ -728,13 +813,15 @@ static CompactSpace compact_space(const pic_geom_t *g, int n, int max_keep, int 
 template <int D>
 static cudaError_t launch_move(const CompactParams &cp, const RopeParams &rp, long long items,
                                pic_stream_t stream) {
-  // the long form's CTAs stay
-  if (cp.flags)
-    return launch_dependent(compact_move_kernel<D, true>,
-                            dim3((unsigned)std::min(items, kMoveCtas * 152LL)), dim3(kMoveThreads), 0, stream,
+  if (!cp.flags)
+    return launch_dependent(compact_short_kernel<D>, dim3((unsigned)items), dim3(kMoveThreads), 0, stream,
                             cp, rp);
-  return launch_dependent(compact_move_kernel<D, false>, dim3((unsigned)items), dim3(kMoveThreads), 0,
-                          stream, cp, rp);
+  void (*kernel)(CompactParams, RopeParams) =
+      cp.lgroup > 1 ? compact_move_kernel<D, true> : compact_move_kernel<D, false>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldBytes);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3((unsigned)std::min(items, kLongCtas * 152LL)), dim3(kMoveThreads),
+                          kHeldBytes, stream, cp, rp);
 }
 
 }  // namespace pages
@@ -846,6 +933,13 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
   cp.hgroup = std::min(heads_per_group(geom), cp.hkv);
   cp.hgroups = (cp.hkv + cp.hgroup - 1) / cp.hgroup;
   cp.layers = layer_end - layer_begin;
+  // Long lists of narrow rows: as many layers a CTA as it holds, if they turn alike and
+  // two segments an SM are left
+  cp.lgroup = 1;
+  if (max_keep > kShort && !rp.layer_theta)
+    cp.lgroup = (int)std::max(1LL, std::min<long long>(heads_per_group(geom) / cp.hkv,
+                                                       (long long)n * cp.layers * cp.segs / (2 * 152)));
+  cp.lhs = (cp.layers + cp.lgroup - 1) / cp.lgroup * cp.hgroups;
   cp.layer_begin = layer_begin;
   cp.rotate = rotate != 0;
   cp.num_pages = num_pages;
@@ -876,7 +970,7 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
     cp.ticket = reinterpret_cast<int32_t *>(ws + cw.ticket);
     cp.flags = reinterpret_cast<int32_t *>(ws + cw.flags);
   }
-  const long long items = (long long)n * cp.layers * cp.hgroups * (cp.flags ? cp.segs : 1);
+  const long long items = (long long)n * cp.lhs * (cp.flags ? cp.segs : 1);
   if (items > INT32_MAX / 2)
     return fail(PIC_ERR_UNSUPPORTED, "%s: problem too large for one launch", who);
   if (items == 0) return fail(PIC_ERR_INVALID_ARG, "%s: no layers", who);

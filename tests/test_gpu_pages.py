@@ -272,6 +272,20 @@ def test_compact(cuda_lib, dim, hkv, style, rotate):
         m.check()
 
 
+@pytest.mark.parametrize("dim,hkv,layers", [(64, 1, 21), (64, 2, 14), (64, 3, 13), (128, 1, 11), (128, 2, 9)])
+def test_compact_long_lists_of_narrow_rows(cuda_lib, dim, hkv, layers):
+    """Several layers a CTA, the last group with fewer, in part of the layers too."""
+    m = Model(3, 70, 300, layers=layers, heads=(hkv, hkv), dim=dim)
+    for r in range(3):
+        m.place(r, 1000)
+    m.up()
+    m.compact([2, 0, 1], [np.sort(m.rng.choice(990, n, replace=False)).tolist() for n in (800, 33, 640)],
+              start=[3, 10, 1], rotate=True)
+    m.check()
+    m.compact([2], [list(range(1, 700, 2))], start=[50], rotate=False, layers=(2, layers))
+    m.check()
+
+
 def test_compact_many_rows_at_once(cuda_lib):
     m = Model(64, 20, 2000, layers=3, heads=(8, 8), dim=128)
     for r in range(64):
