@@ -244,7 +244,7 @@ PIC_DEV void deal_shares(const Params &p, int first) {
 // One CTA per token, behind `dealers` CTAs that deal out the work.  A thread takes
 // a chunk (8 pairs) of a query or key head, and a value piece: the host gives the
 // CTAs as many threads as there are chunks, up to kAppendMax.  Bound by its chain of
-// loads (lengths and parents, the page, cos/sin): 4 to 5 us for 4 to 256 tokens.  One
+// loads (lengths and parents, the page, cos/sin): 3.8 to 5 us for 4 to 256 tokens.  One
 // place in the code rotates, because a call starts with cold instruction caches (three chunks a
 // thread, their rotations unrolled, took 5.3 us instead of 4.9, 16 x 16 tokens).
 constexpr int kAppendMax = 512;
@@ -906,8 +906,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 // shared memory in a fixed order.  One warp per row where there are many rows, four
 // where a unit may be split over many CTAs (see `launch`; 76 partials of two units by
 // one load after the other had cost 11 of 27.5 us).  Bound by its chain of loads (the
-// request and the deal, then the partials): 2.7 us for 16 rows, 4.9 for 1024 rows of
-// about five partials, 7.6 for 3200 rows of d = 64.
+// request and the deal, then the partials): 2.7 us for 16 rows, 4.7 for 1024 rows of
+// about five partials, 6.4 for 3200 rows of d = 64.
 template <int D, int kWarps>
 __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   constexpr int CPL = D / 32, kRows = 4 / kWarps, U = 8;
