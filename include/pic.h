@@ -575,9 +575,8 @@ pic_status_t pic_attend_decode_noalloc(const pic_geom_t *geom, int32_t layer, in
  *         its ancestors:  softmax(R(p_i) q[b][i][h] . k / sqrt(d)) v
  * (the key of a rejected branch never shows).  lse[b][i][h] (nullable): the
  * natural-log sum-exp of those scores.  Rows i >= n_b of out and lse are not
- * written.  A drafted token's key and value have to be finite: those of another
- * branch of its own request enter with weight zero.  Slots behind the drafts
- * may hold anything.
+ * written.  Infinities and NaN of a drafted token's key and value show in the rows
+ * that see it and in no others.  Slots behind the drafts may hold anything.
  *
  * q: bf16 [batch][max_draft][Hq][d]; k_new, v_new: bf16
  * [batch][max_draft][Hkv][d] (un-rotated); ctx_len, draft_len: int32 [batch];

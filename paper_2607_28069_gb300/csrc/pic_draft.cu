@@ -38,6 +38,10 @@ constexpr int kCtas = 152;         // one per SM
 constexpr int NSK = 3, NSV = 2;    // ring stages of K and V
 constexpr int NQB = 2;             // query tiles
 constexpr int kThreads = 384;      // K producer, MMA, V producer, ring, two softmax warpgroups
+// The bound for the compiler at d = 64: 127 registers a thread instead of 154, so that CTAs
+// of the append and the merge fit beside one on an SM and begin early (5 ragged requests
+// of up to 9001 keys 23.2 and 21.1 us, 24 of 3000 to 10000 21.9 and 20.0).
+constexpr int kThreads64 = 448;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;    // S_t at 128 t, O_t at 256 + D t
 // Named barriers (0: __syncthreads): P_t from warpgroup t to the MMA warp, the
@@ -62,7 +66,7 @@ enum {
   B_KEMPTY = B_KFULL + NSK,
   B_VFULL = B_KEMPTY + NSK,
   B_VEMPTY = B_VFULL + NSV,
-  B_VFIX = B_VEMPTY + NSV,   // per V stage: the rows behind the last draft are cleared
+  B_VFIX = B_VEMPTY + NSV,   // per V stage: what must not meet a weight of zero is cleared
   B_SFULL = B_VFIX + NSV,    // S_t
   B_OEND = B_SFULL + 2,      // a segment's last PV of warpgroup t
   B_ODONE = B_OEND + 2,      // a segment's O read by both warpgroups
@@ -79,6 +83,7 @@ struct Params {
   __nv_bfloat16 *k_cache, *v_cache;  // at the layer
   __nv_bfloat16 *qp;                 // workspace: packed rotated queries
   uint64_t *mask;                    // workspace: [batch][max_draft] ancestor bits
+  int32_t *wild;                     // workspace: [batch][max_draft] the value has an infinity or NaN
   struct Share *share;               // workspace: [kCtas] each CTA's start
   int32_t *rows;                     // workspace: [kCtas][32] K/V rows of its first 32 pages
   int4 *req;                         // workspace: [batch] first step, ctx_len, draft_len as dealt
@@ -89,6 +94,14 @@ struct Params {
   int32_t *status;
   float scale_log2;
 };
+
+// The ring warp's waits, in one place in the code: 11 KB less of it, which a call with
+// cold instruction caches feels (one request of 4288 keys 14.5 and 14.2 us); the
+// producers' waits as calls too cost 0.3% of long contexts.
+__device__ __noinline__ bool ring_wait(uint32_t bar, uint32_t parity, volatile int *abort, int32_t *status,
+                                       int detail) {
+  return mbar_wait(bar, parity, abort, status, detail);
+}
 
 PIC_DEV void st_global32(void *p, const float *f) {
   asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]),
@@ -240,6 +253,29 @@ PIC_DEV void deal_shares(const Params &p, int first) {
   }
 }
 
+// Of 8 bf16 values: whether there is an infinity or a NaN among them; zeros in their place.
+PIC_DEV uint32_t wild_halves(uint32_t w) { return __vcmpeq2(w & 0x7f807f80u, 0x7f807f80u); }
+PIC_DEV bool has_wild(const uint4 &v) {
+  return (wild_halves(v.x) | wild_halves(v.y) | wild_halves(v.z) | wild_halves(v.w)) != 0;
+}
+PIC_DEV uint4 without_wild(const uint4 &v) {
+  return make_uint4(v.x & ~wild_halves(v.x), v.y & ~wild_halves(v.y), v.z & ~wild_halves(v.z),
+                    v.w & ~wild_halves(v.w));
+}
+// Request b's tokens with such a value, from what lane l read for tokens l and l + 32.
+struct Wild {
+  int a, b;
+  PIC_DEV Wild(const Params &p, int req, int n) {
+    const int lane = threadIdx.x & 31;
+    const int32_t *w = p.wild + (size_t)req * p.max_draft;
+    a = lane < n ? w[lane] : 0;
+    b = lane + 32 < n ? w[lane + 32] : 0;
+  }
+  PIC_DEV uint64_t tokens() const {
+    return __ballot_sync(0xffffffffu, a != 0) | (uint64_t)__ballot_sync(0xffffffffu, b != 0) << 32;
+  }
+};
+
 // ------------------------------------------------------------------ append
 // One CTA per token, behind `dealers` CTAs that deal out the work.  A thread takes
 // a chunk (8 pairs) of a query or key head, and a value piece: the host gives the
@@ -335,6 +371,7 @@ __global__ void __launch_bounds__(kAppendMax) draft_append_kernel(Params p, Rope
     if (p.parent) line = ancestors(p, up, b, i);
     if (tid == 0) {
       p.mask[tok] = line;
+      p.wild[tok] = 0;  // (a thread that finds one writes 1 behind a barrier)
       depth = __popcll(line) - 1;
       if (page < 0 || page >= p.num_pages) dev_fail(p.status, PIC_DEV_BAD_PAGE, b);
     }
@@ -354,13 +391,16 @@ __global__ void __launch_bounds__(kAppendMax) draft_append_kernel(Params p, Rope
       dst = p.k_cache + (((size_t)page * p.Hkv + hk) * 16 + slot % 16) * D;
     if (dst) rotate_store(qa, qb, dst, pc, rp.style, cs + 8 * (tid % KC));
   }
+  bool wild = false;
   if (page >= 0)
 #pragma unroll 1
     for (int u = tid; u < pieces; u += threads) {
       const int hk = u / (D / 8), c = u % (D / 8);
-      st_global16(p.v_cache + (((size_t)page * p.Hkv + hk) * 16 + slot % 16) * D + c * 8,
-                  u == tid ? vn : ld_stream(v_src + u * 8));
+      if (u != tid) vn = ld_stream(v_src + u * 8);
+      wild |= has_wild(vn);
+      st_global16(p.v_cache + (((size_t)page * p.Hkv + hk) * 16 + slot % 16) * D + c * 8, vn);
     }
+  if (wild) p.wild[tok] = 1;
 }
 
 // ---------------------------------------------------------------- schedule
@@ -416,6 +456,7 @@ struct Segments {
   PIC_DEV int slot(int t) const { return (2 * cta + (first ? 1 : 0)) * 2 + t; }
   // key tiles of warpgroup t (see draft_attn_kernel)
   PIC_DEV int count(int t) const { return two ? n : (n + 1 - t) / 2; }
+  PIC_DEV int drafts() const { return (kt0 + n) * BN > r.ctx ? r.n : 0; }  // 0: the segment holds none
 };
 
 // --------------------------------------------------------------- attention
@@ -448,7 +489,7 @@ struct Segments {
 // have no limit, so after a wait that ran out every role still walks all segments
 // and meets each barrier; the MMA warp then issues nothing but its commits.
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(D == 64 ? kThreads64 : kThreads, 1)
     draft_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
                       const __grid_constant__ CUtensorMap tm_k,
                       const __grid_constant__ CUtensorMap tm_v, Params p) {
@@ -504,6 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     while (sg.next()) {
       const int n = sg.count(t);
+      const Wild wild(p, sg.b, sg.drafts());
       // this thread's row: token rr / G, query head hk G + rr % G
       auto row_of = [&]() { return (2 * sg.pair + (sg.two ? t : 0)) * BM + row; };
       float m_used = -INFINITY, l = 0.f;
@@ -669,6 +711,28 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(B_ODONE));
+      // infinities and NaN in the values of the segment's drafts lo .. hi - 1, which were
+      // taken out of PV, for the rows that see them
+      const int lo = max(0, sg.kt0 * BN - sg.r.ctx), hi = min(kMaxDraft, (sg.kt0 + sg.n) * BN - sg.r.ctx);
+      uint64_t seen = hi > lo ? wild.tokens() : 0;
+      if (seen && store) {
+        seen &= p.mask[(size_t)sg.b * p.max_draft + rr / p.G] & (~0ull >> (64 - hi + lo) << lo);
+#pragma unroll 1
+        for (; seen; seen &= seen - 1) {
+          const size_t token = (size_t)sg.b * p.max_draft + __ffsll((long long)seen) - 1;
+          const __nv_bfloat16 *v = p.v_new + (token * p.Hkv + sg.hk) * D;
+#pragma unroll 1
+          for (int e = c_begin * 32; e < c_end * 32; ++e) {
+            const float x = __bfloat162float(v[e]);
+            if (fabsf(x) <= 3.4e38f) continue;
+            if (whole)
+              p.out[o_row * D + e] = __float2bfloat16(__bfloat162float(p.out[o_row * D + e]) + x);
+            else
+              p.part_o[p_row * D + e] += x;
+          }
+        }
+      }
+      __syncwarp();
       if (store && (sg.two || t == 0)) {
         if (!whole)
           p.part_ml[p_row] = make_float2(l == 0.f ? -INFINITY : M, l);
@@ -696,6 +760,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     while (ok && sg.next()) {
       const int keys = sg.r.ctx + sg.r.n;
+      const Wild wild(p, sg.b, is_k ? 0 : sg.drafts());
       if (is_k)
         for (int t = 0; t <= (sg.two ? 1 : 0); ++t, ++nq) {
           const int qb = nq % NQB;
@@ -742,19 +807,26 @@ __global__ void __launch_bounds__(kThreads, 1)
         if ((j & 3) == 0) next = entry(j + 4);
         ++g;
         if (is_k) continue;
-        if (kt == sg.r.tiles - 1) {
-          // Rows behind the last draft may hold anything, and a weight of zero
-          // does not silence an infinity: they are cleared before PV reads them
+        // A weight of zero does not silence an infinity.  Before PV reads them, rows
+        // behind the last draft, which may hold anything, are cleared, and the drafts'
+        // own infinities and NaN (rows that do not see them have weight zero there).
+        const bool end = kt == sg.r.tiles - 1;
+        if ((kt + 1) * BN > sg.r.ctx && (end || wild.tokens())) {
           if (!wait(b_full + st, ((g - 1) / nst) & 1)) break;
           const int r0 = keys - kt * BN, r1 = (r0 + 15) & ~15;  // the rest of its page
           constexpr int CH = D / 8;
-          for (int e = lane; e < (r1 - r0) * CH; e += 32) {
-            const int row = r0 + e / CH, ch = e % CH, rr = row & 15;
+          auto piece = [&](int row, int ch) {
+            const int rr = row & 15;
             const uint32_t off =
                 PANELS == 2 ? (uint32_t)((rr >> 3) * 2048 + (ch >> 3) * 1024 + (rr & 7) * 128 +
                                          (((ch & 7) ^ (rr & 7)) << 4))
                             : (uint32_t)(rr * 128 + ((ch ^ (rr & 7)) << 4));
-            sts128(ring + st * L::kTile + (row >> 4) * kPageBytes + off, make_uint4(0, 0, 0, 0));
+            return ring + st * L::kTile + (row >> 4) * kPageBytes + off;
+          };
+          const int z0 = wild.tokens() ? max(0, sg.r.ctx - kt * BN) : r0, z1 = end ? r1 : BN;
+          for (int e = lane; e < (z1 - z0) * CH; e += 32) {
+            const uint32_t at = piece(z0 + e / CH, e % CH);
+            sts128(at, z0 + e / CH >= r0 ? make_uint4(0, 0, 0, 0) : without_wild(lds128(at)));
           }
           fence_proxy_async();
           __syncwarp();
@@ -842,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // The MMA warp's waits, in its order.
     bool ok = true;
     auto wait = [&](int i, uint32_t parity) {
-      if (ok) ok = mbar_wait(bar(i), parity, abort_flag, p.status, detail);
+      if (ok) ok = ring_wait(bar(i), parity, abort_flag, p.status, detail);
     };
     auto meet = [&]() {
       ok = __all_sync(0xffffffffu, ok);
@@ -875,7 +947,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             wait(B_KFULL + g % NSK, (g / NSK) & 1);
             pv_g[t] = g;
             pv_s[t] = m == 0 ? s : 0;
-            pv_fix[t] = sg.kt0 + j == sg.r.tiles - 1;
+            pv_fix[t] = (sg.kt0 + j + 1) * BN > sg.r.ctx;  // holds drafts
           }
           meet();
         }
@@ -1009,7 +1081,7 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
 // -------------------------------------------------------------------- host
 struct Plan {
   int r_pad;
-  size_t q_bytes, mask_bytes, share_bytes, rows_bytes, req_bytes, o_bytes, ml_bytes, total;
+  size_t q_bytes, mask_bytes, wild_bytes, share_bytes, rows_bytes, req_bytes, o_bytes, ml_bytes, total;
 };
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
@@ -1019,12 +1091,13 @@ inline Plan plan(const pic_geom_t *g, int batch, int max_draft) {
   pl.r_pad = rt_max * BM;
   pl.q_bytes = align256((size_t)batch * g->num_kv_heads * pl.r_pad * g->head_dim * 2);
   pl.mask_bytes = align256((size_t)batch * max_draft * 8);
+  pl.wild_bytes = align256((size_t)batch * max_draft * 4);
   pl.share_bytes = align256(kCtas * sizeof(Share));
   pl.rows_bytes = align256(kCtas * 32 * 4);
   pl.req_bytes = align256((size_t)batch * sizeof(int4));
   pl.o_bytes = align256((size_t)4 * kCtas * BM * g->head_dim * 4);
   pl.ml_bytes = align256((size_t)4 * kCtas * BM * sizeof(float2));
-  pl.total = pl.q_bytes + pl.mask_bytes + pl.share_bytes + pl.rows_bytes + pl.req_bytes + pl.o_bytes + pl.ml_bytes;
+  pl.total = pl.q_bytes + pl.mask_bytes + pl.wild_bytes + pl.share_bytes + pl.rows_bytes + pl.req_bytes + pl.o_bytes + pl.ml_bytes;
   return pl;
 }
 
@@ -1133,6 +1206,8 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   ws += pl.q_bytes;
   p.mask = reinterpret_cast<uint64_t *>(ws);
   ws += pl.mask_bytes;
+  p.wild = reinterpret_cast<int32_t *>(ws);
+  ws += pl.wild_bytes;
   p.share = reinterpret_cast<Share *>(ws);
   ws += pl.share_bytes;
   p.rows = reinterpret_cast<int32_t *>(ws);

@@ -283,3 +283,57 @@ def test_a_nan_in_a_visible_key_shows(cuda_lib, ctx, at):
     assert torch.equal(torch.isnan(s["lse"]).cpu(), bad)
     nan = torch.isnan(s["out"]).cpu()
     assert torch.equal(nan.any(-1), bad) and torch.equal(nan.all(-1), bad)
+
+
+@pytest.mark.parametrize("heads,dim,ctx,T", [((4, 2), 64, 100, 9), ((4, 1), 128, 9000, 9), ((8, 1), 128, 9080, 64),
+                                             ((32, 2), 64, 2040, 40), ((16, 1), 128, 0, 64), ((8, 2), 128, 250, 30)])
+def test_infinities_and_nan_of_another_branch_do_not_show(cuda_lib, heads, dim, ctx, T):
+    """Drafted values with infinities and NaN: rows that do not see them are, bit for bit,
+    those of the same call with zeros in their places; rows that do have them where they
+    are, and elsewhere the same bits.  Keys of another branch may be NaN, too."""
+    lens = [T, max(1, T - 3), T]
+    ctxs = [ctx, 77, 3]
+    s = draw(heads, dim, 0, ctxs, lens, T, True, layers=1, seed=T)
+    G, hkv = heads[0] // heads[1], heads[1]
+    rng = np.random.default_rng(ctx)
+    vals = torch.zeros((3, T, hkv, dim))  # what is added to the values
+    for b in range(2):  # request 2 stays finite
+        for i in rng.choice(lens[b], max(1, T // 6), replace=False):
+            h, c = rng.integers(0, hkv), rng.choice(dim, 3, replace=False)
+            vals[b, i, h, c[0]], vals[b, i, h, c[1]] = float("inf"), float("-inf")
+            vals[b, i, h, c[2]] = float("nan")
+    wild = vals != 0
+    clean = s["v"].clone()
+    clean[wild.cuda()] = 0
+    kc, vc = s["kc"].clone(), s["vc"].clone()
+    call(dict(s, v=clean))
+    out, lse = s["out"].clone(), s["lse"].clone()
+    assert bool(torch.isfinite(out.float()).all())
+    dirty = clean.clone()
+    dirty[wild.cuda()] = vals[wild].bfloat16().cuda()
+    s2 = dict(s, v=dirty, kc=kc, vc=vc, out=torch.full_like(out, 7.0), lse=torch.full_like(lse, 7.0))
+    call(s2)
+    want = out.float().cpu()
+    for b in range(3):
+        line = line_of(s["par"][b], lens[b])
+        for i in range(lens[b]):
+            add = vals[b, line[i]].sum(0)  # inf - inf and NaN: NaN
+            want[b, i] += add.repeat_interleave(G, 0)
+    got = s2["out"].float().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(got, 1.5), torch.nan_to_num(want, 1.5))
+    assert torch.equal(s2["lse"], lse)
+    # the stored values are what was given
+    t = torch.arange(lens[0])
+    page = s["bt"].cpu()[0][(ctx + t) // 16].long()
+    assert torch.equal(vc[0].cpu()[page, :, (ctx + t) % 16].view(torch.int16), dirty[0, :lens[0]].cpu().view(torch.int16))
+    # a key that is NaN shows where it is seen only
+    leaf = lens[0] - 1
+    k = s["k"].clone()
+    k[0, leaf] = float("nan")
+    s3 = dict(s, k=k, v=clean, out=torch.full_like(out, 7.0), lse=torch.full_like(lse, 7.0))
+    call(s3)
+    rest = [i for i in range(lens[0]) if i != leaf]
+    assert torch.equal(s3["out"][0, rest], out[0, rest]) and torch.equal(s3["out"][1:], out[1:])
+    assert bool(torch.isnan(s3["out"][0, leaf].float()).all())
+    assert cuda_lib.pic_device_status() == (0, 0)
