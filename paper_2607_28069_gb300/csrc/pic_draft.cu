@@ -38,10 +38,12 @@ constexpr int kCtas = 152;         // one per SM
 constexpr int NSK = 3, NSV = 2;    // ring stages of K and V
 constexpr int NQB = 2;             // query tiles
 constexpr int kThreads = 384;      // K producer, MMA, V producer, ring, two softmax warpgroups
-// The bound for the compiler at d = 64: 127 registers a thread instead of 154, so that CTAs
-// of the append and the merge fit beside one on an SM and begin early (5 ragged requests
-// of up to 9001 keys 23.2 and 21.1 us, 24 of 3000 to 10000 21.9 and 20.0).
-constexpr int kThreads64 = 448;
+// The bound for the compiler: 127 registers a thread instead of 154.  With those, and with
+// no shared memory to spare for an alignment, CTAs of the append and of the merge (one warp
+// a row: none of either) fit beside one on an SM and begin early.  us with and without:
+// 5 ragged requests, d = 64, 21.1 and 23.2; 24, d = 64, 20.0 and 21.9; d = 128, 4 of 16k
+// with 256 rows 67.9 and 68.5, 4 of 139k 333.7 and 334.4, 24 tokens of 4 x 1000 15.3 and 14.9.
+constexpr int kBoundThreads = 448;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;    // S_t at 128 t, O_t at 256 + D t
 // Named barriers (0: __syncthreads): P_t from warpgroup t to the MMA warp, the
@@ -56,7 +58,7 @@ struct Layout {
   static constexpr int kV = kK + NSK * kTile;
   static constexpr int kML = kV + NSV * kTile;  // float [2][BM]: the warpgroups' m, then l
   static constexpr int kBar = kML + 2 * BM * 4;
-  static constexpr int kAlloc = kBar + 256 + 1024;
+  static constexpr int kAlloc = kBar + 256;
 };
 
 enum {
@@ -489,7 +491,7 @@ struct Segments {
 // have no limit, so after a wait that ran out every role still walks all segments
 // and meets each barrier; the MMA warp then issues nothing but its commits.
 template <int D>
-__global__ void __launch_bounds__(D == 64 ? kThreads64 : kThreads, 1)
+__global__ void __launch_bounds__(kBoundThreads, 1)
     draft_attn_kernel(const __grid_constant__ CUtensorMap tm_q,
                       const __grid_constant__ CUtensorMap tm_k,
                       const __grid_constant__ CUtensorMap tm_v, Params p) {
@@ -501,10 +503,12 @@ __global__ void __launch_bounds__(D == 64 ? kThreads64 : kThreads, 1)
   constexpr uint32_t kPageBytes = 16 * D * 2;
   constexpr uint32_t kGroupStride = PANELS == 2 ? 2048 : 1024;
   constexpr uint32_t kPanelOff = PANELS == 2 ? 1024 : BN * 128;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                              ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
+  if (sbase & 1023) {  // the tiles' swizzle counts on the array's alignment
+    if (threadIdx.x == 0) dev_fail(p.status, PIC_DEV_BAD_REQUEST, -1);
+    return;
+  }
   auto bar = [&](int i) { return sbase + L::kBar + 8u * (uint32_t)i; };
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::kBar + 8 * B_COUNT);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kBar + 8 * B_COUNT + 8);
@@ -983,8 +987,8 @@ __global__ void __launch_bounds__(D == 64 ? kThreads64 : kThreads, 1)
 template <int D, int kWarps>
 __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   constexpr int CPL = D / 32, kRows = 4 / kWarps, U = 8;
+  constexpr int KW = ((kCtas + kWarps - 1) / kWarps + 31) / 32;  // partials of a lane
   __shared__ float acc_s[4][D], m_s[4], l_s[4];
-  __shared__ float2 w_s[4][(kCtas + kWarps - 1) / kWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int h = blockIdx.x * kRows + warp / kWarps, i = blockIdx.y, b = blockIdx.z;
@@ -1019,32 +1023,33 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
     }
   };
   if (mine > 0) load(0);  // beside the (m, l) pairs
-#pragma unroll 1
-  for (int c = lane; c < mine; c += 32) {
-    const float2 ml = p.part_ml[part_row(c)];
-    w_s[warp][c] = ml;
-    M = fmaxf(M, ml.x);
+  float w[KW];  // lane's partials: c = lane, lane + 32, ...
+  float2 ml[KW];
+#pragma unroll
+  for (int k = 0; k < KW; ++k) {
+    ml[k] = lane + 32 * k < mine ? p.part_ml[part_row(lane + 32 * k)] : make_float2(-INFINITY, 0.f);
+    M = fmaxf(M, ml[k].x);
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-#pragma unroll 1
-  for (int c = lane; c < mine; c += 32) {
-    const float2 ml = w_s[warp][c];
-    const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
-    l = fmaf(w, ml.y, l);
-    w_s[warp][c].x = w;
+#pragma unroll
+  for (int k = 0; k < KW; ++k) {
+    w[k] = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - M);
+    l = fmaf(w[k], ml[k].y, l);
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-  __syncwarp();
 #pragma unroll
   for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
 #pragma unroll 1
   for (int c0 = 0; c0 < mine; c0 += U) {
     if (c0) load(c0);
+    float wc = w[0];
+#pragma unroll
+    for (int k = 1; k < KW; ++k) wc = c0 >= 32 * k ? w[k] : wc;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      const float wk = c0 + k < mine ? w_s[warp][c0 + k].x : 0.f;
+      const float wk = __shfl_sync(0xffffffffu, wc, (c0 + k) & 31);  // 0 past the end
       if (wk != 0.f)  // 0: past the end, or no key of the part was visible
 #pragma unroll
         for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wk, v[k][e], acc[e]);
