@@ -978,15 +978,15 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
 // o = sum_c w_c O_c / sum_c w_c l_c, w_c = 2^(m_c - M), over the CTAs that hold
 // key tiles of a row's unit.  kWarps warps per (token, query head), each with its
 // share of the partials: the (m, l) pairs of all of them first (a lane per
-// partial), then the O rows, eight loads in flight; the warps' sums are combined in
+// partial), then the O rows, U loads in flight; the warps' sums are combined in
 // shared memory in a fixed order.  One warp per row where there are many rows, four
 // where a unit may be split over many CTAs (see `launch`; 76 partials of two units by
 // one load after the other had cost 11 of 27.5 us).  Bound by its chain of loads (the
 // request and the deal, then the partials): 2.7 us for 16 rows, 4.7 for 1024 rows of
 // about five partials, 6.4 for 3200 rows of d = 64.
-template <int D, int kWarps>
+template <int D, int kWarps, int U>
 __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
-  constexpr int CPL = D / 32, kRows = 4 / kWarps, U = 8;
+  constexpr int CPL = D / 32, kRows = 4 / kWarps;
   constexpr int KW = ((kCtas + kWarps - 1) / kWarps + 31) / 32;  // partials of a lane
   __shared__ float acc_s[4][D], m_s[4], l_s[4];
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1128,11 +1128,12 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tk, const CU
   // 24 of 32, d = 64, 21.8 and 21.1.
   const long long units = (long long)p.batch * p.Hkv * ((p.r_pad / BM + 1) / 2);
   const long long rows = (long long)p.batch * p.max_draft * p.Hq;
-  if (units >= 24 || rows > 20 * kCtas)
-    return launch_dependent(draft_merge_kernel<D, 1>, dim3((p.Hq + 3) / 4, p.max_draft, p.batch),
-                            dim3(128), 0, stream, p);
-  return launch_dependent(draft_merge_kernel<D, 4>, dim3(p.Hq, p.max_draft, p.batch), dim3(128), 0,
-                          stream, p);
+  // Four loads in flight instead of eight where units are few CTAs' (64 units of 112 rows
+  // 171.0 and 169.8 us, 48 of 40, d = 64, 15.1 and 14.5; but 40 of 32 19.4 and 20.1).
+  const bool one = units >= 24 || rows > 20 * kCtas;
+  void (*merge)(Params) = !one ? draft_merge_kernel<D, 4, 8>
+                               : units >= 48 ? draft_merge_kernel<D, 1, 4> : draft_merge_kernel<D, 1, 8>;
+  return launch_dependent(merge, dim3(one ? (p.Hq + 3) / 4 : p.Hq, p.max_draft, p.batch), dim3(128), 0, stream, p);
 }
 
 }  // namespace draft
