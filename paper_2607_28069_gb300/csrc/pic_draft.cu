@@ -1180,8 +1180,9 @@ extern "C" pic_status_t pic_attend_draft(const pic_geom_t *geom, int32_t layer, 
   if (rows_total + 16 >= INT32_MAX || (long long)batch * Hkv * pl.r_pad >= INT32_MAX ||
       (double)batch * Hkv * (pl.r_pad / BM) * (max_pages / 8 + 1) >= INT32_MAX)
     return fail(PIC_ERR_UNSUPPORTED, "%s: cache or queries have more than 2^31 rows", who);
-  if (batch > 65535 || max_pages > INT32_MAX / 16 - 16)
-    return fail(PIC_ERR_UNSUPPORTED, "%s: batch %d, max_pages %d", who, batch, max_pages);
+  if (batch > 65535) return fail(PIC_ERR_UNSUPPORTED, "%s: grid too large", who);
+  if (max_pages > INT32_MAX / 16 - 16)
+    return fail(PIC_ERR_UNSUPPORTED, "%s: max_pages %d: positions beyond 32 bits", who, max_pages);
   if (!workspace || workspace_bytes < pl.total || (reinterpret_cast<uintptr_t>(workspace) & 255))
     return fail(PIC_ERR_WORKSPACE, "%s: workspace needs %zu bytes, 256-aligned", who, pl.total);
 

@@ -120,3 +120,9 @@ def test_pages(lib):
         return lib.pic_page_free(n, row, 4, FAKE, FAKE, 4, 9, FAKE, NULL)
 
     assert free(row=NULL) == 1 and free(n=4097) == 2 and free(n=0) == 0
+
+
+def test_attend_draft_positions_stay_within_32_bits(lib):
+    g = geom(num_q_heads=4, num_kv_heads=1)
+    assert attend(g, batch=1, max_pages=(2 ** 31 - 1) // 16 - 15) == 2 and "beyond 32 bits" in error()
+    assert attend(g, batch=1, max_pages=2 ** 31 - 1) == 2 and "beyond 32 bits" in error()
