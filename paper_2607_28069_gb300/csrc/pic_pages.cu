@@ -384,7 +384,9 @@ PIC_DEV int compact_entry(const CompactParams &p, int j, int s, int i, int *k_ou
   const int32_t *t = p.block_table + (size_t)p.row[j] * p.max_pages;
   const int32_t *kp = p.keep + (size_t)j * p.max_keep;
   const int k = kp[i], before = i > 0 ? kp[i - 1] : -1;
-  if (k < i || before >= k) return PIC_DEV_BAD_POSITION;  // ascending from >= 0 on: never below i
+  // Ascending from >= 0 on: never below i.  The entry before is judged here too: it may
+  // be another CTA's, and what follows here takes it as an index.
+  if (k < i || before < i - 1 || before >= k) return PIC_DEV_BAD_POSITION;
   if ((long long)s + k >= (long long)p.max_pages * kPage) return PIC_DEV_BLOCK_TABLE_SHORT;
   const int a = t[(s + k) / kPage], z = t[(s + i) / kPage];
   if (a < 0 || a >= p.num_pages || z < 0 || z >= p.num_pages) return PIC_DEV_BAD_PAGE;
