@@ -661,6 +661,11 @@ pic_status_t pic_verify_draft(int32_t batch, int32_t max_draft, int32_t vocab,
  * call cannot serve is left as it is, reported through pic_device_status
  * (detail: its index in the list) and gets -1 in `result`.  At most 4096 rows a
  * call.
+ * Rows share pages from their starts on, through pic_page_fork, and a row is only
+ * given room in pages of its own.  One that is cut (by pic_page_compact, or by a
+ * caller who lowers its ctx_len) to end inside a page that others use can be read, and
+ * forked, which gives the branch its own copy of that page, but not appended to:
+ * pic_page_reserve refuses it.
  */
 
 /*
@@ -668,7 +673,8 @@ pic_status_t pic_verify_draft(int32_t batch, int32_t max_draft, int32_t vocab,
  * ctx_len: missing pages up to position ctx_len + extra - 1 are allocated.
  * result int32 [n]: the pages the row then needs.  One launch.
  * Device checks: rows, lengths (BAD_REQUEST), max_pages (BLOCK_TABLE_SHORT),
- * free pages (NO_FREE_PAGE).
+ * free pages (NO_FREE_PAGE), and that the page of position ctx_len, where the row has
+ * one and extra > 0, has no other user (SHARED_PAGE).
  */
 pic_status_t pic_page_reserve(int32_t n, const int32_t *row, int32_t extra, int32_t rows,
                               const int32_t *ctx_len, int32_t *block_table, int32_t max_pages,
@@ -715,7 +721,8 @@ pic_status_t pic_page_fork(const pic_geom_t *geom, int32_t n, const int32_t *src
  * done so.
  * Device checks: rows, lengths (BAD_REQUEST), keep lists (BAD_POSITION),
  * max_pages (BLOCK_TABLE_SHORT), page ids (BAD_PAGE), and every page a position
- * moves into has this row as its only user (SHARED_PAGE).
+ * moves into has this row as its only user, as has, with reserve > 0, the page of the
+ * position behind the new length (SHARED_PAGE).
  */
 size_t pic_page_compact_workspace_size(const pic_geom_t *geom, int32_t n, int32_t max_keep);
 

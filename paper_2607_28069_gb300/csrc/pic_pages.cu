@@ -79,6 +79,14 @@ PIC_DEV int block_scan(int v, int *warp_sums, int *total) {
 }
 static_assert(kPlanThreads == 32 * 32, "a lane per warp sum");
 
+// Whether a row may not be appended to in page `page` of its table (-1: none yet), because
+// other rows read it.  Rows share pages from their starts on (a fork shares the full pages
+// of its source's context, and nothing else shares any), so if the page of a row's next
+// position is its own, those behind are.
+PIC_DEV bool used_by_others(int page, const int32_t *page_refs, long long num_pages) {
+  return page >= 0 && page < num_pages && page_refs[page] > 1;
+}
+
 // One CTA: what each listed row needs, then the free pages in ascending order,
 // the k-th of them to the row whose range of the needs' prefix sum holds k.  One CTA,
 // because the k-th free page depends on all below it and the counts are few (a pool
@@ -146,6 +154,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
           at = lo;
           need = max(0, (int)want - lo);
           res = (int)want;
+          if (p.extra > 0 && used_by_others(tr[len / kPage], p.page_refs, p.num_pages))
+            code = PIC_DEV_SHARED_PAGE;
         }
       }
       if (code != PIC_DEV_OK) {
@@ -344,7 +354,7 @@ static_assert(kSeg == 16, "half a warp looks a segment's positions up");
 constexpr int kCheckThreads = 1024;  // kept positions of a checking CTA
 
 struct CompactParams {
-  int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, lgroup, lhs, layers, layer_begin, rotate, dim;
+  int n, rows, max_pages, max_keep, segs, hkv, hgroup, hgroups, lgroup, lhs, layers, layer_begin, rotate, dim, reserve;
   long long num_pages, layer_elems;
   const int32_t *row, *start, *keep, *keep_len;
   const int32_t *ctx_len, *block_table, *page_refs;
@@ -376,6 +386,14 @@ PIC_DEV int compact_start(const CompactParams &p, int j, int *code) {
     return -1;
   }
   return s;
+}
+
+// Room behind the kept positions, from s on, is asked for: the page of the next position.
+PIC_DEV int compact_end(const CompactParams &p, int j, int s) {
+  const int r = p.row[j], e = (s + p.keep_len[j]) / kPage;
+  if (p.reserve == 0 || e >= p.max_pages) return PIC_DEV_OK;
+  return used_by_others(p.block_table[(size_t)r * p.max_pages + e], p.page_refs, p.num_pages)
+             ? PIC_DEV_SHARED_PAGE : PIC_DEV_OK;
 }
 
 // Entry i of a keep list: its checks and its slots, as page * 16 + row of the page.
@@ -418,6 +436,9 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
     if (code == PIC_DEV_OK)
       p.slot[(size_t)j * p.max_keep + i0 + tid] = make_longlong2(elem(slot.x), elem(slot.y));
   }
+  // (a thread that mostly has no entry)
+  if (blockIdx.x == gridDim.x - 1 && tid == kCheckThreads - 1 && s >= 0 && code == PIC_DEV_OK)
+    code = compact_end(p, j, s);
   if (code != PIC_DEV_OK && (s >= 0 || (tid == 0 && i0 == 0))) dev_fail(p.status, code, j);
   const bool bad = __syncthreads_or(code != PIC_DEV_OK);
   if (tid == 0) p.bad[j * p.checks + blockIdx.x] = bad;
@@ -505,6 +526,7 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) compact_short_kernel(
     k_of[tid / kSeg][tid % kSeg] = k;
     slot_of[tid / kSeg][tid % kSeg] = slot;
   }
+  if (tid == kMoveThreads - 1 && s >= 0) code = compact_end(p, j, s);
   const bool bad = __syncthreads_or(code != PIC_DEV_OK);
   if (lh == 0) {  // one CTA of a row reports
     if (code != PIC_DEV_OK && (tid == 0 || s >= 0)) dev_fail(p.status, code, j);
@@ -946,6 +968,7 @@ extern "C" pic_status_t pic_page_compact(const pic_geom_t *geom, int32_t n, cons
   cp.rotate = rotate != 0;
   cp.num_pages = num_pages;
   cp.dim = geom->head_dim;
+  cp.reserve = reserve;
   cp.layer_elems = (long long)num_pages * cp.hkv * kPage * geom->head_dim;
   cp.row = row;
   cp.start = start;
