@@ -48,6 +48,7 @@ struct PlanParams {
 };
 
 constexpr int kPlanThreads = 1024;
+constexpr int kScanBytes = 2 * 32 * 4;  // static shared memory
 // A large pool's first pages are mostly all in use: kSkip loads of a thread pass over
 // 32768 of them by one barrier.  16 rows x 4 pages (us, without and with, the calls'
 // other work included): the first 130000 of 140000 pages in use 24 and 13, 950000 of
@@ -99,6 +100,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
   extern __shared__ int32_t sh[];
   int32_t *first = sh, *col0 = sh + p.n + 1, *len_of = col0 + p.n;  // len_of: fork
   __shared__ int warp_sums[2][32];
+  static_assert(sizeof(warp_sums) == kScanBytes, "the host counts with it");
   const int tid = threadIdx.x;
   int carry = 0, turn = 0;
   // the counts of four pages; the first ones go out before the needs are known
@@ -799,7 +801,7 @@ static pic_status_t launched(const char *who, cudaError_t e) {
 template <bool kFork, bool kLarge>
 static cudaError_t launch_plan(const PlanParams &pp, pic_stream_t stream) {
   const size_t smem = (size_t)(pp.n + 1 + pp.n * (kFork ? 2 : 1)) * 4;
-  if (smem > 48 * 1024) {
+  if (smem + kScanBytes > 48 * 1024) {  // (the default limit counts the static part too)
     const cudaError_t e = cudaFuncSetAttribute(plan_kernel<kFork, kLarge>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                (int)smem);
