@@ -420,13 +420,21 @@ class DraftDecoder:
                          workspace=self.ws_compact)
 
     def fork(self, src, dst):
-        """Rows dst (not in use) become branches of rows src: two lists of row numbers."""
+        """Rows dst (not in use) become branches of rows src: two lists of row numbers.
+
+        Returns the branches' lengths.  Where the device could not make one (no free
+        pages, a table too short: pic_device_status) its length is -1, and its row stays
+        empty and out of use.  Waits for the device: forks are made between steps, not in
+        a captured one."""
         if len(src) != len(dst) or set(dst) & set(self.in_use) or len(set(dst)) < len(dst):
             raise ValueError("fork: every branch needs a row of its own that is not in use")
+        result = torch.empty(len(dst), dtype=torch.int32, device=self.block_table.device)
         pic_page_fork(self.geom, self._rows(src), self._rows(dst), self.ctx_len, self.block_table,
                       self.num_pages, self.page_refs, self.path.k_cache, self.path.v_cache,
-                      self.result[:len(dst)], reserve=self.max_draft)
-        self._use(self.in_use + list(dst))
+                      result, reserve=self.max_draft)
+        lengths = result.tolist()
+        self._use(self.in_use + [row for row, n in zip(dst, lengths) if n >= 0])
+        return lengths
 
     def release(self, rows):
         """The listed rows end: their pages go back."""
