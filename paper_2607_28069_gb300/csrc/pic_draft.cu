@@ -984,6 +984,12 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
 // one load after the other had cost 11 of 27.5 us).  Bound by its chain of loads (the
 // request and the deal, then the partials): 2.7 us for 16 rows, 4.7 for 1024 rows of
 // about five partials, 6.4 for 3200 rows of d = 64.
+// acc + w v.  A weight that has underflowed to 0 does not hide an infinity or a NaN.
+constexpr float kFloatMax = 3.402823466e38f;
+PIC_DEV float weigh(float w, float v, float acc) {
+  return w != 0.f || fabsf(v) <= kFloatMax ? fmaf(w, v, acc) : acc + v;
+}
+
 template <int D, int kWarps, int U>
 __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
   constexpr int CPL = D / 32, kRows = 4 / kWarps;
@@ -1050,11 +1056,28 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const float wk = __shfl_sync(0xffffffffu, wc, (c0 + k) & 31);  // 0 past the end
-      if (wk != 0.f)  // 0: past the end, or no key of the part was visible
+      if (wk != 0.f)
 #pragma unroll
         for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wk, v[k][e], acc[e]);
     }
   }
+  // Infinities and NaN of parts whose weight underflowed to 0 (rare: in the loop
+  // above they cost 5 ragged requests, d = 64, 1.3 us of 20.1, apart 0.2).  Adding those of the other
+  // parts once more changes nothing.
+  bool under = false;
+#pragma unroll
+  for (int k = 0; k < KW; ++k) under |= lane + 32 * k < mine && w[k] == 0.f;
+  if (__any_sync(0xffffffffu, under))
+#pragma unroll 1
+    for (int c = 0; c < mine; ++c)
+#pragma unroll 1
+      for (int e = 0; e < CPL; ++e) {
+        const float x = p.part_o[part_row(c) * D + lane * CPL + e];
+        if (fabsf(x) <= kFloatMax) continue;
+#pragma unroll
+        for (int q = 0; q < CPL; ++q)
+          if (q == e) acc[q] += x;
+      }
   const size_t o_row = ((size_t)b * p.max_draft + i) * p.Hq + h;
   if constexpr (kWarps == 4) {
 #pragma unroll
@@ -1072,7 +1095,7 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
       const float wc = mw[c] == -INFINITY ? 0.f : ex2(mw[c] - M);
       l = fmaf(wc, l_s[c], l);
 #pragma unroll
-      for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wc, acc_s[c][lane * CPL + e], acc[e]);
+      for (int e = 0; e < CPL; ++e) acc[e] = weigh(wc, acc_s[c][lane * CPL + e], acc[e]);
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
