@@ -270,7 +270,7 @@ pic_status_t pic::compose_layout(const pic_geom_t *geom, int32_t batch, int32_t 
   a.status = status;
   dim3 grid((max_ctx + kSlotsPerCta - 1) / kSlotsPerCta, batch);
   const size_t smem = (size_t)max_docs * (sizeof(long long) + 3 * sizeof(int32_t)) + 16;
-  if (smem > 48 * 1024) {
+  if (smem > 47 * 1024) {  // (the default limit of 48 KB counts the static part too)
     cudaError_t e = cudaFuncSetAttribute(compose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          (int)smem);
     if (e != cudaSuccess) return cuda_fail(e, "pic_compose smem attribute");
