@@ -747,8 +747,8 @@ pic_status_t pic_page_free(int32_t n, const int32_t *row, int32_t rows, int32_t 
 /*
  * pic_page_copy -- the K and V of whole pages, layers [layer_begin,
  * layer_end): page src_page[i] of the source cache (src_pages pages a layer) to
- * page dst_page[i] of the destination cache (dst_pages pages a layer), which
- * may be the same cache: no page may then be both a source and a destination.
+ * page dst_page[i] of the destination cache (dst_pages pages a layer; both in the
+ * memory of this GPU), which may be the same cache: no page may then be both a source and a destination.
  * Entries where both are -1 are skipped.  Any n >= 0.  One launch.  Device
  * check: page ids (BAD_PAGE).
  */

@@ -471,7 +471,8 @@ def pic_verify_draft(tokens, draft_len, target_prob, uniform, path, path_len, ne
 
 def pic_page_reserve(row, extra: int, ctx_len, block_table, num_pages: int, page_refs, result,
                      stream=None):
-    """Pages for `extra` positions behind each listed row's ctx_len."""
+    """Pages for `extra` positions behind each listed row's ctx_len; none for a row whose
+    next position falls into a page that other rows use."""
     st = (_nat or _native()).page_reserve(row, extra, ctx_len, block_table, num_pages, page_refs,
                                           result, stream)
     if st:

@@ -5,7 +5,7 @@
 // tokens and query heads: a request's queries of one kv head are packed into
 // rows r = token * G + head of 128-row tiles (one TMEM lane per row), so with up
 // to 128 rows a key costs 4 d flops a row for the 4 d bytes that it and its
-// value take: HBM-bound below about 280 rows.  What a chain's causal mask or a
+// value take: below about 280 rows a key tile's bytes take longer than its MMAs.  What a chain's causal mask or a
 // tree's ancestor mask hides lies within the last 64 slots; every earlier key
 // is visible to every row.
 //
@@ -22,9 +22,9 @@
 //
 // Measured, whole calls: 4 requests of 139k keys, 32 rows of each of 8 kv heads, 330
 // us (2.29 GB: 6.92 TB/s; a plain copy runs at 6.79); 16 of 33k, 112 rows of 4 kv
-// heads, 169 us (6.4 TB/s); 4 of 16k, 256 rows of 8 kv heads, 69 us, 39 of them the
-// keys' and values' time at the copy rate, the rest the launches around it and 23 MB of
-// partial states; one of 4288 keys 14.6 us, three dependent launches.
+// heads, 169 us (6.4 TB/s); 4 of 16k, 256 rows of 8 kv heads, 67.6 us (4.0 TB/s; the
+// attention 58.6 of them); d = 64, 16 of 139k, 64 rows of 2 kv heads, 204 us (5.6 TB/s),
+// 8 of 100k 85 us (4.8); one of 4288 keys 14.5 us, three dependent launches.
 #include <algorithm>
 
 #include "pic_internal.cuh"
@@ -282,7 +282,7 @@ struct Wild {
 // One CTA per token, behind `dealers` CTAs that deal out the work.  A thread takes
 // a chunk (8 pairs) of a query or key head, and a value piece: the host gives the
 // CTAs as many threads as there are chunks, up to kAppendMax.  Bound by its chain of
-// loads (lengths and parents, the page, cos/sin): 3.8 to 5 us for 4 to 256 tokens.  One
+// loads (lengths and parents, the page, cos/sin): 3.6 to 5.5 us for 4 to 256 tokens.  One
 // place in the code rotates, because a call starts with cold instruction caches (three chunks a
 // thread, their rotations unrolled, took 5.3 us instead of 4.9, 16 x 16 tokens).
 constexpr int kAppendMax = 512;
@@ -478,8 +478,11 @@ struct Segments {
 // (most of that the output's own rounding; 0.0034 to 0.0038 and 0.0033 to 0.0036 with
 // queries scaled by 2).
 //
-// Bound by HBM up to 256 rows of a kv head: 322 us for 4 x 139k keys (7.1 TB/s), 162 us cold
-// for 16 x 33k (6.65 TB/s, DRAM 84% busy, tensor pipe 37%).  With 512 rows a key tile of
+// Bound by HBM with one row tile of d = 128: 325 us for 4 x 139k keys (7.0 TB/s), 163 us cold
+// for 16 x 33k (6.6 TB/s, DRAM 84% busy, tensor pipe 37%).  With two row tiles (4 x 16k keys, 256
+// rows: 58.6 us, DRAM 58% busy, tensor pipe 60%) and with d = 64, whose key tile is half the
+// bytes (16 x 139k: 200 us, DRAM 72%; 8 x 100k: 81 us, 65%; tensor pipe 30%, issue slots 40%),
+// neither is at its limit: the chain of a key tile's MMAs and softmax.  With 512 rows a key tile of
 // two row tiles takes about 2750 cycles where its MMAs need 2080; for short contexts
 // set-up, first tiles and the epilogue count (7.2 us with two key tiles in all).
 // Against the short loops below: all scores of a row in registers were 6% slower; half
@@ -982,8 +985,8 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
 // shared memory in a fixed order.  One warp per row where there are many rows, four
 // where a unit may be split over many CTAs (see `launch`; 76 partials of two units by
 // one load after the other had cost 11 of 27.5 us).  Bound by its chain of loads (the
-// request and the deal, then the partials): 2.7 us for 16 rows, 4.7 for 1024 rows of
-// about five partials, 6.4 for 3200 rows of d = 64.
+// request and the deal, then the partials): 2.7 us for 16 rows, 4.5 for 1024 rows of
+// about five partials, 5.5 for 3200 rows of d = 64, 7.6 for 8192 rows.
 // acc + w v.  A weight that has underflowed to 0 does not hide an infinity or a NaN.
 constexpr float kFloatMax = 3.402823466e38f;
 PIC_DEV float weigh(float w, float v, float acc) {
@@ -1061,9 +1064,9 @@ __global__ void __launch_bounds__(128) draft_merge_kernel(Params p) {
         for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wk, v[k][e], acc[e]);
     }
   }
-  // Infinities and NaN of parts whose weight underflowed to 0 (rare: in the loop
-  // above they cost 5 ragged requests, d = 64, 1.3 us of 20.1, apart 0.2).  Adding those of the other
-  // parts once more changes nothing.
+  // Infinities and NaN of parts whose weight underflowed to 0 (rare: in the loop above
+  // they cost 5 ragged requests, d = 64, 1.3 us of 20.1, apart 0.2).  Adding those of the
+  // other parts once more changes nothing.
   bool under = false;
 #pragma unroll
   for (int k = 0; k < KW; ++k) under |= lane + 32 * k < mine && w[k] == 0.f;

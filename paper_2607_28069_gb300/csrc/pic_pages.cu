@@ -91,8 +91,8 @@ PIC_DEV bool used_by_others(int page, const int32_t *page_refs, long long num_pa
 // One CTA: what each listed row needs, then the free pages in ascending order,
 // the k-th of them to the row whose range of the needs' prefix sum holds k.  One CTA,
 // because the k-th free page depends on all below it and the counts are few (a pool
-// of 280 GB has some 10^5 pages).  Bound by dependent loads and barriers: 4.3 us for
-// 8 rows, 5.4 to 6 for 64 branches.
+// of 280 GB has some 10^5 pages).  Bound by dependent loads and barriers: 4.6 to 5 us
+// for 8 rows (0.4 of it the use count of each row's next page), 5.2 to 5.7 for 64 branches.
 // kLarge: pools of kSkipped pages or more.
 template <bool kFork, bool kLarge>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PlanParams p) {
@@ -476,10 +476,10 @@ __global__ void __launch_bounds__(kCheckThreads) compact_check_kernel(CompactPar
 // kept) are worked off by a CTA per (row, layer, head group), which needs no flags -- a
 // segment's targets lie below the next one's sources -- and checks the list itself,
 // so the call is a launch shorter.
-// Measured: 9001 of 15001 positions, 8 heads, 4 layers, 57 us (295 MB read and
-// written: 5.2 TB/s; 53 without the rotation): a row of a head is 256 bytes, reads and
+// Measured: 9001 of 15001 positions, 8 heads, 4 layers, 58 us (295 MB read and
+// written: 5.1 TB/s; 53 without the rotation): a row of a head is 256 bytes, reads and
 // writes of that size alternate, and issue slots are over half busy with addresses and
-// rotations.  The short form: 8 rows that keep 5 of 16, 32 layers, 5.5 us, latency.
+// rotations.  The short form: 8 rows that keep 5 of 16, 32 layers, 5 us, latency.
 
 // The units of a segment of group lh (heads, with kLayers of several layers): unit u =
 // (position, K or V, row of the group, chunk), thread tid's are tid, tid + kMoveThreads, ...

@@ -20,8 +20,10 @@
 // Small trees: every token's draw at once, a cluster each, whether the walk gets there
 // or not (the random number of a token depends on its depth alone), then the walk.
 //
-// Measured: 64 chains of 8 over 2^17 entries, one row or two of each read, 12.1 us
-// (67 MB at least: 5.5 TB/s), bound by HBM and the single wave of 512 CTAs.  A tree level by
+// Measured: 64 chains of 8 over 2^17 entries, 35 of them refused (two rows read, else one: 52
+// MB), 14.8 us on changing inputs, the kernel 10.8 on repeated ones.  Not HBM's rate (DRAM 37%
+// busy with cold caches): one wave of equal clusters, in which those of a refused request read
+// twice the others' bytes, behind two dependent round trips (tokens, their p and q).  A tree level by
 // level: 3.9 us for the first and 2.5 for each further one, a chain of the row's loads,
 // two cluster barriers and the search; at once, 16 tokens over 50001 entries, 5.6 us.
 #include <algorithm>
@@ -42,7 +44,9 @@ constexpr int kWideBatch = 12;
 // Trees whose tokens are all drawn at once (us of the call, level by level and at once;
 // random trees, two levels on average): 1 request x 16 tokens x 50001 entries 5.8 and
 // 5.4, 4 x 16 10.4 and 6.8, 8 x 16 12.8 and 11.1, 16 x 16 (256 draws) 11.6 and 17.0; x
-// 131072 entries 4 x 8 8.4 and 6.8, 8 x 8 (2^23 in all) 10.9 and 9.7, 4 x 16 9.7 and 10.5.
+// 131072 entries 4 x 8 8.4 and 6.8, 8 x 8 10.9 and 9.7, 4 x 16 9.7 and 10.5: with the
+// last two, of 2^23 entries each, neither form is the faster one throughout, and from there on
+// trees go level by level, which reads less.
 constexpr int kNodes = 152;
 constexpr long long kNodeEntries = 1 << 23;
 
