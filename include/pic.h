@@ -757,6 +757,111 @@ pic_status_t pic_page_copy(const pic_geom_t *geom, int32_t n, const int32_t *src
                            int64_t src_pages, void *k_dst, void *v_dst, int64_t dst_pages,
                            int32_t layer_begin, int32_t layer_end, pic_stream_t stream);
 
+/* ===========================================================================
+ * Decoding branches of linked contexts together.  A linked context that was
+ * forked (pic_page_fork) is read by all its branches in the same pages; one step
+ * plans the batch once (pic_share_plan), then per layer appends (pic_append_normed)
+ * and attends (pic_attend_shared), every shared key read once.
+ * ======================================================================== */
+
+/*
+ * pic_append_normed -- the append of a Reader that norms its query and key
+ * heads: for request b < batch and token t < num_tokens[b] (NULL: max_tokens),
+ * at position p = pos[b][t] (pos NULL: ctx_len[r] + t) of block-table row
+ * r = row[b] (row NULL: b), and every head x of q and k_new,
+ *     N(x) = x / sqrt(mean(x^2) + eps) * weight     (weight NULL: N(x) = x)
+ *     k_cache[layer][slot(p)] = R(p) N(k_new[b][t]),  v_cache... = v_new[b][t]
+ *     queries: R(p) N(q[b][t])
+ * in fp32, rounded to bf16 once (with a weight, magnitudes beyond 2^60 overflow).
+ * The queries go to q_out, bf16 [batch][max_tokens][Hq][d] (rows
+ * t >= num_tokens[b] not written), or, with q_out NULL, GQA-packed into the
+ * prefill workspace as pic_append_inline leaves them (those rows zeros), which
+ * pic_attend_prefill then reads with NULL projections.
+ *
+ * q, k_new, v_new: bf16, element (b, t, h, i) at base + b * stride[0] +
+ * t * stride[1] + h * stride[2] + i (strides in elements, HOST arrays, not
+ * negative, multiples of 8), for instance slices of one fused projection.
+ * q_weight, k_weight: bf16 [d] or NULL.  num_tokens, row: int32 [batch]; pos:
+ * int32 [batch][max_tokens]; ctx_len: int32 [rows] (may be NULL with pos);
+ * block_table: int32 [rows][max_pages].  Tokens of one call have slots of their
+ * own.  One launch, no workspace of its own.
+ * Device checks: rows, a row named twice, token counts (BAD_REQUEST; the request
+ * is treated as empty), positions (BAD_POSITION, BLOCK_TABLE_SHORT), page ids
+ * (BAD_PAGE): the key and value of such a token are not written, its query is
+ * (at a bad position unrotated).
+ */
+pic_status_t pic_append_normed(const pic_geom_t *geom, int32_t layer, int32_t batch,
+                               int32_t max_tokens, const void *q, const int64_t *q_stride,
+                               const void *k_new, const int64_t *k_stride, const void *v_new,
+                               const int64_t *v_stride, const void *q_weight,
+                               const void *k_weight, float eps, const int32_t *num_tokens,
+                               const int32_t *pos, const int32_t *row, const int32_t *ctx_len,
+                               int32_t rows, const int32_t *block_table, int32_t max_pages,
+                               int64_t num_pages, void *k_cache, void *v_cache, void *q_out,
+                               void *workspace, size_t workspace_bytes, pic_stream_t stream);
+
+/*
+ * pic_share_plan -- which of the listed rows read the same pages.
+ *
+ * Entry i < n <= 4096 is block-table row row[i] (row NULL: i; a row may be listed
+ * several times) and sees keys_i = ctx_len[row] + pos_offset + 1 positions
+ * (pos_offset 0: the one at ctx_len, about to be appended, is the last).  Entries
+ * i and i + 1 share common_i tiles of 128 positions: the leading tiles in which
+ * their rows name the same valid pages, at most min(keys) / 128.  List the
+ * branches of a context side by side, deeper common parts closer.
+ *
+ * The plan begins with its nodes, int32 [2 n][8]: {begin, end, tile_begin,
+ * tile_end, row, keys, parent, level}.  Node j < n: entry j's own tiles (begin =
+ * j, end = j + 1, its row and keys).  Node n + i, where common_i > 0 and no
+ * boundary before i in its run has the same count: the entries [begin, end) that
+ * all share common_i tiles, the tiles below them not of its parent, row the first
+ * entry's, keys = 128 tile_end.  A run of entries whose boundaries all have
+ * counts of common_i or more is [begin, end); the parent is the run around the
+ * larger neighbouring boundary (the left one if they are equal).  parent: a
+ * node, or -1; level: how many nodes are above.  At most four shared levels:
+ * deeper nodes are left out, and their entries read those tiles on their own.  Nodes
+ * that do not exist are {0, 0, 0, 0, -1, 0, -1, -1}.  What follows the nodes is
+ * private to the library; the plan belongs to the geometry's heads, the block
+ * table's shape and n, and holds for every layer while lengths and pages stay.
+ *
+ * ctx_len: int32 [rows]; block_table: int32 [rows][max_pages]; plan:
+ * pic_share_plan_size(n) bytes, 16-byte aligned (0 for n outside 1 .. 4096).
+ * Two launches, no workspace.  Device checks: rows, lengths (BAD_REQUEST),
+ * keys beyond the table (BLOCK_TABLE_SHORT): such an entry has keys -1 and no
+ * tiles, and the attention leaves its output alone.
+ */
+size_t pic_share_plan_size(int32_t n);
+
+pic_status_t pic_share_plan(const pic_geom_t *geom, int32_t n, const int32_t *row, int32_t rows,
+                            const int32_t *ctx_len, int32_t pos_offset,
+                            const int32_t *block_table, int32_t max_pages, int64_t num_pages,
+                            int32_t *plan, size_t plan_bytes, pic_stream_t stream);
+
+/*
+ * pic_attend_shared -- attention of one token per entry of a plan over the
+ * paged cache:
+ *     out[i][h] = sum over s < keys_i of softmax_s(q[i][h] . k_s / sqrt(d)) v_s
+ * (q rotated already, the token's own key appended).  lse[i][h] (nullable): the
+ * natural-log sum-exp of those scores.  keys_i = 0: zeros, lse -infinity.  A
+ * node's keys and values are read once for all its entries.  Slots behind
+ * keys_i may hold anything.
+ *
+ * q, out: bf16 [n][Hq][d]; lse: float [n][Hq] or NULL; block_table, max_pages:
+ * as the plan was made with; Hq / Hkv <= 128.  workspace: >=
+ * pic_shared_workspace_size(...) bytes, 256-byte aligned; its contents do not
+ * matter before or after.  Runs on the tensor cores (tcgen05.mma, TMEM, TMA); the
+ * work is dealt to the SMs by the plan.  Launches: attention, merge.
+ * Device checks: a plan of other sizes (BAD_REQUEST, nothing is written), page
+ * ids (BAD_PAGE; such a page's keys and values read as zeros).
+ */
+size_t pic_shared_workspace_size(const pic_geom_t *geom, int32_t n);
+
+pic_status_t pic_attend_shared(const pic_geom_t *geom, int32_t layer, int32_t n, const void *q,
+                               int32_t rows, const int32_t *block_table, int32_t max_pages,
+                               int64_t num_pages, const void *k_cache, const void *v_cache,
+                               const int32_t *plan, size_t plan_bytes, void *out, float *lse,
+                               void *workspace, size_t workspace_bytes, pic_stream_t stream);
+
 #ifdef __cplusplus
 } /* extern "C" */
 #endif

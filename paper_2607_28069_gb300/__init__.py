@@ -27,7 +27,8 @@ __all__ = [
     "pic_attend_decode", "pic_decode_workspace_size", "pic_device_status", "PicError",
     "pic_draft_workspace_size", "pic_attend_draft", "pic_verify_draft", "pic_page_reserve",
     "pic_page_fork", "pic_page_compact_workspace_size", "pic_page_compact", "pic_page_free",
-    "pic_page_copy",
+    "pic_page_copy", "pic_append_normed", "pic_share_plan_size", "pic_share_plan", "share_nodes",
+    "pic_shared_workspace_size", "pic_attend_shared",
     "EXPORTED_SYMBOLS", "ROPE_HALF", "ROPE_INTERLEAVED",
 ]
 
@@ -50,7 +51,8 @@ EXPORTED_SYMBOLS = (
     "pic_attend_decode", "pic_attend_decode_noalloc", "pic_copy_async", "pic_launch_probe",
     "pic_wait_probe", "pic_draft_workspace_size", "pic_attend_draft", "pic_verify_draft",
     "pic_page_reserve", "pic_page_fork", "pic_page_compact_workspace_size", "pic_page_compact",
-    "pic_page_free", "pic_page_copy",
+    "pic_page_free", "pic_page_copy", "pic_append_normed", "pic_share_plan_size", "pic_share_plan",
+    "pic_shared_workspace_size", "pic_attend_shared",
 )
 
 DEVICE_CODES = {
@@ -118,6 +120,7 @@ def load():
             raise RuntimeError(f"{path} is missing: run __graft_entry__.build() first")
     lib = ctypes.CDLL(_LIB_PATH)
     P, I32, I64, SZ, D = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_double
+    F = ctypes.c_float
     G = ctypes.POINTER(_Geom)
     sig = {
         "pic_abi_version": (I32, []),
@@ -164,6 +167,12 @@ def load():
                                    I32, I32, P, P, SZ, P]),
         "pic_page_free": (I32, [I32, P, I32, P, P, I32, I64, P, P]),
         "pic_page_copy": (I32, [G, I32, P, P, P, P, I64, P, P, I64, I32, I32, P]),
+        "pic_append_normed": (I32, [G, I32, I32, I32, P, P, P, P, P, P, P, P, F, P, P, P, P, I32, P,
+                                    I32, I64, P, P, P, P, SZ, P]),
+        "pic_share_plan_size": (SZ, [I32]),
+        "pic_share_plan": (I32, [G, I32, P, I32, P, I32, P, I32, I64, P, SZ, P]),
+        "pic_shared_workspace_size": (SZ, [G, I32]),
+        "pic_attend_shared": (I32, [G, I32, I32, P, I32, P, I32, I64, P, P, P, SZ, P, P, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -524,3 +533,56 @@ def pic_page_copy(geom: Geometry, src_page, dst_page, k_src, v_src, k_dst, v_dst
         geom.num_layers if layer_end is None else layer_end, stream)
     if st:
         _check(st, "pic_page_copy")
+
+
+# -- decoding branches of a linked context together (see include/pic.h)
+def pic_append_normed(geom: Geometry, layer: int, q, k_new, v_new, block_table, num_pages: int,
+                      k_cache, v_cache, q_out=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                      num_tokens=None, pos=None, row=None, ctx_len=None, workspace=None, stream=None):
+    """Norm of every query and key head (weights bf16 [d]; None: no norm), rotation and append:
+    q [B][T][Hq][d], k_new and v_new [B][T][Hkv][d], of any strides but the last dimension's.
+    Positions pos [B][T], or ctx_len[row[b]] + t; row [B] (None: b) names block-table rows;
+    num_tokens [B] (None: T each).  The rotated queries go to q_out [B][T][Hq][d], or packed into
+    the prefill workspace, as pic_append_inline leaves them."""
+    st = (_nat or _native()).append_normed(
+        geom, layer, q, k_new, v_new, q_weight, k_weight, eps, num_tokens, pos, row, ctx_len,
+        block_table, num_pages, k_cache, v_cache, q_out, workspace, stream)
+    if st:
+        _check(st, "pic_append_normed")
+
+
+def pic_share_plan_size(n: int) -> int:
+    """Bytes of a plan of n entries (a quarter as many int32 elements); 0 beyond 4096."""
+    return load().pic_share_plan_size(n)
+
+
+def pic_share_plan(geom: Geometry, ctx_len, block_table, num_pages: int, plan, row=None,
+                   pos_offset: int = 0, stream=None):
+    """Which of the entries row [n] (None: all rows) read the same pages, for pic_attend_shared:
+    entry i sees positions 0 .. ctx_len[row[i]] + pos_offset.  plan: int32, of
+    pic_share_plan_size(n) bytes."""
+    st = (_nat or _native()).share_plan(geom, row, ctx_len, pos_offset, block_table, num_pages, plan,
+                                        stream)
+    if st:
+        _check(st, "pic_share_plan")
+
+
+def share_nodes(plan, n: int):
+    """The nodes of a plan of n entries, a view [2 n][8] of it: begin and end of the entries, begin
+    and end of their 128-position tiles, block-table row, keys, parent, level (see include/pic.h)."""
+    return plan[:16 * n].view(2 * n, 8)
+
+
+def pic_shared_workspace_size(geom: Geometry, n: int) -> int:
+    g = geom._c()
+    return load().pic_shared_workspace_size(ctypes.byref(g), n)
+
+
+def pic_attend_shared(geom: Geometry, layer: int, q, block_table, num_pages: int, k_cache, v_cache,
+                      plan, out, lse=None, workspace=None, stream=None):
+    """Attention of one token per entry of a plan, a shared key read once: q and out [n][Hq][d] (q
+    rotated; [n][1][Hq][d] alike), lse float32 [n][Hq] or None."""
+    st = (_nat or _native()).attend_shared(geom, layer, q, block_table, num_pages, k_cache, v_cache,
+                                           plan, out, lse, workspace, stream)
+    if st:
+        _check(st, "pic_attend_shared")

@@ -825,6 +825,121 @@ PyObject *page_copy(PyObject *, PyObject *const *v, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------- decoding branches of a context
+// Heads [batch][tokens][heads][d] in any strides but the last dimension's: data and strides.
+const void *heads_of(const View &w, const char *name, int64_t heads, int64_t d, int64_t *strides) {
+  if (!w) raise(PyExc_ValueError, "%s is required%s", name);
+  if (!w.t->is_cuda()) raise(PyExc_ValueError, "%s must be a CUDA tensor%s", name);
+  if (w.t->scalar_type() != at::kBFloat16) raise(PyExc_ValueError, "%s must be torch.bfloat16%s", name);
+  if (w.dim() != 4 || w.size(2) != heads || w.size(3) != d)
+    raise(PyExc_ValueError, "%s must be [batch][tokens][heads][head_dim]%s", name);
+  if (w.t->stride(w.skip + 3) != 1)
+    raise(PyExc_ValueError, "%s must be contiguous in its last dimension%s", name);
+  for (int i = 0; i < 3; ++i) strides[i] = w.size(i) > 1 ? w.t->stride(w.skip + i) : 0;
+  return w.data();
+}
+
+PyObject *append_normed(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    Geom g(a.next());
+    const int32_t layer = a.i32();
+    int64_t qs[3], ks[3], vs[3];
+    const int64_t d = g.g.head_dim, Hq = g.g.num_q_heads, Hkv = g.g.num_kv_heads;
+    const View qv = view_of(a.next(), "q");
+    const void *q = heads_of(qv, "q", Hq, d, qs);
+    const int64_t B = qv.size(0), T = qv.size(1);
+    const void *kv[2];
+    for (int i = 0; i < 2; ++i) {
+      const char *name = i ? "v_new" : "k_new";
+      const View w = view_of(a.next(), name);
+      kv[i] = heads_of(w, name, Hkv, d, i ? vs : ks);
+      if (w.size(0) != B || w.size(1) != T)
+        raise(PyExc_ValueError, "%s must have the requests and tokens of q%s", name);
+    }
+    const void *wq = sized<void>(a, at::kBFloat16, "q_weight", d, true);
+    const void *wk = sized<void>(a, at::kBFloat16, "k_weight", d, true);
+    const double eps = PyFloat_AsDouble(a.next());
+    if (PyErr_Occurred()) throw PyErrorSet();
+    const int32_t *count = sized<int32_t>(a, at::kInt, "num_tokens", B, true);
+    const int32_t *pos = sized<int32_t>(a, at::kInt, "pos", B * T, true);
+    const int32_t *row = sized<int32_t>(a, at::kInt, "row", B, true);
+    const View cv = view_of(a.next(), "ctx_len");
+    const int32_t *ctx = static_cast<int32_t *>(checked(cv, at::kInt, "ctx_len", true));
+    const View bt = view_of(a.next(), "block_table");
+    const int32_t *table = static_cast<int32_t *>(checked(bt, at::kInt, "block_table"));
+    need_2d(bt, "block_table");
+    if (cv && cv.numel() != bt.size(0)) raise(PyExc_ValueError, "%s must have an entry per row%s", "ctx_len");
+    int64_t num_pages = a.integer();
+    void *kc = cache_of(a, g, "k_cache", &num_pages), *vc = cache_of(a, g, "v_cache", &num_pages);
+    void *out = sized<void>(a, at::kBFloat16, "q_out", B * T * Hq * d, true);
+    const View wv = view_of(a.next(), "workspace");
+    void *ws = checked(wv, at::kByte, "workspace", true);
+    const size_t bytes = wv ? (size_t)wv.numel() : 0;
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_append_normed(&g.g, layer, (int32_t)B, (int32_t)T, q, qs, kv[0], ks, kv[1], vs, wq, wk,
+                               (float)eps, count, pos, row, ctx, (int32_t)bt.size(0), table,
+                               (int32_t)bt.size(1), num_pages, kc, vc, out, ws, bytes, s);
+    });
+  });
+}
+
+PyObject *share_plan(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    Geom g(a.next());
+    const View rv = view_of(a.next(), "row");
+    const int32_t *row = static_cast<int32_t *>(checked(rv, at::kInt, "row", true));
+    const View cv = view_of(a.next(), "ctx_len");
+    const int32_t *ctx = static_cast<int32_t *>(checked(cv, at::kInt, "ctx_len"));
+    const int32_t pos_offset = a.i32();
+    const View bt = view_of(a.next(), "block_table");
+    const int32_t *table = static_cast<int32_t *>(checked(bt, at::kInt, "block_table"));
+    need_2d(bt, "block_table");
+    if (cv.numel() != bt.size(0)) raise(PyExc_ValueError, "%s must have an entry per row%s", "ctx_len");
+    const int64_t num_pages = a.integer();
+    const View pv = view_of(a.next(), "plan");
+    int32_t *plan = static_cast<int32_t *>(checked(pv, at::kInt, "plan"));
+    const int64_t entries = rv ? rv.numel() : bt.size(0);
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_share_plan(&g.g, (int32_t)std::min<int64_t>(entries, INT32_MAX), row,
+                            (int32_t)bt.size(0), ctx, pos_offset, table, (int32_t)bt.size(1), num_pages,
+                            plan, (size_t)pv.numel() * 4, s);
+    });
+  });
+}
+
+PyObject *attend_shared(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    Geom g(a.next());
+    const int32_t layer = a.i32();
+    const View qv = view_of(a.next(), "q");
+    const void *q = checked(qv, at::kBFloat16, "q");
+    const int64_t k = qv.dim();  // [n][Hq][d], or a token each: [n][1][Hq][d]
+    if ((k != 3 && (k != 4 || qv.size(1) != 1)) || qv.size(k - 2) != g.g.num_q_heads ||
+        qv.size(k - 1) != g.g.head_dim)
+      raise(PyExc_ValueError, "%s must be [entries][num_q_heads][head_dim]%s", "q");
+    const int64_t entries = qv.size(0);
+    const View bt = view_of(a.next(), "block_table");
+    const int32_t *table = static_cast<int32_t *>(checked(bt, at::kInt, "block_table"));
+    need_2d(bt, "block_table");
+    int64_t num_pages = a.integer();
+    const void *kc = cache_of(a, g, "k_cache", &num_pages), *vc = cache_of(a, g, "v_cache", &num_pages);
+    const View pv = view_of(a.next(), "plan");
+    const int32_t *plan = static_cast<int32_t *>(checked(pv, at::kInt, "plan"));
+    void *out = sized<void>(a, at::kBFloat16, "out", qv.numel());
+    float *lse = sized<float>(a, at::kFloat, "lse", entries * g.g.num_q_heads, true);
+    const View wv = view_of(a.next(), "workspace");
+    void *ws = checked(wv, at::kByte, "workspace");
+    const pic_stream_t s = stream_of(a.next());
+    return unlocked([&] {
+      return pic_attend_shared(&g.g, layer, (int32_t)std::min<int64_t>(entries, INT32_MAX), q,
+                               (int32_t)bt.size(0), table, (int32_t)bt.size(1), num_pages, kc, vc, plan,
+                               (size_t)pv.numel() * 4, out, lse, ws, (size_t)wv.numel(), s);
+    });
+  });
+}
+
 #define FAST(name, fn) {name, (PyCFunction)(void (*)(void))(fn), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     FAST("compose", compose),
@@ -846,6 +961,9 @@ PyMethodDef methods[] = {
     FAST("page_compact", page_compact),
     FAST("page_free", page_free),
     FAST("page_copy", page_copy),
+    FAST("append_normed", append_normed),
+    FAST("share_plan", share_plan),
+    FAST("attend_shared", attend_shared),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pic_native", nullptr, -1, methods,
