@@ -862,6 +862,39 @@ pic_status_t pic_attend_shared(const pic_geom_t *geom, int32_t layer, int32_t n,
                                const int32_t *plan, size_t plan_bytes, void *out, float *lse,
                                void *workspace, size_t workspace_bytes, pic_stream_t stream);
 
+/*
+ * pic_sample -- the next token of every row of logits, from given random
+ * numbers.
+ *
+ * Row b: vocab logits x (fp32, or bf16 with bf16 != 0) at logits + b * stride
+ * elements.  Of temperature T, top-k k, top-p P and min-p m, one each per row
+ * (NULL: 1, 0, 1, 0), and the largest logit M (a NaN counts as -infinity):
+ *  - weights: s = min(log2(e) / T, 1e30), z = (x - M) s (0 where x = M),
+ *    j = rint(z), f = z - j, e = 1 + f (c1 + f (c2 + f (c3 + f (c4 + f c5)))),
+ *    from the inside out, each operation rounded to fp32, c = {0.6931470036506653,
+ *    0.24022242426872253, 0.05550733581185341, 0.009671512991189957,
+ *    0.001326472731307149}; w = trunc(2^36 e 2^j), 0 where z < -37 or NaN.
+ *  - the order: entries with w > 0, logit descending, then index ascending.
+ *  - k > 0: only the first k stay.
+ *  - P < 1: of those the fewest first ones whose sum of w reaches
+ *    floor(S floor(2^24 max(P, 0)) / 2^24), S the sum of all that stayed; at
+ *    least one.
+ *  - of those with w >= trunc(2^36 m), m taken into [0, 1], the kept ones.
+ *  - T <= 0 or NaN: the first entry with x = M alone.
+ *  - the token: with S the kept ones' sum, the first by index whose running sum
+ *    of kept weights exceeds floor(S floor(2^24 u) / 2^24), u = uniform[b] taken
+ *    into [0, 1 - 2^-24].
+ * Whole numbers have no order of summation, so the result is the same on every
+ * run.  token int32 [batch]; kept (nullable) int32 [batch]: how many entries were
+ * kept; logprob (nullable) float [batch]: ln(w / S) of the token.  A row without a
+ * logit above -infinity: token -1, kept 0, logprob NaN.
+ * vocab <= 2^24.  One launch, no workspace, no device checks.
+ */
+pic_status_t pic_sample(int32_t batch, int32_t vocab, const void *logits, int32_t bf16,
+                        int64_t stride, const float *temperature, const int32_t *top_k,
+                        const float *top_p, const float *min_p, const float *uniform,
+                        int32_t *token, float *logprob, int32_t *kept, pic_stream_t stream);
+
 #ifdef __cplusplus
 } /* extern "C" */
 #endif

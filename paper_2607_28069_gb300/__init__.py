@@ -28,7 +28,7 @@ __all__ = [
     "pic_draft_workspace_size", "pic_attend_draft", "pic_verify_draft", "pic_page_reserve",
     "pic_page_fork", "pic_page_compact_workspace_size", "pic_page_compact", "pic_page_free",
     "pic_page_copy", "pic_append_normed", "pic_share_plan_size", "pic_share_plan", "share_nodes",
-    "pic_shared_workspace_size", "pic_attend_shared",
+    "pic_shared_workspace_size", "pic_attend_shared", "pic_sample",
     "EXPORTED_SYMBOLS", "ROPE_HALF", "ROPE_INTERLEAVED",
 ]
 
@@ -52,7 +52,7 @@ EXPORTED_SYMBOLS = (
     "pic_wait_probe", "pic_draft_workspace_size", "pic_attend_draft", "pic_verify_draft",
     "pic_page_reserve", "pic_page_fork", "pic_page_compact_workspace_size", "pic_page_compact",
     "pic_page_free", "pic_page_copy", "pic_append_normed", "pic_share_plan_size", "pic_share_plan",
-    "pic_shared_workspace_size", "pic_attend_shared",
+    "pic_shared_workspace_size", "pic_attend_shared", "pic_sample",
 )
 
 DEVICE_CODES = {
@@ -172,6 +172,7 @@ def load():
         "pic_share_plan_size": (SZ, [I32]),
         "pic_share_plan": (I32, [G, I32, P, I32, P, I32, P, I32, I64, P, SZ, P]),
         "pic_shared_workspace_size": (SZ, [G, I32]),
+        "pic_sample": (I32, [I32, I32, P, I32, I64, P, P, P, P, P, P, P, P, P]),
         "pic_attend_shared": (I32, [G, I32, I32, P, I32, P, I32, I64, P, P, P, SZ, P, P, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
@@ -586,3 +587,14 @@ def pic_attend_shared(geom: Geometry, layer: int, q, block_table, num_pages: int
                                            plan, out, lse, workspace, stream)
     if st:
         _check(st, "pic_attend_shared")
+
+
+def pic_sample(logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None,
+               logprob=None, kept=None, stream=None):
+    """The next token of each row of logits [B][V] (float32 or bfloat16, rows of any stride) from
+    uniform [B]; temperature, top_k (int32), top_p, min_p, each [B] or None.  Fills token [B] and,
+    where given, the token's log-probability among the kept entries and their number."""
+    st = (_nat or _native()).sample(logits, uniform, token, temperature, top_k, top_p, min_p, logprob,
+                                    kept, stream)
+    if st:
+        _check(st, "pic_sample")

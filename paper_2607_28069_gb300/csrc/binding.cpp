@@ -940,6 +940,34 @@ PyObject *attend_shared(PyObject *, PyObject *const *v, Py_ssize_t n) {
   });
 }
 
+PyObject *sample(PyObject *, PyObject *const *v, Py_ssize_t n) {
+  return guarded(v, n, [](Args &a) {
+    const View lv = view_of(a.next(), "logits");
+    need_2d(lv, "logits");
+    if (!lv.t->is_cuda()) raise(PyExc_ValueError, "%s must be a CUDA tensor%s", "logits");
+    const bool bf16 = lv.t->scalar_type() == at::kBFloat16;
+    if (!bf16 && lv.t->scalar_type() != at::kFloat)
+      raise(PyExc_ValueError, "%s must be torch.float32 or torch.bfloat16%s", "logits");
+    const int64_t B = lv.size(0), V = lv.size(1);
+    if (V != 1 && lv.t->stride(lv.skip + 1) != 1)
+      raise(PyExc_ValueError, "%s must be contiguous in its last dimension%s", "logits");
+    const float *u = sized<float>(a, at::kFloat, "uniform", B);
+    int32_t *token = sized<int32_t>(a, at::kInt, "token", B);
+    const float *temp = sized<float>(a, at::kFloat, "temperature", B, true);
+    const int32_t *top_k = sized<int32_t>(a, at::kInt, "top_k", B, true);
+    const float *top_p = sized<float>(a, at::kFloat, "top_p", B, true);
+    const float *min_p = sized<float>(a, at::kFloat, "min_p", B, true);
+    float *logprob = sized<float>(a, at::kFloat, "logprob", B, true);
+    int32_t *kept = sized<int32_t>(a, at::kInt, "kept", B, true);
+    const pic_stream_t s = stream_of(a.next());
+    const int64_t stride = B > 1 ? lv.t->stride(lv.skip) : 0;
+    return unlocked([&] {
+      return pic_sample((int32_t)std::min<int64_t>(B, INT32_MAX), (int32_t)std::min<int64_t>(V, INT32_MAX),
+                        lv.data(), bf16, stride, temp, top_k, top_p, min_p, u, token, logprob, kept, s);
+    });
+  });
+}
+
 #define FAST(name, fn) {name, (PyCFunction)(void (*)(void))(fn), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     FAST("compose", compose),
@@ -964,6 +992,7 @@ PyMethodDef methods[] = {
     FAST("append_normed", append_normed),
     FAST("share_plan", share_plan),
     FAST("attend_shared", attend_shared),
+    FAST("sample", sample),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pic_native", nullptr, -1, methods,
