@@ -13,6 +13,8 @@
 // far as it fits; sums go through distributed shared memory.  A warp takes chunks of 1024
 // entries, 16 bytes a lane from aligned addresses whatever the row's start.
 #include <algorithm>
+#include <cstdlib>
+#include <type_traits>
 
 #include "pic_internal.cuh"
 
@@ -21,13 +23,20 @@ namespace sample {
 
 constexpr int kMaxVocab = 1 << 24;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kChunk = 1024;
+constexpr int kChunk = 256;  // entries of a warp at a time, 8 a lane
 constexpr int kMaxCluster = 16;
 constexpr int kBins = 2048;
-constexpr float kBinsPerOctave = 54.f;  // 37 octaves of weights in 1998 bins
+constexpr float kBinsPerOctave = 56.f;  // the 36 octaves of weights in 2017 bins
 constexpr int kList = 256;              // entries of a bin that are ranked
 constexpr int kSlots = 8;
+constexpr int kSmall = 4096;             // entries of a CTA's part that go into a histogram at once
 
+#ifdef PIC_STAMP
+__device__ long long g_stamp[32 + 64 * 16];
+#define STAMP(i) do { if (cluster_rank() == 0 && threadIdx.x == 0) { long long t_; asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t_)); if (blockIdx.x == 0) g_stamp[i] = t_; int r_ = blockIdx.x / cluster_size(); if (r_ < 64) g_stamp[32 + r_ * 16 + i] = t_; } } while (0)
+#else
+#define STAMP(i)
+#endif
 struct Params {
   int vocab, hold_chunks, bins;  // bins: shared memory holds the histogram and the list
   long long stride;
@@ -36,38 +45,54 @@ struct Params {
   const int32_t *top_k;
   int32_t *token, *kept;
   float *logprob;
+  int32_t *status;
 };
 
 struct alignas(16) Fixed {
   uint64_t slot[kSlots][kMaxCluster][2];  // values from every CTA of the cluster
   uint64_t warp[kWarps][2];
-  uint64_t tile[32 * 33];                 // the measures of the chunk that is searched
+  uint64_t bar[kSlots];                   // mbarriers of the slots
+  uint64_t list_bar[2];
   int32_t found, pad[3];
 };
+struct alignas(16) Sum2 {
+  uint64_t sum, count;
+};
+struct alignas(16) Entry {
+  uint64_t weight;
+  uint32_t key;
+  int32_t index;
+};
 struct alignas(16) Bins {
-  uint64_t sum[kBins], all_sum[kBins];      // this CTA's, the cluster's
-  uint32_t count[kBins], all_count[kBins];
-  uint64_t list_w[kList];
-  uint32_t list_key[kList], list_idx[kList];
-  uint32_t list_n, first, pick[2];          // pick: the entry found
+  uint32_t count[kBins];    // entries, and their weights in parts of 12 bits: sums of 32 bits each
+  uint32_t part[3][kBins];
+  Entry list[2][kList];     // (a CTA may be at its second while another is at its first)
+  Sum2 rank[kList];         // of the second half of the list ahead of an entry
+  uint32_t list_n, first, pick_key;
+  int32_t pick_index;
   uint64_t pick_sum, before_sum;
-  uint32_t bin, before_count;
+  uint32_t at, before_count, members, pad;
+  Sum2 seg[kBins];  // of the bins that this CTA adds up for the cluster: the first kBins / cluster size
 };
 
-PIC_DEV void st_cluster64(uint32_t addr, uint64_t v) {
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+// 16 bytes to another CTA of the cluster (addresses from map_to_rank), counted by its mbarrier.
+PIC_DEV void send(uint32_t addr, uint64_t a, uint64_t b, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.u64 [%0], {%1, %2}, [%3];" ::"r"(addr),
+               "l"(a), "l"(b), "r"(bar)
+               : "memory");
 }
 PIC_DEV void st_cluster32(uint32_t addr, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
-PIC_DEV uint64_t ld_cluster64(uint32_t addr) {
-  uint64_t v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
-  return v;
-}
 PIC_DEV uint32_t ld_cluster32(uint32_t addr) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+PIC_DEV uint4 ld_cluster128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
 PIC_DEV int cluster_size() {
@@ -89,104 +114,147 @@ PIC_DEV uint64_t scan64(uint64_t v) {  // inclusive prefix sum over the warp
   }
   return v;
 }
-// floor(total floor(2^24 u) / 2^24) for u taken into [0, top]
+// floor(total floor(2^24 u) / 2^24) for 2^24 u taken into [0, top]
 PIC_DEV uint64_t share_of(uint64_t total, float u, float top) {
   const uint64_t n = (uint64_t)fminf(fmaxf(u, 0.f) * 16777216.f, top);
   return (__umul64hi(total, n) << 40) | ((total * n) >> 24);
 }
-// Logits as whole numbers in the same order (a NaN counts as -infinity; -0 as 0).
+// Logits as whole numbers in the same order (-0 as 0).
 PIC_DEV uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x == 0.f ? 0.f : x);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+PIC_DEV float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+// Of two packed floats: a b + c rounded towards zero.
+PIC_DEV uint64_t fma2_rz(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+PIC_DEV uint32_t lo32(uint64_t v) { return (uint32_t)v; }
+PIC_DEV uint32_t hi32(uint64_t v) { return (uint32_t)(v >> 32); }
+PIC_DEV uint64_t both(float v) { return f2pack(v, v); }
 
-// The rule of the weights: e = 2^z for z = fl((x - M) s) >= -37, else 0, by rounding z to a
-// whole number and a polynomial of degree 5 in the rest, each operation rounded to fp32; the
-// weight is trunc(2^36 e).
+// The rule of the weights: for z = fl((x - M) s), e = 2^z by rounding z to a whole number and a
+// polynomial of degree 5 in the rest, each operation rounded to fp32; the weight is
+// trunc(2^36 e).  That is 0 exactly where z < -36 (z is kept at -38 or above, a NaN too), and
+// at least 1 from -36 on.  Pairs of entries go through packed operations.
+constexpr float kLeastZ = -36.f;
 struct Rule {
   float max, scale;
-  PIC_DEV float z(float x) const { return __fmul_rn(x == max ? 0.f : __fsub_rn(x, max), scale); }
-  PIC_DEV float e(float x) const {
-    const float z_ = z(x);
-    const float r = __fadd_rn(z_, 12582912.f);  // 1.5 2^23: the whole number in the low bits
-    const float f = __fsub_rn(z_, __fsub_rn(r, 12582912.f));
-    float p = __fadd_rn(__fmul_rn(f, 0.001326472731307149f), 0.009671512991189957f);
-    p = __fadd_rn(__fmul_rn(p, f), 0.05550733581185341f);
-    p = __fadd_rn(__fmul_rn(p, f), 0.24022242426872253f);
-    p = __fadd_rn(__fmul_rn(p, f), 0.6931470036506653f);
-    p = __fadd_rn(__fmul_rn(p, f), 1.f);
-    const float v = __uint_as_float(__float_as_uint(p) + (__float_as_uint(r) << 23));
-    return z_ >= -37.f && x > -INFINITY ? v : 0.f;
+  PIC_DEV float z(float x) const { return __fmul_rn(__fsub_rn(x, max), scale); }
+  PIC_DEV uint64_t e2(float x0, float x1) const {
+    uint64_t z = mul2(add2(f2pack(x0, x1), both(-max)), both(scale));
+    float z0, z1;
+    f2unpack(z, z0, z1);
+    z = f2pack(fmaxf(z0, -38.f), fmaxf(z1, -38.f));
+    const uint64_t r = add2(z, both(12582912.f));  // 1.5 2^23: the whole number in the low bits
+    const uint64_t f = fma2(add2(r, both(-12582912.f)), both(-1.f), z);  // exact
+    // The sums as fma(product, 1, c), the same rounding: a packed product and sum would be
+    // contracted into one operation whatever their rounding says.
+    auto step = [&](uint64_t p, float c) { return fma2(mul2(p, f), both(1.f), both(c)); };
+    uint64_t p = step(both(0.001326472731307149f), 0.009671512991189957f);
+    p = step(p, 0.05550733581185341f);
+    p = step(p, 0.24022242426872253f);
+    p = step(p, 0.6931470036506653f);
+    p = step(p, 1.f);
+    const uint32_t v0 = lo32(p) + (lo32(r) << 23), v1 = hi32(p) + (hi32(r) << 23);
+    return (uint64_t)v1 << 32 | v0;
   }
-  PIC_DEV uint64_t weight(float x) const { return (uint64_t)(e(x) * 68719476736.f); }
+  // One weight in parts: hi = trunc(2^13 e) and the next 23 bits.
+  PIC_DEV uint64_t weight(float x) const;
 };
 // Sums of weights in two 32-bit parts: hi = trunc(2^13 e), lo the next 23 bits, taken from the
 // low bits of a float by adding 2^23 with rounding towards zero (the 2^23's are taken out once).
+// (Conversions to 64 bits are issued at a small fraction of the fp32 rate.)
+constexpr uint32_t kTwo23 = 0x4b000000u;  // the bits of 2^23
 struct Sum {
   uint32_t hi = 0, lo = 0, n = 0;
-  PIC_DEV void add(float e) {
-    const float h = __fmaf_rz(e, 8192.f, 8388608.f);
-    const float r = fmaf(e, 8192.f, 8388608.f - h);  // exact, in [0, 1)
-    hi += __float_as_uint(h);
-    lo += __float_as_uint(__fmaf_rz(r, 8388608.f, 8388608.f));
-    n += e >= 1.4551915228366852e-11f;  // 2^-36: a weight
+  PIC_DEV void add(uint64_t e) {
+    const uint64_t h = fma2_rz(e, both(8192.f), both(8388608.f));
+    const uint64_t r = fma2(e, both(8192.f), fma2(h, both(-1.f), both(8388608.f)));  // exact, in [0, 1)
+    const uint64_t l = fma2_rz(r, both(8388608.f), both(8388608.f));
+    hi += lo32(h) + hi32(h);
+    lo += lo32(l) + hi32(l);
+    constexpr uint32_t kOne = 0x2d800000u;  // the bits of 2^-36: a weight
+    n += (uint32_t)(lo32(e) >= kOne) + (uint32_t)(hi32(e) >= kOne);
   }
-  PIC_DEV uint64_t total(uint32_t entries) const {
-    constexpr uint32_t kTwo23 = 0x4b000000u;  // the bits of 2^23
-    return ((uint64_t)(hi - entries * kTwo23) << 23) + (lo - entries * kTwo23);
+  // Of 8 entries a lane, over the warp (sums of at most 2^21 and 2^31).
+  PIC_DEV uint64_t warp_total() {
+    n = __reduce_add_sync(0xffffffffu, n);
+    return ((uint64_t)__reduce_add_sync(0xffffffffu, hi - 8u * kTwo23) << 23) +
+           __reduce_add_sync(0xffffffffu, lo - 8u * kTwo23);
   }
 };
+PIC_DEV uint64_t Rule::weight(float x) const {
+  const uint64_t e = e2(x, x);
+  const uint64_t h = fma2_rz(e, both(8192.f), both(8388608.f));
+  const uint64_t r = fma2(e, both(8192.f), fma2(h, both(-1.f), both(8388608.f)));
+  const uint64_t l = fma2_rz(r, both(8388608.f), both(8388608.f));
+  return ((uint64_t)(lo32(h) - kTwo23) << 23) + (lo32(l) - kTwo23);
+}
 
-// A CTA's part of a row: chunks [c0, c1) of 1024 entries from the aligned address at or below
+// A CTA's part of a row: chunks [c0, c1) of 256 entries from the aligned address at or below
 // the row's start (`lead` entries before it); the first `hold` of them are in shared memory.
 template <typename T>
 struct Part {
-  static constexpr int E = 16 / (int)sizeof(T);        // entries of 16 bytes
-  static constexpr int G = kChunk / 32 / E;            // such pieces of a lane
+  static constexpr int E = 16 / (int)sizeof(T);  // entries of 16 bytes
+  static constexpr int G = 8 / E;                // such pieces of a lane
   const uint4 *base;
   uint4 *held;
   int lead, vocab, c0, c1, hold;
-  // Entries of piece g of chunk c: x[0 .. E), NaN and what is outside the row as -infinity.
-  // kLoad: from memory, and into shared memory where that has room.
-  PIC_DEV int index(int c, int g) const { return c * kChunk + (g * 32 + (threadIdx.x & 31)) * E - lead; }
-  template <bool kLoad>
-  PIC_DEV uint4 raw(int c, int g) const {
-    const int lane = threadIdx.x & 31;
-    const int at = (c - c0) * (kChunk / E) + g * 32 + lane;
-    if (!kLoad && c - c0 < hold) return held[at];
-    const int i = index(c, g);
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (i + E > 0 && i < vocab) v = __ldg(base + (size_t)c * (kChunk / E) + g * 32 + lane);
-    return v;
+  PIC_DEV int index(int c, int k) const {  // of entry k < 8 of this lane
+    return c * kChunk + (k / E * 32 + (int)(threadIdx.x & 31)) * E + k % E - lead;
   }
-  PIC_DEV void keep(int c, int g, const uint4 &v) const {
-    if (c - c0 < hold) held[(c - c0) * (kChunk / E) + g * 32 + (threadIdx.x & 31)] = v;
-  }
-  PIC_DEV void entries(int c, int g, const uint4 &v, float *x) const {
-    if constexpr (E == 4) {
-      x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y);
-      x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
-    } else {
-      unpack8(v, x);
-    }
-    const int i = index(c, g);
-    const bool inside = i >= 0 && i + E <= vocab;
+  PIC_DEV bool edge(int c) const { return c * kChunk < lead || (c + 1) * kChunk > lead + vocab; }
+  PIC_DEV void fetch(int c, uint4 *v) const {  // from memory
 #pragma unroll
-    for (int k = 0; k < E; ++k) {
-      x[k] = fmaxf(x[k], -INFINITY);
-      if (!inside && (i + k < 0 || i + k >= vocab)) x[k] = -INFINITY;
-    }
-  }
-  // work(c, g, x) for this warp's chunks
-  template <typename F>
-  PIC_DEV void pieces(int c, F &&work) const {
-#pragma unroll 2
     for (int g = 0; g < G; ++g) {
-      float x[E];
-      entries(c, g, raw<false>(c, g), x);
-      work(g, x);
+      const int i = index(c, g * E);
+      v[g] = make_uint4(0, 0, 0, 0);
+      if (i + E > 0 && i < vocab) v[g] = __ldg(base + (size_t)c * (kChunk / E) + g * 32 + (threadIdx.x & 31));
     }
   }
+  PIC_DEV void keep(int c, const uint4 *v) const {
+    if (c - c0 < hold)
+#pragma unroll
+      for (int g = 0; g < G; ++g) held[(c - c0) * (kChunk / E) + g * 32 + (threadIdx.x & 31)] = v[g];
+  }
+  // This lane's entries of a chunk, what is outside the row as -infinity.
+  PIC_DEV void entries(int c, const uint4 *v, float *x) const {
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+      if constexpr (E == 4) {
+        x[4 * g] = __uint_as_float(v[g].x), x[4 * g + 1] = __uint_as_float(v[g].y);
+        x[4 * g + 2] = __uint_as_float(v[g].z), x[4 * g + 3] = __uint_as_float(v[g].w);
+      } else {
+        unpack8(v[g], x);
+      }
+    if (edge(c))
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = index(c, k);
+        if (i < 0 || i >= vocab) x[k] = -INFINITY;
+      }
+  }
+  PIC_DEV void load(int c, float *x) const {
+    uint4 v[G];
+    if (c - c0 < hold) {
+#pragma unroll
+      for (int g = 0; g < G; ++g) v[g] = held[(c - c0) * (kChunk / E) + g * 32 + (threadIdx.x & 31)];
+    } else {
+      fetch(c, v);
+    }
+    entries(c, v, x);
+  }
+};
+
+// What is kept so far: entries before or at (key, index) in the order; x: the key's logit.
+struct Last {
+  uint32_t key = 0;
+  int index = 0x7fffffff;
+  float x = -INFINITY;
+  PIC_DEV bool keeps(float v, int i) const { return v > x || (v == x && i <= index); }
 };
 
 template <typename T>
@@ -195,64 +263,80 @@ struct Row {
   Fixed &fx;
   uint64_t *chunk;  // a sum for each of this CTA's chunks
   int rank, C, turn;
+  int32_t *status;
   PIC_DEV Row(Fixed &f) : fx(f) {}
 
-  // Two values of each CTA of the cluster (given by thread 0) to all of them: slot to read.
+  // Two values of each CTA (of its first warp) to all CTAs of the cluster: the slot to read.
+  // What else the CTAs have written is not ordered by this (see meet).
   PIC_DEV int exchange(uint64_t a, uint64_t b) {
-    const int t = turn;
-    turn = (turn + 1) % kSlots;
-    // thread j writes to CTA j
-    if ((int)threadIdx.x < C) {
-      const uint32_t dst = map_to_rank(smem_u32(&fx.slot[t][rank][0]), threadIdx.x);
-      st_cluster64(dst, a);
-      st_cluster64(dst + 8, b);
+    const int t = turn % kSlots;
+    const uint32_t parity = turn / kSlots & 1, bar = smem_u32(&fx.bar[t]);
+    ++turn;
+    if ((int)threadIdx.x < C) {  // thread j writes to CTA j
+      if (threadIdx.x == 0) mbar_expect_tx(bar, 16 * C);
+      send(map_to_rank(smem_u32(&fx.slot[t][rank][0]), threadIdx.x), a, b, map_to_rank(bar, threadIdx.x));
     }
-    cluster_sync_all();
+    mbar_wait_no_flag(bar, parity, status, -3, kWaitLimitNs);
     return t;
   }
-  // Sums of a and b (lane 0 of each warp) over the CTA: in all threads of warp 0.
+  // Sums of a and b (the same in all lanes of a warp) over the CTA: in warp 0.
   PIC_DEV void cta_sum(uint64_t &a, uint64_t &b) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (lane == 0) fx.warp[warp][0] = a, fx.warp[warp][1] = b;
     __syncthreads();
     if (warp == 0) {
-      a = warp_sum(lane < kWarps ? fx.warp[lane][0] : 0);
-      b = warp_sum(lane < kWarps ? fx.warp[lane][1] : 0);
+      a = lane < kWarps ? fx.warp[lane][0] : 0;
+      b = lane < kWarps ? fx.warp[lane][1] : 0;
+#pragma unroll
+      for (int o = kWarps / 2; o; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+      }
     }
   }
-  // measure(x, i): a whole number for an entry.  Every chunk's sum stays in `chunk`; gives the
-  // row's total, this CTA's part [before, before + own) of it, and the number of entries with
-  // a measure.
+  struct Total {
+    uint64_t all, before, own, count;  // the row's, ahead of this CTA's part, this part's; entries
+  };
+  // The values of the CTAs in slot t, lane c the one of CTA c.
+  PIC_DEV Total total(int t) const {
+    const int lane = threadIdx.x & 31;
+    const uint64_t v = lane < C ? fx.slot[t][lane][0] : 0, n = lane < C ? fx.slot[t][lane][1] : 0;
+    uint64_t all = v, count = n, before = lane < rank ? v : 0;
+#pragma unroll
+    for (int o = kMaxCluster / 2; o; o >>= 1) {
+      all += __shfl_xor_sync(0xffffffffu, all, o);
+      count += __shfl_xor_sync(0xffffffffu, count, o);
+      before += __shfl_xor_sync(0xffffffffu, before, o);
+    }
+    all = __shfl_sync(0xffffffffu, all, 0), count = __shfl_sync(0xffffffffu, count, 0);
+    return Total{all, __shfl_sync(0xffffffffu, before, 0), __shfl_sync(0xffffffffu, v, rank), count};
+  }
+  // work(c, x, n): the sum of chunk c over the warp, n its number of entries (the same in all
+  // lanes).  Every chunk's sum stays in `chunk`.
   template <typename F>
-  PIC_DEV void sums(F &&chunk_sum, uint64_t &total, uint64_t &before, uint64_t &own, uint64_t &count) {
+  PIC_DEV Total sums(F &&work) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint64_t mine = 0, num = 0;
 #pragma unroll 1
     for (int c = part.c0 + warp; c < part.c1; c += kWarps) {
+      float x[8];
+      part.load(c, x);
       uint32_t n = 0;
-      const uint64_t s = warp_sum(chunk_sum(c, n));
+      const uint64_t s = work(c, x, n);
       if (lane == 0) chunk[c - part.c0] = s;
       mine += s;
-      num += __reduce_add_sync(0xffffffffu, n);
+      num += n;
     }
     cta_sum(mine, num);
-    const int t = exchange(mine, num);
-    total = before = own = count = 0;
-    for (int c = 0; c < C; ++c) {
-      const uint64_t v = fx.slot[t][c][0];
-      if (c < rank) before += v;
-      if (c == rank) own = v;
-      total += v;
-      count += fx.slot[t][c][1];
-    }
+    return total(exchange(mine, num));
   }
-  // The first entry whose running sum of measures exceeds `at` (below the total), by the CTA that
-  // holds it: done(index, its measure) in one warp, all lanes.
+  // The first entry whose running sum of measures exceeds `at` (below the total), by the CTA
+  // that holds it: done(index, its measure) in one lane.
   template <typename F, typename D>
-  PIC_DEV void find(uint64_t at, uint64_t before, uint64_t own, F &&measure, D &&done) {
-    if (threadIdx.x >= 32 || at < before || at >= before + own) return;
+  PIC_DEV void find(uint64_t at, const Total &t, F &&measure, D &&done) {
+    if (threadIdx.x >= 32 || at < t.before || at >= t.before + t.own) return;
     const int lane = threadIdx.x & 31, n = part.c1 - part.c0;
-    uint64_t left = at - before;
+    uint64_t left = at - t.before;
     int c = 0;
     for (int i = 0;; i += 32) {
       const uint64_t v = i + lane < n ? chunk[i + lane] : 0, x = scan64(v);
@@ -265,33 +349,289 @@ struct Row {
       }
       left -= __shfl_sync(0xffffffffu, x, 31);
     }
-    part.pieces(c, [&](int g, const float *x) {
-      const int i = part.index(c, g);
+    float x[8];
+    part.load(c, x);
+    constexpr int E = Part<T>::E;
 #pragma unroll
-      for (int k = 0; k < Part<T>::E; ++k) {
-        const int at_ = (g * 32 + lane) * Part<T>::E + k;
-        fx.tile[(at_ >> 5) * 33 + (at_ & 31)] = measure(x[k], i + k);
+    for (int g = 0; g < Part<T>::G; ++g) {  // (a lane's E entries follow each other)
+      uint64_t w[E], s = 0;
+#pragma unroll
+      for (int k = 0; k < E; ++k) s += w[k] = measure(x[g * E + k], part.index(c, g * E + k));
+      const uint64_t in = scan64(s), all = __shfl_sync(0xffffffffu, in, 31);
+      if (all <= left) {
+        left -= all;
+        continue;
       }
-    });
-    __syncwarp();
-    uint64_t v = 0;  // lane l: entries 32 l .. 32 l + 31
-#pragma unroll 8
-    for (int k = 0; k < 32; ++k) v += fx.tile[lane * 33 + k];
-    uint64_t x = scan64(v);
-    const int row = __ffs(__ballot_sync(0xffffffffu, x > left)) - 1;
-    left -= __shfl_sync(0xffffffffu, x - v, row & 31);
-    v = fx.tile[(row & 31) * 33 + lane];
-    x = scan64(v);
-    const int l = __ffs(__ballot_sync(0xffffffffu, x > left)) - 1;
-    done(c * kChunk + (row & 31) * 32 + (l & 31) - part.lead, __shfl_sync(0xffffffffu, v, l & 31));
+      if (in <= left || in - s > left) return;
+      left -= in - s;
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        if (w[k] > left) return done(part.index(c, g * E + k), w[k]);
+        left -= w[k];
+      }
+      return;
+    }
   }
-};
+  // Entries that equal v, up to `last`: their number and each chunk's.
+  PIC_DEV Total equals(float v, const Last &last) {
+    return sums([&](int c, const float *x, uint32_t &n) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) n += x[k] == v && last.keeps(x[k], part.index(c, k));
+      n = __reduce_add_sync(0xffffffffu, n);
+      return (uint64_t)n;
+    });
+  }
 
-// What is kept so far: entries before or at (key, index) in the order.
-struct Last {
-  uint32_t key = 0;
-  int index = 0x7fffffff;
-  PIC_DEV bool keeps(uint32_t k, int i) const { return k > key || (k == key && i <= index); }
+  // ---- the entry up to which a count or a sum is reached
+  // work(x, z, index) for the entries with z in [z_min, z_max] that `last` keeps.
+  template <typename F>
+  PIC_DEV void each(const Rule &rule, const Last &last, float z_min, float z_max, F &&work) {
+    const int warp = threadIdx.x >> 5;
+#pragma unroll 1
+    for (int c = part.c0 + warp; c < part.c1; c += kWarps) {
+      float x[8], z[8];
+      part.load(c, x);
+      bool some = false;
+#pragma unroll
+      for (int k = 0; k < 8; k += 2) {
+        f2unpack(mul2(add2(f2pack(x[k], x[k + 1]), both(-rule.max)), both(rule.scale)), z[k], z[k + 1]);
+        some |= (z[k] >= z_min && z[k] <= z_max) || (z[k + 1] >= z_min && z[k + 1] <= z_max);
+      }
+      if (!__any_sync(0xffffffffu, some)) continue;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (z[k] >= z_min && z[k] <= z_max && last.keeps(x[k], part.index(c, k))) work(x[k], z[k], part.index(c, k));
+    }
+  }
+  PIC_DEV void clear(Bins &bn) const {
+    uint4 *b = reinterpret_cast<uint4 *>(bn.count);  // and the parts behind
+    for (int i = threadIdx.x; i < kBins; i += kThreads) b[i] = make_uint4(0, 0, 0, 0);
+  }
+  template <bool kSums>
+  PIC_DEV void count_in(Bins &bn, int bin, uint64_t w) const {
+    atomicAdd(&bn.count[bin], 1u);
+    if constexpr (kSums) {
+      atomicAdd(&bn.part[0][bin], (uint32_t)w & 4095u);
+      atomicAdd(&bn.part[1][bin], (uint32_t)(w >> 12) & 4095u);
+      if (w >> 24) atomicAdd(&bn.part[2][bin], (uint32_t)(w >> 24));
+    }
+  }
+  // The histograms of all CTAs added up, each CTA an equal part of the bins: the slot with the
+  // parts' sums and counts.
+  template <bool kSums>
+  PIC_DEV int add_up(Bins &bn) {
+    const int tid = threadIdx.x;
+    cluster_sync_all();
+    const int per = kBins / C, parts = per < kThreads ? kThreads / per : 1;  // threads a bin
+    uint64_t s_all = 0, n_all = 0;
+    for (int i0 = 0; i0 < per * parts; i0 += kThreads) {
+      const int i = (i0 + tid) / parts, j = (i0 + tid) % parts;
+      const uint32_t src = smem_u32(&bn.count[rank * per + i]);
+      uint32_t n = 0, a = 0, d = 0, e = 0;
+      uint64_t s = 0;
+#pragma unroll 4
+      for (int c = j; c < C; c += parts) {
+        const uint32_t at = map_to_rank(src, c);
+        n += ld_cluster32(at);
+        if constexpr (kSums) {
+          a = ld_cluster32(at + 4 * kBins), d = ld_cluster32(at + 8 * kBins), e = ld_cluster32(at + 12 * kBins);
+          s += a + ((uint64_t)d << 12) + ((uint64_t)e << 24);
+        }
+      }
+      for (int o = 1; o < parts; o <<= 1) {
+        if constexpr (kSums) s += __shfl_xor_sync(0xffffffffu, s, o);
+        n += __shfl_xor_sync(0xffffffffu, n, o);
+      }
+      if (j == 0) {
+        bn.seg[i].sum = s, bn.seg[i].count = n;
+        s_all += s, n_all += n;
+      }
+    }
+    s_all = warp_sum(s_all), n_all = warp_sum(n_all);
+    __syncthreads();
+    cta_sum(s_all, n_all);
+    const int t = exchange(s_all, n_all);
+    cluster_sync_all();
+    return t;
+  }
+  struct Where {
+    int bin;
+    uint32_t count, members;  // entries ahead of the bin; its own
+    uint64_t sum;             // of those ahead
+  };
+  // The bin in which the target is reached, each CTA for itself; `base` ahead of the histogram.
+  template <bool kCount>
+  PIC_DEV Where locate(Bins &bn, int t, uint64_t target, uint64_t sum0, uint32_t count0) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = kBins / C;
+    const uint64_t v = lane < C ? fx.slot[t][lane][0] : 0, m = lane < C ? fx.slot[t][lane][1] : 0;
+    const uint64_t v_in = scan64(v), m_in = scan64(m);
+    const unsigned reached = __ballot_sync(0xffffffffu, lane < C && (kCount ? count0 + m_in : sum0 + v_in) >= target);
+    const int owner = reached ? __ffs(reached) - 1 : C - 1;
+    sum0 += __shfl_sync(0xffffffffu, v_in - v, owner);
+    count0 += (uint32_t)__shfl_sync(0xffffffffu, m_in - m, owner);
+    if (tid == 0) bn.list_n = 0, bn.at = 0, bn.members = 0;
+    for (int i0 = 0; i0 < per; i0 += kThreads) {
+      const int i = i0 + tid;
+      uint64_t s = 0, n = 0;
+      if (i < per) {
+        const uint4 q = ld_cluster128(map_to_rank(smem_u32(&bn.seg[i]), owner));
+        s = (uint64_t)q.y << 32 | q.x, n = q.z;
+      }
+      const uint64_t s_in = scan64(s), n_in = scan64(n);
+      __syncthreads();
+      if (lane == 31) fx.warp[warp][0] = s_in, fx.warp[warp][1] = n_in;
+      __syncthreads();
+      const uint64_t ws = lane < kWarps ? fx.warp[lane][0] : 0, wn = lane < kWarps ? fx.warp[lane][1] : 0;
+      const uint64_t ws_in = scan64(ws), wn_in = scan64(wn);
+      const uint64_t s_at = sum0 + s_in - s + __shfl_sync(0xffffffffu, ws_in - ws, warp);
+      const uint64_t n_at = count0 + n_in - n + __shfl_sync(0xffffffffu, wn_in - wn, warp);
+      sum0 += __shfl_sync(0xffffffffu, ws_in, 31), count0 += (uint32_t)__shfl_sync(0xffffffffu, wn_in, 31);
+      const uint64_t now = kCount ? n_at : s_at, then = kCount ? n_at + n : s_at + s;
+      if (now < target && then >= target)
+        bn.at = owner * per + i, bn.before_sum = s_at, bn.before_count = (uint32_t)n_at, bn.members = (uint32_t)n;
+    }
+    __syncthreads();
+    return Where{(int)bn.at, bn.before_count, bn.members, bn.before_sum};
+  }
+
+  struct Hist {  // what the bins hold
+    int slot;
+    bool there, sums;
+  };
+  // The first entry in the order, of those that `last` keeps, with which their count (kCount) or
+  // their sum reaches `target`, into `last`; returns the sum up to it (where weights are
+  // counted).  Entries with z < z_min come behind it.  h: a histogram over z that is there
+  // already, of all entries.
+  template <bool kCount>
+  PIC_DEV uint64_t select(Bins &bn, const Rule &rule, Last &last, uint64_t target, float z_min, Hist &h) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool with_sums = !kCount || h.there;  // (then also the refinements')
+    uint32_t lo = 0, hi = 0xffffffffu;  // its key is one of [lo, hi]
+    int shift = -1, zbin = -1;          // shift < 0: bins over z
+    uint64_t sum0 = 0;                  // of the entries ahead of the bin
+    uint32_t count0 = 0;
+    float z_max = 0.f;
+    auto bin_of = [&](float x, float z) -> int {
+      const int zb = (int)(-z * kBinsPerOctave);
+      if (shift < 0) return zb;
+      const uint32_t key = key_of(x);
+      return zb != zbin || key < lo || key > hi ? -1 : (int)((hi - key) >> shift);
+    };
+    for (;;) {
+      if (!h.there) {
+        clear(bn);
+        __syncthreads();
+        each(rule, last, z_min, z_max, [&](float x, float z, int) {
+          const int k = bin_of(x, z);
+          if (k < 0) return;
+          if (with_sums) count_in<true>(bn, k, rule.weight(x));
+          else count_in<false>(bn, k, 0);
+        });
+        h.slot = with_sums ? add_up<true>(bn) : add_up<false>(bn);
+      }
+      STAMP(6);
+      const Where at = locate<kCount>(bn, h.slot, target, sum0, count0);
+      STAMP(7);
+#ifdef PIC_STAMP
+      if (blockIdx.x == 0 && threadIdx.x == 0) g_stamp[20] = at.members, g_stamp[21] = shift;
+#endif
+      sum0 = at.sum, count0 = at.count;
+      if (shift < 0) {  // (one 2^-10 of a bin on either side for the rounding of -z bins)
+        z_max = fminf(z_max, -((float)at.bin - 0.001f) / kBinsPerOctave);
+        z_min = fmaxf(z_min, -((float)at.bin + 1.001f) / kBinsPerOctave);
+      }
+      const int members = (int)at.members;
+      if (members <= kList) {
+        // gathered by every CTA: this one's entries behind those of the CTAs before it
+        const uint32_t bar = smem_u32(&fx.list_bar[lists & 1]);
+        Entry *list = bn.list[lists & 1];
+        if (warp == 0) {
+          uint32_t n = lane < rank ? ld_cluster32(map_to_rank(smem_u32(&bn.count[at.bin]), lane)) : 0;
+          n = __reduce_add_sync(0xffffffffu, n);
+          if (lane == 0) {
+            bn.first = n;
+            mbar_expect_tx(bar, 16 * (uint32_t)members);
+          }
+        }
+        __syncthreads();
+        each(rule, last, z_min, z_max, [&](float x, float z, int i) {
+          if (bin_of(x, z) != at.bin) return;
+          const uint32_t e = bn.first + atomicAdd(&bn.list_n, 1u);
+          if (e >= kList) return;
+          const uint64_t w = with_sums ? rule.weight(x) : 0;
+          const uint32_t dst = smem_u32(&list[e]);
+          for (int c = 0; c < C; ++c)
+            send(map_to_rank(dst, c), w, (uint64_t)(uint32_t)i << 32 | key_of(x), map_to_rank(bar, c));
+        });
+        STAMP(8);
+        mbar_wait_no_flag(bar, lists++ >> 1 & 1, status, -3, kWaitLimitNs);
+        STAMP(9);
+        // two threads an entry, each half of the entries ahead of it
+        static_assert(kThreads == 2 * kList, "two threads an entry");
+        const int i = tid % kList, half = tid / kList;
+        uint64_t s = 0, w = 0;
+        uint32_t n = 0, key = 0;
+        int index = 0;
+        if (i < members) {
+          w = list[i].weight, key = list[i].key, index = list[i].index;
+          const int j1 = half ? members : members / 2;
+#pragma unroll 4
+          for (int j = half ? members / 2 : 0; j < j1; ++j) {
+            const Entry e = list[j];
+            if (e.key > key || (e.key == key && e.index <= index)) s += e.weight, ++n;
+          }
+          if (half) bn.rank[i].sum = s, bn.rank[i].count = n;
+        }
+        __syncthreads();
+        if (!half && i < members) {
+          s += sum0 + bn.rank[i].sum, n += count0 + (uint32_t)bn.rank[i].count;
+          if (kCount ? n == target : s >= target && s - w < target)
+            bn.pick_key = key, bn.pick_index = index, bn.pick_sum = s;
+        }
+        __syncthreads();
+        last = Last{bn.pick_key, bn.pick_index, logit_of(bn.pick_key)};
+        return bn.pick_sum;
+      }
+      h.there = false;  // (taken to pieces)
+      if (shift == 0) {  // entries of one key: by index
+        const uint32_t key = hi - (uint32_t)at.bin;
+        const float v = logit_of(key);
+        const uint64_t w = rule.weight(v), r = kCount ? target - count0 : (target - sum0 - 1) / w + 1;
+        const Total tot = equals(v, last);
+        find(r - 1, tot, [&](float x, int i) -> uint64_t { return x == v && last.keeps(x, i); },
+             [&](int i, uint64_t) {
+               for (int c = 0; c < C; ++c) st_cluster32(map_to_rank(smem_u32(&fx.found), c), (uint32_t)i);
+             });
+        cluster_sync_all();
+        last = Last{key, fx.found, v};
+        return sum0 + r * w;
+      }
+      if (shift < 0) {  // the bin's keys
+        zbin = at.bin;
+        uint32_t k_lo = 0xffffffffu, k_hi = 0;
+        each(rule, last, z_min, z_max, [&](float x, float z, int) {
+          if (bin_of(x, z) != at.bin) return;
+          k_lo = min(k_lo, key_of(x)), k_hi = max(k_hi, key_of(x));
+        });
+        k_lo = __reduce_min_sync(0xffffffffu, k_lo), k_hi = __reduce_max_sync(0xffffffffu, k_hi);
+        __syncthreads();
+        if (lane == 0) fx.warp[warp][0] = k_lo, fx.warp[warp][1] = k_hi;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) k_lo = min(k_lo, (uint32_t)fx.warp[w][0]), k_hi = max(k_hi, (uint32_t)fx.warp[w][1]);
+        const int t2 = exchange(k_lo, k_hi);
+        lo = 0xffffffffu, hi = 0;
+        for (int c = 0; c < C; ++c)
+          lo = min(lo, (uint32_t)fx.slot[t2][c][0]), hi = max(hi, (uint32_t)fx.slot[t2][c][1]);
+      } else {
+        const uint32_t top = hi - ((uint32_t)at.bin << shift);
+        lo = max(lo, top - ((1u << shift) - 1));
+        hi = top;
+      }
+      shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
+      cluster_sync_all();  // (the histogram and its sums are read by the other CTAs until here)
+    }
+  }
+  uint32_t lists = 0;  // gathered so far
 };
 
 template <typename T>
@@ -299,11 +639,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
   pdl_entry();
   extern __shared__ __align__(16) uint8_t smem[];
   Fixed &fx = *reinterpret_cast<Fixed *>(smem);
-  // every CTA of the cluster runs before another one writes to its shared memory
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < kSlots; ++i) mbar_init(smem_u32(&fx.bar[i]), 1);
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&fx.list_bar[i]), 1);
+    fence_mbar_init();
+  }
+  // every CTA of the cluster runs before another one writes to its shared memory
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   Row<T> row(fx);
-  row.rank = (int)cluster_rank(), row.C = cluster_size(), row.turn = 0;
+  row.rank = (int)cluster_rank(), row.C = cluster_size(), row.turn = 0, row.status = p.status;
   const int b = blockIdx.x / row.C;
   Part<T> &part = row.part;
   {
@@ -312,53 +657,57 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
     part.lead = (int)(a & 15) / (int)sizeof(T);
     part.vocab = p.vocab;
     const int chunks = (part.lead + p.vocab + kChunk - 1) / kChunk;
-    part.c0 = (int)((long long)chunks * row.rank / row.C);
-    part.c1 = (int)((long long)chunks * (row.rank + 1) / row.C);
+    part.c0 = chunks * row.rank / row.C;
+    part.c1 = chunks * (row.rank + 1) / row.C;
     part.hold = p.hold_chunks;
   }
   uint8_t *at = smem + sizeof(Fixed);
   Bins *bins = p.bins ? reinterpret_cast<Bins *>(at) : nullptr;
-  if (p.bins) at += sizeof(Bins);
+  if (p.bins) at += sizeof(Bins) - sizeof(Sum2) * (kBins - kBins / row.C);  // (see launch)
   part.held = reinterpret_cast<uint4 *>(at);
+  STAMP(0);
   row.chunk = reinterpret_cast<uint64_t *>(at + (size_t)p.hold_chunks * kChunk * sizeof(T));
+
+  // ---- the largest logit, and as much of the row as fits into shared memory
+  constexpr int U = 4;  // chunks in flight
+  float m = -INFINITY;
+#pragma unroll 1
+  for (int c = part.c0 + warp; c < part.c1; c += U * kWarps) {
+    uint4 v[U][Part<T>::G];
+#pragma unroll
+    for (int q = 0; q < U; ++q)
+      if (c + q * kWarps < part.c1) part.fetch(c + q * kWarps, v[q]);
+#pragma unroll
+    for (int q = 0; q < U; ++q)
+      if (c + q * kWarps < part.c1) {
+        part.keep(c + q * kWarps, v[q]);
+        float x[8];
+        part.entries(c + q * kWarps, v[q], x);
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) m = max3f(m, x[k], x[k + 1]);  // (a NaN is passed over)
+      }
+  }
+  STAMP(1);
+  if (bins) row.clear(*bins);
   // this row's settings
   const float temp = p.temperature ? p.temperature[b] : 1.f, u = p.uniform[b];
   const int top_k = p.top_k ? p.top_k[b] : 0;
   const float top_p = p.top_p ? p.top_p[b] : 1.f, min_p = p.min_p ? p.min_p[b] : 0.f;
-
-  // ---- the largest logit, and as much of the row as fits into shared memory
-  float m = -INFINITY;
-#pragma unroll 1
-  for (int c = part.c0 + warp; c < part.c1; c += kWarps) {
-    uint4 v[Part<T>::G];
-#pragma unroll
-    for (int g = 0; g < Part<T>::G; ++g) v[g] = part.template raw<true>(c, g);
-#pragma unroll
-    for (int g = 0; g < Part<T>::G; ++g) {
-      part.keep(c, g, v[g]);
-      float x[Part<T>::E];
-      part.entries(c, g, v[g], x);
-#pragma unroll
-      for (int k = 0; k < Part<T>::E; ++k) m = fmaxf(m, x[k]);
-    }
-  }
 #pragma unroll
   for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float *warp_max = reinterpret_cast<float *>(fx.tile);
-  if (lane == 0) warp_max[warp] = m;
-  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  if (lane == 0) fx.warp[warp][0] = __float_as_uint(m);
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   __syncthreads();
-  if (warp == 0) {
-    m = lane < kWarps ? warp_max[lane] : -INFINITY;
+  auto lanes_max = [&](const uint64_t *v, int n) {  // of v[0], v[2], ...
+    m = lane < n ? __uint_as_float((uint32_t)v[2 * lane]) : -INFINITY;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  }
-  {
-    const int t = row.exchange(__float_as_uint(m), 0);
-    m = -INFINITY;
-    for (int c = 0; c < row.C; ++c) m = fmaxf(m, __uint_as_float((uint32_t)fx.slot[t][c][0]));
-  }
+    for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    m = __shfl_sync(0xffffffffu, m, 0);
+  };
+  if (warp == 0) lanes_max(&fx.warp[0][0], kWarps);
+  lanes_max(&fx.slot[row.exchange(__float_as_uint(m), 0)][0][0], row.C);
   const bool writer = row.rank == 0 && tid == 0;
+  STAMP(2);
   if (m == -INFINITY) {  // no entry has a weight
     if (writer) {
       p.token[b] = -1;
@@ -367,245 +716,107 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
     }
     return;
   }
-  uint64_t total, before, own, count;
-  if (!(temp > 0.f)) {  // the first entry of the largest logit
-    auto first = [&](float x, int) -> uint64_t { return x == m; };
-    row.sums([&](int c, uint32_t &) {
-      uint64_t s = 0;
-      part.pieces(c, [&](int, const float *x) {
-#pragma unroll
-        for (int k = 0; k < Part<T>::E; ++k) s += x[k] == m;
-      });
-      return s;
-    }, total, before, own, count);
-    row.find(0, before, own, first, [&](int i, uint64_t) {
-      if (lane) return;
-      p.token[b] = i;
-      if (p.kept) p.kept[b] = 1;
-      if (p.logprob) p.logprob[b] = 0.f;
-    });
+  const bool greedy = !(temp > 0.f);
+  if (greedy || m == INFINITY) {  // only entries that equal the largest have a weight, 2^36 each
+    const typename Row<T>::Total t = row.equals(m, Last());
+    uint64_t n = greedy ? 1 : t.all;
+    if (top_k > 0) n = min(n, (uint64_t)top_k);
+    if (top_p < 1.f) n = min(n, max((share_of(n << 36, top_p, 16777216.f) + ((uint64_t)1 << 36) - 1) >> 36, (uint64_t)1));
+    row.find(share_of(n << 36, u, 16777215.f) >> 36, t, [&](float x, int) -> uint64_t { return x == m; },
+             [&](int i, uint64_t) {
+               p.token[b] = i;
+               if (p.kept) p.kept[b] = (int32_t)n;
+               if (p.logprob) p.logprob[b] = -logf((float)n);
+             });
     return;
   }
   const Rule rule{m, fminf(__fdiv_rn(1.4426950408889634f, temp), 1e30f)};
-  row.sums([&](int c, uint32_t &n) {
-    Sum s;
-    part.pieces(c, [&](int, const float *x) {
-#pragma unroll
-      for (int k = 0; k < Part<T>::E; ++k) s.add(rule.e(x[k]));
-    });
-    n = s.n;
-    return s.total(32);
-  }, total, before, own, count);
-
-  // ---- the last entry that top-k and then top-p keep
+  const bool by_k = top_k > 0 && top_k < p.vocab, by_p = top_p < 1.f;
+  const uint64_t least = max((uint64_t)(fminf(fmaxf(min_p, 0.f), 1.f) * 68719476736.f), (uint64_t)1);
   Last last;
-  bool cut = false;
-  auto select = [&](bool by_count, uint64_t target, float z_min) {
-    // the first entry, in the order, with which the count or the sum reaches `target`; entries
-    // with z < z_min come behind it
-    Bins &bn = *bins;
-    uint32_t lo = 0, hi = 0xffffffffu;  // its key is one of [lo, hi]
-    int shift = -1, zbin = -1;          // shift < 0: bins over z
-    uint64_t sum0 = 0;                  // of the entries ahead of the bin
-    uint32_t count0 = 0;
-    auto bin_of = [&](float x, uint32_t key) -> int {
-      const int zb = min(kBins - 1, (int)(-rule.z(x) * kBinsPerOctave));
-      if (shift < 0) return zb;
-      return zb != zbin || key < lo || key > hi ? -1 : (int)((hi - key) >> shift);
-    };
-    auto each = [&](auto &&work) {  // work(x, key, index, weight) for what is kept so far
-#pragma unroll 1
-      for (int c = part.c0 + warp; c < part.c1; c += kWarps)
-        part.pieces(c, [&](int g, const float *x) {
+  // The sums of what is kept: of all entries, and (kCut) of those that `last` keeps of a weight
+  // of `least` or more.
+  auto kept_sums = [&](auto kCut, uint64_t least_) {
+    return row.sums([&](int c, const float *x, uint32_t &n) -> uint64_t {
+      Sum s;
+      if constexpr (kCut) {
+        float top = x[0];
 #pragma unroll
-          for (int k = 0; k < Part<T>::E; ++k) {
-            if (!(rule.z(x[k]) >= z_min)) continue;
-            const int i = part.index(c, g) + k;
-            const uint32_t key = key_of(x[k]);
-            if (!last.keeps(key, i)) continue;
-            const uint64_t w = rule.weight(x[k]);
-            if (w) work(x[k], key, i, w);
-          }
-        });
-    };
-    for (;;) {
-      for (int i = tid; i < kBins; i += kThreads) bn.sum[i] = 0, bn.count[i] = 0;
-      if (tid == 0) bn.list_n = 0, bn.bin = 0, bn.before_sum = sum0, bn.before_count = count0;
-      __syncthreads();
-      each([&](float x, uint32_t key, int, uint64_t w) {
-        const int k = bin_of(x, key);
-        if (k < 0) return;
-        atomicAdd(&bn.count[k], 1u);
-        atomicAdd(reinterpret_cast<unsigned long long *>(&bn.sum[k]), (unsigned long long)w);
-      });
-      cluster_sync_all();
-      const int per = kBins / row.C;  // bins that this CTA adds up for all
-      for (int i = row.rank * per + tid; i < (row.rank + 1) * per; i += kThreads) {
-        uint64_t s = 0;
-        uint32_t n = 0;
-        for (int c = 0; c < row.C; ++c) {
-          s += ld_cluster64(map_to_rank(smem_u32(&bn.sum[i]), c));
-          n += ld_cluster32(map_to_rank(smem_u32(&bn.count[i]), c));
-        }
-        for (int c = 0; c < row.C; ++c) {
-          st_cluster64(map_to_rank(smem_u32(&bn.all_sum[i]), c), s);
-          st_cluster32(map_to_rank(smem_u32(&bn.all_count[i]), c), n);
-        }
-      }
-      cluster_sync_all();
-      // the bin in which the target is reached (every CTA for itself)
-      {
-        constexpr int kPer = kBins / kThreads;
-        uint64_t s = 0;
-        uint64_t n = 0;
-        for (int k = 0; k < kPer; ++k) s += bn.all_sum[tid * kPer + k], n += bn.all_count[tid * kPer + k];
-        const uint64_t s_in = scan64(s), n_in = scan64(n);
-        if (lane == 31) fx.warp[warp][0] = s_in, fx.warp[warp][1] = n_in;
-        __syncthreads();
-        uint64_t s_at = sum0 + s_in - s, n_at = count0 + n_in - n;
-        for (int w = 0; w < warp; ++w) s_at += fx.warp[w][0], n_at += fx.warp[w][1];
-        for (int k = 0; k < kPer; ++k) {
-          const uint64_t ds = bn.all_sum[tid * kPer + k], dn = bn.all_count[tid * kPer + k];
-          const uint64_t now = by_count ? n_at : s_at, then = by_count ? n_at + dn : s_at + ds;
-          if (now < target && then >= target) {
-            bn.bin = tid * kPer + k, bn.before_sum = s_at, bn.before_count = (uint32_t)n_at;
-          }
-          s_at += ds, n_at += dn;
-        }
-        __syncthreads();
-      }
-      const int bin = bn.bin;
-      sum0 = bn.before_sum, count0 = bn.before_count;
-      const uint32_t members = bn.all_count[bin];
-      if (members <= kList) {
-        // gathered by every CTA: this one's entries behind those of the CTAs before it
-        if (tid == 0) {
-          uint32_t first = 0;
-          for (int c = 0; c < row.rank; ++c) first += ld_cluster32(map_to_rank(smem_u32(&bn.count[bin]), c));
-          bn.first = first;
-        }
-        __syncthreads();
-        each([&](float x, uint32_t key, int i, uint64_t w) {
-          if (bin_of(x, key) != bin) return;
-          const uint32_t at_ = bn.first + atomicAdd(&bn.list_n, 1u);
-          for (int c = 0; c < row.C; ++c) {
-            st_cluster64(map_to_rank(smem_u32(&bn.list_w[at_]), c), w);
-            st_cluster32(map_to_rank(smem_u32(&bn.list_key[at_]), c), key);
-            st_cluster32(map_to_rank(smem_u32(&bn.list_idx[at_]), c), (uint32_t)i);
-          }
-        });
-        cluster_sync_all();
-        for (int i = warp; i < (int)members; i += kWarps) {
-          const uint32_t key = bn.list_key[i], idx = bn.list_idx[i];
-          uint64_t s = 0;
-          uint32_t n = 0;
-          for (int j = lane; j < (int)members; j += 32) {
-            const uint32_t kj = bn.list_key[j];
-            if (kj > key || (kj == key && bn.list_idx[j] <= idx)) s += bn.list_w[j], ++n;
-          }
-          s = sum0 + warp_sum(s);
-          n = count0 + __reduce_add_sync(0xffffffffu, n);
-          const uint64_t w = bn.list_w[i];
-          const bool here = by_count ? n == target : s >= target && s - w < target;
-          if (here && lane == 0) bn.pick[0] = key, bn.pick[1] = idx, bn.pick_sum = s;
-        }
-        __syncthreads();
-        last.key = bn.pick[0], last.index = (int)bn.pick[1];
-        return bn.pick_sum;
-      }
-      if (shift == 0) {  // entries of one key
-        const uint32_t key = hi - (uint32_t)bin;
-        const uint64_t w = bn.all_sum[bin] / members;
-        const uint64_t r = by_count ? target - count0 : (target - sum0 + w - 1) / w;
-        auto same = [&](float x, int i) -> uint64_t {
-          const uint32_t k = key_of(x);
-          return k == key && last.keeps(k, i);
-        };
-        uint64_t tot, bef, mine, num;
-        row.sums([&](int c, uint32_t &) {
-          uint64_t s = 0;
-          part.pieces(c, [&](int g, const float *x) {
+        for (int k = 1; k < 8; ++k) top = fmaxf(top, x[k]);
+        if (!__any_sync(0xffffffffu, top >= last.x)) return 0;
+        const float least_e = (float)least_ * 1.4551915228366852e-11f;  // (at most 25 bits: exact)
 #pragma unroll
-            for (int k = 0; k < Part<T>::E; ++k) s += same(x[k], part.index(c, g) + k);
-          });
-          return s;
-        }, tot, bef, mine, num);
-        row.find(r - 1, bef, mine, same, [&](int i, uint64_t) {
-          if (lane < row.C) st_cluster32(map_to_rank(smem_u32(&fx.found), lane), (uint32_t)i);
-        });
-        cluster_sync_all();
-        last.key = key, last.index = fx.found;
-        return sum0 + r * w;
-      }
-      if (shift < 0) {  // the bin's keys
-        zbin = bin;
-        uint32_t k_lo = 0xffffffffu, k_hi = 0;
-        each([&](float x, uint32_t key, int, uint64_t) {
-          if (bin_of(x, key) != bin) return;
-          k_lo = min(k_lo, key), k_hi = max(k_hi, key);
-        });
-        k_lo = __reduce_min_sync(0xffffffffu, k_lo), k_hi = __reduce_max_sync(0xffffffffu, k_hi);
-        __syncthreads();
-        if (lane == 0) fx.warp[warp][0] = k_lo, fx.warp[warp][1] = k_hi;
-        __syncthreads();
-        for (int w = 0; w < kWarps; ++w) k_lo = min(k_lo, (uint32_t)fx.warp[w][0]), k_hi = max(k_hi, (uint32_t)fx.warp[w][1]);
-        const int t = row.exchange(k_lo, k_hi);
-        lo = 0xffffffffu, hi = 0;
-        for (int c = 0; c < row.C; ++c)
-          lo = min(lo, (uint32_t)fx.slot[t][c][0]), hi = max(hi, (uint32_t)fx.slot[t][c][1]);
+        for (int k = 0; k < 8; k += 2) {
+          float e0, e1;
+          f2unpack(rule.e2(x[k], x[k + 1]), e0, e1);
+          e0 = last.keeps(x[k], part.index(c, k)) && e0 >= least_e ? e0 : 0.f;
+          e1 = last.keeps(x[k + 1], part.index(c, k + 1)) && e1 >= least_e ? e1 : 0.f;
+          s.add(f2pack(e0, e1));
+        }
       } else {
-        const uint32_t top = hi - ((uint32_t)bin << shift);
-        lo = max(lo, top - ((1u << shift) - 1));
-        hi = top;
-      }
-      shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
-      // (the histogram is read by the other CTAs until here)
-      cluster_sync_all();
-    }
-  };
-  if (bins) {
-    uint64_t sum_k = total;
-    if (top_k > 0 && (uint64_t)top_k < count) sum_k = select(true, (uint64_t)top_k, -38.f), cut = true;
-    if (top_p < 1.f) {
-      const uint64_t target = max(share_of(sum_k, top_p, 16777216.f), (uint64_t)1);
-      // entries whose weights are too small to add up to what top-p leaves out: all of them
-      // together have less than (sum_k - target)
-      const float rest = (float)(sum_k - target) * (0.999f / (float)p.vocab);
-      const float z_min = rest >= 1.f ? __log2f(rest) - 36.01f : -38.f;
-      if (cut) cluster_sync_all();  // (the first selection's lists are read until here)
-      select(false, target, z_min);
-      cut = true;
-    }
-  }
-  const uint64_t least = (uint64_t)(fminf(fmaxf(min_p, 0.f), 1.f) * 68719476736.f);
-  auto measure = [&](float x, int i) -> uint64_t {
-    if (cut && !last.keeps(key_of(x), i)) return 0;
-    const uint64_t w = rule.weight(x);
-    return w >= least ? w : 0;
-  };
-  if (cut || least > 1) {
-    const uint32_t key_min = cut ? last.key : 0;
-    row.sums([&](int c, uint32_t &n) {
-      uint64_t s = 0;
-      part.pieces(c, [&](int g, const float *x) {
-        const int i = part.index(c, g);
 #pragma unroll
-        for (int k = 0; k < Part<T>::E; ++k)
-          if (key_of(x[k]) >= key_min) {
-            const uint64_t w = measure(x[k], i + k);
-            s += w, n += w > 0;
-          }
+        for (int k = 0; k < 8; k += 2) s.add(rule.e2(x[k], x[k + 1]));
+      }
+      const uint64_t all = s.warp_total();
+      n = s.n;
+      return all;
+    });
+  };
+  using No = std::integral_constant<bool, false>;
+  using Yes = std::integral_constant<bool, true>;
+  typename Row<T>::Total t;
+  bool changed = least > 1;
+  if (bins && (by_k || by_p)) {
+    typename Row<T>::Hist h{0, part.vocab <= kSmall * row.C, true};
+    if (h.there) {
+      // a small part: the histogram of all entries at once, from which the sums come too
+      row.each(rule, last, kLeastZ, 0.f, [&](float x, float z, int) {
+        row.template count_in<true>(*bins, (int)(-z * kBinsPerOctave), rule.weight(x));
       });
-      return s;
-    }, total, before, own, count);
+      STAMP(5);
+      h.slot = row.template add_up<true>(*bins);
+      t = row.total(h.slot);
+    } else {
+      t = kept_sums(No(), 1);
+    }
+    STAMP(3);
+    if (by_k && (uint64_t)top_k < t.count) {
+      t.all = row.template select<true>(*bins, rule, last, (uint64_t)top_k, kLeastZ, h);
+      changed = true;
+      if (by_p && !h.there) {
+        h.there = false;
+        t = kept_sums(Yes(), 1);
+        cluster_sync_all();  // (the histogram's sums are read until here)
+      }
+    }
+    if (by_p) {
+      const uint64_t target = max(share_of(t.all, top_p, 16777216.f), (uint64_t)1);
+      // Entries whose weights are too small to add up to what top-p leaves out: all of them
+      // together have less than all - target.
+      const float rest = (float)(t.all - target) * (0.999f / (float)p.vocab);
+      const float z_min = rest >= 1.f ? fmaxf(__log2f(rest) - 36.01f, kLeastZ) : kLeastZ;
+      row.template select<false>(*bins, rule, last, target, h.there ? kLeastZ : z_min, h);
+    }
+    changed |= by_p || h.there;  // (a histogram leaves no sums of chunks)
+  } else if (!changed) {
+    t = kept_sums(No(), 1);
   }
-  const uint64_t draw = share_of(total, u, 16777215.f);
-  row.find(draw, before, own, measure, [&](int i, uint64_t w) {
-    if (lane) return;
-    p.token[b] = i;
-    if (p.logprob) p.logprob[b] = (float)log((double)w / (double)total);
-  });
-  if (writer && p.kept) p.kept[b] = (int32_t)count;
+  STAMP(10);
+  if (changed) t = kept_sums(Yes(), least);
+  STAMP(11);
+  row.find(share_of(t.all, u, 16777215.f), t,
+           [&](float x, int i) -> uint64_t {
+             const uint64_t w = last.keeps(x, i) ? rule.weight(x) : 0;
+             return w >= least ? w : 0;
+           },
+           [&](int i, uint64_t w) {
+             p.token[b] = i;
+             // ln(w / S), near 0 from S - w
+             if (p.logprob)
+               p.logprob[b] = w > t.all - w ? log1pf(-(float)(t.all - w) / (float)t.all) : logf((float)w / (float)t.all);
+           });
+  if (writer && p.kept) p.kept[b] = (int32_t)t.count;
+  STAMP(12);
 }
 
 template <typename T>
@@ -614,7 +825,9 @@ static cudaError_t launch(Params p, int batch, cudaStream_t stream) {
   auto attempt = [&](int C) {
     const int chunks = (p.vocab + 16 / (int)sizeof(T) - 1 + kChunk - 1) / kChunk;
     const int mine = (chunks + C - 1) / C;
-    const size_t fixed = sizeof(Fixed) + (p.bins ? sizeof(Bins) : 0) + (size_t)mine * 8 + 16;
+    // (of Bins::seg a CTA uses the first kBins / C)
+    const size_t bins = sizeof(Bins) - sizeof(Sum2) * (kBins - kBins / C);
+    const size_t fixed = sizeof(Fixed) + (p.bins ? bins : 0) + (size_t)mine * 8 + 16;
     const size_t room = fixed < kSmem ? kSmem - fixed : 0;
     p.hold_chunks = (int)std::min<size_t>(mine, room / (kChunk * sizeof(T)));
     const size_t smem = fixed + (size_t)p.hold_chunks * kChunk * sizeof(T);
@@ -626,9 +839,12 @@ static cudaError_t launch(Params p, int batch, cudaStream_t stream) {
     return launch_dependent_cluster(sample_kernel<T>, dim3((unsigned)(batch * C)), dim3(kThreads), smem,
                                     stream, C, p);
   };
-  if (batch <= 12) {
+  const char *env = getenv("PIC_C");
+  if (env) return attempt(atoi(env));
+  if (batch <= 12 || p.vocab > (1 << 22)) {
     if (attempt(16) == cudaSuccess) return cudaSuccess;
     cudaGetLastError();  // (where the device places no such clusters)
+    return attempt(8);
   }
   return attempt(batch <= 38 ? 8 : 4);
 }
@@ -652,7 +868,12 @@ extern "C" pic_status_t pic_sample(int32_t batch, int32_t vocab, const void *log
   if (reinterpret_cast<uintptr_t>(logits) % (bf16 ? 2 : 4))
     return fail(PIC_ERR_INVALID_ARG, "%s: misaligned logits", who);
   Params p{vocab, 0, top_k || top_p, stride, logits, temperature, top_p, min_p, uniform, top_k, token, kept,
-           logprob};
+           logprob, device_status_ptr()};
+  if (!p.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
   const cudaError_t e = bf16 ? launch<__nv_bfloat16>(p, batch, stream) : launch<float>(p, batch, stream);
   return e == cudaSuccess ? PIC_OK : cuda_fail(e, who);
 }
+
+#ifdef PIC_STAMP
+extern "C" void pic_stamps(long long *h) { cudaMemcpyFromSymbol(h, pic::sample::g_stamp, sizeof(long long) * (32 + 1024)); }
+#endif
