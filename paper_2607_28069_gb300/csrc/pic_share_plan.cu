@@ -87,16 +87,13 @@ __global__ void __launch_bounds__(1024) common_kernel(PlanParams p) {
   }
 }
 
-// Nearest value below x (kEqual: at most x) left or right of leaf c of a tree of minima with
-// `leaves` leaves (node 1 the root, leaf c at leaves + c); -1: none.
-template <bool kEqual>
-PIC_DEV int nearest(const int *tree, int leaves, int c, int x, bool right) {
-  auto has = [&](int node) { return kEqual ? tree[node] <= x : tree[node] < x; };
+// Nearest value of at most x left (or right) of leaf c of a tree of minima with `leaves` leaves
+// (node 1 the root, leaf c at leaves + c); -1: none.
+__device__ __noinline__ int nearest(const int *tree, int leaves, int c, int x, bool right) {
   int at = leaves + c;
   for (;;) {  // up until a sibling on the wanted side holds one
     if (at == 1) return -1;
-    const bool is_right = at & 1;
-    if (is_right != right && has(at ^ 1)) {
+    if (((at & 1) != 0) != right && tree[at ^ 1] <= x) {
       at ^= 1;
       break;
     }
@@ -104,17 +101,17 @@ PIC_DEV int nearest(const int *tree, int leaves, int c, int x, bool right) {
   }
   while (at < leaves) {
     at = 2 * at + (right ? 0 : 1);
-    if (!has(at)) at ^= 1;
+    if (tree[at] > x) at ^= 1;
   }
   return at - leaves;
 }
 
 struct Scratch {  // plan_kernel's shared memory, by columns: boundary i (entries i, i + 1) is column i + 1
-  int *tree;
+  int *tree, *keys, *row;
   uint16_t *left, *right, *rep, *jump;  // of every column with a count
+  long long *base;                      // first step of node k in the order of the work
+  uint16_t *item;                       // items ahead of it
   uint8_t *level;
-  long long *base;      // first step of node k in the order of the work
-  uint16_t *item;       // items ahead of it
   size_t bytes;
   __host__ __device__ Scratch(void *smem, int n, int leaves) {
     uint8_t *p = static_cast<uint8_t *>(smem), *p0 = p;
@@ -125,6 +122,8 @@ struct Scratch {  // plan_kernel's shared memory, by columns: boundary i (entrie
     };
     base = reinterpret_cast<long long *>(take(8 * (size_t)2 * n));
     tree = reinterpret_cast<int *>(take(8 * (size_t)leaves));
+    keys = reinterpret_cast<int *>(take(4 * (size_t)n));
+    row = reinterpret_cast<int *>(take(4 * (size_t)n));
     left = reinterpret_cast<uint16_t *>(take(2 * (size_t)(n + 1)));
     right = reinterpret_cast<uint16_t *>(take(2 * (size_t)(n + 1)));
     rep = reinterpret_cast<uint16_t *>(take(2 * (size_t)(n + 1)));
@@ -136,35 +135,25 @@ struct Scratch {  // plan_kernel's shared memory, by columns: boundary i (entrie
 };
 constexpr int kNoLevel = 255;
 
-PIC_DEV long long scan_add(long long v, long long *warp_sums, long long *total) {
-  const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x / 32;
-  long long x = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();
-  if (lane == 31) warp_sums[tid >> 5] = x;
-  __syncthreads();
-  long long before = 0, all = 0;
-  for (int w = 0; w < warps; ++w) {
-    if (w < (tid >> 5)) before += warp_sums[w];
-    all += warp_sums[w];
-  }
-  *total = all;
-  return before + x - v;  // exclusive
+// a / b for 0 <= a, 0 < b and a quotient below 2^20: a rounded estimate, then exact.
+PIC_DEV int quotient(long long a, long long b) {
+  int q = (int)((float)a / (float)b);
+  while (q > 0 && q * b > a) --q;
+  while ((q + 1) * b <= a) ++q;
+  return q;
 }
 
 __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
   pdl_entry();
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ long long warp_sums[32];
-  const int n = p.n, tid = threadIdx.x, threads = blockDim.x, leaves = p.tree;
+  __shared__ long long warp_cost[32];
+  __shared__ int warp_items[32];
+  const int n = p.n, tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, leaves = p.tree;
   Scratch s(smem, n, leaves);
   View v(p.plan, n);
   int *val = s.tree + leaves;  // column c: entries c - 1 and c; 0 at both ends
   for (int c = tid; c < leaves; c += threads) val[c] = c >= 1 && c < n ? v.common[c - 1] : 0;
+  for (int i = tid; i < n; i += threads) s.keys[i] = v.keys[i], s.row[i] = p.row ? p.row[i] : i;
   for (int w = leaves >> 1; w >= 1; w >>= 1) {
     __syncthreads();
     for (int k = tid; k < w; k += threads) s.tree[w + k] = min(s.tree[2 * (w + k)], s.tree[2 * (w + k) + 1]);
@@ -175,9 +164,9 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
     const int x = val[c];
     int l = 0, r = n, rep = 0;
     if (x > 0) {
-      l = nearest<false>(s.tree, leaves, c, x, false);
-      r = nearest<false>(s.tree, leaves, c, x, true);
-      rep = nearest<true>(s.tree, leaves, l, x, true);
+      l = nearest(s.tree, leaves, c, x - 1, false);
+      r = nearest(s.tree, leaves, c, x - 1, true);
+      rep = nearest(s.tree, leaves, l, x, true);
     }
     s.left[c] = l, s.right[c] = r, s.rep[c] = rep;
     s.level[c] = kNoLevel;
@@ -212,107 +201,132 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
       __syncthreads();
     }
 
-  auto leaf_up = [&](int i) {  // the column of the node above entry i's own tiles, or 0
-    const int c = val[i] >= val[i + 1] ? i : i + 1;
-    return val[c] > 0 ? (int)s.jump[s.rep[c]] : 0;
-  };
-  // Node k in the order of the work, shared nodes first: its entries and tiles; returns its number.
+  // Node k in the order of the work, shared nodes (k = column - 1) first; its number is k + n,
+  // or k - n for an entry's own tiles.
   auto node_of = [&](int k, Node *o) {
     *o = Node{0, 0, 0, 0, -1, 0, -1, -1};
-    if (k < n) {  // node n + k: column k + 1
+    int up;
+    if (k < n) {
       const int c = k + 1;
-      if (c >= n || val[c] == 0 || s.rep[c] != c || s.level[c] == kNoLevel) return n + k;
-      const int up = parent_of(c);
+      if (c >= n || val[c] == 0 || s.rep[c] != c || s.level[c] == kNoLevel) return;
+      up = parent_of(c);
       o->begin = s.left[c], o->end = s.right[c];
-      o->tile_begin = up ? val[up] : 0, o->tile_end = val[c];
-      o->row = p.row ? p.row[o->begin] : o->begin;
+      o->tile_end = val[c];
+      o->row = s.row[o->begin];
       o->keys = val[c] * BN;
-      o->parent = up ? n + up - 1 : -1;
       o->level = s.level[c];
-      return n + k;
+    } else {
+      const int i = k - n, keys = s.keys[i];
+      o->begin = i, o->end = i + 1;
+      o->keys = keys;
+      if (keys < 0) return;
+      const int c = val[i] >= val[i + 1] ? i : i + 1;  // the deeper node beside it
+      up = val[c] > 0 ? (int)s.jump[s.rep[c]] : 0;
+      o->tile_end = (keys + BN - 1) / BN;
+      o->row = s.row[i];
+      o->level = up ? s.level[up] + 1 : 0;
     }
-    const int i = k - n, keys = v.keys[i];
-    o->begin = i, o->end = i + 1;
-    if (keys < 0) {
-      o->keys = -1;
-      return i;
-    }
-    const int up = leaf_up(i);
     o->tile_begin = up ? val[up] : 0;
-    o->tile_end = (keys + BN - 1) / BN;
-    o->row = p.row ? p.row[i] : i;
-    o->keys = keys;
     o->parent = up ? n + up - 1 : -1;
-    o->level = up ? s.level[up] + 1 : 0;
-    return i;
   };
-  const int per = (2 * n + threads - 1) / threads;
-  long long cost = 0, items = 0, total, count;
-  for (int k = tid * per; k < min(2 * n, (tid + 1) * per); ++k) {
-    Node o;
-    const int j = node_of(k, &o);
-    v.nodes[j] = o;
-    const int tiles = o.tile_end - o.tile_begin;
-    if (tiles > 0) cost += p.hkv * Units(o.end - o.begin, tiles, p.ept).per_head(), ++items;
-  }
-  long long at = scan_add(cost, warp_sums, &total);
-  int item = (int)scan_add(items, warp_sums, &count);
-  for (int k = tid * per; k < min(2 * n, (tid + 1) * per); ++k) {
-    Node o;
-    node_of(k, &o);
+  long long at = 0;  // steps and items of the rounds before
+  int items = 0;
+#pragma unroll 1
+  for (int k0 = 0; k0 < 2 * n; k0 += threads) {
+    const int k = k0 + tid;
+    Node o{0, 0, 0, 0, -1, 0, -1, -1};
+    if (k < 2 * n) {
+      node_of(k, &o);
+      int4 *dst = reinterpret_cast<int4 *>(v.nodes + (k < n ? k + n : k - n));
+      dst[0] = make_int4(o.begin, o.end, o.tile_begin, o.tile_end);
+      dst[1] = make_int4(o.row, o.keys, o.parent, o.level);
+    }
     const int tiles = o.tile_end - o.tile_begin, m = o.end - o.begin;
-    s.base[k] = at, s.item[k] = item;
-    if (tiles <= 0) continue;
-    v.items[item] = Item{o.begin, m, o.tile_begin, tiles, o.row, o.keys, o.level, k >= n};
-    at += p.hkv * Units(m, tiles, p.ept).per_head();
-    ++item;
+    const long long cost = tiles > 0 ? p.hkv * Units(m, tiles, p.ept).per_head() : 0;
+    // steps and items ahead, over the CTA
+    const unsigned there = __ballot_sync(0xffffffffu, tiles > 0);
+    long long x = cost;
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, w);
+      if (lane >= w) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) warp_cost[warp] = x, warp_items[warp] = __popc(there);
+    __syncthreads();
+    long long ahead = at + x - cost;
+    int item = items + __popc(there & ((1u << lane) - 1));
+    for (int w = 0; w < threads / 32; ++w) {
+      if (w < warp) ahead += warp_cost[w], item += warp_items[w];
+      at += warp_cost[w], items += warp_items[w];
+    }
+    if (k < 2 * n) s.base[k] = ahead, s.item[k] = item;
+    if (tiles > 0) {
+      int4 *dst = reinterpret_cast<int4 *>(v.items + item);
+      dst[0] = make_int4(o.begin, m, o.tile_begin, tiles);
+      dst[1] = make_int4(o.row, o.keys, o.level, k >= n);
+    }
   }
+  const long long total = at;
   __syncthreads();
+  // each CTA's first unit: lane l < kShares of a warp finds the one of CTA kShares warp + l
+  const int ctas = (int)min((long long)kCtas, max(1ll, total / (kUnit + kOne)));
+  if (tid == 0) *v.head = Header{kMagic, n, p.hkv, p.ept, p.rows, p.max_pages, items, ctas, total, 0};
+  constexpr int kShares = 5;
+  static_assert(kShares * 32 >= kCtas, "a warp's share of the CTAs");
+  for (int c0 = warp * kShares; c0 < kCtas; c0 += threads / 32 * kShares) {
+    const int c = c0 + lane;
+    int first_page = 0, row = -1, last_page = 0;  // of its first tiles
+    if (lane < kShares && c < kCtas) {
+      Share sh{0, 0, 0, 0, 0, 0, 0, 0};
+      if (c < ctas && total > 0) {
+        const Deal deal(total, ctas);
+        sh.pos = deal.first(c), sh.end = deal.first(c + 1);
+        int lo = 0, hi = 2 * n - 1;  // the last node that begins at or before pos
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (s.base[mid] <= sh.pos) lo = mid;
+          else hi = mid - 1;
+        }
+        Node o;
+        node_of(lo, &o);
+        const Units u(o.end - o.begin, o.tile_end - o.tile_begin, p.ept);
+        sh.item = s.item[lo];
+        const long long off = sh.pos - s.base[lo], head = u.per_head();
+        sh.hk = quotient(off, head);
+        const long long in = off - sh.hk * head;
+        sh.pair = quotient(in, u.pair_cost());
+        sh.unit0 = s.base[lo] + sh.hk * head + sh.pair * u.pair_cost();
+        const int w = u.weight(sh.pair);
+        const int kt = max(0, (int)(sh.pos - sh.unit0) - kUnit + w - 1) / w;
+        first_page = (o.tile_begin + kt) * 8, row = o.row, last_page = (o.keys + 15) / 16;
+      }
+      v.shares[c] = sh;
+    }
+#pragma unroll
+    for (int j = 0; j < kShares; ++j) {
+      const int r = __shfl_sync(0xffffffffu, row, j), pg = __shfl_sync(0xffffffffu, first_page, j) + lane;
+      const int end = __shfl_sync(0xffffffffu, last_page, j);
+      int page = -1;
+      if (r >= 0 && pg < end) page = p.block_table[(size_t)r * p.max_pages + pg];
+      if (c0 + j < kCtas) v.first_pages[(c0 + j) * kFirstPages + lane] = page;
+    }
+  }
   // each entry's chain, by level
   for (int i = tid; i < n; i += threads) {
     Link *chain = v.chain + (size_t)i * kDepth;
     Node o;
     int k = n + i;
     node_of(k, &o);
+#pragma unroll 1
     for (int level = kDepth - 1; level >= 0; --level) {
-      const bool there = level == o.level && o.tile_end > o.tile_begin;
-      chain[level] = there ? Link{s.base[k], o.tile_end - o.tile_begin, o.begin, o.end - o.begin,
-                                  k >= n && o.level == 0, {0, 0}}
-                           : Link{0, 0, 0, 0, 0, {0, 0}};
+      Link l{0, 0, 0, 0, 0, {0, 0}};
+      if (level == o.level && o.tile_end > o.tile_begin)
+        l = Link{s.base[k], o.tile_end - o.tile_begin, o.begin, o.end - o.begin, k >= n && o.level == 0, {0, 0}};
+      *reinterpret_cast<int4 *>(chain + level) = *reinterpret_cast<int4 *>(&l);
+      *(reinterpret_cast<int4 *>(chain + level) + 1) = *(reinterpret_cast<int4 *>(&l) + 1);
       if (level == o.level && o.parent >= 0) k = o.parent - n, node_of(k, &o);
     }
-  }
-  const int ctas = (int)min((long long)kCtas, max(1ll, total / (kUnit + kOne)));
-  const Deal deal(total, ctas);
-  if (tid == 0) *v.head = Header{kMagic, n, p.hkv, p.ept, p.rows, p.max_pages, (int)count, ctas, total, 0};
-  // each CTA's first unit and pages, a warp each
-  const int lane = tid & 31;
-  for (int c = tid >> 5; c < kCtas; c += threads / 32) {
-    Share sh{0, 0, 0, 0, 0, 0, 0, 0};
-    int page = -1;
-    if (c < ctas && total > 0) {
-      sh.pos = deal.first(c), sh.end = deal.first(c + 1);
-      int lo = 0, hi = 2 * n - 1;  // the last node that begins at or before pos
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (s.base[mid] <= sh.pos) lo = mid;
-        else hi = mid - 1;
-      }
-      const Item it = v.items[s.item[lo]];
-      const Units u(it.m, it.tiles, p.ept);
-      sh.item = s.item[lo];
-      const long long off = sh.pos - s.base[lo], head = u.per_head();
-      sh.hk = (int)(off / head);
-      const long long in = off - sh.hk * head;
-      sh.pair = (int)(in / u.pair_cost());
-      sh.unit0 = s.base[lo] + sh.hk * head + sh.pair * u.pair_cost();
-      const int w = u.weight(sh.pair);
-      const int kt = max(0, (int)((sh.pos - sh.unit0 - kUnit + w - 1) / w));
-      const long long pidx = (long long)(it.tile_begin + kt) * 8 + lane;
-      if (pidx * 16 < it.keys) page = p.block_table[(size_t)it.row * p.max_pages + pidx];
-    }
-    if (lane == 0) v.shares[c] = sh;
-    v.first_pages[c * kFirstPages + lane] = page;
   }
 }
 
