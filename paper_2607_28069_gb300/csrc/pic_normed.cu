@@ -46,8 +46,11 @@ PIC_DEV void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+#ifndef MAXREG
+#define MAXREG
+#endif
 template <int D>
-__global__ void __launch_bounds__(kMaxThreads) append_kernel(Params p, RopeParams rp) {
+__global__ void MAXREG __launch_bounds__(kMaxThreads) append_kernel(Params p, RopeParams rp) {
   constexpr int KC = D / 16, VC = D / 8;
   pdl_entry();
   extern __shared__ __align__(16) uint8_t ring[];  // [kStages][48 bytes of each thread], 16 at a time
@@ -292,8 +295,9 @@ extern "C" pic_status_t pic_append_normed(const pic_geom_t *geom, int32_t layer,
   const int units = (p.Hq + p.Hkv) * (D / 16);
   const int threads = std::min(kMaxThreads, (units + 31) / 32 * 32);
   const char *env = getenv("PIC_RUN");
-  const long long tokens = (long long)batch * max_tokens;
-  p.run = env ? atoi(env) : (int)std::min<long long>(8, std::max<long long>(1, tokens / (4 * 152)));
+  // as many CTAs as an SM holds, if that leaves each a token
+  const long long tokens = (long long)batch * max_tokens, resident = 152ll * std::max(1, 65536 / (64 * threads));
+  p.run = env ? atoi(env) : (int)std::min<long long>(kMaxRun, (tokens + resident - 1) / resident);
   const dim3 grid((unsigned)(batch * ((max_tokens + p.run - 1) / p.run)));
   const size_t smem = (size_t)kStages * 48 * threads;
   cudaError_t e = cudaFuncSetAttribute(D == 128 ? append_kernel<128> : append_kernel<64>,

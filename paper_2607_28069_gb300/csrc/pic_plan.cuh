@@ -94,7 +94,7 @@ struct Deal {
   int ctas, r;
   float inv;
   __host__ __device__ Deal(long long total_, int ctas_)
-      : total(total_), q(total_ / ctas_), ctas(ctas_), r((int)(total_ - q * ctas_)), inv((float)ctas_ / (float)(total_ > 0 ? total_ : 1)) {}
+      : total(total_), q(total_ >> 31 ? total_ / ctas_ : (int)total_ / ctas_), ctas(ctas_), r((int)(total_ - q * ctas_)), inv((float)ctas_ / (float)(total_ > 0 ? total_ : 1)) {}
   __host__ __device__ long long first(int c) const { return q * c + r * c / ctas; }
   // The CTA whose share holds step t: an estimate, then exact.
   __host__ __device__ int owner(long long t) const {

@@ -64,15 +64,16 @@ __global__ void __launch_bounds__(1024) common_kernel(PlanParams p) {
     const int32_t *ta = p.block_table + (size_t)a.row * p.max_pages;
     const int32_t *tb = p.block_table + (size_t)b.row * p.max_pages;
     int diff = pages;
-    for (int j0 = tid; j0 < pages; j0 += 8 * blockDim.x) {
-      int x[8], y[8];
+    constexpr int U = 10;  // entries in flight
+    for (int j0 = tid; j0 < pages; j0 += U * blockDim.x) {
+      int x[U], y[U];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < U; ++k) {
         const int j = min(j0 + k * (int)blockDim.x, pages - 1);
         x[k] = ta[j], y[k] = tb[j];
       }
 #pragma unroll
-      for (int k = 7; k >= 0; --k) {
+      for (int k = U - 1; k >= 0; --k) {
         const int j = j0 + k * (int)blockDim.x;
         if (j < pages && (x[k] != y[k] || x[k] < 0 || x[k] >= p.num_pages)) diff = min(diff, j);
       }
@@ -254,12 +255,19 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
     __syncthreads();
     if (lane == 31) warp_cost[warp] = x, warp_items[warp] = __popc(there);
     __syncthreads();
-    long long ahead = at + x - cost;
-    int item = items + __popc(there & ((1u << lane) - 1));
-    for (int w = 0; w < threads / 32; ++w) {
-      if (w < warp) ahead += warp_cost[w], item += warp_items[w];
-      at += warp_cost[w], items += warp_items[w];
+    long long of_warps = lane < threads / 32 ? warp_cost[lane] : 0;
+    int items_of = lane < threads / 32 ? warp_items[lane] : 0;
+    const long long mine = __shfl_sync(0xffffffffu, of_warps, warp);
+    const int items_mine = __shfl_sync(0xffffffffu, items_of, warp);
+#pragma unroll
+    for (int w = 1; w < 32; w <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, of_warps, w);
+      const int z = __shfl_up_sync(0xffffffffu, items_of, w);
+      if (lane >= w) of_warps += y, items_of += z;
     }
+    const long long ahead = at + __shfl_sync(0xffffffffu, of_warps, warp) - mine + x - cost;
+    const int item = items + __shfl_sync(0xffffffffu, items_of, warp) - items_mine + __popc(there & ((1u << lane) - 1));
+    at += __shfl_sync(0xffffffffu, of_warps, 31), items += __shfl_sync(0xffffffffu, items_of, 31);
     if (k < 2 * n) s.base[k] = ahead, s.item[k] = item;
     if (tiles > 0) {
       int4 *dst = reinterpret_cast<int4 *>(v.items + item);
