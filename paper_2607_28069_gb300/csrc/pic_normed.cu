@@ -6,13 +6,13 @@
 // angle p theta_i is reduced exactly, as whole numbers.  q, k and v are read where the
 // projection left them: any strides of requests, tokens and heads.
 //
-// A CTA takes a run of tokens of a request, a thread of it a chunk of 8 pairs of a query or
-// key head (and 16 bytes of a value head), KC = d / 16 neighbouring lanes a head: the mean of
-// squares takes log2 KC shuffles.  Positions, pages and the rotation's cos and sin are formed
-// for the run at once, while the first tokens' projections are under way to shared memory;
-// each thread copies what it will read itself, so the ring needs no barrier.
+// The tokens are dealt to the CTAs that the GPU holds at once in equal shares: of all requests'
+// tokens, in order.  A thread takes a chunk of 8 pairs of a query or key head (and 16 bytes of
+// a value head), KC = d / 16 neighbouring lanes a head: the mean of squares takes log2 KC
+// shuffles.  Positions, pages and the rotation's cos and sin are formed for up to 16 tokens at
+// once, while the first tokens' projections are under way to shared memory; each thread
+// copies what it will read itself, so that ring needs no barrier.
 #include <algorithm>
-#include <cstdlib>
 
 #include "pic_internal.cuh"
 
@@ -20,7 +20,8 @@ namespace pic {
 namespace normed {
 
 constexpr int kMaxThreads = 512;
-constexpr int kMaxRun = 16;  // tokens of a CTA
+constexpr int kMaxRun = 16;  // tokens of a CTA at a time
+constexpr int kMaxRagged = 1024;
 constexpr int kStages = 4;   // tokens in flight
 
 struct Params {
@@ -33,7 +34,6 @@ struct Params {
   __nv_bfloat16 *q_out;              // [batch][max_tokens][Hq][d], or with r_pad the prefill's packed rows
   uint64_t turn[64];  // of the frequencies (where the geometry has one table)
   float eps;
-  int run;
   int32_t *status;
 };
 
@@ -46,89 +46,151 @@ PIC_DEV void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-#ifndef MAXREG
-#define MAXREG
-#endif
-template <int D>
-__global__ void MAXREG __launch_bounds__(kMaxThreads) append_kernel(Params p, RopeParams rp) {
+template <int D, bool kRagged>
+__global__ void __launch_bounds__(kMaxThreads, 2) append_kernel(Params p, RopeParams rp) {
   constexpr int KC = D / 16, VC = D / 8;
   pdl_entry();
   extern __shared__ __align__(16) uint8_t ring[];  // [kStages][48 bytes of each thread], 16 at a time
-  __shared__ float2 cs[kMaxRun][D / 2];
-  __shared__ int at_s[kMaxRun], page_s[kMaxRun];
+  __shared__ __align__(16) float2 cs[kMaxRun][D / 2];
+  __shared__ int at_s[kMaxRun], page_s[kMaxRun], row_s[kMaxRun];  // page_s: -2 left alone
+  __shared__ int2 tok_s[kMaxRun];  // request, token
   __shared__ uint64_t turn_s[D / 2];
-  const int tid = threadIdx.x, threads = blockDim.x;
-  const int runs = (p.max_tokens + p.run - 1) / p.run;
-  const int b = blockIdx.x / runs, t0 = blockIdx.x % runs * p.run;
-  const int slots = min(p.run, p.max_tokens - t0);
+  __shared__ int first_s[kRagged ? kMaxRagged : 1], warp_s[kMaxThreads / 32];
+  const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31;
   // (The threads are a multiple of KC: a thread's chunk of a head is always the same.)
   const int units = (p.Hq + p.Hkv) * KC, pieces = p.Hkv * VC;
   const PairChunk pc = pair_chunk(tid % KC, D / 2, rp.style);
-  auto head = [&](int u, int t) {
-    const int h = u / KC;
-    return h < p.Hq ? p.q + b * p.qs[0] + t * p.qs[1] + h * p.qs[2]
-                    : p.k + b * p.ks[0] + t * p.ks[1] + (h - p.Hq) * p.ks[2];
-  };
-  auto value = [&](int u, int t) { return p.v + b * p.vs[0] + t * p.vs[1] + (u / VC) * p.vs[2] + u % VC * 8; };
-  const uint32_t mine = smem_u32(ring) + tid * 16, third = threads * 16;
-  auto fetch = [&](int j) {  // token t0 + j
-    if (j < slots) {
-      const uint32_t dst = mine + j % kStages * 3 * third;
-      if (tid < units) {
-        const __nv_bfloat16 *src = head(tid, t0 + j);
-        copy16(dst, src + pc.off_a);
-        copy16(dst + third, src + pc.off_b);
-      }
-      if (tid < pieces) copy16(dst + 2 * third, value(tid, t0 + j));
-    }
-    copies_commit();
-  };
-  // The projections go out before anything is known of the request.
-#pragma unroll
-  for (int j = 0; j < kStages - 1; ++j) fetch(j);
   uint4 wa = make_uint4(0, 0, 0, 0), wb = wa;  // this thread's weights
   auto weights = [&](int u) {
     const __nv_bfloat16 *w = u / KC < p.Hq ? p.wq : p.wk;
     if (w) wa = __ldg(reinterpret_cast<const uint4 *>(w + pc.off_a)), wb = __ldg(reinterpret_cast<const uint4 *>(w + pc.off_b));
     return w != nullptr;
   };
-  bool norm = weights(tid);
-  const int row = p.row ? p.row[b] : b;
-  int n = p.num_tokens ? p.num_tokens[b] : p.max_tokens;
-  const long long pos = p.pos && tid < slots ? (long long)p.pos[(size_t)b * p.max_tokens + t0 + tid] : 0;
-  for (int i = tid; i < D / 2; i += threads)
-    turn_s[i] = rp.layer_theta ? rope_turn(rope_theta(rp, p.layer, i)) : p.turn[i];
-  bool twice = false;  // the row named before
-  if (p.row)
-    for (int j = tid; j < b; j += threads) twice |= p.row[j] == row;
-  const bool known = row >= 0 && row < p.rows && n >= 0 && n <= p.max_tokens;
-  if (tid < slots && known) {
-    const long long at = p.pos ? pos : (long long)p.ctx_len[row] + t0 + tid;
-    const bool ok = at >= 0 && at < (long long)p.max_pages * 16;
-    int page = ok && t0 + tid < n ? p.block_table[(size_t)row * p.max_pages + at / 16] : -1;
-    at_s[tid] = ok ? (int)at : 0;
-    if (t0 + tid < n) {
-      if (at < 0) dev_fail(p.status, PIC_DEV_BAD_POSITION, b);
-      else if (!ok) dev_fail(p.status, PIC_DEV_BLOCK_TABLE_SHORT, b);
-      else if (page < 0 || page >= p.num_pages) dev_fail(p.status, PIC_DEV_BAD_PAGE, b);
-    }
-    page_s[tid] = page >= p.num_pages ? -1 : page;
-  }
-  if (__syncthreads_or(twice) || !known) {
-    if (tid == 0 && t0 == 0) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
-    n = 0;
-  }
-  auto q_row = [&](int h, int t) {
-    return p.r_pad ? ((size_t)(b * p.Hkv + h / p.G) * p.r_pad + t * p.G + h % p.G) * D
-                   : (((size_t)b * p.max_tokens + t) * p.Hq + h) * D;
+  auto count_of = [&](int b) {  // tokens of request b, 0 where they are none
+    const int n = p.num_tokens ? p.num_tokens[b] : p.max_tokens;
+    return n < 0 || n > p.max_tokens ? 0 : n;
   };
-  const int live = min(max(n - t0, 0), slots);
-  if (p.r_pad)  // the prefill multiplies every packed row
-    for (int t = t0 + live; t < t0 + slots; ++t)
-      for (int u = tid; u < p.Hq * VC; u += threads)
-        st_global16(p.q_out + q_row(u / VC, t) + u % VC * 8, make_uint4(0, 0, 0, 0));
-  for (int e = tid; e < live * (D / 2); e += threads)
-    cs[e / (D / 2)][e % (D / 2)] = rope_cos_sin_turn(at_s[e / (D / 2)], turn_s[e % (D / 2)]);
+  int all = p.batch * p.max_tokens;
+  if constexpr (kRagged) {  // first_s: tokens of the requests before
+    int at = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += threads) {
+      const int n = b0 + tid < p.batch ? count_of(b0 + tid) : 0;
+      int x = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      __syncthreads();
+      if (lane == 31) warp_s[tid >> 5] = x;
+      __syncthreads();
+      x += at - n;
+      for (int w = 0; w < threads / 32; ++w) {
+        if (w < (tid >> 5)) x += warp_s[w];
+        at += warp_s[w];
+      }
+      if (b0 + tid < p.batch) first_s[b0 + tid] = x;
+    }
+    all = at;
+  }
+  auto q_row = [&](int h, int2 tok) {
+    return p.r_pad ? ((size_t)(tok.x * p.Hkv + h / p.G) * p.r_pad + tok.y * p.G + h % p.G) * D
+                   : (((size_t)tok.x * p.max_tokens + tok.y) * p.Hq + h) * D;
+  };
+  auto zero = [&](int2 tok) {  // (the prefill multiplies every packed row)
+    for (int u = tid; u < p.Hq * VC; u += threads)
+      st_global16(p.q_out + q_row(u / VC, tok) + u % VC * 8, make_uint4(0, 0, 0, 0));
+  };
+  auto head = [&](int u, int2 tok) {
+    const int h = u / KC;
+    return h < p.Hq ? p.q + tok.x * p.qs[0] + tok.y * p.qs[1] + h * p.qs[2]
+                    : p.k + tok.x * p.ks[0] + tok.y * p.ks[1] + (h - p.Hq) * p.ks[2];
+  };
+  auto value = [&](int u, int2 tok) {
+    return p.v + tok.x * p.vs[0] + tok.y * p.vs[1] + (u / VC) * p.vs[2] + u % VC * 8;
+  };
+  const uint32_t mine = smem_u32(ring) + tid * 16, third = threads * 16;
+  const int each = all / (int)gridDim.x, more = all % (int)gridDim.x, cta = blockIdx.x;
+  const int share0 = each * cta + min(cta, more), share1 = share0 + each + (cta < more ? 1 : 0);
+  bool norm = false;
+#pragma unroll 1
+  for (int s0 = share0; s0 < share1 || s0 == share0; s0 += kMaxRun) {
+  const int slots = min(kMaxRun, share1 - s0);
+  if (kRagged || s0 > share0) __syncthreads();  // (what was formed for the tokens before has been read)
+  auto dense = [&](int i) { return p.max_tokens == 1 ? make_int2(i, 0) : make_int2(i / p.max_tokens, i % p.max_tokens); };
+  if (tid < slots) {
+    const int i = s0 + tid;
+    int2 tok = dense(i);
+    if constexpr (kRagged) {
+      int lo = 0, hi = p.batch - 1;  // the last request that begins at or before it
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (first_s[mid] <= i) lo = mid;
+        else hi = mid - 1;
+      }
+      tok = make_int2(lo, i - first_s[lo]);
+    }
+    tok_s[tid] = tok;
+  }
+  if constexpr (kRagged) __syncthreads();
+  auto fetch = [&](int j) {
+    if (j < slots) {
+      const uint32_t dst = mine + j % kStages * 3 * third;
+      const int2 tok = kRagged ? tok_s[j] : dense(s0 + j);
+      if (tid < units) {
+        const __nv_bfloat16 *src = head(tid, tok);
+        copy16(dst, src + pc.off_a);
+        copy16(dst + third, src + pc.off_b);
+      }
+      if (tid < pieces) copy16(dst + 2 * third, value(tid, tok));
+    }
+    copies_commit();
+  };
+  // The projections go out before anything more is known of the requests.
+#pragma unroll
+  for (int j = 0; j < kStages - 1; ++j) fetch(j);
+  if (s0 == share0) {
+    norm = weights(tid);
+    for (int i = tid; i < D / 2; i += threads)
+      turn_s[i] = rp.layer_theta ? rope_turn(rope_theta(rp, p.layer, i)) : p.turn[i];
+  }
+  if (tid < slots) {
+    const int b = tok_s[tid].x, t = tok_s[tid].y;
+    const int row = p.row ? p.row[b] : b, n = count_of(b);
+    const long long pos = p.pos ? (long long)p.pos[(size_t)b * p.max_tokens + t] : 0;
+    int page = -2;
+    long long at = 0;
+    if (row < 0 || row >= p.rows) {
+      dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
+    } else if (t < n) {
+      at = p.pos ? pos : (long long)p.ctx_len[row] + t;
+      const bool ok = at >= 0 && at < (long long)p.max_pages * 16;
+      page = ok ? p.block_table[(size_t)row * p.max_pages + at / 16] : -1;
+      if (!ok) dev_fail(p.status, at < 0 ? PIC_DEV_BAD_POSITION : PIC_DEV_BLOCK_TABLE_SHORT, b);
+      else if (page < 0 || page >= p.num_pages) dev_fail(p.status, PIC_DEV_BAD_PAGE, b);
+      if (page < 0 || page >= p.num_pages) page = -1;
+      if (!ok) at = 0;
+    }
+    at_s[tid] = (int)at, page_s[tid] = page, row_s[tid] = row;
+  }
+  __syncthreads();
+  if (p.row) {  // rows named before: left alone
+    for (int j = tid >> 5; j < slots; j += threads / 32) {
+      const int b = tok_s[j].x, row = row_s[j];
+      bool twice = false;
+      for (int i = lane; i < b; i += 32) twice |= p.row[i] == row;
+      if (__any_sync(0xffffffffu, twice) && lane == 0 && page_s[j] != -2) {
+        dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
+        page_s[j] = -2;
+      }
+    }
+  }
+  // pairs 8 c + 2 q, 8 c + 2 q + 1 of chunk c at q KC + c: neighbouring lanes read neighbouring
+  // 16 bytes (a chunk's 64 bytes in a row took four times the shared memory's cycles)
+  for (int e = tid; e < slots * (D / 2); e += threads) {
+    const int i = e % (D / 2);
+    cs[e / (D / 2)][((i / 2 % 4) * KC + i / 8) * 2 + i % 2] = rope_cos_sin_turn(at_s[e / (D / 2)], turn_s[i]);
+  }
   __syncthreads();
   // one chunk: norm, rotation, store
   auto work = [&](int u, int j, const uint4 &xa, const uint4 &xb) {
@@ -154,11 +216,16 @@ __global__ void MAXREG __launch_bounds__(kMaxThreads) append_kernel(Params p, Ro
     const int h = u / KC, page = page_s[j];
     __nv_bfloat16 *dst = nullptr;
     if (h < p.Hq)
-      dst = p.q_out + q_row(h, t0 + j);
+      dst = page != -2 ? p.q_out + q_row(h, tok_s[j]) : nullptr;
     else if (page >= 0)
       dst = p.k_cache + (((size_t)page * p.Hkv + h - p.Hq) * 16 + (at_s[j] & 15)) * D;
     if (!dst) return;
-    const float2 *r = cs[j] + 8 * (tid % KC);
+    float2 r[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 x = *reinterpret_cast<const float4 *>(&cs[j][(q * KC + tid % KC) * 2]);
+      r[2 * q] = make_float2(x.x, x.y), r[2 * q + 1] = make_float2(x.z, x.w);
+    }
     if (rp.style == PIC_ROPE_HALF) {
       rotate8(a, c, r);
     } else {
@@ -178,13 +245,14 @@ __global__ void MAXREG __launch_bounds__(kMaxThreads) append_kernel(Params p, Ro
       st_global16(p.v_cache + (((size_t)page_s[j] * p.Hkv + u / VC) * 16 + (at_s[j] & 15)) * D + u % VC * 8, x);
   };
 #pragma unroll 1
-  for (int j = 0; j < live; ++j) {
+  for (int j = 0; j < slots; ++j) {
     copies_wait<kStages - 2>();
     const uint32_t src = mine + j % kStages * 3 * third;
     const uint4 xa = lds128(src), xb = lds128(src + third), xv = lds128(src + 2 * third);
     fetch(j + kStages - 1);
     work(tid, j, xa, xb);
     if (tid < pieces) store_value(tid, j, xv);
+    if (p.r_pad && page_s[j] == -2) zero(tok_s[j]);
   }
   copies_wait<0>();
   // heads beyond the CTA's threads
@@ -193,14 +261,22 @@ __global__ void MAXREG __launch_bounds__(kMaxThreads) append_kernel(Params p, Ro
     const int u = u0 + tid;
     if (u < units) norm = weights(u);
 #pragma unroll 1
-    for (int j = 0; j < live; ++j) {
-      const __nv_bfloat16 *src = head(min(u, units - 1), t0 + j);
+    for (int j = 0; j < slots; ++j) {
+      const __nv_bfloat16 *src = head(min(u, units - 1), tok_s[j]);
       work(u, j, ld_stream(src + pc.off_a), ld_stream(src + pc.off_b));
     }
   }
+  if (units > threads) norm = weights(tid);
 #pragma unroll 1
   for (int u = threads + tid; u < pieces; u += threads)
-    for (int j = 0; j < live; ++j) store_value(u, j, ld_stream(value(u, t0 + j)));
+    for (int j = 0; j < slots; ++j) store_value(u, j, ld_stream(value(u, tok_s[j])));
+  }
+  if (p.num_tokens && tid == 0)  // counts that are none
+    for (int b = blockIdx.x; b < p.batch; b += gridDim.x)
+      if (p.num_tokens[b] < 0 || p.num_tokens[b] > p.max_tokens) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
+  if (p.r_pad && p.num_tokens)
+    for (int tok = blockIdx.x; tok < p.batch * p.max_tokens; tok += gridDim.x)
+      if (tok % p.max_tokens >= count_of(tok / p.max_tokens)) zero(make_int2(tok / p.max_tokens, tok % p.max_tokens));
 }
 
 }  // namespace normed
@@ -248,7 +324,7 @@ extern "C" pic_status_t pic_append_normed(const pic_geom_t *geom, int32_t layer,
   }
   if (low & 15)
     return fail(PIC_ERR_INVALID_ARG, "%s: bf16 tensors and their strides must be multiples of 16 bytes", who);
-  if ((long long)batch * max_tokens >= INT32_MAX || max_pages > INT32_MAX / 16 - 16)
+  if ((long long)batch * max_tokens > INT32_MAX - 65536 || max_pages > INT32_MAX / 16 - 16)
     return fail(PIC_ERR_UNSUPPORTED, "%s: 2^31 tokens or positions", who);
   Params p;
   p.batch = batch;
@@ -294,16 +370,16 @@ extern "C" pic_status_t pic_append_normed(const pic_geom_t *geom, int32_t layer,
   if (!p.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
   const int units = (p.Hq + p.Hkv) * (D / 16);
   const int threads = std::min(kMaxThreads, (units + 31) / 32 * 32);
-  const char *env = getenv("PIC_RUN");
-  // as many CTAs as an SM holds, if that leaves each a token
-  const long long tokens = (long long)batch * max_tokens, resident = 152ll * std::max(1, 65536 / (64 * threads));
-  p.run = env ? atoi(env) : (int)std::min<long long>(kMaxRun, (tokens + resident - 1) / resident);
-  const dim3 grid((unsigned)(batch * ((max_tokens + p.run - 1) / p.run)));
+  // as many CTAs as the SMs hold
+  const long long tokens = (long long)batch * max_tokens;
+  const long long resident = 152ll * std::min(8, std::max(1, 65536 / (64 * threads)));
+  const bool ragged = num_tokens && batch > 1 && max_tokens > 1 && batch <= kMaxRagged;
+  void (*kernel)(Params, RopeParams) = D == 128 ? ragged ? append_kernel<128, true> : append_kernel<128, false>
+                                                : ragged ? append_kernel<64, true> : append_kernel<64, false>;
+  const dim3 grid((unsigned)std::min(tokens, resident));
   const size_t smem = (size_t)kStages * 48 * threads;
-  cudaError_t e = cudaFuncSetAttribute(D == 128 ? append_kernel<128> : append_kernel<64>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, kStages * 48 * kMaxThreads);
-  if (e == cudaSuccess)
-    e = D == 128 ? launch_dependent(append_kernel<128>, grid, dim3(threads), smem, stream, p, rp)
-                 : launch_dependent(append_kernel<64>, grid, dim3(threads), smem, stream, p, rp);
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       kStages * 48 * kMaxThreads);
+  if (e == cudaSuccess) e = launch_dependent(kernel, grid, dim3(threads), smem, stream, p, rp);
   return e == cudaSuccess ? PIC_OK : cuda_fail(e, who);
 }
