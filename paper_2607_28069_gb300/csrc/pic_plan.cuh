@@ -36,6 +36,7 @@ struct alignas(16) Share {  // of a CTA: its first unit
   long long pos, end, unit0;
   int32_t item, hk, pair, pad;
   long long pad2;
+  Item it;  // the item
 };
 struct alignas(16) Link {  // a node of an entry's chain, by level
   long long base;

@@ -13,6 +13,7 @@
 //     others leave partial states.
 //  2. merge_kernel: log-sum-exp merge along each entry's chain of nodes.
 #include <algorithm>
+#include <cstdlib>
 
 #include "pic_plan.cuh"
 
@@ -25,7 +26,6 @@ constexpr int kThreads = 384;    // K producer, MMA, V producer, ring, two softm
 constexpr int kBoundThreads = 448;  // 127 registers a thread: merge CTAs fit beside one on an SM
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;  // S_t at 128 t, O_t at 256 + D t
-constexpr int kItems = 40;       // items of a CTA's share kept in shared memory
 // Named barriers (0: __syncthreads): P_t from warpgroup t to the MMA warp, the ring warp's
 // word to the MMA warp, the two warpgroups' exchange.
 constexpr int kNbP = 1, kNbRing = 3, kNbPair = 4;
@@ -36,9 +36,8 @@ struct Layout {
   static constexpr int kQ = 0;
   static constexpr int kK = kQ + NQB * kTile;
   static constexpr int kV = kK + NSK * kTile;
-  static constexpr int kML = kV + NSV * kTile;  // float [2][BM]: the warpgroups' m, then l
-  static constexpr int kItem = kML + 2 * BM * 4;
-  static constexpr int kBar = kItem + kItems * (int)sizeof(Item);
+  static constexpr int kML = kV + NSV * kTile;  // float2 [2][BM]: the warpgroups' m and l
+  static constexpr int kBar = kML + 2 * BM * 8;
   static constexpr int kAlloc = kBar + 256;
 };
 static_assert(Layout<128>::kAlloc <= 227 * 1024, "shared memory");
@@ -83,49 +82,40 @@ PIC_DEV bool plan_fits(const Params &p, const Header &h) {
 struct Segments {
   const Params &p;
   const View v;
-  uint32_t items_s;       // shared memory: items first .. first + kItems - 1
-  int first_item, n_items;
+  int n_items;
   long long pos, end, unit0, cost;
   int item, cta;
   bool started;
-  Item it;
+  Item it, ahead;  // the item; the one behind it, on its way
   int rt, hk, pair;
   // the present segment
   int kt0, n;        // of the item's tiles
   bool two;          // two row tiles
   bool first, last;  // holds the unit's first, last key tile
 
-  PIC_DEV Segments(const Params &pp, int cta_, uint32_t items)
-      : p(pp), v(pp.plan, pp.n), items_s(items), cta(cta_), started(false) {
+  PIC_DEV Segments(const Params &pp, int cta_) : p(pp), v(pp.plan, pp.n), cta(cta_), started(false) {
     const Header h = *v.head;
     const Share s = v.shares[cta];
     pos = s.pos, end = plan_fits(p, h) ? s.end : s.pos;
-    unit0 = s.unit0, first_item = item = s.item, n_items = h.items;
+    unit0 = s.unit0, item = s.item, n_items = h.items;
     hk = s.hk, pair = s.pair;
-    it.m = it.tiles = rt = kt0 = n = 0;
+    it = s.it;
+    rt = (it.m + p.ept - 1) / p.ept;
+    kt0 = n = 0;
     two = first = last = false;
     cost = 0;
+    if (pos < end) look_ahead();
   }
   PIC_DEV void take(const Segments &o) {
-    pos = o.pos, unit0 = o.unit0, cost = o.cost, item = o.item, started = o.started, it = o.it;
+    pos = o.pos, unit0 = o.unit0, cost = o.cost, item = o.item, started = o.started, it = o.it, ahead = o.ahead;
     rt = o.rt, hk = o.hk, pair = o.pair, kt0 = o.kt0, n = o.n, two = o.two, first = o.first, last = o.last;
   }
-  PIC_DEV void load_item() {
-    const int at = item - first_item;
-    if (at < kItems) {
-      const uint4 a = lds128(items_s + at * 32), b = lds128(items_s + at * 32 + 16);
-      it = Item{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
-    } else {
-      it = v.items[item];
-    }
-    rt = (it.m + p.ept - 1) / p.ept;
-  }
+  PIC_DEV void look_ahead() { ahead = v.items[min(item + 1, n_items - 1)]; }
   PIC_DEV bool next() {
     for (;;) {
       if (pos >= end) return false;
       if (!started) {
         started = true;
-        load_item();
       } else {
         unit0 += cost;
         if (unit0 >= end) {
@@ -140,7 +130,9 @@ struct Segments {
               pos = end;
               return false;
             }
-            load_item();
+            it = ahead;
+            rt = (it.m + p.ept - 1) / p.ept;
+            look_ahead();
           }
         }
       }
@@ -172,6 +164,9 @@ PIC_DEV int page_row(const Params &p, int page, int hk) {
   return (int)(p.layer_row0 + ((long long)page * p.Hkv + hk) * 16);
 }
 
+PIC_DEV void arrive_twice(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 2;" ::"r"(bar) : "memory");
+}
 PIC_DEV void st_global32(void *p, const float *f) {
   asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]),
                "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7])
@@ -234,28 +229,24 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
     tmem_alloc(smem_u32(tmem_slot), kTmemCols);
     tmem_relinquish();
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  {  // the share's items
-    const View v(p.plan, p.n);
-    const int first = v.shares[blockIdx.x].item, left = v.head->items - first;
-    if (plan_fits(p, *v.head) && (int)threadIdx.x < min(left, kItems) * 2)
-      sts128(sbase + L::kItem + threadIdx.x * 16, reinterpret_cast<const uint4 *>(v.items + first)[threadIdx.x]);
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tbase = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int detail = -2;
 
-  Segments sg(p, (int)blockIdx.x, sbase + L::kItem);
+  int first4 = -1;  // (the producers': the first pages come with the share)
+  if (warp == 0 || warp == 2) first4 = View(p.plan, p.n).first_pages[blockIdx.x * kFirstPages + lane];
+  Segments sg(p, (int)blockIdx.x);
   if (threadIdx.x == 0 && blockIdx.x == 0 && !plan_fits(p, *sg.v.head)) dev_fail(p.status, PIC_DEV_BAD_REQUEST, -1);
   if (warp >= 4) {
     // ===================================================== softmax
     const int t = (warp - 4) >> 2, wq = warp & 3, row = wq * 32 + lane;
     const uint32_t tl = tbase + ((uint32_t)(wq * 32) << 16);
     const uint32_t tS = tl + t * 128, tO = tl + kColO + t * D;
-    float *ml_s = reinterpret_cast<float *>(smem + L::kML);
+    float2 *ml_s = reinterpret_cast<float2 *>(smem + L::kML);
     int nS = 0, nEnd = 0;  // tiles and segments of this warpgroup
     bool ok = true;
     // The MMA warp commits every S_t and every segment's end, also after an abort
@@ -264,7 +255,8 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
       ok = mbar_wait_while(ok, bar(i), parity, p.status, detail, 4 * kWaitLimitNs);
       if (was && !ok) *abort_flag = 1;
     };
-    while (sg.next()) {
+    bool more = sg.next();
+    while (more) {
       const int n = sg.count(t);
       const int rows = sg.tile_rows(sg.two ? t : 0);
       const bool live = wq * 32 < rows;  // of the warp
@@ -357,60 +349,54 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
         __syncwarp();
         named_bar_arrive(kNbP + t, 128 + 32);
       }
-      // ---- the segment's rows: after its last PV, o = w_0 O_0 + w_1 O_1 (with one
-      // row tile), or O_t alone
+      // ---- the segment's rows: after its last PV, o = w_0 O_0 + w_1 O_1 (with one row tile
+      // and several key tiles), or O_t alone.  Where they go, and the next segment, while the
+      // PV is under way.
+      const bool two = sg.two, both = !two && sg.n > 1, whole = sg.first && sg.last;
+      const int tile = 2 * sg.pair + (two ? t : 0);
+      const int entry = sg.it.begin + tile * p.ept + row / p.G;
+      const size_t o_row = (size_t)entry * p.Hq + sg.hk * p.G + row % p.G;
+      const bool done = whole && sg.it.leaf && sg.it.level == 0;  // all of the entry's keys
+      // partial states: a CTA has at most one segment that ends a unit begun elsewhere or lies
+      // inside one (0), and one that begins a unit and leaves its end to others (1)
+      const size_t p_row = whole ? kPieceRows + (size_t)sg.it.level * p.n * p.Hq + o_row
+                                 : ((size_t)(2 * sg.cta + (sg.first ? 1 : 0)) * 2 + (two ? t : 0)) * BM + row;
+      more = sg.next();
       if (n > 0) {
         wait(B_OEND + t, nEnd & 1);
         ++nEnd;
         tc_fence_after();
       }
       float M = m_used, w0 = 1.f, w1 = 0.f;
-      if (!sg.two) {  // m, then l through one array of shared memory
-        auto exchange = [&](float v) {
-          ml_s[t * BM + row] = v;
-          named_bar_sync(kNbPair, 256);
-          const float other = ml_s[(t ^ 1) * BM + row];
-          named_bar_sync(kNbPair, 256);
-          return other;
-        };
+      if (both) {  // (read before the next segment's PV, and so before the next write)
+        ml_s[t * BM + row] = make_float2(m_used, l);
         tc_fence_before();
-        const float mo = exchange(m_used), lo = exchange(l);
+        named_bar_sync(kNbPair, 256);
         tc_fence_after();
-        M = fmaxf(m_used, mo);
+        const float2 o = ml_s[(t ^ 1) * BM + row];
+        M = fmaxf(m_used, o.x);
         const float wt = m_used == -INFINITY ? 0.f : ex2(m_used - M);
-        const float wo = mo == -INFINITY ? 0.f : ex2(mo - M);
-        l = t ? fmaf(lo, wo, l * wt) : fmaf(l, wt, lo * wo);  // l_0 w_0 + l_1 w_1 in both
+        const float wo = o.x == -INFINITY ? 0.f : ex2(o.x - M);
+        l = t ? fmaf(o.y, wo, l * wt) : fmaf(l, wt, o.y * wo);  // l_0 w_0 + l_1 w_1 in both
         w0 = t ? wo : wt;
         w1 = t ? wt : wo;
       }
-      if (live) {
-        const int tile = 2 * sg.pair + (sg.two ? t : 0);
-        const bool store = row < rows && ok && !*abort_flag, whole = sg.first && sg.last;
-        const int entry = sg.it.begin + tile * p.ept + row / p.G, head = sg.hk * p.G + row % p.G;
-        const size_t o_row = (size_t)entry * p.Hq + head;
-        const bool done = whole && sg.it.leaf && sg.it.level == 0;  // all of the entry's keys
-        // partial states: a CTA has at most one segment that ends a unit begun elsewhere or lies
-        // inside one (0), and one that begins a unit and leaves its end to others (1)
-        const size_t p_row = whole ? kPieceRows + ((size_t)sg.it.level * p.n + entry) * p.Hq + head
-                                   : ((size_t)(2 * sg.cta + (sg.first ? 1 : 0)) * 2 + (sg.two ? t : 0)) * BM + row;
+      if (live && (two || both || t == 0)) {
+        const bool store = row < rows && ok && !*abort_flag;
         const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
-        const int c_begin = sg.two ? 0 : t * (D / 64), c_end = sg.two ? D / 32 : (t + 1) * (D / 64);
-        const uint32_t tA = sg.two ? tO : tl + kColO;
+        const int c_begin = both ? t * (D / 64) : 0, c_end = both ? (t + 1) * (D / 64) : D / 32;
+        const uint32_t tA = two ? tO : tl + kColO;
 #pragma unroll 1
         for (int c = c_begin; c < c_end; ++c) {
           float o[32];
           tmem_ld32(tA + c * 32, reinterpret_cast<uint32_t *>(o));
           tmem_wait_ld();
-          if (!sg.two) {
+          if (both) {
+            float o1[32];
+            tmem_ld32(tA + D + c * 32, reinterpret_cast<uint32_t *>(o1));
+            tmem_wait_ld();
 #pragma unroll
-            for (int q = 0; q < 32; ++q) o[q] *= w0;
-            if (sg.n > 1) {  // (with one tile O_1 was never written)
-              float o1[32];
-              tmem_ld32(tA + D + c * 32, reinterpret_cast<uint32_t *>(o1));
-              tmem_wait_ld();
-#pragma unroll
-              for (int q = 0; q < 32; ++q) o[q] = fmaf(o1[q], w1, o[q]);
-            }
+            for (int q = 0; q < 32; ++q) o[q] = fmaf(o1[q], w1, o[q] * w0);
           }
           if (done) {
 #pragma unroll
@@ -425,7 +411,7 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
             for (int q = 0; q < 32; q += 8) st_global32(p.part_o + p_row * D + c * 32 + q, o + q);
           }
         }
-        if (store && (sg.two || t == 0)) {
+        if (store && (two || t == 0)) {
           if (!done)
             p.part_ml[p_row] = make_float2(l == 0.f ? -INFINITY : M, l);
           else if (p.lse)
@@ -434,7 +420,12 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_ODONE));
+      // Of a segment of a single tile warpgroup 1 has nothing: it does not wait for the segment
+      // and would be ahead with its arrivals, so warpgroup 0 arrives for both.
+      if (lane == 0 && (two || both))
+        mbar_arrive(bar(B_ODONE));
+      else if (lane == 0 && t == 0)
+        arrive_twice(bar(B_ODONE));
     }
   } else if (warp == 0 || warp == 2) {
     // ===================================================== TMA producers
@@ -453,7 +444,6 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
       return j + lane / 8 < a.n && pidx * 16 < a.it.keys ? p.block_table[(size_t)a.it.row * p.max_pages + pidx] : -2;
     };
     Segments ahead = sg;
-    int first4 = sg.v.first_pages[blockIdx.x * kFirstPages + lane];
     bool more = ahead.next();
     if (more && (ahead.item != sg.item || ahead.hk != sg.hk || ahead.pair != sg.pair))
       first4 = entry(ahead, 0);  // (no tile of the share's first unit begins in it)
@@ -666,19 +656,28 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
 
 // ------------------------------------------------------------------- merge
 // o = sum_c w_c O_c / sum_c w_c l_c, w_c = 2^(m_c - M), over the parts of an entry's nodes: one
-// state for a unit that lay within a CTA, else one for each of its CTAs.  A warp per (entry,
-// query head).
+// state for a unit that lay within a CTA, else one for each of its CTAs.  kWarps warps per
+// (entry, query head), each with its share of the parts: the (m, l) pairs of all of them first
+// (a lane per part), then the O rows, U loads in flight; the warps' sums are combined in shared
+// memory in a fixed order.
 constexpr float kFloatMax = 3.402823466e38f;
-constexpr int kMergeWarps = 4;
+// acc + w v.  A weight that has underflowed to 0 does not hide an infinity or a NaN.
+PIC_DEV float weigh(float w, float v, float acc) {
+  return w != 0.f || fabsf(v) <= kFloatMax ? fmaf(w, v, acc) : acc + v;
+}
 
-template <int D>
-__global__ void __launch_bounds__(32 * kMergeWarps) merge_kernel(Params p) {
-  constexpr int CPL = D / 32, U = 4;
+template <int D, int kWarps, int U>
+__global__ void __launch_bounds__(128) merge_kernel(Params p) {
+  constexpr int CPL = D / 32, kRows = 4 / kWarps;
+  constexpr int kParts = kCtas + 2 * kDepth;  // at most: neighbouring nodes' CTAs overlap by one
+  constexpr int KW = ((kParts + kWarps - 1) / kWarps + 31) / 32;  // parts of a lane
+  __shared__ float acc_s[4][D], m_s[4], l_s[4];
+  __shared__ size_t row_s[4][KW * 32];  // the rows of a warp's parts
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long work = (long long)blockIdx.x * kMergeWarps + warp;
-  const int entry = (int)(work / p.Hq), h = (int)(work % p.Hq);
-  if (entry >= p.n) return;
+  const int work = blockIdx.x * kRows + warp / kWarps;
+  const int entry = work / p.Hq, h = work - entry * p.Hq;
+  if (entry >= p.n) return;  // (kWarps = 4: the whole CTA)
   const View v(p.plan, p.n);
   const Header hd = *v.head;
   const int keys = v.keys[entry];
@@ -686,100 +685,127 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_kernel(Params p) {
   Link k{0, 0, 0, 0, 0, {0, 0}};
   if (lane < kDepth) k = v.chain[(size_t)entry * kDepth + lane];
   if (!plan_fits(p, hd) || keys < 0) return;  // an entry that is left alone
-  const Deal deal(hd.total, hd.ctas);
-  const int hk = h / p.G, e = entry - k.begin, tile = e / p.ept, pair = tile / 2;
-  int count = 0, c0 = 0, t = 0;
+  int count = 0, c0 = 0, piece = 0;
   if (k.tiles > 0) {
+    const Deal deal(hd.total, hd.ctas);
+    const int e = entry - k.begin, tile = e / p.ept, pair = tile / 2;
     const Units u(k.m, k.tiles, p.ept);
-    const long long unit0 = k.base + hk * u.per_head() + pair * u.pair_cost();
+    const long long unit0 = k.base + h / p.G * u.per_head() + pair * u.pair_cost();
     const int w = u.weight(pair);
     c0 = deal.owner(tile_step(unit0, 0, w));
     count = deal.owner(tile_step(unit0, k.tiles - 1, w)) - c0 + 1;
-    t = u.two(pair) ? tile & 1 : 0;
+    piece = (u.two(pair) ? tile & 1 : 0) * BM + (e - tile * p.ept) * p.G + h % p.G;
   }
-  const int piece = t * BM + e % p.ept * p.G + h % p.G;  // of the first CTA's slot: + 2 (2 cta + 1) BM
-  int pre[kDepth + 1], at[kDepth], off[kDepth];
-  pre[0] = 0;
+  int end = count;  // parts up to this level's
 #pragma unroll
-  for (int j = 0; j < kDepth; ++j) {
-    pre[j + 1] = pre[j] + __shfl_sync(0xffffffffu, count, j);
-    at[j] = __shfl_sync(0xffffffffu, c0, j);
-    off[j] = __shfl_sync(0xffffffffu, piece, j);
+  for (int o = 1; o < 8; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, end, o);
+    if (lane >= o) end += y;
   }
-  const int parts = pre[kDepth];
+  const int parts = __shfl_sync(0xffffffffu, end, kDepth - 1);
   if (parts == 1 && __any_sync(0xffffffffu, k.alone)) return;  // done by its CTA
-  auto part_row = [&](int c) {
-    size_t r = 0;
+  // this warp's parts are w0, w0 + kWarps, ...
+  const int w0 = warp % kWarps, mine = (parts - w0 + kWarps - 1) / kWarps;
+  float w[KW], l = 0.f, M = -INFINITY;
+  float2 ml[KW];
 #pragma unroll
-    for (int j = 0; j < kDepth; ++j)
-      if (c >= pre[j] && c < pre[j + 1]) {
-        const int i = c - pre[j];
-        r = pre[j + 1] - pre[j] == 1 ? kPieceRows + ((size_t)j * p.n + entry) * p.Hq + h
-                                     : ((size_t)(at[j] + i) * 2 + (i == 0 ? 1 : 0)) * 2 * BM + off[j];
-      }
-    return r;
-  };
-  float M = -INFINITY, l = 0.f, acc[CPL];
+  for (int q = 0; q < KW; ++q) {
+    const int c = (lane + 32 * q) * kWarps + w0;
+    size_t row = 0;
 #pragma unroll
-  for (int q = 0; q < CPL; ++q) acc[q] = 0.f;
-  bool under = false;
-  for (int b = 0; b < parts; b += 32) {
-    const float2 ml = b + lane < parts ? p.part_ml[part_row(b + lane)] : make_float2(-INFINITY, 0.f);
-    float m = ml.x;
+    for (int j = 0; j < kDepth; ++j) {
+      const int e1 = __shfl_sync(0xffffffffu, end, j), n = __shfl_sync(0xffffffffu, count, j);
+      const int at = __shfl_sync(0xffffffffu, c0, j), off = __shfl_sync(0xffffffffu, piece, j), i = c - (e1 - n);
+      if (i >= 0 && i < n)
+        row = n == 1 ? kPieceRows + ((size_t)j * p.n + entry) * p.Hq + h
+                     : ((size_t)(at + i) * 2 + (i == 0 ? 1 : 0)) * 2 * BM + off;
+    }
+    row_s[warp][lane + 32 * q] = row;
+    ml[q] = lane + 32 * q < mine ? p.part_ml[row] : make_float2(-INFINITY, 0.f);
+  }
+  __syncwarp();
+  float x[U][CPL], acc[CPL];
+  auto load = [&](int b) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    m = fmaxf(m, M);
-    const float old = M == -INFINITY ? 0.f : ex2(M - m);
-    M = m;
-    l *= old;
-#pragma unroll
-    for (int q = 0; q < CPL; ++q) acc[q] *= old;
-    const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - M);
-    under |= b + lane < parts && w == 0.f;
-    l = fmaf(w, ml.y, l);
-#pragma unroll 1
-    for (int c = b; c < min(b + 32, parts); c += U) {
-      float x[U][CPL];
-#pragma unroll
-      for (int k2 = 0; k2 < U; ++k2) {
-        const float *src = p.part_o + part_row(min(c + k2, parts - 1)) * D + lane * CPL;
-        if constexpr (CPL == 4) {
-          const float4 f = *reinterpret_cast<const float4 *>(src);
-          x[k2][0] = f.x, x[k2][1] = f.y, x[k2][2] = f.z, x[k2][3] = f.w;
-        } else {
-          const float2 f = *reinterpret_cast<const float2 *>(src);
-          x[k2][0] = f.x, x[k2][1] = f.y;
-        }
-      }
-#pragma unroll
-      for (int k2 = 0; k2 < U; ++k2) {
-        const float wk = c + k2 < parts ? __shfl_sync(0xffffffffu, w, (c + k2) & 31) : 0.f;
-        if (wk != 0.f)
-#pragma unroll
-          for (int q = 0; q < CPL; ++q) acc[q] = fmaf(wk, x[k2][q], acc[q]);
+    for (int q = 0; q < U; ++q) {
+      const float *src = p.part_o + row_s[warp][min(b + q, mine - 1)] * D + lane * CPL;
+      if constexpr (CPL == 4) {
+        const float4 f = *reinterpret_cast<const float4 *>(src);
+        x[q][0] = f.x, x[q][1] = f.y, x[q][2] = f.z, x[q][3] = f.w;
+      } else {
+        const float2 f = *reinterpret_cast<const float2 *>(src);
+        x[q][0] = f.x, x[q][1] = f.y;
       }
     }
+  };
+  if (mine > 0) load(0);  // beside the (m, l) pairs
+#pragma unroll
+  for (int q = 0; q < KW; ++q) M = fmaxf(M, ml[q].x);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+#pragma unroll
+  for (int q = 0; q < KW; ++q) {
+    w[q] = ml[q].x == -INFINITY ? 0.f : ex2(ml[q].x - M);
+    l = fmaf(w[q], ml[q].y, l);
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+#pragma unroll
+  for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
+#pragma unroll 1
+  for (int b = 0; b < mine; b += U) {
+    if (b) load(b);
+    float wc = w[0];
+#pragma unroll
+    for (int q = 1; q < KW; ++q) wc = b >= 32 * q ? w[q] : wc;
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const float wk = __shfl_sync(0xffffffffu, wc, (b + q) & 31);  // 0 past the end
+      if (wk != 0.f)
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wk, x[q][e], acc[e]);
+    }
+  }
   // Infinities and NaN of parts whose weight underflowed to 0 (rare).  Adding those of the
   // other parts once more changes nothing.
+  bool under = false;
+#pragma unroll
+  for (int q = 0; q < KW; ++q) under |= lane + 32 * q < mine && w[q] == 0.f;
   if (__any_sync(0xffffffffu, under))
 #pragma unroll 1
-    for (int c = 0; c < parts; ++c)
+    for (int c = 0; c < mine; ++c)
 #pragma unroll 1
-      for (int q0 = 0; q0 < CPL; ++q0) {
-        const float x = p.part_o[part_row(c) * D + lane * CPL + q0];
-        if (fabsf(x) <= kFloatMax) continue;
+      for (int e = 0; e < CPL; ++e) {
+        const float y = p.part_o[row_s[warp][c] * D + lane * CPL + e];
+        if (fabsf(y) <= kFloatMax) continue;
 #pragma unroll
         for (int q = 0; q < CPL; ++q)
-          if (q == q0) acc[q] += x;
+          if (q == e) acc[q] += y;
       }
   const size_t o_row = (size_t)entry * p.Hq + h;
+  if constexpr (kWarps == 4) {
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) acc_s[warp][lane * CPL + e] = acc[e];
+    if (lane == 0) m_s[warp] = M, l_s[warp] = l;
+    __syncthreads();
+    if (warp) return;
+    const float mw[4] = {m_s[0], m_s[1], m_s[2], m_s[3]};
+    M = fmaxf(fmaxf(mw[0], mw[1]), fmaxf(mw[2], mw[3]));
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float wc = mw[c] == -INFINITY ? 0.f : ex2(mw[c] - M);
+      l = fmaf(wc, l_s[c], l);
+#pragma unroll
+      for (int e = 0; e < CPL; ++e) acc[e] = weigh(wc, acc_s[c][lane * CPL + e], acc[e]);
+    }
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN stays one)
   __nv_bfloat162 *dst = reinterpret_cast<__nv_bfloat162 *>(p.out + o_row * D + lane * CPL);
 #pragma unroll
-  for (int q = 0; q < CPL; q += 2) dst[q / 2] = __floats2bfloat162_rn(acc[q] * inv, acc[q + 1] * inv);
+  for (int e = 0; e < CPL; e += 2) dst[e / 2] = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
   if (lane == 0 && p.lse)
     p.lse[o_row] = l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994531f;
 }
@@ -800,8 +826,10 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tq1, const C
                        tq1, tk, tv, p);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)p.n * p.Hq;
-  return launch_dependent(merge_kernel<D>, dim3((unsigned)((rows + kMergeWarps - 1) / kMergeWarps)),
-                          dim3(32 * kMergeWarps), 0, stream, p);
+  const char *env = getenv("PIC_MW");
+  const bool one = env ? atoi(env) == 1 : rows > 8 * kCtas;
+  return launch_dependent(one ? merge_kernel<D, 1, 8> : merge_kernel<D, 4, 8>,
+                          dim3((unsigned)(one ? (rows + 3) / 4 : rows)), dim3(128), 0, stream, p);
 }
 
 }  // namespace share

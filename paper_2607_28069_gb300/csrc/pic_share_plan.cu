@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
     const int c = c0 + lane;
     int first_page = 0, row = -1, last_page = 0;  // of its first tiles
     if (lane < kShares && c < kCtas) {
-      Share sh{0, 0, 0, 0, 0, 0, 0, 0};
+      Share sh{0, 0, 0, 0, 0, 0, 0, 0, Item{0, 0, 0, 0, -1, 0, 0, 0}};
       if (c < ctas && total > 0) {
         const Deal deal(total, ctas);
         sh.pos = deal.first(c), sh.end = deal.first(c + 1);
@@ -300,6 +300,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
         node_of(lo, &o);
         const Units u(o.end - o.begin, o.tile_end - o.tile_begin, p.ept);
         sh.item = s.item[lo];
+        sh.it = Item{o.begin, o.end - o.begin, o.tile_begin, o.tile_end - o.tile_begin, o.row, o.keys, o.level, lo >= n};
         const long long off = sh.pos - s.base[lo], head = u.per_head();
         sh.hk = quotient(off, head);
         const long long in = off - sh.hk * head;
