@@ -99,7 +99,8 @@ __global__ void __launch_bounds__(kMaxThreads, 2) append_kernel(Params p, RopePa
   };
   auto zero = [&](int2 tok) {  // (the prefill multiplies every packed row)
     for (int u = tid; u < p.Hq * VC; u += threads)
-      st_global16(p.q_out + q_row(u / VC, tok) + u % VC * 8, make_uint4(0, 0, 0, 0));
+      if (tok.y * p.G + u / VC % p.G < p.r_pad)
+        st_global16(p.q_out + q_row(u / VC, tok) + u % VC * 8, make_uint4(0, 0, 0, 0));
   };
   auto head = [&](int u, int2 tok) {
     const int h = u / KC;
@@ -274,9 +275,13 @@ __global__ void __launch_bounds__(kMaxThreads, 2) append_kernel(Params p, RopePa
   if (p.num_tokens && tid == 0)  // counts that are none
     for (int b = blockIdx.x; b < p.batch; b += gridDim.x)
       if (p.num_tokens[b] < 0 || p.num_tokens[b] > p.max_tokens) dev_fail(p.status, PIC_DEV_BAD_REQUEST, b);
-  if (p.r_pad && p.num_tokens)
-    for (int tok = blockIdx.x; tok < p.batch * p.max_tokens; tok += gridDim.x)
-      if (tok % p.max_tokens >= count_of(tok / p.max_tokens)) zero(make_int2(tok / p.max_tokens, tok % p.max_tokens));
+  if (p.r_pad) {  // the rows behind each request's
+    const int each = (p.r_pad + p.G - 1) / p.G;
+    for (long long i = blockIdx.x; i < (long long)p.batch * each; i += gridDim.x) {
+      const int b = (int)(i / each), t = (int)(i % each);
+      if (t >= count_of(b)) zero(make_int2(b, t));
+    }
+  }
 }
 
 }  // namespace normed

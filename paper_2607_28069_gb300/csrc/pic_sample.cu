@@ -64,8 +64,9 @@ struct alignas(16) Entry {
   int32_t index;
 };
 struct alignas(16) Bins {
-  uint32_t count[kBins];    // entries, and their weights in parts of 12 bits: sums of 32 bits each
-  uint32_t part[3][kBins];
+  // Entries, and their weights in parts of 12 bits and one for a weight of 2^36 (taken as one
+  // less): sums of 32 bits for up to 2^20 + 256 entries.
+  uint32_t count[kBins], part[4][kBins];
   Entry list[2][kList];     // (a CTA may be at its second while another is at its first)
   Sum2 rank[kList];         // of the second half of the list ahead of an entry
   uint32_t list_n, first, pick_key;
@@ -405,12 +406,16 @@ struct Row {
   }
   PIC_DEV void clear(Bins &bn) const {
     uint4 *b = reinterpret_cast<uint4 *>(bn.count);  // and the parts behind
-    for (int i = threadIdx.x; i < kBins; i += kThreads) b[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < 5 * kBins / 4; i += kThreads) b[i] = make_uint4(0, 0, 0, 0);
   }
   template <bool kSums>
   PIC_DEV void count_in(Bins &bn, int bin, uint64_t w) const {
     atomicAdd(&bn.count[bin], 1u);
     if constexpr (kSums) {
+      if (w >> 36) {
+        atomicAdd(&bn.part[3][bin], 1u);
+        --w;
+      }
       atomicAdd(&bn.part[0][bin], (uint32_t)w & 4095u);
       atomicAdd(&bn.part[1][bin], (uint32_t)(w >> 12) & 4095u);
       if (w >> 24) atomicAdd(&bn.part[2][bin], (uint32_t)(w >> 24));
@@ -435,7 +440,7 @@ struct Row {
         n += ld_cluster32(at);
         if constexpr (kSums) {
           a = ld_cluster32(at + 4 * kBins), d = ld_cluster32(at + 8 * kBins), e = ld_cluster32(at + 12 * kBins);
-          s += a + ((uint64_t)d << 12) + ((uint64_t)e << 24);
+          s += a + ((uint64_t)d << 12) + ((uint64_t)e << 24) + ld_cluster32(at + 16 * kBins);
         }
       }
       for (int o = 1; o < parts; o <<= 1) {
@@ -501,11 +506,12 @@ struct Row {
   // The first entry in the order, of those that `last` keeps, with which their count (kCount) or
   // their sum reaches `target`, into `last`; returns the sum up to it (where weights are
   // counted).  Entries with z < z_min come behind it.  h: a histogram over z that is there
-  // already, of all entries.
+  // already, of all entries, and so of some behind `last`.
   template <bool kCount>
   PIC_DEV uint64_t select(Bins &bn, const Rule &rule, Last &last, uint64_t target, float z_min, Hist &h) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool with_sums = !kCount || h.there;  // (then also the refinements')
+    const Last among = h.there ? Last() : last;  // (what is sought is among what `last` keeps either way)
     uint32_t lo = 0, hi = 0xffffffffu;  // its key is one of [lo, hi]
     int shift = -1, zbin = -1;          // shift < 0: bins over z
     uint64_t sum0 = 0;                  // of the entries ahead of the bin
@@ -521,7 +527,7 @@ struct Row {
       if (!h.there) {
         clear(bn);
         __syncthreads();
-        each(rule, last, z_min, z_max, [&](float x, float z, int) {
+        each(rule, among, z_min, z_max, [&](float x, float z, int) {
           const int k = bin_of(x, z);
           if (k < 0) return;
           if (with_sums) count_in<true>(bn, k, rule.weight(x));
@@ -554,7 +560,7 @@ struct Row {
           }
         }
         __syncthreads();
-        each(rule, last, z_min, z_max, [&](float x, float z, int i) {
+        each(rule, among, z_min, z_max, [&](float x, float z, int i) {
           if (bin_of(x, z) != at.bin) return;
           const uint32_t e = bn.first + atomicAdd(&bn.list_n, 1u);
           if (e >= kList) return;
@@ -597,8 +603,8 @@ struct Row {
         const uint32_t key = hi - (uint32_t)at.bin;
         const float v = logit_of(key);
         const uint64_t w = rule.weight(v), r = kCount ? target - count0 : (target - sum0 - 1) / w + 1;
-        const Total tot = equals(v, last);
-        find(r - 1, tot, [&](float x, int i) -> uint64_t { return x == v && last.keeps(x, i); },
+        const Total tot = equals(v, among);
+        find(r - 1, tot, [&](float x, int i) -> uint64_t { return x == v && among.keeps(x, i); },
              [&](int i, uint64_t) {
                for (int c = 0; c < C; ++c) st_cluster32(map_to_rank(smem_u32(&fx.found), c), (uint32_t)i);
              });
@@ -609,7 +615,7 @@ struct Row {
       if (shift < 0) {  // the bin's keys
         zbin = at.bin;
         uint32_t k_lo = 0xffffffffu, k_hi = 0;
-        each(rule, last, z_min, z_max, [&](float x, float z, int) {
+        each(rule, among, z_min, z_max, [&](float x, float z, int) {
           if (bin_of(x, z) != at.bin) return;
           k_lo = min(k_lo, key_of(x)), k_hi = max(k_hi, key_of(x));
         });
@@ -825,6 +831,8 @@ static cudaError_t launch(Params p, int batch, cudaStream_t stream) {
   auto attempt = [&](int C) {
     const int chunks = (p.vocab + 16 / (int)sizeof(T) - 1 + kChunk - 1) / kChunk;
     const int mine = (chunks + C - 1) / C;
+    // (see Bins: 4095 times the entries of a part stay below 2^32)
+    if (p.bins && 4095ll * mine * kChunk >= 1ll << 32) return cudaErrorInvalidConfiguration;
     // (of Bins::seg a CTA uses the first kBins / C)
     const size_t bins = sizeof(Bins) - sizeof(Sum2) * (kBins - kBins / C);
     const size_t fixed = sizeof(Fixed) + (p.bins ? bins : 0) + (size_t)mine * 8 + 16;

@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
   const long long total = at;
   __syncthreads();
   // each CTA's first unit: lane l < kShares of a warp finds the one of CTA kShares warp + l
-  const int ctas = (int)min((long long)kCtas, max(1ll, total / (kUnit + kOne)));
+  const int ctas = (int)min((long long)kCtas, max(1ll, total / kLeast));
   if (tid == 0) *v.head = Header{kMagic, n, p.hkv, p.ept, p.rows, p.max_pages, items, ctas, total, 0};
   constexpr int kShares = 5;
   static_assert(kShares * 32 >= kCtas, "a warp's share of the CTAs");

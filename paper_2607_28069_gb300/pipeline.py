@@ -8,12 +8,13 @@ from __future__ import annotations
 
 import torch
 
-from . import (Geometry, _check, _native, pic_append_inline, pic_attend_decode, pic_attend_draft,
-               pic_attend_prefill, pic_attend_prefill_fused, pic_compose, pic_copy_async,
-               pic_decode_workspace_size, pic_draft_workspace_size, pic_link, pic_page_compact,
-               pic_page_compact_workspace_size, pic_page_fork, pic_page_free, pic_page_reserve,
-               pic_prefill_fused_workspace_size, pic_prefill_plan_splits, pic_relocate,
-               pic_relocate_mapped, pic_verify_draft)
+from . import (Geometry, _check, _native, pic_append_inline, pic_append_normed, pic_attend_decode,
+               pic_attend_draft, pic_attend_prefill, pic_attend_prefill_fused, pic_attend_shared,
+               pic_compose, pic_copy_async, pic_decode_workspace_size, pic_draft_workspace_size,
+               pic_link, pic_page_compact, pic_page_compact_workspace_size, pic_page_fork,
+               pic_page_free, pic_page_reserve, pic_prefill_fused_workspace_size,
+               pic_prefill_plan_splits, pic_relocate, pic_relocate_mapped, pic_sample,
+               pic_share_plan, pic_share_plan_size, pic_shared_workspace_size, pic_verify_draft)
 from .workloads import Workload
 
 
@@ -345,13 +346,74 @@ class CacheHitPath:
             self.decode(step, layer)
 
 
-class DraftDecoder:
-    """Speculative decoding over the contexts that a CacheHitPath has linked.
+class _Rows:
+    """Rows of a block table over the cache of a CacheHitPath.
 
     Rows 0 .. B - 1 are the path's requests as its prefill left them; further rows
     are empty until ``fork`` makes them branches.  Every row's pages come from the
     path's cache, whose pages beyond the requests' own (a workload with a larger
-    ``num_pages``, or decode steps it does not take) are the free ones.  One step:
+    ``num_pages``, or decode steps it does not take) are the free ones.
+    ``reserve``: positions that a step appends to a row, at most.
+    """
+
+    def __init__(self, path: CacheHitPath, reserve: int, rows: int | None, max_new: int):
+        wl, dev = path.wl, path.k_cache.device
+        self.path, self.geom, self.reserve = path, path.geom, reserve
+        self.num_pages = wl.num_pages
+        B, have = wl.block_table.shape
+        self.rows = max(B, rows or B)
+        page = wl.spec.page_size
+        max_pages = max(have, -(-(path.max_ctx + max_new + reserve) // page))
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.block_table = torch.full((self.rows, max_pages), -1, **i32)
+        self.block_table[:B, :have] = wl.block_table
+        self.ctx_len = torch.zeros(self.rows, **i32)
+        self.ctx_len[:B] = path.ctx_len
+        used = wl.block_table[wl.block_table >= 0].long()
+        self.page_refs = torch.bincount(used, minlength=self.num_pages).to(torch.int32)
+        self.result = torch.empty(self.rows, **i32)
+        self._use(range(B))
+
+    def _use(self, rows):
+        self.in_use = list(rows)
+        self._active = self._rows(self.in_use)
+
+    def _rows(self, rows):
+        return torch.tensor(list(rows), dtype=torch.int32, device=self.block_table.device)
+
+    def begin(self):
+        pic_page_reserve(self._active, self.reserve, self.ctx_len, self.block_table,
+                         self.num_pages, self.page_refs, self.result[:len(self.in_use)])
+
+    def fork(self, src, dst):
+        """Rows dst (not in use) become branches of rows src: two lists of row numbers.
+
+        Returns the branches' lengths.  Where the device could not make one (no free
+        pages, a table too short: pic_device_status) its length is -1, and its row stays
+        empty and out of use.  Waits for the device: forks are made between steps, not in
+        a captured one."""
+        if len(src) != len(dst) or set(dst) & set(self.in_use) or len(set(dst)) < len(dst):
+            raise ValueError("fork: every branch needs a row of its own that is not in use")
+        result = torch.empty(len(dst), dtype=torch.int32, device=self.block_table.device)
+        pic_page_fork(self.geom, self._rows(src), self._rows(dst), self.ctx_len, self.block_table,
+                      self.num_pages, self.page_refs, self.path.k_cache, self.path.v_cache,
+                      result, reserve=self.reserve)
+        lengths = result.tolist()
+        self._use(self._joined([(a, b) for a, b, n in zip(src, dst, lengths) if n >= 0]))
+        return lengths
+
+    def _joined(self, branches):  # the rows in use with new (source, branch) pairs
+        return sorted(self.in_use + [b for _, b in branches])
+
+    def release(self, rows):
+        """The listed rows end: their pages go back."""
+        pic_page_free(self._rows(rows), self.block_table, self.num_pages, self.page_refs, self.ctx_len)
+        self._use([r for r in self.in_use if r not in set(rows)])
+
+
+class DraftDecoder(_Rows):
+    """Speculative decoding over the contexts that a CacheHitPath has linked, and over
+    their branches (see _Rows).  One step:
 
     * ``begin`` -- room for max_draft tokens behind every row in use;
     * ``attend`` per layer -- the drafts' keys and values appended, their attention
@@ -365,23 +427,11 @@ class DraftDecoder:
 
     def __init__(self, path: CacheHitPath, max_draft: int, rows: int | None = None,
                  max_new: int = 256):
-        wl, dev = path.wl, path.k_cache.device
-        self.path, self.geom, self.max_draft = path, path.geom, max_draft
-        self.num_pages = wl.num_pages
-        B, have = wl.block_table.shape
-        self.rows = max(B, rows or B)
-        page = wl.spec.page_size
-        max_pages = max(have, -(-(path.max_ctx + max_new + max_draft) // page))
+        super().__init__(path, max_draft, rows, max_new)
+        self.max_draft = max_draft
+        dev = path.k_cache.device
         i32 = dict(dtype=torch.int32, device=dev)
-        self.block_table = torch.full((self.rows, max_pages), -1, **i32)
-        self.block_table[:B, :have] = wl.block_table
-        self.ctx_len = torch.zeros(self.rows, **i32)
-        self.ctx_len[:B] = path.ctx_len
-        used = wl.block_table[wl.block_table >= 0].long()
-        self.page_refs = torch.bincount(used, minlength=self.num_pages).to(torch.int32)
         self.all_rows = torch.arange(self.rows, **i32)
-        self._use(range(B))
-        self.result = torch.empty(self.rows, **i32)
         self.path_idx = torch.empty((self.rows, max_draft), **i32)
         self.path_len = torch.empty(self.rows, **i32)
         self.next_token = torch.empty(self.rows, **i32)
@@ -392,17 +442,6 @@ class DraftDecoder:
                               device=dev)
         self.ws_compact = torch.empty(pic_page_compact_workspace_size(g, self.rows, max_draft),
                                       dtype=torch.uint8, device=dev)
-
-    def _use(self, rows):
-        self.in_use = sorted(rows)
-        self._active = self._rows(self.in_use)
-
-    def _rows(self, rows):
-        return torch.tensor(list(rows), dtype=torch.int32, device=self.block_table.device)
-
-    def begin(self):
-        pic_page_reserve(self._active, self.max_draft, self.ctx_len, self.block_table,
-                         self.num_pages, self.page_refs, self.result[:len(self.in_use)])
 
     def attend(self, layer: int, q, k, v, draft_len, parent=None, lse=None):
         """Drafts of one layer: q [rows][max_draft][Hq][d], k and v
@@ -419,24 +458,62 @@ class DraftDecoder:
                          self.path.v_cache, self.result, reserve=self.max_draft,
                          workspace=self.ws_compact)
 
-    def fork(self, src, dst):
-        """Rows dst (not in use) become branches of rows src: two lists of row numbers.
 
-        Returns the branches' lengths.  Where the device could not make one (no free
-        pages, a table too short: pic_device_status) its length is -1, and its row stays
-        empty and out of use.  Waits for the device: forks are made between steps, not in
-        a captured one."""
-        if len(src) != len(dst) or set(dst) & set(self.in_use) or len(set(dst)) < len(dst):
-            raise ValueError("fork: every branch needs a row of its own that is not in use")
-        result = torch.empty(len(dst), dtype=torch.int32, device=self.block_table.device)
-        pic_page_fork(self.geom, self._rows(src), self._rows(dst), self.ctx_len, self.block_table,
-                      self.num_pages, self.page_refs, self.path.k_cache, self.path.v_cache,
-                      result, reserve=self.max_draft)
-        lengths = result.tolist()
-        self._use(self.in_use + [row for row, n in zip(dst, lengths) if n >= 0])
-        return lengths
+class BranchDecoder(_Rows):
+    """Decoding of branches of linked contexts together, a token a step, for Readers with or
+    without norms of their query and key heads.  ``in_use`` lists the rows of a step, a branch
+    behind what it was forked from, so that those that share pages are neighbours.  One step,
+    with n = len(in_use) and everything in that order:
 
-    def release(self, rows):
-        """The listed rows end: their pages go back."""
-        pic_page_free(self._rows(rows), self.block_table, self.num_pages, self.page_refs, self.ctx_len)
-        self._use(set(self.in_use) - set(rows))
+    * ``begin`` -- room for a position behind every row, and the plan of the pages they share;
+    * ``attend`` per layer -- from the layer's projections (q [n][1][Hq][d], k and v
+      [n][1][Hkv][d], of any strides): norm, rotation, append, and the attention, shared keys
+      read once, in ``out[layer]`` [n][Hq][d];
+    * ``sample`` -- from logits [n][vocab]: ``token``, its ``logprob``, the number of entries it
+      was drawn from (``kept``); ctx_len advances.
+
+    All device work, no synchronisation: a step can be captured in a CUDA graph (until the
+    next fork or release).
+    """
+
+    def __init__(self, path: CacheHitPath, rows: int | None = None, max_new: int = 256,
+                 q_weight=None, k_weight=None, eps: float = 1e-6):
+        super().__init__(path, 1, rows, max_new)
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, eps
+
+    def _use(self, rows):
+        super()._use(rows)
+        g, dev, n = self.geom, self.block_table.device, len(self.in_use)
+        bf16 = dict(dtype=torch.bfloat16, device=dev)
+        self.q_rot = torch.empty((n, 1, g.num_q_heads, g.head_dim), **bf16)
+        self.out = torch.empty((g.num_layers, n, g.num_q_heads, g.head_dim), **bf16)
+        self.token = torch.empty(n, dtype=torch.int32, device=dev)
+        self.kept = torch.empty(n, dtype=torch.int32, device=dev)
+        self.logprob = torch.empty(n, dtype=torch.float32, device=dev)
+        self.plan = torch.empty(pic_share_plan_size(n) // 4, dtype=torch.int32, device=dev)
+        self.ws = torch.empty(pic_shared_workspace_size(g, n), dtype=torch.uint8, device=dev)
+        self._index, self._one = self._active.long(), torch.ones(n, dtype=torch.int32, device=dev)
+
+    def _joined(self, branches):
+        order = list(self.in_use)
+        for src, dst in branches:
+            order.insert(order.index(src) + 1, dst)
+        return order
+
+    def begin(self):
+        super().begin()
+        pic_share_plan(self.geom, self.ctx_len, self.block_table, self.num_pages, self.plan,
+                       row=self._active)
+
+    def attend(self, layer: int, q, k, v, lse=None):
+        kc, vc = self.path.k_cache, self.path.v_cache
+        pic_append_normed(self.geom, layer, q, k, v, self.block_table, self.num_pages, kc, vc,
+                          self.q_rot, q_weight=self.q_weight, k_weight=self.k_weight, eps=self.eps,
+                          row=self._active, ctx_len=self.ctx_len)
+        pic_attend_shared(self.geom, layer, self.q_rot, self.block_table, self.num_pages, kc, vc,
+                          self.plan, (self.out, layer), lse=lse, workspace=self.ws)
+
+    def sample(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
+        pic_sample(logits, uniform, self.token, temperature=temperature, top_k=top_k, top_p=top_p,
+                   min_p=min_p, logprob=self.logprob, kept=self.kept)
+        self.ctx_len.index_add_(0, self._index, self._one)
