@@ -36,10 +36,11 @@ struct Layout {
   static constexpr int kQ = 0;
   static constexpr int kK = kQ + NQB * kTile;
   static constexpr int kV = kK + NSK * kTile;
-  static constexpr int kML = kV + NSV * kTile;  // float2 [2][BM]: the warpgroups' m and l
-  static constexpr int kBar = kML + 2 * BM * 8;
+  static constexpr int kML = kV + NSV * kTile;  // float2 [2][BM / 2]: the warpgroups' m and l
+  static constexpr int kBar = kML + BM * 8;
   static constexpr int kAlloc = kBar + 256;
 };
+// (CTAs of the merge, without shared memory, fit beside one on an SM and begin early.)
 static_assert(Layout<128>::kAlloc <= 227 * 1024, "shared memory");
 
 enum {
@@ -369,11 +370,18 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
       }
       float M = m_used, w0 = 1.f, w1 = 0.f;
       if (both) {  // (read before the next segment's PV, and so before the next write)
-        ml_s[t * BM + row] = make_float2(m_used, l);
+        constexpr int kHalf = BM / 2;
+        float2 o = make_float2(0.f, 0.f);
         tc_fence_before();
-        named_bar_sync(kNbPair, 256);
+#pragma unroll 1
+        for (int half = 0; half * kHalf < rows; ++half) {
+          const bool mine = row / kHalf == half;
+          if (half) named_bar_sync(kNbPair, 256);  // (the first half has been read)
+          if (mine) ml_s[t * kHalf + row % kHalf] = make_float2(m_used, l);
+          named_bar_sync(kNbPair, 256);
+          if (mine) o = ml_s[(t ^ 1) * kHalf + row % kHalf];
+        }
         tc_fence_after();
-        const float2 o = ml_s[(t ^ 1) * BM + row];
         M = fmaxf(m_used, o.x);
         const float wt = m_used == -INFINITY ? 0.f : ex2(m_used - M);
         const float wo = o.x == -INFINITY ? 0.f : ex2(o.x - M);
@@ -671,9 +679,8 @@ __global__ void __launch_bounds__(128) merge_kernel(Params p) {
   constexpr int CPL = D / 32, kRows = 4 / kWarps;
   constexpr int kParts = kCtas + 2 * kDepth;  // at most: neighbouring nodes' CTAs overlap by one
   constexpr int KW = ((kParts + kWarps - 1) / kWarps + 31) / 32;  // parts of a lane
-  __shared__ float acc_s[4][D], m_s[4], l_s[4];
-  __shared__ size_t row_s[4][KW * 32];  // the rows of a warp's parts
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  pdl_entry();
+  __shared__ float acc_s[kWarps == 4 ? 4 : 1][kWarps == 4 ? D : 1], m_s[4], l_s[4];  // (with one warp a row unused)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int work = blockIdx.x * kRows + warp / kWarps;
   const int entry = work / p.Hq, h = work - entry * p.Hq;
@@ -708,27 +715,33 @@ __global__ void __launch_bounds__(128) merge_kernel(Params p) {
   const int w0 = warp % kWarps, mine = (parts - w0 + kWarps - 1) / kWarps;
   float w[KW], l = 0.f, M = -INFINITY;
   float2 ml[KW];
+  uint32_t rows[KW];  // of the lane's parts
 #pragma unroll
   for (int q = 0; q < KW; ++q) {
     const int c = (lane + 32 * q) * kWarps + w0;
-    size_t row = 0;
+    uint32_t row = 0;
 #pragma unroll
     for (int j = 0; j < kDepth; ++j) {
       const int e1 = __shfl_sync(0xffffffffu, end, j), n = __shfl_sync(0xffffffffu, count, j);
       const int at = __shfl_sync(0xffffffffu, c0, j), off = __shfl_sync(0xffffffffu, piece, j), i = c - (e1 - n);
       if (i >= 0 && i < n)
-        row = n == 1 ? kPieceRows + ((size_t)j * p.n + entry) * p.Hq + h
-                     : ((size_t)(at + i) * 2 + (i == 0 ? 1 : 0)) * 2 * BM + off;
+        row = n == 1 ? (uint32_t)kPieceRows + ((uint32_t)j * p.n + entry) * p.Hq + h
+                     : (uint32_t)((at + i) * 2 + (i == 0 ? 1 : 0)) * 2 * BM + off;
     }
-    row_s[warp][lane + 32 * q] = row;
+    rows[q] = row;
     ml[q] = lane + 32 * q < mine ? p.part_ml[row] : make_float2(-INFINITY, 0.f);
   }
-  __syncwarp();
   float x[U][CPL], acc[CPL];
+  auto row_of = [&](int c) {  // of this warp's part c (all lanes alike)
+    uint32_t r = rows[0];
+#pragma unroll
+    for (int q = 1; q < KW; ++q) r = c >= 32 * q ? rows[q] : r;
+    return (size_t)__shfl_sync(0xffffffffu, r, c & 31);
+  };
   auto load = [&](int b) {
 #pragma unroll
     for (int q = 0; q < U; ++q) {
-      const float *src = p.part_o + row_s[warp][min(b + q, mine - 1)] * D + lane * CPL;
+      const float *src = p.part_o + row_of(min(b + q, mine - 1)) * D + lane * CPL;
       if constexpr (CPL == 4) {
         const float4 f = *reinterpret_cast<const float4 *>(src);
         x[q][0] = f.x, x[q][1] = f.y, x[q][2] = f.z, x[q][3] = f.w;
@@ -776,7 +789,7 @@ __global__ void __launch_bounds__(128) merge_kernel(Params p) {
     for (int c = 0; c < mine; ++c)
 #pragma unroll 1
       for (int e = 0; e < CPL; ++e) {
-        const float y = p.part_o[row_s[warp][c] * D + lane * CPL + e];
+        const float y = p.part_o[row_of(c) * D + lane * CPL + e];
         if (fabsf(y) <= kFloatMax) continue;
 #pragma unroll
         for (int q = 0; q < CPL; ++q)
@@ -826,8 +839,13 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tq1, const C
                        tq1, tk, tv, p);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)p.n * p.Hq;
+  // Four warps a row where few units are split over all CTAs, which leaves each row many parts (us
+  // of the call, one warp and four: 2 x 16 entries of 16 heads of 2 kv heads 31.4 and 26.4, 64 of
+  // 4 heads of one 22.4 and 18.8; but 8 x 6 of 8 heads of 2 20.4 and 22.4, 4 of 4 heads of 2,
+  // 4.3k keys, 12.5 and 13.3).
+  const int units = p.Hkv * (((p.n + p.ept - 1) / p.ept + 1) / 2);
   const char *env = getenv("PIC_MW");
-  const bool one = env ? atoi(env) == 1 : rows > 8 * kCtas;
+  const bool one = env ? atoi(env) == 1 : units > 4 || (long long)units * (p.max_pages / 8) < 2 * kCtas;
   return launch_dependent(one ? merge_kernel<D, 1, 8> : merge_kernel<D, 4, 8>,
                           dim3((unsigned)(one ? (rows + 3) / 4 : rows)), dim3(128), 0, stream, p);
 }
@@ -871,7 +889,7 @@ extern "C" pic_status_t pic_attend_shared(const pic_geom_t *geom, int32_t layer,
   const long long rows_total = (long long)geom->num_layers * num_pages * Hkv * 16;
   if (num_pages > INT32_MAX || rows_total + 16 >= INT32_MAX)
     return fail(PIC_ERR_UNSUPPORTED, "%s: cache has more than 2^31 rows", who);
-  if ((long long)n * geom->num_q_heads >= INT32_MAX)
+  if (kPieceRows + (long long)kDepth * n * geom->num_q_heads >= INT32_MAX)
     return fail(PIC_ERR_UNSUPPORTED, "%s: grid too large", who);
   if (max_pages > INT32_MAX / 16 - 16)
     return fail(PIC_ERR_UNSUPPORTED, "%s: max_pages %d: positions beyond 32 bits", who, max_pages);
