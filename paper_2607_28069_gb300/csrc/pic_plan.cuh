@@ -30,7 +30,7 @@ struct Node {  // public: include/pic.h
 };
 struct alignas(16) Header {
   int32_t magic, n, hkv, ept, rows, max_pages, items, ctas;
-  long long total, pad;
+  long long total, q;  // steps; q: total / ctas
 };
 struct alignas(16) Item {  // a node with tiles
   int32_t begin, m, tile_begin, tiles, row, keys, level, leaf;
@@ -92,18 +92,21 @@ struct Units {
   }
 };
 
-// Steps are dealt to `ctas` CTAs in equal shares: CTA c's first is floor(total c / ctas).
+// Steps are dealt to `ctas` CTAs in equal shares: CTA c's first is floor(total c / ctas) =
+// q c + floor(r c / ctas).
 struct Deal {
-  long long total, q;
+  long long q;
   int ctas, r;
-  float inv;
-  __host__ __device__ Deal(long long total_, int ctas_)
-      : total(total_), q(total_ >> 31 ? total_ / ctas_ : (int)total_ / ctas_), ctas(ctas_), r((int)(total_ - q * ctas_)), inv((float)ctas_ / (float)(total_ > 0 ? total_ : 1)) {}
-  __host__ __device__ long long first(int c) const { return q * c + r * c / ctas; }
+  float part, inv;  // 1 / ctas, ctas / total
+  PIC_DEV Deal(long long total, int n, long long quotient)
+      : q(quotient), ctas(n), r((int)(total - quotient * n)), part(1.f / (float)n), inv((float)n / (float)max(total, 1ll)) {}
+  PIC_DEV Deal(long long total, int n) : Deal(total, n, total >> 31 ? total / n : (long long)((int)total / n)) {}
+  // (r c < 2^15: (r c + 1/2) / ctas is at least 1 / 304 away from a whole number, far more than
+  // its rounding)
+  PIC_DEV long long first(int c) const { return q * c + (int)(((float)(r * c) + 0.5f) * part); }
   // The CTA whose share holds step t: an estimate, then exact.
-  __host__ __device__ int owner(long long t) const {
-    int c = (int)((float)t * inv);
-    c = c < 0 ? 0 : c >= ctas ? ctas - 1 : c;
+  PIC_DEV int owner(long long t) const {
+    int c = max(0, min(ctas - 1, (int)((float)t * inv)));
     while (c > 0 && first(c) > t) --c;
     while (c + 1 < ctas && first(c + 1) <= t) ++c;
     return c;

@@ -13,7 +13,6 @@
 //     others leave partial states.
 //  2. merge_kernel: log-sum-exp merge along each entry's chain of nodes.
 #include <algorithm>
-#include <cstdlib>
 
 #include "pic_plan.cuh"
 
@@ -665,9 +664,9 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
 // ------------------------------------------------------------------- merge
 // o = sum_c w_c O_c / sum_c w_c l_c, w_c = 2^(m_c - M), over the parts of an entry's nodes: one
 // state for a unit that lay within a CTA, else one for each of its CTAs.  kWarps warps per
-// (entry, query head), each with its share of the parts: the (m, l) pairs of all of them first
-// (a lane per part), then the O rows, U loads in flight; the warps' sums are combined in shared
-// memory in a fixed order.
+// (entry, query head), each with its share of the parts, 32 at a time: their (m, l) pairs, a lane
+// each, and their O rows, U loads in flight; the warps' sums are combined in shared memory in a
+// fixed order.  Short loops: a call begins with cold instruction caches.
 constexpr float kFloatMax = 3.402823466e38f;
 // acc + w v.  A weight that has underflowed to 0 does not hide an infinity or a NaN.
 PIC_DEV float weigh(float w, float v, float acc) {
@@ -677,8 +676,6 @@ PIC_DEV float weigh(float w, float v, float acc) {
 template <int D, int kWarps, int U>
 __global__ void __launch_bounds__(128) merge_kernel(Params p) {
   constexpr int CPL = D / 32, kRows = 4 / kWarps;
-  constexpr int kParts = kCtas + 2 * kDepth;  // at most: neighbouring nodes' CTAs overlap by one
-  constexpr int KW = ((kParts + kWarps - 1) / kWarps + 31) / 32;  // parts of a lane
   pdl_entry();
   __shared__ float acc_s[kWarps == 4 ? 4 : 1][kWarps == 4 ? D : 1], m_s[4], l_s[4];  // (with one warp a row unused)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -694,7 +691,7 @@ __global__ void __launch_bounds__(128) merge_kernel(Params p) {
   if (!plan_fits(p, hd) || keys < 0) return;  // an entry that is left alone
   int count = 0, c0 = 0, piece = 0;
   if (k.tiles > 0) {
-    const Deal deal(hd.total, hd.ctas);
+    const Deal deal(hd.total, hd.ctas, hd.q);
     const int e = entry - k.begin, tile = e / p.ept, pair = tile / 2;
     const Units u(k.m, k.tiles, p.ept);
     const long long unit0 = k.base + h / p.G * u.per_head() + pair * u.pair_cost();
@@ -713,14 +710,14 @@ __global__ void __launch_bounds__(128) merge_kernel(Params p) {
   if (parts == 1 && __any_sync(0xffffffffu, k.alone)) return;  // done by its CTA
   // this warp's parts are w0, w0 + kWarps, ...
   const int w0 = warp % kWarps, mine = (parts - w0 + kWarps - 1) / kWarps;
-  float w[KW], l = 0.f, M = -INFINITY;
-  float2 ml[KW];
-  uint32_t rows[KW];  // of the lane's parts
+  float l = 0.f, M = -INFINITY, acc[CPL];
 #pragma unroll
-  for (int q = 0; q < KW; ++q) {
-    const int c = (lane + 32 * q) * kWarps + w0;
-    uint32_t row = 0;
-#pragma unroll
+  for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
+#pragma unroll 1
+  for (int b = 0; b < mine; b += 32) {
+    const int c = (b + lane) * kWarps + w0;
+    uint32_t row = 0;  // of the lane's part
+#pragma unroll 1
     for (int j = 0; j < kDepth; ++j) {
       const int e1 = __shfl_sync(0xffffffffu, end, j), n = __shfl_sync(0xffffffffu, count, j);
       const int at = __shfl_sync(0xffffffffu, c0, j), off = __shfl_sync(0xffffffffu, piece, j), i = c - (e1 - n);
@@ -728,73 +725,58 @@ __global__ void __launch_bounds__(128) merge_kernel(Params p) {
         row = n == 1 ? (uint32_t)kPieceRows + ((uint32_t)j * p.n + entry) * p.Hq + h
                      : (uint32_t)((at + i) * 2 + (i == 0 ? 1 : 0)) * 2 * BM + off;
     }
-    rows[q] = row;
-    ml[q] = lane + 32 * q < mine ? p.part_ml[row] : make_float2(-INFINITY, 0.f);
-  }
-  float x[U][CPL], acc[CPL];
-  auto row_of = [&](int c) {  // of this warp's part c (all lanes alike)
-    uint32_t r = rows[0];
+    const bool there = b + lane < mine;
+    const float2 ml = there ? p.part_ml[row] : make_float2(-INFINITY, 0.f);
+    const int last = min(32, mine - b) - 1;
+    float x[U][CPL];
+    auto load = [&](int k) {
 #pragma unroll
-    for (int q = 1; q < KW; ++q) r = c >= 32 * q ? rows[q] : r;
-    return (size_t)__shfl_sync(0xffffffffu, r, c & 31);
-  };
-  auto load = [&](int b) {
+      for (int q = 0; q < U; ++q) {
+        const float *src = p.part_o + (size_t)__shfl_sync(0xffffffffu, row, min(k + q, last)) * D + lane * CPL;
+        if constexpr (CPL == 4) {
+          const float4 f = *reinterpret_cast<const float4 *>(src);
+          x[q][0] = f.x, x[q][1] = f.y, x[q][2] = f.z, x[q][3] = f.w;
+        } else {
+          const float2 f = *reinterpret_cast<const float2 *>(src);
+          x[q][0] = f.x, x[q][1] = f.y;
+        }
+      }
+    };
+    load(0);  // beside the (m, l) pairs
+    float m = ml.x;
 #pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const float *src = p.part_o + row_of(min(b + q, mine - 1)) * D + lane * CPL;
-      if constexpr (CPL == 4) {
-        const float4 f = *reinterpret_cast<const float4 *>(src);
-        x[q][0] = f.x, x[q][1] = f.y, x[q][2] = f.z, x[q][3] = f.w;
-      } else {
-        const float2 f = *reinterpret_cast<const float2 *>(src);
-        x[q][0] = f.x, x[q][1] = f.y;
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    m = fmaxf(m, M);
+    const float old = M == -INFINITY ? 0.f : ex2(M - m), w = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
+    if (b) {
+      l *= old;
+#pragma unroll
+      for (int e = 0; e < CPL; ++e) acc[e] = weigh(old, acc[e], 0.f);
+    }
+    M = m;
+    l = fmaf(w, ml.y, l);
+#pragma unroll 1
+    for (int k = 0; k <= last; k += U) {
+      if (k) load(k);
+#pragma unroll
+      for (int q = 0; q < U; ++q) {
+        const float wk = k + q <= last ? __shfl_sync(0xffffffffu, w, (k + q) & 31) : 0.f;
+        if (wk != 0.f)
+#pragma unroll
+          for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wk, x[q][e], acc[e]);
       }
     }
-  };
-  if (mine > 0) load(0);  // beside the (m, l) pairs
+    // Infinities and NaN of parts whose weight underflowed to 0 (rare)
+    unsigned under = __ballot_sync(0xffffffffu, there && w == 0.f);
+#pragma unroll 1
+    for (; under; under &= under - 1) {
+      const size_t r = __shfl_sync(0xffffffffu, row, __ffs(under) - 1);
 #pragma unroll
-  for (int q = 0; q < KW; ++q) M = fmaxf(M, ml[q].x);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-#pragma unroll
-  for (int q = 0; q < KW; ++q) {
-    w[q] = ml[q].x == -INFINITY ? 0.f : ex2(ml[q].x - M);
-    l = fmaf(w[q], ml[q].y, l);
+      for (int e = 0; e < CPL; ++e) acc[e] = weigh(0.f, p.part_o[r * D + lane * CPL + e], acc[e]);
+    }
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-#pragma unroll
-  for (int e = 0; e < CPL; ++e) acc[e] = 0.f;
-#pragma unroll 1
-  for (int b = 0; b < mine; b += U) {
-    if (b) load(b);
-    float wc = w[0];
-#pragma unroll
-    for (int q = 1; q < KW; ++q) wc = b >= 32 * q ? w[q] : wc;
-#pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const float wk = __shfl_sync(0xffffffffu, wc, (b + q) & 31);  // 0 past the end
-      if (wk != 0.f)
-#pragma unroll
-        for (int e = 0; e < CPL; ++e) acc[e] = fmaf(wk, x[q][e], acc[e]);
-    }
-  }
-  // Infinities and NaN of parts whose weight underflowed to 0 (rare).  Adding those of the
-  // other parts once more changes nothing.
-  bool under = false;
-#pragma unroll
-  for (int q = 0; q < KW; ++q) under |= lane + 32 * q < mine && w[q] == 0.f;
-  if (__any_sync(0xffffffffu, under))
-#pragma unroll 1
-    for (int c = 0; c < mine; ++c)
-#pragma unroll 1
-      for (int e = 0; e < CPL; ++e) {
-        const float y = p.part_o[row_of(c) * D + lane * CPL + e];
-        if (fabsf(y) <= kFloatMax) continue;
-#pragma unroll
-        for (int q = 0; q < CPL; ++q)
-          if (q == e) acc[q] += y;
-      }
   const size_t o_row = (size_t)entry * p.Hq + h;
   if constexpr (kWarps == 4) {
 #pragma unroll
@@ -839,13 +821,12 @@ static cudaError_t launch(const CUtensorMap &tq, const CUtensorMap &tq1, const C
                        tq1, tk, tv, p);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)p.n * p.Hq;
-  // Four warps a row where few units are split over all CTAs, which leaves each row many parts (us
-  // of the call, one warp and four: 2 x 16 entries of 16 heads of 2 kv heads 31.4 and 26.4, 64 of
-  // 4 heads of one 22.4 and 18.8; but 8 x 6 of 8 heads of 2 20.4 and 22.4, 4 of 4 heads of 2,
-  // 4.3k keys, 12.5 and 13.3).
+  // Four warps a row where one or two units are split over all CTAs, which leaves each row many
+  // parts (us of the call, one warp and four: 2 entries of 4 heads of one kv head, 60k keys, 24.4
+  // and 15.9, 3 of 4 heads of 2, 100k keys, 32.0 and 30.7; but 16 of 7 heads of 4, 20k keys, 25.4
+  // and 26.4, 64 of 7 heads of 4, 33k keys, 47.8 and 49.9).
   const int units = p.Hkv * (((p.n + p.ept - 1) / p.ept + 1) / 2);
-  const char *env = getenv("PIC_MW");
-  const bool one = env ? atoi(env) == 1 : units > 4 || (long long)units * (p.max_pages / 8) < 2 * kCtas;
+  const bool one = units > 2 || (long long)units * (p.max_pages / 8) < 2 * kCtas;
   return launch_dependent(one ? merge_kernel<D, 1, 8> : merge_kernel<D, 4, 8>,
                           dim3((unsigned)(one ? (rows + 3) / 4 : rows)), dim3(128), 0, stream, p);
 }

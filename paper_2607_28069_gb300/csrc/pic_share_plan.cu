@@ -279,7 +279,8 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
   __syncthreads();
   // each CTA's first unit: lane l < kShares of a warp finds the one of CTA kShares warp + l
   const int ctas = (int)min((long long)kCtas, max(1ll, total / kLeast));
-  if (tid == 0) *v.head = Header{kMagic, n, p.hkv, p.ept, p.rows, p.max_pages, items, ctas, total, 0};
+  const Deal deal(total, ctas);
+  if (tid == 0) *v.head = Header{kMagic, n, p.hkv, p.ept, p.rows, p.max_pages, items, ctas, total, deal.q};
   constexpr int kShares = 5;
   static_assert(kShares * 32 >= kCtas, "a warp's share of the CTAs");
   for (int c0 = warp * kShares; c0 < kCtas; c0 += threads / 32 * kShares) {
@@ -288,7 +289,6 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
     if (lane < kShares && c < kCtas) {
       Share sh{0, 0, 0, 0, 0, 0, 0, 0, Item{0, 0, 0, 0, -1, 0, 0, 0}};
       if (c < ctas && total > 0) {
-        const Deal deal(total, ctas);
         sh.pos = deal.first(c), sh.end = deal.first(c + 1);
         int lo = 0, hi = 2 * n - 1;  // the last node that begins at or before pos
         while (lo < hi) {
