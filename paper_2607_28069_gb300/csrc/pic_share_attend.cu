@@ -464,10 +464,8 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
     };
     while (ok && more) {
       sg.take(ahead);
-      more = ahead.next();
       const int keys = sg.it.keys;
       int now = first4;
-      if (more) first4 = entry(ahead, 0);
       if (is_k)
         for (int t = 0; t <= (sg.two ? 1 : 0); ++t, ++nq) {
           const int qb = nq % NQB;
@@ -504,6 +502,11 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
             tma_load_2d(dst, tmap, 0, y, bar(b_full + st));
         }
         ++g;
+        // the next segment and its first pages, when this one's first tiles are on their way
+        if (j == min(2, sg.n - 1)) {
+          more = ahead.next();
+          if (more) first4 = entry(ahead, 0);
+        }
         if (is_k) continue;
         // A weight of zero does not silence an infinity: of the last key tile, rows behind the
         // keys, which may hold anything, are cleared before PV reads them (to the end of their
