@@ -20,7 +20,7 @@ constexpr int BM = 128, BN = 128;  // rows of a row tile, positions of a key til
 constexpr int kFirstPages = 32;
 constexpr int32_t kMagic = 0x50534831;
 // Costs of a key tile in a unit of one and of two row tiles, and of a unit besides.
-constexpr int kOne = 3, kTwo = 5, kUnit = 10;
+constexpr int kOne = 3, kTwo = 5, kUnit = 8;
 // A CTA's least share: it holds the first step of a key tile of any unit around it.
 constexpr int kLeast = 2 * kOne;
 static_assert(kLeast >= kTwo && kLeast >= kOne, "every CTA within a unit has a tile of it");
