@@ -59,19 +59,14 @@ struct alignas(16) Sum2 {
   uint64_t sum, count;
 };
 struct alignas(16) Entry {
-  uint64_t weight;
-  uint32_t key;
-  int32_t index;
+  uint64_t weight, place;  // place: key << 32 | ~index, larger for what comes ahead in the order
 };
 struct alignas(16) Bins {
-  // Entries, and their weights in parts of 12 bits and one for a weight of 2^36 (taken as one
-  // less): sums of 32 bits for up to 2^20 + 256 entries.
-  uint32_t count[kBins], part[4][kBins];
+  uint32_t count[kBins], low[kBins], high[kBins];  // entries; their weights' sum in 64 bits
   Entry list[2][kList];     // (a CTA may be at its second while another is at its first)
   Sum2 rank[kList];         // of the second half of the list ahead of an entry
-  uint32_t list_n, first, pick_key;
-  int32_t pick_index;
-  uint64_t pick_sum, before_sum;
+  uint32_t list_n, first;
+  uint64_t pick, pick_sum, before_sum;
   uint32_t at, before_count, members, pad;
   Sum2 seg[kBins];  // of the bins that this CTA adds up for the cluster: the first kBins / cluster size
 };
@@ -406,19 +401,14 @@ struct Row {
   }
   PIC_DEV void clear(Bins &bn) const {
     uint4 *b = reinterpret_cast<uint4 *>(bn.count);  // and the parts behind
-    for (int i = threadIdx.x; i < 5 * kBins / 4; i += kThreads) b[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < 3 * kBins / 4; i += kThreads) b[i] = make_uint4(0, 0, 0, 0);
   }
   template <bool kSums>
   PIC_DEV void count_in(Bins &bn, int bin, uint64_t w) const {
     atomicAdd(&bn.count[bin], 1u);
     if constexpr (kSums) {
-      if (w >> 36) {
-        atomicAdd(&bn.part[3][bin], 1u);
-        --w;
-      }
-      atomicAdd(&bn.part[0][bin], (uint32_t)w & 4095u);
-      atomicAdd(&bn.part[1][bin], (uint32_t)(w >> 12) & 4095u);
-      if (w >> 24) atomicAdd(&bn.part[2][bin], (uint32_t)(w >> 24));
+      const uint32_t lo = (uint32_t)w, old = atomicAdd(&bn.low[bin], lo), hi = (uint32_t)(w >> 32) + (old + lo < old);
+      if (hi) atomicAdd(&bn.high[bin], hi);
     }
   }
   // The histograms of all CTAs added up, each CTA an equal part of the bins: the slot with the
@@ -432,16 +422,13 @@ struct Row {
     for (int i0 = 0; i0 < per * parts; i0 += kThreads) {
       const int i = (i0 + tid) / parts, j = (i0 + tid) % parts;
       const uint32_t src = smem_u32(&bn.count[rank * per + i]);
-      uint32_t n = 0, a = 0, d = 0, e = 0;
+      uint32_t n = 0;
       uint64_t s = 0;
 #pragma unroll 4
       for (int c = j; c < C; c += parts) {
         const uint32_t at = map_to_rank(src, c);
         n += ld_cluster32(at);
-        if constexpr (kSums) {
-          a = ld_cluster32(at + 4 * kBins), d = ld_cluster32(at + 8 * kBins), e = ld_cluster32(at + 12 * kBins);
-          s += a + ((uint64_t)d << 12) + ((uint64_t)e << 24) + ld_cluster32(at + 16 * kBins);
-        }
+        if constexpr (kSums) s += (uint64_t)ld_cluster32(at + 8 * kBins) << 32 | ld_cluster32(at + 4 * kBins);
       }
       for (int o = 1; o < parts; o <<= 1) {
         if constexpr (kSums) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -567,7 +554,7 @@ struct Row {
           const uint64_t w = with_sums ? rule.weight(x) : 0;
           const uint32_t dst = smem_u32(&list[e]);
           for (int c = 0; c < C; ++c)
-            send(map_to_rank(dst, c), w, (uint64_t)(uint32_t)i << 32 | key_of(x), map_to_rank(bar, c));
+            send(map_to_rank(dst, c), w, (uint64_t)key_of(x) << 32 | ~(uint32_t)i, map_to_rank(bar, c));
         });
         STAMP(8);
         mbar_wait_no_flag(bar, lists++ >> 1 & 1, status, -3, kWaitLimitNs);
@@ -575,27 +562,24 @@ struct Row {
         // two threads an entry, each half of the entries ahead of it
         static_assert(kThreads == 2 * kList, "two threads an entry");
         const int i = tid % kList, half = tid / kList;
-        uint64_t s = 0, w = 0;
-        uint32_t n = 0, key = 0;
-        int index = 0;
+        uint64_t s = 0, w = 0, place = 0;
+        uint32_t n = 0;
         if (i < members) {
-          w = list[i].weight, key = list[i].key, index = list[i].index;
+          w = list[i].weight, place = list[i].place;
           const int j1 = half ? members : members / 2;
 #pragma unroll 4
-          for (int j = half ? members / 2 : 0; j < j1; ++j) {
-            const Entry e = list[j];
-            if (e.key > key || (e.key == key && e.index <= index)) s += e.weight, ++n;
-          }
+          for (int j = half ? members / 2 : 0; j < j1; ++j)
+            if (list[j].place >= place) s += list[j].weight, ++n;
           if (half) bn.rank[i].sum = s, bn.rank[i].count = n;
         }
         __syncthreads();
         if (!half && i < members) {
           s += sum0 + bn.rank[i].sum, n += count0 + (uint32_t)bn.rank[i].count;
-          if (kCount ? n == target : s >= target && s - w < target)
-            bn.pick_key = key, bn.pick_index = index, bn.pick_sum = s;
+          if (kCount ? n == target : s >= target && s - w < target) bn.pick = place, bn.pick_sum = s;
         }
         __syncthreads();
-        last = Last{bn.pick_key, bn.pick_index, logit_of(bn.pick_key)};
+        const uint32_t key = (uint32_t)(bn.pick >> 32);
+        last = Last{key, (int)~(uint32_t)bn.pick, logit_of(key)};
         return bn.pick_sum;
       }
       h.there = false;  // (taken to pieces)
@@ -751,12 +735,22 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
         for (int k = 1; k < 8; ++k) top = fmaxf(top, x[k]);
         if (!__any_sync(0xffffffffu, top >= last.x)) return 0;
         const float least_e = (float)least_ * 1.4551915228366852e-11f;  // (at most 25 bits: exact)
+        unsigned keep = 0;  // one bit an entry
+        bool tie = false;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          keep |= x[k] > last.x ? 1u << k : 0u;
+          tie |= x[k] == last.x;
+        }
+        if (__any_sync(0xffffffffu, tie))
+#pragma unroll
+          for (int k = 0; k < 8; ++k) keep |= x[k] == last.x && part.index(c, k) <= last.index ? 1u << k : 0u;
 #pragma unroll
         for (int k = 0; k < 8; k += 2) {
           float e0, e1;
           f2unpack(rule.e2(x[k], x[k + 1]), e0, e1);
-          e0 = last.keeps(x[k], part.index(c, k)) && e0 >= least_e ? e0 : 0.f;
-          e1 = last.keeps(x[k + 1], part.index(c, k + 1)) && e1 >= least_e ? e1 : 0.f;
+          e0 = (keep >> k & 1) && e0 >= least_e ? e0 : 0.f;
+          e1 = (keep >> (k + 1) & 1) && e1 >= least_e ? e1 : 0.f;
           s.add(f2pack(e0, e1));
         }
       } else {
@@ -831,8 +825,6 @@ static cudaError_t launch(Params p, int batch, cudaStream_t stream) {
   auto attempt = [&](int C) {
     const int chunks = (p.vocab + 16 / (int)sizeof(T) - 1 + kChunk - 1) / kChunk;
     const int mine = (chunks + C - 1) / C;
-    // (see Bins: 4095 times the entries of a part stay below 2^32)
-    if (p.bins && 4095ll * mine * kChunk >= 1ll << 32) return cudaErrorInvalidConfiguration;
     // (of Bins::seg a CTA uses the first kBins / C)
     const size_t bins = sizeof(Bins) - sizeof(Sum2) * (kBins - kBins / C);
     const size_t fixed = sizeof(Fixed) + (p.bins ? bins : 0) + (size_t)mine * 8 + 16;
