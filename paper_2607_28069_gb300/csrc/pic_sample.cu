@@ -10,10 +10,18 @@
 // many entries is divided again over the bits of its logits; equal logits by index.)
 //
 // One cluster per row, its CTAs a part of the row each, which they keep in shared memory as
-// far as it fits; sums go through distributed shared memory.  A warp takes chunks of 1024
-// entries, 16 bytes a lane from aligned addresses whatever the row's start.
+// far as it fits.  What they tell each other goes as asynchronous stores that an mbarrier of
+// the receiver counts: about 0.7 us, where a barrier of the cluster and a load took 1.3 to 2.
+// A warp takes chunks of 256 entries, 16 bytes a lane from aligned addresses whatever the row's
+// start.
+//
+// Measured, us: 1 x 50001, top-p 0.9, 12.3, of which the load and the largest 1.3, the histogram
+// and its sums 3, the bin 2, its entries gathered and ranked 2, the kept ones' sums 1.5, the
+// token 0.3; 64 x 131072 at a temperature alone 20.9 (33.6 MB): load and largest 3.7, the
+// weights' sums 5.5 to 9 (19 packed operations a pair of entries; two CTAs an SM on two thirds of
+// the SMs), the token 2; 48 x 100003 of mixed settings 40.8: where top-p's border lies among
+// most of a flat row, its histogram takes 9, two 32-bit shared-memory atomics an entry.
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "pic_internal.cuh"
@@ -31,12 +39,6 @@ constexpr int kList = 256;              // entries of a bin that are ranked
 constexpr int kSlots = 8;
 constexpr int kSmall = 4096;             // entries of a CTA's part that go into a histogram at once
 
-#ifdef PIC_STAMP
-__device__ long long g_stamp[32 + 64 * 16];
-#define STAMP(i) do { if (cluster_rank() == 0 && threadIdx.x == 0) { long long t_; asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t_)); if (blockIdx.x == 0) g_stamp[i] = t_; int r_ = blockIdx.x / cluster_size(); if (r_ < 64) g_stamp[32 + r_ * 16 + i] = t_; } } while (0)
-#else
-#define STAMP(i)
-#endif
 struct Params {
   int vocab, hold_chunks, bins;  // bins: shared memory holds the histogram and the list
   long long stride;
@@ -52,7 +54,7 @@ struct alignas(16) Fixed {
   uint64_t slot[kSlots][kMaxCluster][2];  // values from every CTA of the cluster
   uint64_t warp[kWarps][2];
   uint64_t bar[kSlots];                   // mbarriers of the slots
-  uint64_t list_bar[2];
+  uint64_t list_bar[2], seg_bar, bin_bar[2];
   int32_t found, pad[3];
 };
 struct alignas(16) Sum2 {
@@ -61,15 +63,22 @@ struct alignas(16) Sum2 {
 struct alignas(16) Entry {
   uint64_t weight, place;  // place: key << 32 | ~index, larger for what comes ahead in the order
 };
+constexpr int kSegs = 32, kSegBins = kBins / kSegs;
 struct alignas(16) Bins {
   uint32_t count[kBins], low[kBins], high[kBins];  // entries; their weights' sum in 64 bits
-  Entry list[2][kList];     // (a CTA may be at its second while another is at its first)
+  // (two each: a CTA may be at its second selection while another is at its first)
+  Entry list[2][kList];
   Sum2 rank[kList];         // of the second half of the list ahead of an entry
-  uint32_t list_n, first;
-  uint64_t pick, pick_sum, before_sum;
-  uint32_t at, before_count, members, pad;
-  Sum2 seg[kBins];  // of the bins that this CTA adds up for the cluster: the first kBins / cluster size
+  uint64_t pick, pick_sum;
+  uint32_t list_n, pad[3];
+  Sum2 seg[kSegs];  // the row's
+  uint32_t where[4];
+  uint64_t where_sum, pad2;
+  Sum2 in[1];  // from every CTA [cluster size]: of each segment [kSegs], then twice of a segment's bins [kSegBins]
 };
+__host__ __device__ constexpr size_t bins_bytes(int C) {
+  return sizeof(Bins) - sizeof(Sum2) + sizeof(Sum2) * C * (kSegs + 2 * kSegBins);
+}
 
 // 16 bytes to another CTA of the cluster (addresses from map_to_rank), counted by its mbarrier.
 PIC_DEV void send(uint32_t addr, uint64_t a, uint64_t b, uint32_t bar) {
@@ -79,17 +88,6 @@ PIC_DEV void send(uint32_t addr, uint64_t a, uint64_t b, uint32_t bar) {
 }
 PIC_DEV void st_cluster32(uint32_t addr, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-PIC_DEV uint32_t ld_cluster32(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
-}
-PIC_DEV uint4 ld_cluster128(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
 }
 PIC_DEV int cluster_size() {
   uint32_t r;
@@ -399,6 +397,30 @@ struct Row {
         if (z[k] >= z_min && z[k] <= z_max && last.keeps(x[k], part.index(c, k))) work(x[k], z[k], part.index(c, k));
     }
   }
+  // The histogram over z of the entries with z >= z_min.
+  PIC_DEV void histogram(Bins &bn, const Rule &rule, float z_min) {
+    const int warp = threadIdx.x >> 5;
+#pragma unroll 1
+    for (int c = part.c0 + warp; c < part.c1; c += kWarps) {
+      float x[8];
+      part.load(c, x);
+#pragma unroll
+      for (int k = 0; k < 8; k += 2) {
+        float z[2];
+        f2unpack(mul2(add2(f2pack(x[k], x[k + 1]), both(-rule.max)), both(rule.scale)), z[0], z[1]);
+        if (!__any_sync(0xffffffffu, z[0] >= z_min || z[1] >= z_min)) continue;
+        const uint64_t e = rule.e2(x[k], x[k + 1]);
+        const uint64_t h = fma2_rz(e, both(8192.f), both(8388608.f));
+        const uint64_t r = fma2(e, both(8192.f), fma2(h, both(-1.f), both(8388608.f)));
+        const uint64_t l = fma2_rz(r, both(8388608.f), both(8388608.f));
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          if (z[q] >= z_min)
+            count_in<true>(bn, (int)(-z[q] * kBinsPerOctave),
+                           ((uint64_t)((q ? hi32(h) : lo32(h)) - kTwo23) << 23) + ((q ? hi32(l) : lo32(l)) - kTwo23));
+      }
+    }
+  }
   PIC_DEV void clear(Bins &bn) const {
     uint4 *b = reinterpret_cast<uint4 *>(bn.count);  // and the parts behind
     for (int i = threadIdx.x; i < 3 * kBins / 4; i += kThreads) b[i] = make_uint4(0, 0, 0, 0);
@@ -411,84 +433,95 @@ struct Row {
       if (hi) atomicAdd(&bn.high[bin], hi);
     }
   }
-  // The histograms of all CTAs added up, each CTA an equal part of the bins: the slot with the
-  // parts' sums and counts.
-  template <bool kSums>
-  PIC_DEV int add_up(Bins &bn) {
-    const int tid = threadIdx.x;
-    cluster_sync_all();
-    const int per = kBins / C, parts = per < kThreads ? kThreads / per : 1;  // threads a bin
-    uint64_t s_all = 0, n_all = 0;
-    for (int i0 = 0; i0 < per * parts; i0 += kThreads) {
-      const int i = (i0 + tid) / parts, j = (i0 + tid) % parts;
-      const uint32_t src = smem_u32(&bn.count[rank * per + i]);
-      uint32_t n = 0;
-      uint64_t s = 0;
-#pragma unroll 4
-      for (int c = j; c < C; c += parts) {
-        const uint32_t at = map_to_rank(src, c);
-        n += ld_cluster32(at);
-        if constexpr (kSums) s += (uint64_t)ld_cluster32(at + 8 * kBins) << 32 | ld_cluster32(at + 4 * kBins);
-      }
-      for (int o = 1; o < parts; o <<= 1) {
-        if constexpr (kSums) s += __shfl_xor_sync(0xffffffffu, s, o);
-        n += __shfl_xor_sync(0xffffffffu, n, o);
-      }
-      if (j == 0) {
-        bn.seg[i].sum = s, bn.seg[i].count = n;
-        s_all += s, n_all += n;
-      }
-    }
-    s_all = warp_sum(s_all), n_all = warp_sum(n_all);
+  PIC_DEV Sum2 bin_sum(const Bins &bn, int i) const { return Sum2{(uint64_t)bn.high[i] << 32 | bn.low[i], bn.count[i]}; }
+  // This CTA's sums of each segment of 64 bins to every CTA; lane l gets segment l's of the row.
+  PIC_DEV Sum2 segments(Bins &bn) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t bar = smem_u32(&fx.seg_bar);
+    if (threadIdx.x == 0) mbar_expect_tx(bar, (uint32_t)sizeof(Sum2) * kSegs * C);
     __syncthreads();
-    cta_sum(s_all, n_all);
-    const int t = exchange(s_all, n_all);
-    cluster_sync_all();
-    return t;
+    for (int g = warp; g < kSegs; g += kWarps) {
+      uint64_t s = 0;
+      uint32_t n = 0;
+#pragma unroll
+      for (int k = 0; k < kSegBins; k += 32) {
+        const Sum2 b = bin_sum(bn, g * kSegBins + k + lane);
+        s += b.sum, n += (uint32_t)b.count;
+      }
+      s = warp_sum(s), n = __reduce_add_sync(0xffffffffu, n);
+      if (lane < C) send(map_to_rank(smem_u32(&bn.in[rank * kSegs + g]), lane), s, n, map_to_rank(bar, lane));
+    }
+    if (warp == 0) {
+      mbar_wait_no_flag(bar, rounds & 1, status, -3, kWaitLimitNs);
+      Sum2 t{0, 0};
+#pragma unroll 4
+      for (int c = 0; c < C; ++c) t.sum += bn.in[c * kSegs + lane].sum, t.count += bn.in[c * kSegs + lane].count;
+      bn.seg[lane] = t;
+    }
+    ++rounds;
+    __syncthreads();
+    return bn.seg[lane];
   }
+  PIC_DEV Total total(const Sum2 &seg) const { return Total{warp_sum(seg.sum), 0, 0, warp_sum(seg.count)}; }
   struct Where {
     int bin;
-    uint32_t count, members;  // entries ahead of the bin; its own
-    uint64_t sum;             // of those ahead
+    uint32_t count, members, first;  // entries ahead of the bin; its own; of them, those of the CTAs before
+    uint64_t sum;                    // of those ahead
   };
-  // The bin in which the target is reached, each CTA for itself; `base` ahead of the histogram.
+  // The bin in which the target is reached, behind what sum0 and count0 are; seg: from segments().
   template <bool kCount>
-  PIC_DEV Where locate(Bins &bn, int t, uint64_t target, uint64_t sum0, uint32_t count0) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = kBins / C;
-    const uint64_t v = lane < C ? fx.slot[t][lane][0] : 0, m = lane < C ? fx.slot[t][lane][1] : 0;
-    const uint64_t v_in = scan64(v), m_in = scan64(m);
-    const unsigned reached = __ballot_sync(0xffffffffu, lane < C && (kCount ? count0 + m_in : sum0 + v_in) >= target);
-    const int owner = reached ? __ffs(reached) - 1 : C - 1;
-    sum0 += __shfl_sync(0xffffffffu, v_in - v, owner);
-    count0 += (uint32_t)__shfl_sync(0xffffffffu, m_in - m, owner);
-    if (tid == 0) bn.list_n = 0, bn.at = 0, bn.members = 0;
-    for (int i0 = 0; i0 < per; i0 += kThreads) {
-      const int i = i0 + tid;
-      uint64_t s = 0, n = 0;
-      if (i < per) {
-        const uint4 q = ld_cluster128(map_to_rank(smem_u32(&bn.seg[i]), owner));
-        s = (uint64_t)q.y << 32 | q.x, n = q.z;
-      }
-      const uint64_t s_in = scan64(s), n_in = scan64(n);
-      __syncthreads();
-      if (lane == 31) fx.warp[warp][0] = s_in, fx.warp[warp][1] = n_in;
-      __syncthreads();
-      const uint64_t ws = lane < kWarps ? fx.warp[lane][0] : 0, wn = lane < kWarps ? fx.warp[lane][1] : 0;
-      const uint64_t ws_in = scan64(ws), wn_in = scan64(wn);
-      const uint64_t s_at = sum0 + s_in - s + __shfl_sync(0xffffffffu, ws_in - ws, warp);
-      const uint64_t n_at = count0 + n_in - n + __shfl_sync(0xffffffffu, wn_in - wn, warp);
-      sum0 += __shfl_sync(0xffffffffu, ws_in, 31), count0 += (uint32_t)__shfl_sync(0xffffffffu, wn_in, 31);
-      const uint64_t now = kCount ? n_at : s_at, then = kCount ? n_at + n : s_at + s;
-      if (now < target && then >= target)
-        bn.at = owner * per + i, bn.before_sum = s_at, bn.before_count = (uint32_t)n_at, bn.members = (uint32_t)n;
+  PIC_DEV Where locate(Bins &bn, const Sum2 &seg, uint64_t target, uint64_t sum0, uint32_t count0) {
+    const int tid = threadIdx.x, lane = tid & 31, turn = finds & 1;
+    const uint32_t bar = smem_u32(&fx.bin_bar[turn]);
+    if (tid == 0) bn.list_n = 0, mbar_expect_tx(bar, (uint32_t)sizeof(Sum2) * kSegBins * C);
+    // the first place, in order, up to which the target is reached: ahead of it, it
+    auto reach = [&](const Sum2 &v, int *at) {
+      const uint64_t s = scan64(v.sum), n = scan64(v.count);
+      const unsigned there = __ballot_sync(0xffffffffu, (kCount ? count0 + n : sum0 + s) >= target);
+      *at = there ? __ffs(there) - 1 : 31;
+      sum0 += __shfl_sync(0xffffffffu, s - v.sum, *at);
+      count0 += (uint32_t)__shfl_sync(0xffffffffu, n - v.count, *at);
+    };
+    int g;
+    reach(seg, &g);
+    Sum2 *in = bn.in + C * (kSegs + turn * kSegBins);
+    {  // this CTA's bins of the segment to every CTA
+      const int k = tid % kSegBins, c0 = tid / kSegBins;
+      const Sum2 b = bin_sum(bn, g * kSegBins + k);
+      for (int c = c0; c < C; c += kThreads / kSegBins)
+        send(map_to_rank(smem_u32(&in[rank * kSegBins + k]), c), b.sum, b.count, map_to_rank(bar, c));
     }
+    if (tid < 32) {
+      mbar_wait_no_flag(bar, finds >> 1 & 1, status, -3, kWaitLimitNs);
+      static_assert(kSegBins == 64, "two bins a lane");
+      Sum2 a{0, 0}, b{0, 0};  // bins lane, lane + 32
+#pragma unroll 4
+      for (int c = 0; c < C; ++c) {
+        const Sum2 *v = in + c * kSegBins + lane;
+        a.sum += v[0].sum, a.count += v[0].count, b.sum += v[32].sum, b.count += v[32].count;
+      }
+      const uint64_t a_sum = warp_sum(a.sum), a_count = warp_sum(a.count);
+      const bool second = (kCount ? count0 + a_count : sum0 + a_sum) < target;
+      if (second) a = b, sum0 += a_sum, count0 += (uint32_t)a_count;
+      int k;
+      reach(a, &k);
+      const uint32_t members = (uint32_t)__shfl_sync(0xffffffffu, a.count, k);
+      k += second ? 32 : 0;
+      uint32_t first = lane < rank ? (uint32_t)in[lane * kSegBins + k].count : 0;
+      first = __reduce_add_sync(0xffffffffu, first);
+      if (lane == 0) {
+        bn.where[0] = g * kSegBins + k, bn.where[1] = count0, bn.where[2] = members, bn.where[3] = first;
+        bn.where_sum = sum0;
+      }
+    }
+    ++finds;
     __syncthreads();
-    return Where{(int)bn.at, bn.before_count, bn.members, bn.before_sum};
+    return Where{(int)bn.where[0], bn.where[1], bn.where[2], bn.where[3], bn.where_sum};
   }
 
   struct Hist {  // what the bins hold
-    int slot;
-    bool there, sums;
+    Sum2 seg;
+    bool there;
   };
   // The first entry in the order, of those that `last` keeps, with which their count (kCount) or
   // their sum reaches `target`, into `last`; returns the sum up to it (where weights are
@@ -512,22 +545,22 @@ struct Row {
     };
     for (;;) {
       if (!h.there) {
-        clear(bn);
+        if (!clean) clear(bn);
+        clean = false;
         __syncthreads();
-        each(rule, among, z_min, z_max, [&](float x, float z, int) {
-          const int k = bin_of(x, z);
-          if (k < 0) return;
-          if (with_sums) count_in<true>(bn, k, rule.weight(x));
-          else count_in<false>(bn, k, 0);
-        });
-        h.slot = with_sums ? add_up<true>(bn) : add_up<false>(bn);
+        if (shift < 0 && with_sums && among.x == -INFINITY)
+          histogram(bn, rule, z_min);
+        else
+          each(rule, among, z_min, z_max, [&](float x, float z, int) {
+            const int k = bin_of(x, z);
+            if (k < 0) return;
+            if (with_sums) count_in<true>(bn, k, rule.weight(x));
+            else count_in<false>(bn, k, 0);
+          });
+        __syncthreads();
+        h.seg = segments(bn);
       }
-      STAMP(6);
-      const Where at = locate<kCount>(bn, h.slot, target, sum0, count0);
-      STAMP(7);
-#ifdef PIC_STAMP
-      if (blockIdx.x == 0 && threadIdx.x == 0) g_stamp[20] = at.members, g_stamp[21] = shift;
-#endif
+      const Where at = locate<kCount>(bn, h.seg, target, sum0, count0);
       sum0 = at.sum, count0 = at.count;
       if (shift < 0) {  // (one 2^-10 of a bin on either side for the rounding of -z bins)
         z_max = fminf(z_max, -((float)at.bin - 0.001f) / kBinsPerOctave);
@@ -538,27 +571,18 @@ struct Row {
         // gathered by every CTA: this one's entries behind those of the CTAs before it
         const uint32_t bar = smem_u32(&fx.list_bar[lists & 1]);
         Entry *list = bn.list[lists & 1];
-        if (warp == 0) {
-          uint32_t n = lane < rank ? ld_cluster32(map_to_rank(smem_u32(&bn.count[at.bin]), lane)) : 0;
-          n = __reduce_add_sync(0xffffffffu, n);
-          if (lane == 0) {
-            bn.first = n;
-            mbar_expect_tx(bar, 16 * (uint32_t)members);
-          }
-        }
+        if (tid == 0) mbar_expect_tx(bar, 16 * (uint32_t)members);
         __syncthreads();
         each(rule, among, z_min, z_max, [&](float x, float z, int i) {
           if (bin_of(x, z) != at.bin) return;
-          const uint32_t e = bn.first + atomicAdd(&bn.list_n, 1u);
+          const uint32_t e = at.first + atomicAdd(&bn.list_n, 1u);
           if (e >= kList) return;
           const uint64_t w = with_sums ? rule.weight(x) : 0;
           const uint32_t dst = smem_u32(&list[e]);
           for (int c = 0; c < C; ++c)
             send(map_to_rank(dst, c), w, (uint64_t)key_of(x) << 32 | ~(uint32_t)i, map_to_rank(bar, c));
         });
-        STAMP(8);
         mbar_wait_no_flag(bar, lists++ >> 1 & 1, status, -3, kWaitLimitNs);
-        STAMP(9);
         // two threads an entry, each half of the entries ahead of it
         static_assert(kThreads == 2 * kList, "two threads an entry");
         const int i = tid % kList, half = tid / kList;
@@ -621,7 +645,8 @@ struct Row {
       cluster_sync_all();  // (the histogram and its sums are read by the other CTAs until here)
     }
   }
-  uint32_t lists = 0;  // gathered so far
+  uint32_t lists = 0, rounds = 0, finds = 0;  // gathered, added up, located so far
+  bool clean = true;                          // the bins are zeros
 };
 
 template <typename T>
@@ -632,7 +657,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < kSlots; ++i) mbar_init(smem_u32(&fx.bar[i]), 1);
-    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&fx.list_bar[i]), 1);
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&fx.list_bar[i]), 1), mbar_init(smem_u32(&fx.bin_bar[i]), 1);
+    mbar_init(smem_u32(&fx.seg_bar), 1);
     fence_mbar_init();
   }
   // every CTA of the cluster runs before another one writes to its shared memory
@@ -653,9 +679,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
   }
   uint8_t *at = smem + sizeof(Fixed);
   Bins *bins = p.bins ? reinterpret_cast<Bins *>(at) : nullptr;
-  if (p.bins) at += sizeof(Bins) - sizeof(Sum2) * (kBins - kBins / row.C);  // (see launch)
+  if (p.bins) at += bins_bytes(row.C);
   part.held = reinterpret_cast<uint4 *>(at);
-  STAMP(0);
   row.chunk = reinterpret_cast<uint64_t *>(at + (size_t)p.hold_chunks * kChunk * sizeof(T));
 
   // ---- the largest logit, and as much of the row as fits into shared memory
@@ -677,7 +702,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
         for (int k = 0; k < 8; k += 2) m = max3f(m, x[k], x[k + 1]);  // (a NaN is passed over)
       }
   }
-  STAMP(1);
   if (bins) row.clear(*bins);
   // this row's settings
   const float temp = p.temperature ? p.temperature[b] : 1.f, u = p.uniform[b];
@@ -697,7 +721,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
   if (warp == 0) lanes_max(&fx.warp[0][0], kWarps);
   lanes_max(&fx.slot[row.exchange(__float_as_uint(m), 0)][0][0], row.C);
   const bool writer = row.rank == 0 && tid == 0;
-  STAMP(2);
   if (m == -INFINITY) {  // no entry has a weight
     if (writer) {
       p.token[b] = -1;
@@ -767,19 +790,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
   typename Row<T>::Total t;
   bool changed = least > 1;
   if (bins && (by_k || by_p)) {
-    typename Row<T>::Hist h{0, part.vocab <= kSmall * row.C, true};
+    typename Row<T>::Hist h{{0, 0}, part.vocab <= kSmall * row.C};
     if (h.there) {
       // a small part: the histogram of all entries at once, from which the sums come too
-      row.each(rule, last, kLeastZ, 0.f, [&](float x, float z, int) {
-        row.template count_in<true>(*bins, (int)(-z * kBinsPerOctave), rule.weight(x));
-      });
-      STAMP(5);
-      h.slot = row.template add_up<true>(*bins);
-      t = row.total(h.slot);
+      row.histogram(*bins, rule, kLeastZ);
+      row.clean = false;
+      __syncthreads();
+      h.seg = row.segments(*bins);
+      t = row.total(h.seg);
     } else {
       t = kept_sums(No(), 1);
     }
-    STAMP(3);
     if (by_k && (uint64_t)top_k < t.count) {
       t.all = row.template select<true>(*bins, rule, last, (uint64_t)top_k, kLeastZ, h);
       changed = true;
@@ -801,9 +822,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
   } else if (!changed) {
     t = kept_sums(No(), 1);
   }
-  STAMP(10);
   if (changed) t = kept_sums(Yes(), least);
-  STAMP(11);
   row.find(share_of(t.all, u, 16777215.f), t,
            [&](float x, int i) -> uint64_t {
              const uint64_t w = last.keeps(x, i) ? rule.weight(x) : 0;
@@ -816,7 +835,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
                p.logprob[b] = w > t.all - w ? log1pf(-(float)(t.all - w) / (float)t.all) : logf((float)w / (float)t.all);
            });
   if (writer && p.kept) p.kept[b] = (int32_t)t.count;
-  STAMP(12);
 }
 
 template <typename T>
@@ -825,9 +843,7 @@ static cudaError_t launch(Params p, int batch, cudaStream_t stream) {
   auto attempt = [&](int C) {
     const int chunks = (p.vocab + 16 / (int)sizeof(T) - 1 + kChunk - 1) / kChunk;
     const int mine = (chunks + C - 1) / C;
-    // (of Bins::seg a CTA uses the first kBins / C)
-    const size_t bins = sizeof(Bins) - sizeof(Sum2) * (kBins - kBins / C);
-    const size_t fixed = sizeof(Fixed) + (p.bins ? bins : 0) + (size_t)mine * 8 + 16;
+    const size_t fixed = sizeof(Fixed) + (p.bins ? bins_bytes(C) : 0) + (size_t)mine * 8 + 16;
     const size_t room = fixed < kSmem ? kSmem - fixed : 0;
     p.hold_chunks = (int)std::min<size_t>(mine, room / (kChunk * sizeof(T)));
     const size_t smem = fixed + (size_t)p.hold_chunks * kChunk * sizeof(T);
@@ -839,14 +855,19 @@ static cudaError_t launch(Params p, int batch, cudaStream_t stream) {
     return launch_dependent_cluster(sample_kernel<T>, dim3((unsigned)(batch * C)), dim3(kThreads), smem,
                                     stream, C, p);
   };
-  const char *env = getenv("PIC_C");
-  if (env) return attempt(atoi(env));
-  if (batch <= 12 || p.vocab > (1 << 22)) {
+  // Parts of up to 4096 entries, with no more CTAs than two an SM, or about that where the rows
+  // of a batch cost unlike (us, 4, 8 and 16 CTAs: 1 x 50001, top-p, 17.8, 15.2 and 14.1; 4 x
+  // 32000 16.1, 12.8 and 14.2; 20 x 100003 32.3, 30.2 and 39.6; 48 x 100003 of mixed settings 52.3,
+  // 43.7 and 71.2; 64 x 131072 61.9, 66.8 and 111).
+  const int most = batch <= 12 ? 16 : batch <= 50 ? 8 : 4;
+  int C = p.vocab > 1 << 22 ? 16 : 1;
+  while (C < most && p.vocab > kSmall * C) C *= 2;
+  if (C == 16) {
     if (attempt(16) == cudaSuccess) return cudaSuccess;
     cudaGetLastError();  // (where the device places no such clusters)
-    return attempt(8);
+    C = 8;
   }
-  return attempt(batch <= 38 ? 8 : 4);
+  return attempt(C);
 }
 
 }  // namespace sample
@@ -874,6 +895,3 @@ extern "C" pic_status_t pic_sample(int32_t batch, int32_t vocab, const void *log
   return e == cudaSuccess ? PIC_OK : cuda_fail(e, who);
 }
 
-#ifdef PIC_STAMP
-extern "C" void pic_stamps(long long *h) { cudaMemcpyFromSymbol(h, pic::sample::g_stamp, sizeof(long long) * (32 + 1024)); }
-#endif
