@@ -782,7 +782,8 @@ pic_status_t pic_page_copy(const pic_geom_t *geom, int32_t n, const int32_t *src
  * t * stride[1] + h * stride[2] + i (strides in elements, HOST arrays, not
  * negative, multiples of 8), for instance slices of one fused projection.
  * q_weight, k_weight: bf16 [d] or NULL.  num_tokens, row: int32 [batch]; pos:
- * int32 [batch][max_tokens]; ctx_len: int32 [rows] (may be NULL with pos);
+ * int32 [batch][max_tokens]; ctx_len: int32 [rows] (may be NULL with pos); a row
+ * list has at most 4096 rows;
  * block_table: int32 [rows][max_pages].  Tokens of one call have slots of their
  * own.  One launch, no workspace of its own.
  * Device checks: rows, a row named twice, token counts (BAD_REQUEST; the request
@@ -847,7 +848,7 @@ pic_status_t pic_share_plan(const pic_geom_t *geom, int32_t n, const int32_t *ro
  * keys_i may hold anything.
  *
  * q, out: bf16 [n][Hq][d]; lse: float [n][Hq] or NULL; block_table, max_pages:
- * as the plan was made with; Hq / Hkv <= 128.  workspace: >=
+ * as the plan was made with; Hq / Hkv <= 128; out is memory of its own.  workspace: >=
  * pic_shared_workspace_size(...) bytes, 256-byte aligned; its contents do not
  * matter before or after.  Runs on the tensor cores (tcgen05.mma, TMEM, TMA); the
  * work is dealt to the SMs by the plan.  Launches: attention, merge.

@@ -571,7 +571,7 @@ def pic_share_plan(geom: Geometry, ctx_len, block_table, num_pages: int, plan, r
 def share_nodes(plan, n: int):
     """The nodes of a plan of n entries, a view [2 n][8] of it: begin and end of the entries, begin
     and end of their 128-position tiles, block-table row, keys, parent, level (see include/pic.h)."""
-    return plan[:16 * n].view(2 * n, 8)
+    return plan.as_strided((2 * n, 8), (8, 1))
 
 
 def pic_shared_workspace_size(geom: Geometry, n: int) -> int:

@@ -50,6 +50,7 @@ const char *dtype_name(at::ScalarType t) {
 struct Args {
   PyObject *const *v;
   Py_ssize_t n, i = 0;
+  int device = -1;  // the current device, where tensors have to be on it
   PyObject *next() {
     if (i >= n) {
       PyErr_SetString(PyExc_TypeError, "too few arguments");
@@ -117,6 +118,11 @@ View view_of(PyObject *o, const char *name) {
   return w;
 }
 
+// A tensor of a call that says so (Args::device) has to be on the current device.
+void here(const Args &a, const View &w, const char *name) {
+  if (a.device >= 0 && w && w.t->is_cuda() && w.t->get_device() != a.device)
+    raise(PyExc_ValueError, "%s must be on the current device%s", name);
+}
 void *checked(const View &w, at::ScalarType dtype, const char *name, bool optional = false,
               bool pinned_ok = false) {
   if (!w) {
@@ -632,6 +638,7 @@ template <typename T>
 T *sized(Args &a, at::ScalarType dtype, const char *name, int64_t n, bool optional = false) {
   const View w = view_of(a.next(), name);
   T *p = static_cast<T *>(checked(w, dtype, name, optional));
+  here(a, w, name);
   if (w && w.numel() != n) raise(PyExc_ValueError, "%s has the wrong number of elements%s", name);
   return p;
 }
@@ -639,6 +646,7 @@ T *sized(Args &a, at::ScalarType dtype, const char *name, int64_t n, bool option
 void *cache_of(Args &a, const Geom &g, const char *name, int64_t *pages) {
   const View w = view_of(a.next(), name);
   void *p = checked(w, at::kBFloat16, name);
+  here(a, w, name);
   if (w.dim() != 5 || w.size(0) != g.g.num_layers || w.size(2) != g.g.num_kv_heads ||
       w.size(3) != g.g.page_size || w.size(4) != g.g.head_dim || (*pages >= 0 && w.size(1) != *pages))
     raise(PyExc_ValueError, "%s must be [num_layers][num_pages][num_kv_heads][page_size][head_dim]%s",
@@ -826,6 +834,17 @@ PyObject *page_copy(PyObject *, PyObject *const *v, Py_ssize_t n) {
 }
 
 // ------------------------------------------- decoding branches of a context
+int current_device() {  // (-1: none; the call then fails on its own)
+  int d = -1;
+  return cudaGetDevice(&d) == cudaSuccess ? d : -1;
+}
+// A tensor of the current device, whole.
+template <typename T = void>
+T *local(Args &a, const View &w, at::ScalarType dtype, const char *name, bool optional = false) {
+  T *p = static_cast<T *>(checked(w, dtype, name, optional));
+  here(a, w, name);
+  return p;
+}
 // Heads [batch][tokens][heads][d] in any strides but the last dimension's: data and strides.
 const void *heads_of(const View &w, const char *name, int64_t heads, int64_t d, int64_t *strides) {
   if (!w) raise(PyExc_ValueError, "%s is required%s", name);
@@ -841,18 +860,21 @@ const void *heads_of(const View &w, const char *name, int64_t heads, int64_t d, 
 
 PyObject *append_normed(PyObject *, PyObject *const *v, Py_ssize_t n) {
   return guarded(v, n, [](Args &a) {
+    a.device = current_device();
     Geom g(a.next());
     const int32_t layer = a.i32();
     int64_t qs[3], ks[3], vs[3];
     const int64_t d = g.g.head_dim, Hq = g.g.num_q_heads, Hkv = g.g.num_kv_heads;
     const View qv = view_of(a.next(), "q");
     const void *q = heads_of(qv, "q", Hq, d, qs);
+    here(a, qv, "q");
     const int64_t B = qv.size(0), T = qv.size(1);
     const void *kv[2];
     for (int i = 0; i < 2; ++i) {
       const char *name = i ? "v_new" : "k_new";
       const View w = view_of(a.next(), name);
       kv[i] = heads_of(w, name, Hkv, d, i ? vs : ks);
+      here(a, w, name);
       if (w.size(0) != B || w.size(1) != T)
         raise(PyExc_ValueError, "%s must have the requests and tokens of q%s", name);
     }
@@ -864,16 +886,16 @@ PyObject *append_normed(PyObject *, PyObject *const *v, Py_ssize_t n) {
     const int32_t *pos = sized<int32_t>(a, at::kInt, "pos", B * T, true);
     const int32_t *row = sized<int32_t>(a, at::kInt, "row", B, true);
     const View cv = view_of(a.next(), "ctx_len");
-    const int32_t *ctx = static_cast<int32_t *>(checked(cv, at::kInt, "ctx_len", true));
+    const int32_t *ctx = local<int32_t>(a, cv, at::kInt, "ctx_len", true);
     const View bt = view_of(a.next(), "block_table");
-    const int32_t *table = static_cast<int32_t *>(checked(bt, at::kInt, "block_table"));
+    const int32_t *table = local<int32_t>(a, bt, at::kInt, "block_table");
     need_2d(bt, "block_table");
     if (cv && cv.numel() != bt.size(0)) raise(PyExc_ValueError, "%s must have an entry per row%s", "ctx_len");
     int64_t num_pages = a.integer();
     void *kc = cache_of(a, g, "k_cache", &num_pages), *vc = cache_of(a, g, "v_cache", &num_pages);
     void *out = sized<void>(a, at::kBFloat16, "q_out", B * T * Hq * d, true);
     const View wv = view_of(a.next(), "workspace");
-    void *ws = checked(wv, at::kByte, "workspace", true);
+    void *ws = local(a, wv, at::kByte, "workspace", true);
     const size_t bytes = wv ? (size_t)wv.numel() : 0;
     const pic_stream_t s = stream_of(a.next());
     return unlocked([&] {
@@ -886,19 +908,20 @@ PyObject *append_normed(PyObject *, PyObject *const *v, Py_ssize_t n) {
 
 PyObject *share_plan(PyObject *, PyObject *const *v, Py_ssize_t n) {
   return guarded(v, n, [](Args &a) {
+    a.device = current_device();
     Geom g(a.next());
     const View rv = view_of(a.next(), "row");
-    const int32_t *row = static_cast<int32_t *>(checked(rv, at::kInt, "row", true));
+    const int32_t *row = local<int32_t>(a, rv, at::kInt, "row", true);
     const View cv = view_of(a.next(), "ctx_len");
-    const int32_t *ctx = static_cast<int32_t *>(checked(cv, at::kInt, "ctx_len"));
+    const int32_t *ctx = local<int32_t>(a, cv, at::kInt, "ctx_len");
     const int32_t pos_offset = a.i32();
     const View bt = view_of(a.next(), "block_table");
-    const int32_t *table = static_cast<int32_t *>(checked(bt, at::kInt, "block_table"));
+    const int32_t *table = local<int32_t>(a, bt, at::kInt, "block_table");
     need_2d(bt, "block_table");
     if (cv.numel() != bt.size(0)) raise(PyExc_ValueError, "%s must have an entry per row%s", "ctx_len");
     const int64_t num_pages = a.integer();
     const View pv = view_of(a.next(), "plan");
-    int32_t *plan = static_cast<int32_t *>(checked(pv, at::kInt, "plan"));
+    int32_t *plan = local<int32_t>(a, pv, at::kInt, "plan");
     const int64_t entries = rv ? rv.numel() : bt.size(0);
     const pic_stream_t s = stream_of(a.next());
     return unlocked([&] {
@@ -911,26 +934,27 @@ PyObject *share_plan(PyObject *, PyObject *const *v, Py_ssize_t n) {
 
 PyObject *attend_shared(PyObject *, PyObject *const *v, Py_ssize_t n) {
   return guarded(v, n, [](Args &a) {
+    a.device = current_device();
     Geom g(a.next());
     const int32_t layer = a.i32();
     const View qv = view_of(a.next(), "q");
-    const void *q = checked(qv, at::kBFloat16, "q");
+    const void *q = local(a, qv, at::kBFloat16, "q");
     const int64_t k = qv.dim();  // [n][Hq][d], or a token each: [n][1][Hq][d]
     if ((k != 3 && (k != 4 || qv.size(1) != 1)) || qv.size(k - 2) != g.g.num_q_heads ||
         qv.size(k - 1) != g.g.head_dim)
       raise(PyExc_ValueError, "%s must be [entries][num_q_heads][head_dim]%s", "q");
     const int64_t entries = qv.size(0);
     const View bt = view_of(a.next(), "block_table");
-    const int32_t *table = static_cast<int32_t *>(checked(bt, at::kInt, "block_table"));
+    const int32_t *table = local<int32_t>(a, bt, at::kInt, "block_table");
     need_2d(bt, "block_table");
     int64_t num_pages = a.integer();
     const void *kc = cache_of(a, g, "k_cache", &num_pages), *vc = cache_of(a, g, "v_cache", &num_pages);
     const View pv = view_of(a.next(), "plan");
-    const int32_t *plan = static_cast<int32_t *>(checked(pv, at::kInt, "plan"));
+    const int32_t *plan = local<int32_t>(a, pv, at::kInt, "plan");
     void *out = sized<void>(a, at::kBFloat16, "out", qv.numel());
     float *lse = sized<float>(a, at::kFloat, "lse", entries * g.g.num_q_heads, true);
     const View wv = view_of(a.next(), "workspace");
-    void *ws = checked(wv, at::kByte, "workspace");
+    void *ws = local(a, wv, at::kByte, "workspace");
     const pic_stream_t s = stream_of(a.next());
     return unlocked([&] {
       return pic_attend_shared(&g.g, layer, (int32_t)std::min<int64_t>(entries, INT32_MAX), q,
@@ -942,9 +966,11 @@ PyObject *attend_shared(PyObject *, PyObject *const *v, Py_ssize_t n) {
 
 PyObject *sample(PyObject *, PyObject *const *v, Py_ssize_t n) {
   return guarded(v, n, [](Args &a) {
+    a.device = current_device();
     const View lv = view_of(a.next(), "logits");
     need_2d(lv, "logits");
     if (!lv.t->is_cuda()) raise(PyExc_ValueError, "%s must be a CUDA tensor%s", "logits");
+    here(a, lv, "logits");
     const bool bf16 = lv.t->scalar_type() == at::kBFloat16;
     if (!bf16 && lv.t->scalar_type() != at::kFloat)
       raise(PyExc_ValueError, "%s must be torch.float32 or torch.bfloat16%s", "logits");

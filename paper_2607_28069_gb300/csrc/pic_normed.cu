@@ -22,6 +22,7 @@ namespace normed {
 constexpr int kMaxThreads = 512;
 constexpr int kMaxRun = 16;  // tokens of a CTA at a time
 constexpr int kMaxRagged = 1024;
+constexpr int kMaxList = 4096;
 constexpr int kStages = 4;   // tokens in flight
 
 struct Params {
@@ -312,6 +313,8 @@ extern "C" pic_status_t pic_append_normed(const pic_geom_t *geom, int32_t layer,
     return fail(PIC_ERR_INVALID_ARG, "%s: NULL tensor", who);
   if (!pos && !ctx_len)
     return fail(PIC_ERR_INVALID_ARG, "%s: neither positions nor lengths", who);
+  if (row && batch > kMaxList)
+    return fail(PIC_ERR_UNSUPPORTED, "%s: a list of %d rows (at most %d)", who, batch, kMaxList);
   if (!row && batch > rows)
     return fail(PIC_ERR_INVALID_ARG, "%s: batch %d, block table of %d rows", who, batch, rows);
   if (!q_out == !workspace)

@@ -388,8 +388,10 @@ extern "C" pic_status_t pic_share_plan(const pic_geom_t *geom, int32_t n, const 
   p.status = device_status_ptr();
   if (!p.status) return fail(PIC_ERR_CUDA, "%s: no device status word", who);
   const size_t smem = Scratch(nullptr, n, p.tree).bytes;
-  cudaError_t e = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       (int)Scratch(nullptr, kMaxEntries, 2 * kMaxEntries).bytes);
+  cudaError_t e = cudaSuccess;
+  if (smem > 40 * 1024)
+    e = cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)Scratch(nullptr, kMaxEntries, 2 * kMaxEntries).bytes);
   const int wide = std::min(1024, std::max(128, (max_pages / 8 + 31) / 32 * 32));
   if (e == cudaSuccess) e = launch_dependent(common_kernel, dim3(n), dim3(wide), 0, stream, p);
   if (e == cudaSuccess) e = launch_dependent(plan_kernel, dim3(1), dim3(1024), smem, stream, p);

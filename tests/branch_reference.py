@@ -137,7 +137,8 @@ def attention_close(got, lse, ref, S, A, lse_ref):
     (S + 1): e = S 2^-15 + 2^-19 relative to a weight and absolute on the lse."""
     e = S * 2.0 ** -15 + 2.0 ** -19
     ok = np.abs(got - ref) <= np.abs(ref) * 2.0 ** -8 + A * (2.0 ** -8 + 2 * e) + 2.0 ** -130
-    same = (lse == lse_ref) | (np.abs(lse - lse_ref) <= e + np.abs(lse_ref) * 2.0 ** -22)
+    with np.errstate(invalid="ignore"):  # (-infinity from -infinity)
+        same = (lse == lse_ref) | (np.abs(lse - lse_ref) <= e + np.abs(lse_ref) * 2.0 ** -22)
     return bool(ok.all()), bool(same.all())
 
 

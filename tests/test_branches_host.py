@@ -48,6 +48,7 @@ def test_append_normed(lib):
             (dict(eps=float("nan")), 1, "eps"), (dict(eps=float("inf")), 1, "eps"),
             (dict(stride=(-8, 0, 0)), 1, "negative stride"), (dict(stride=(1024, 4, 128)), 1, "16 bytes"),
             (dict(weight=ctypes.c_void_p(8)), 1, "16 bytes"), (dict(q=ctypes.c_void_p(264)), 1, "16 bytes"),
+            (dict(batch=4097, row=FAKE), 2, "list of 4097 rows"),
             (dict(batch=1 << 20, tokens=1 << 12, rows=1 << 20), 2, "2^31"), (dict(max_pages=1 << 27), 2, "2^31"),
             (dict(out=NULL, ws=FAKE, ws_bytes=64), 4, "workspace needs"),
             (dict(out=NULL, ws=ctypes.c_void_p(64), ws_bytes=1 << 30), 4, "workspace needs")):
