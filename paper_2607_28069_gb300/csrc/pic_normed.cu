@@ -12,6 +12,13 @@
 // shuffles.  Positions, pages and the rotation's cos and sin are formed for up to 16 tokens at
 // once, while the first tokens' projections are under way to shared memory; each thread
 // copies what it will read itself, so that ring needs no barrier.
+//
+// Measured: 8 ragged requests of up to 1067 tokens, 32 + 2 x 8 heads of 128, 28.4 us (140 MB: 4.95
+// TB/s, 73% of a copy's rate): the issue slots are 70% busy with about 380 instructions a chunk,
+// DRAM 37% (the rest of the rows written stays in L2).  Packed operations took 40% fewer of them,
+// but 80 registers or spills, and were no faster.  A run of tokens per CTA instead of equal shares
+// left a fifth of the CTAs without work (32 us); one token a CTA 57.  One request's token 3.5 us:
+// its chain of loads (projections, row and length, page), sine and cosine.
 #include <algorithm>
 
 #include "pic_internal.cuh"

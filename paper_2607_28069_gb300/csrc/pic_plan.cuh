@@ -19,7 +19,10 @@ constexpr int kCtas = 152;         // one per SM
 constexpr int BM = 128, BN = 128;  // rows of a row tile, positions of a key tile
 constexpr int kFirstPages = 32;
 constexpr int32_t kMagic = 0x50534831;
-// Costs of a key tile in a unit of one and of two row tiles, and of a unit besides.
+// Costs of a key tile in a unit of one and of two row tiles, and of a unit besides (0.3 us each: a
+// key tile of two row tiles takes 1.5 us, one of one 0.85, a short unit's last softmax, exchange
+// and stores about 2.5).  Between 7 and 13 the third makes no difference beyond the noise; 3 made
+// 64 entries of 33k keys 62 us instead of 52, as the CTAs of short units were late.
 constexpr int kOne = 3, kTwo = 5, kUnit = 8;
 // A CTA's least share: it holds the first step of a key tile of any unit around it.
 constexpr int kLeast = 2 * kOne;

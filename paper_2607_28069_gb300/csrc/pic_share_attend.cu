@@ -12,6 +12,14 @@
 //     dealt it.  An entry whose keys all lie in one node within one CTA is finished there; the
 //     others leave partial states.
 //  2. merge_kernel: log-sum-exp merge along each entry's chain of nodes.
+//
+// Measured, whole calls: 16 branches of one context of 139k, 8 kv heads (605 MB), 100 us (6.0 TB/s;
+// the attention 93 of them, DRAM 80% busy); 64 branches of one of 33k, 7 heads of 4 kv heads, 47
+// us, the attention 37 with the tensor pipe 39% busy: first tiles after 4.5 us (plan, pages, keys:
+// dependent round trips), then 1.5 us a key tile of two row tiles, where its MMAs need 1.1 and its
+// exponentials as much, 2 for the epilogue's 128 KB a CTA, and the branches' own tiles at 0.85 us
+// each and 2.5 a branch; 48 entries of 8 nested contexts, d = 64, 18.7 us; 4 of 160 keys 8.2, two
+// dependent launches.
 #include <algorithm>
 
 #include "pic_plan.cuh"
