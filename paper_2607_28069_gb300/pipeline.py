@@ -472,8 +472,10 @@ class BranchDecoder(_Rows):
     * ``sample`` -- from logits [n][vocab]: ``token``, its ``logprob``, the number of entries it
       was drawn from (``kept``); ctx_len advances.
 
-    All device work, no synchronisation: a step can be captured in a CUDA graph (until the
-    next fork or release).
+    A row for whose token ``begin`` found no page (``result`` -1, and the device status says so)
+    stays at its length: what the step leaves for it means nothing, and the step is to be taken
+    again when there are pages.  All device work, no synchronisation: a step can be captured in a
+    CUDA graph (until the next fork or release).
     """
 
     def __init__(self, path: CacheHitPath, rows: int | None = None, max_new: int = 256,
@@ -492,7 +494,7 @@ class BranchDecoder(_Rows):
         self.logprob = torch.empty(n, dtype=torch.float32, device=dev)
         self.plan = torch.empty(pic_share_plan_size(n) // 4, dtype=torch.int32, device=dev)
         self.ws = torch.empty(pic_shared_workspace_size(g, n), dtype=torch.uint8, device=dev)
-        self._index, self._one = self._active.long(), torch.ones(n, dtype=torch.int32, device=dev)
+        self._index, self._grown = self._active.long(), torch.empty(n, dtype=torch.int32, device=dev)
 
     def _joined(self, branches):
         order = list(self.in_use)
@@ -516,4 +518,6 @@ class BranchDecoder(_Rows):
     def sample(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
         pic_sample(logits, uniform, self.token, temperature=temperature, top_k=top_k, top_p=top_p,
                    min_p=min_p, logprob=self.logprob, kept=self.kept)
-        self.ctx_len.index_add_(0, self._index, self._one)
+        # a token each where `begin` counted pages for it
+        torch.clamp(self.result[:len(self.in_use)], 0, 1, out=self._grown)
+        self.ctx_len.index_add_(0, self._index, self._grown)

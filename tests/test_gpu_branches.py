@@ -116,3 +116,43 @@ def test_a_captured_step_replays(cuda_lib):
         got.append(rec)
     for a, b in zip(*got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_a_row_without_a_page_waits(cuda_lib):
+    """With no page free, a row at a page's end stays at its length, while others go on; with
+    pages again its steps are taken, and no position was passed over (the free pages hold NaN)."""
+    from paper_2607_28069_gb300 import DEVICE_CODES
+    from paper_2607_28069_gb300.pipeline import BranchDecoder
+    wl, path = linked(1, spare=8)
+    dec = BranchDecoder(path, max_new=64)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    free = dec.page_refs == 0
+    path.k_cache[:, free] = path.v_cache[:, free] = float("nan")
+    dec.page_refs[free] = 1
+    waited, geom = torch.zeros(2, dtype=torch.bool, device="cuda"), dec.geom
+    for n in range(160):
+        if n and bool(waited.all()):
+            break
+        before = dec.ctx_len.clone()
+        room = dec.block_table.gather(1, (before // 16).long()[:, None])[:, 0] >= 0
+        qkv, logits, u = step_inputs(g, 1, 2, 300)
+        run(dec, 1, qkv, logits, u, 0.7)
+        code = cuda_lib.pic_device_status()[0]
+        assert DEVICE_CODES[code] == ("ok" if room.all() else "no free page")
+        assert torch.equal(dec.ctx_len, before + room.int())
+        waited |= ~room
+    assert waited.all()
+    dec.page_refs[free] = 0
+    for n in range(2):
+        before = dec.ctx_len.clone()
+        qkv, logits, u = step_inputs(g, 1, 2, 300)
+        run(dec, 1, qkv, logits, u, 0.7)
+        assert cuda_lib.pic_device_status() == (0, 0) and torch.equal(dec.ctx_len, before + 1)
+    for e, r in enumerate(dec.in_use):
+        at = torch.arange(int(dec.ctx_len[r]), device="cuda")
+        page = dec.block_table[r].long()[at // 16]
+        K, V = (R.f64(c[0][page, :, at % 16]) for c in (path.k_cache, path.v_cache))
+        ref, _, A, S = R.attention(R.f64(dec.q_rot[e, 0]), K, V)
+        out = R.f64(dec.out[0, e])
+        # (the roundings as in attention_close)
+        assert (np.abs(out - ref) <= np.abs(ref) * 2.0 ** -8 + A * (2.0 ** -8 * 1.01 + 2.0 ** -14 * S + 2.0 ** -18)).all()
