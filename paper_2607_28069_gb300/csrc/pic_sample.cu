@@ -856,14 +856,16 @@ static cudaError_t launch(Params p, int batch, cudaStream_t stream) {
                                     stream, C, p);
   };
   // Parts of up to 4096 entries, with no more CTAs than two an SM, or about that where the rows
-  // of a batch cost unlike (us, 4, 8 and 16 CTAs: 1 x 50001, top-p, 17.8, 15.2 and 14.1; 4 x
-  // 32000 16.1, 12.8 and 14.2; 20 x 100003 32.3, 30.2 and 39.6; 48 x 100003 of mixed settings 52.3,
-  // 43.7 and 71.2; 64 x 131072 61.9, 66.8 and 111).
-  const int most = batch <= 12 ? 16 : batch <= 50 ? 8 : 4;
+  // of a batch cost unlike, and no more clusters than the GPCs place at once (us, 4, 8, 12 and 16
+  // CTAs: 1 x 50001, top-p, 17.1, 14.4, 14.2 and 12.3; 14 x 50001 of mixed settings 31.0, 25.7, 26.1
+  // and 17.7; 16 x 131072, mixed, 55.4, 35.7, 33.5 and 33.0, at a temperature alone 11.3, 10.4, 9.0
+  // and 11.2; 20 x 100003 32.0, 28.1, 24.0 and 33.7; 24 x 131072 38.8, 33.0, 36.7 and 39.3; 48 x
+  // 100003, mixed, 50.5, 40.8, 47.8 and 61.2; 64 x 131072 60.7, 62.8, 70.9 and 93.2).
+  const int most = batch <= 15 ? 16 : batch <= 20 ? 12 : batch <= 50 ? 8 : 4;
   int C = p.vocab > 1 << 22 ? 16 : 1;
-  while (C < most && p.vocab > kSmall * C) C *= 2;
-  if (C == 16) {
-    if (attempt(16) == cudaSuccess) return cudaSuccess;
+  while (C < most && p.vocab > kSmall * C) C = std::min(2 * C, most);
+  if (C > 8) {
+    if (attempt(C) == cudaSuccess) return cudaSuccess;
     cudaGetLastError();  // (where the device places no such clusters)
     C = 8;
   }

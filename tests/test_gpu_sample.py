@@ -74,6 +74,13 @@ def test_batches(cuda_lib, B):
     check(cuda_lib, x, rng.random(B).astype(np.float32), *settings(rng, B))
 
 
+@pytest.mark.parametrize("B", [15, 17, 21])
+def test_batches_of_rows_in_more_parts_than_eight(cuda_lib, B):
+    rng = np.random.default_rng(B)
+    x = torch.tensor(rng.normal(0, 2.5, (B, 50021)), device="cuda").bfloat16()
+    check(cuda_lib, x, rng.random(B).astype(np.float32), *settings(rng, B))
+
+
 def test_long_rows_beyond_shared_memory(cuda_lib):
     """Parts of a row that are read again from memory; a row of 2^24 entries."""
     rng = np.random.default_rng(1)
