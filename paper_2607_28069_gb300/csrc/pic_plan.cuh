@@ -28,7 +28,7 @@ constexpr int kOne = 3, kTwo = 5, kUnit = 8;
 constexpr int kLeast = 2 * kOne;
 static_assert(kLeast >= kTwo && kLeast >= kOne, "every CTA within a unit has a tile of it");
 
-struct Node {  // public: include/pic.h
+struct alignas(16) Node {  // public: include/pic.h
   int32_t begin, end, tile_begin, tile_end, row, keys, parent, level;
 };
 struct alignas(16) Header {

@@ -302,8 +302,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
           if (s.base[mid] <= sh.pos) lo = mid;
           else hi = mid - 1;
         }
-        Node o;
-        node_of(lo, &o);
+        const Node o = v.nodes[lo < n ? lo + n : lo - n];
         const Units u(o.end - o.begin, o.tile_end - o.tile_begin, p.ept);
         sh.item = s.item[lo];
         sh.it = Item{o.begin, o.end - o.begin, o.tile_begin, o.tile_end - o.tile_begin, o.row, o.keys, o.level, lo >= n};
@@ -330,9 +329,8 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
   // each entry's chain, by level
   for (int i = tid; i < n; i += threads) {
     Link *chain = v.chain + (size_t)i * kDepth;
-    Node o;
+    Node o = v.nodes[i];
     int k = n + i;
-    node_of(k, &o);
 #pragma unroll 1
     for (int level = kDepth - 1; level >= 0; --level) {
       Link l{0, 0, 0, 0, 0, {0, 0}};
@@ -340,7 +338,7 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
         l = Link{s.base[k], o.tile_end - o.tile_begin, o.begin, o.end - o.begin, k >= n && o.level == 0, {0, 0}};
       *reinterpret_cast<int4 *>(chain + level) = *reinterpret_cast<int4 *>(&l);
       *(reinterpret_cast<int4 *>(chain + level) + 1) = *(reinterpret_cast<int4 *>(&l) + 1);
-      if (level == o.level && o.parent >= 0) k = o.parent - n, node_of(k, &o);
+      if (level == o.level && o.parent >= 0) k = o.parent - n, o = v.nodes[o.parent];
     }
   }
 }
