@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(1024) plan_kernel(PlanParams p) {
       if (c0 + j < kCtas) v.first_pages[(c0 + j) * kFirstPages + lane] = page;
     }
   }
-  // each entry's chain, by level
-  for (int i = tid; i < n; i += threads) {
+  // each entry's chain, by level (the last warps first, which have no shares)
+  for (int i = threads - 1 - tid; i < n; i += threads) {
     Link *chain = v.chain + (size_t)i * kDepth;
     Node o = v.nodes[i];
     int k = n + i;
