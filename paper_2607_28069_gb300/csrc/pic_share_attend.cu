@@ -240,7 +240,6 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
   const uint32_t sbase = smem_u32(smem);
   if (sbase & 1023) {  // the tiles' swizzle counts on the array's alignment
     if (threadIdx.x == 0) dev_fail(p.status, PIC_DEV_BAD_REQUEST, -1);
-    pdl_entry();
     return;
   }
   auto bar = [&](int i) { return sbase + L::kBar + 8u * (uint32_t)i; };
@@ -713,36 +712,24 @@ PIC_DEV float weigh(float w, float v, float acc) {
   return w != 0.f || fabsf(v) <= kFloatMax ? fmaf(w, v, acc) : acc + v;
 }
 
-template <typename T>
-PIC_DEV T ld_l2(const T *src) {
-  static_assert(sizeof(T) % 16 == 0, "whole pieces");
-  union {
-    int4 piece[sizeof(T) / 16];
-    T value;
-  } u;
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof(T) / 16); ++i) u.piece[i] = __ldcg(reinterpret_cast<const int4 *>(src) + i);
-  return u.value;
-}
-
 template <int D, int kWarps, int U>
 __global__ void __launch_bounds__(128) merge_kernel(Params p) {
   constexpr int CPL = D / 32, kRows = 4 / kWarps;
+  pdl_entry();
   __shared__ float acc_s[kWarps == 4 ? 4 : 1][kWarps == 4 ? D : 1], m_s[4], l_s[4];  // (with one warp a row unused)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int work = blockIdx.x * kRows + warp / kWarps;
-  const int entry = min(work / p.Hq, p.n - 1), h = work % p.Hq;
-  // What the plan says of the row, while the attention runs.  (Every CTA of the attention has
-  // waited for the launches before it when the first one of these starts, so the plan is there;
-  // from L2, as an L1 might hold an older one.)
+  const int entry = work / p.Hq, h = work - entry * p.Hq;
+  if (entry >= p.n) return;  // (kWarps = 4: the whole CTA)
   const View v(p.plan, p.n);
-  const Header hd = ld_l2(v.head);
-  const int keys = __ldcg(v.keys + entry);
+  const Header hd = *v.head;
+  const int keys = v.keys[entry];
   // lane j < kDepth: the parts of the chain's node of level j
   Link k{0, 0, 0, 0, 0, {0, 0}};
-  if (lane < kDepth) k = ld_l2(v.chain + (size_t)entry * kDepth + lane);
+  if (lane < kDepth) k = v.chain[(size_t)entry * kDepth + lane];
+  if (!plan_fits(p, hd) || keys < 0) return;  // an entry that is left alone
   int count = 0, c0 = 0, piece = 0;
-  if (k.tiles > 0 && plan_fits(p, hd)) {
+  if (k.tiles > 0) {
     const Deal deal(hd.total, hd.ctas, hd.q);
     const int e = entry - k.begin, tile = e / p.ept, pair = tile / 2;
     const Units u(k.m, k.tiles, p.ept);
@@ -759,8 +746,6 @@ __global__ void __launch_bounds__(128) merge_kernel(Params p) {
     if (lane >= o) end += y;
   }
   const int parts = __shfl_sync(0xffffffffu, end, kDepth - 1);
-  pdl_entry();  // (before any exit: the grid's end stands for the attention's too)
-  if (work / p.Hq >= p.n || !plan_fits(p, hd) || keys < 0) return;  // behind the last, or left alone
   if (parts == 1 && __any_sync(0xffffffffu, k.alone)) return;  // done by its CTA
   // this warp's parts are w0, w0 + kWarps, ...
   const int w0 = warp % kWarps, mine = (parts - w0 + kWarps - 1) / kWarps;
