@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(kBoundThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
   if (sbase & 1023) {  // the tiles' swizzle counts on the array's alignment
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (threadIdx.x == 0) dev_fail(p.status, PIC_DEV_BAD_REQUEST, -1);
     return;
   }
