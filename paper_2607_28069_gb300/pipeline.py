@@ -472,9 +472,10 @@ class BranchDecoder(_Rows):
     * ``sample`` -- from logits [n][vocab]: ``token``, its ``logprob``, the number of entries it
       was drawn from (``kept``); ctx_len advances.
 
-    A row for whose token ``begin`` found no page (``result`` -1, and the device status says so)
-    stays at its length: what the step leaves for it means nothing, and the step is to be taken
-    again when there are pages.  All device work, no synchronisation: a step can be captured in a
+    A row to which ``begin`` gives no room (``result`` -1; the device status says why: no free page,
+    a table at its end, a length lowered into a page that other rows use) writes no keys and
+    values and stays at its length: what the step leaves for it elsewhere means nothing, and the
+    step is to be taken again when there is room.  All device work, no synchronisation: a step can be captured in a
     CUDA graph (until the next fork or release).
     """
 
@@ -494,7 +495,7 @@ class BranchDecoder(_Rows):
         self.logprob = torch.empty(n, dtype=torch.float32, device=dev)
         self.plan = torch.empty(pic_share_plan_size(n) // 4, dtype=torch.int32, device=dev)
         self.ws = torch.empty(pic_shared_workspace_size(g, n), dtype=torch.uint8, device=dev)
-        self._index, self._grown = self._active.long(), torch.empty(n, dtype=torch.int32, device=dev)
+        self._index, self._grown = self._active.long(), torch.zeros(n, dtype=torch.int32, device=dev)
 
     def _joined(self, branches):
         order = list(self.in_use)
@@ -504,6 +505,8 @@ class BranchDecoder(_Rows):
 
     def begin(self):
         super().begin()
+        # a token each where there is room for it, none where a row was refused
+        torch.clamp(self.result[:len(self.in_use)], 0, 1, out=self._grown)
         pic_share_plan(self.geom, self.ctx_len, self.block_table, self.num_pages, self.plan,
                        row=self._active)
 
@@ -511,13 +514,11 @@ class BranchDecoder(_Rows):
         kc, vc = self.path.k_cache, self.path.v_cache
         pic_append_normed(self.geom, layer, q, k, v, self.block_table, self.num_pages, kc, vc,
                           self.q_rot, q_weight=self.q_weight, k_weight=self.k_weight, eps=self.eps,
-                          row=self._active, ctx_len=self.ctx_len)
+                          num_tokens=self._grown, row=self._active, ctx_len=self.ctx_len)
         pic_attend_shared(self.geom, layer, self.q_rot, self.block_table, self.num_pages, kc, vc,
                           self.plan, (self.out, layer), lse=lse, workspace=self.ws)
 
     def sample(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
         pic_sample(logits, uniform, self.token, temperature=temperature, top_k=top_k, top_p=top_p,
                    min_p=min_p, logprob=self.logprob, kept=self.kept)
-        # a token each where `begin` counted pages for it
-        torch.clamp(self.result[:len(self.in_use)], 0, 1, out=self._grown)
         self.ctx_len.index_add_(0, self._index, self._grown)
