@@ -497,6 +497,12 @@ class BranchDecoder(_Rows):
         self.ws = torch.empty(pic_shared_workspace_size(g, n), dtype=torch.uint8, device=dev)
         self._index, self._grown = self._active.long(), torch.zeros(n, dtype=torch.int32, device=dev)
 
+    def fork(self, src, dst):
+        """As _Rows.fork; every source is a row in use when the call is made."""
+        if not set(src) <= set(self.in_use):
+            raise ValueError("fork: every source has to be a row in use")
+        return super().fork(src, dst)
+
     def _joined(self, branches):
         order = list(self.in_use)
         for src, dst in branches:
