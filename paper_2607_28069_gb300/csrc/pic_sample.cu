@@ -136,7 +136,6 @@ PIC_DEV uint64_t both(float v) { return f2pack(v, v); }
 constexpr float kLeastZ = -36.f;
 struct Rule {
   float max, scale;
-  PIC_DEV float z(float x) const { return __fmul_rn(__fsub_rn(x, max), scale); }
   PIC_DEV uint64_t e2(float x0, float x1) const {
     uint64_t z = mul2(add2(f2pack(x0, x1), both(-max)), both(scale));
     float z0, z1;
@@ -434,6 +433,13 @@ struct Row {
     }
   }
   PIC_DEV Sum2 bin_sum(const Bins &bn, int i) const { return Sum2{(uint64_t)bn.high[i] << 32 | bn.low[i], bn.count[i]}; }
+  // Bins, segments and lists take no barrier of the cluster.  Another CTA reads none of this CTA's
+  // bins; what is sent lands in `in` and `list` of the receiver.  A CTA sends segments of a round
+  // after it has located the bin of the round before (or, first of all, the sums that follow it),
+  // for which it needed what every other CTA sends once it has read that round's segments; the
+  // places for a segment's bins and for the list are two each, used in turn, with a location
+  // between two uses of one.  An mbarrier counts a phase's bytes only until its receiver, who waits
+  // for that phase itself, has also announced them, so none runs a phase ahead.
   // This CTA's sums of each segment of 64 bins to every CTA; lane l gets segment l's of the row.
   PIC_DEV Sum2 segments(Bins &bn) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -642,7 +648,6 @@ struct Row {
         hi = top;
       }
       shift = max(0, 32 - __clz((int)(hi - lo)) - 11);
-      cluster_sync_all();  // (the histogram and its sums are read by the other CTAs until here)
     }
   }
   uint32_t lists = 0, rounds = 0, finds = 0;  // gathered, added up, located so far
@@ -804,11 +809,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(Params p) {
     if (by_k && (uint64_t)top_k < t.count) {
       t.all = row.template select<true>(*bins, rule, last, (uint64_t)top_k, kLeastZ, h);
       changed = true;
-      if (by_p && !h.there) {
-        h.there = false;
-        t = kept_sums(Yes(), 1);
-        cluster_sync_all();  // (the histogram's sums are read until here)
-      }
+      if (by_p && !h.there) t = kept_sums(Yes(), 1);
     }
     if (by_p) {
       const uint64_t target = max(share_of(t.all, top_p, 16777216.f), (uint64_t)1);
