@@ -772,7 +772,8 @@ pic_status_t pic_page_copy(const pic_geom_t *geom, int32_t n, const int32_t *src
  *     N(x) = x / sqrt(mean(x^2) + eps) * weight     (weight NULL: N(x) = x)
  *     k_cache[layer][slot(p)] = R(p) N(k_new[b][t]),  v_cache... = v_new[b][t]
  *     queries: R(p) N(q[b][t])
- * in fp32, rounded to bf16 once (with a weight, magnitudes beyond 2^60 overflow).
+ * in fp32, rounded to bf16 once (with a weight, magnitudes beyond 2^60 overflow, and with
+ * eps below 2^-120 heads of magnitudes below 2^-60 underflow).
  * The queries go to q_out, bf16 [batch][max_tokens][Hq][d] (rows
  * t >= num_tokens[b] not written), or, with q_out NULL, GQA-packed into the
  * prefill workspace as pic_append_inline leaves them (those rows zeros), which
@@ -874,7 +875,8 @@ pic_status_t pic_attend_shared(const pic_geom_t *geom, int32_t layer, int32_t n,
  *    j = rint(z), f = z - j, e = 1 + f (c1 + f (c2 + f (c3 + f (c4 + f c5)))),
  *    from the inside out, each operation rounded to fp32, c = {0.6931470036506653,
  *    0.24022242426872253, 0.05550733581185341, 0.009671512991189957,
- *    0.001326472731307149}; w = trunc(2^36 e 2^j), 0 where z < -37 or NaN.
+ *    0.001326472731307149} (2^f within 1.09e-7 of its value, a least-maximum fit with
+ *    e = 1 at f = 0); w = trunc(2^36 e 2^j), 0 where z < -37 or NaN.
  *  - the order: entries with w > 0, logit descending, then index ascending.
  *  - k > 0: only the first k stay.
  *  - P < 1: of those the fewest first ones whose sum of w reaches

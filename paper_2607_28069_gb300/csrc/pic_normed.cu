@@ -17,7 +17,7 @@
 // TB/s, 73% of a copy's rate): the issue slots are 70% busy with about 380 instructions a chunk,
 // DRAM 37% (the rest of the rows written stays in L2).  Packed operations took 40% fewer of them,
 // but 80 registers or spills, and were no faster.  A run of tokens per CTA instead of equal shares
-// left a fifth of the CTAs without work (32 us); one token a CTA 57.  One request's token 3.5 us:
+// left a fifth of the CTAs without work (32 us); one token a CTA 57.  One request's token 4.0 us:
 // its chain of loads (projections, row and length, page), sine and cosine.
 #include <algorithm>
 

@@ -15,12 +15,14 @@
 // A warp takes chunks of 256 entries, 16 bytes a lane from aligned addresses whatever the row's
 // start.
 //
-// Measured, us: 1 x 50001, top-p 0.9, 12.3, of which the load and the largest 1.3, the histogram
-// and its sums 3, the bin 2, its entries gathered and ranked 2, the kept ones' sums 1.5, the
-// token 0.3; 64 x 131072 at a temperature alone 20.9 (33.6 MB): load and largest 3.7, the
-// weights' sums 5.5 to 9 (19 packed operations a pair of entries; two CTAs an SM on two thirds of
-// the SMs), the token 2; 48 x 100003 of mixed settings 40.8: where top-p's border lies among
-// most of a flat row, its histogram takes 9, two 32-bit shared-memory atomics an entry.
+// Measured, us, on inputs that change from call to call: 1 x 50001, top-p 0.9, 12.1, of which the
+// load and the largest 1.3, the histogram and its sums 3, the bin 2, its entries gathered and ranked
+// 2, the kept ones' sums 1.5, the token 0.3; 64 x 131072 at a temperature alone 19.5 (33.6 MB): load
+// and largest 3.7, the weights' sums 5.5 to 9 (19 packed operations a pair of entries; two CTAs an SM
+// on two thirds of the SMs), the token 2; the same with top-p 59.6; 48 x 100003 of mixed settings
+// 42.4: where top-p's border lies among most of a flat row, its histogram takes 9, two 32-bit
+// shared-memory atomics an entry.  64 registers, for two CTAs an SM, spill 50 bytes (fp32) and 14
+// (bf16).
 #include <algorithm>
 #include <type_traits>
 
@@ -133,6 +135,8 @@ PIC_DEV uint64_t both(float v) { return f2pack(v, v); }
 // polynomial of degree 5 in the rest, each operation rounded to fp32; the weight is
 // trunc(2^36 e).  That is 0 exactly where z < -36 (z is kept at -38 or above, a NaN too), and
 // at least 1 from -36 on.  Pairs of entries go through packed operations.
+// The polynomial: a fit of 2^f on [-1/2, 1/2] to the least largest relative error with value 1 at 0,
+// its coefficients rounded to fp32: within 1.09e-7 (0.92e-7 is the least there is).
 constexpr float kLeastZ = -36.f;
 struct Rule {
   float max, scale;
@@ -856,12 +860,22 @@ static cudaError_t launch(Params p, int batch, cudaStream_t stream) {
     return launch_dependent_cluster(sample_kernel<T>, dim3((unsigned)(batch * C)), dim3(kThreads), smem,
                                     stream, C, p);
   };
-  // Parts of up to 4096 entries, with no more CTAs than two an SM, or about that where the rows
-  // of a batch cost unlike, and no more clusters than the GPCs place at once (us, 4, 8, 12 and 16
-  // CTAs: 1 x 50001, top-p, 17.1, 14.4, 14.2 and 12.3; 14 x 50001 of mixed settings 31.0, 25.7, 26.1
-  // and 17.7; 16 x 131072, mixed, 55.4, 35.7, 33.5 and 33.0, at a temperature alone 11.3, 10.4, 9.0
-  // and 11.2; 20 x 100003 32.0, 28.1, 24.0 and 33.7; 24 x 131072 38.8, 33.0, 36.7 and 39.3; 48 x
-  // 100003, mixed, 50.5, 40.8, 47.8 and 61.2; 64 x 131072 60.7, 62.8, 70.9 and 93.2).
+  // Parts of up to 4096 entries, but clusters of 16 up to 15 rows and of 12 up to 20 (with a few
+  // more rows of so large clusters not all are placed at once), of 8 up to 50, else of 4.  Where rows cost
+  // alike, 8 and 4 cross at about 42 rows, with top-p between 50 and 60, and where they cost unlike
+  // at more than 60: 50 is a compromise.
+  // us of 4, 8, 12 and 16 CTAs: 1 x 50001, top-p, 17.1, 14.4, 14.2 and 12.3; 14 x 50001, mixed, 31.0,
+  // 25.7, 26.1 and 17.7; rows of 131072 fp32 at a temperature alone | with top-p | mixed:
+  //   16 rows  11.2 10.5  9.0 11.3 | 38.9 31.1 27.1 34.3 | 60.6 38.2 35.6 32.4
+  //   20       11.4 11.0  9.1 11.5 | 39.4 33.2 27.4 36.6 | 58.4 43.3 36.3 46.3
+  //   24       11.4 11.0 12.7 14.2 | 39.0 33.5 38.2 39.9 | 60.8 44.8 39.0 49.5
+  //   32       11.6 11.2 15.6 17.2 | 38.8 34.1 44.0 52.1 | 60.7 46.1 51.6 60.3
+  //   39       17.2 15.9 17.4 20.3 | 54.7 46.0 46.7 57.9 | 68.8 53.2 58.2 69.5
+  //   44       18.4 18.7 18.9 23.3 | 57.5 52.8 51.1 69.7 | 75.3 55.8 63.9 78.2
+  //   50       19.5 21.5 21.7 26.8 | 58.7 56.5 63.5 75.5 | 78.3 69.1 73.0 91.0
+  //   56       20.0 22.4 24.2 27.7 | 59.9 58.6 65.0 81.0 | 78.4 67.4 74.0 97.2
+  //   64       21.0 23.2 26.2 33.1 | 60.1 61.7 69.4 91.8 | 77.0 69.7 76.2 97.6
+  // (the same inputs in turn, from a graph)
   const int most = batch <= 15 ? 16 : batch <= 20 ? 12 : batch <= 50 ? 8 : 4;
   int C = p.vocab > 1 << 22 ? 16 : 1;
   while (C < most && p.vocab > kSmall * C) C = std::min(2 * C, most);

@@ -13,13 +13,18 @@
 //     others leave partial states.
 //  2. merge_kernel: log-sum-exp merge along each entry's chain of nodes.
 //
-// Measured, whole calls: 16 branches of one context of 139k, 8 kv heads (605 MB), 100 us (6.0 TB/s;
-// the attention 93 of them, DRAM 80% busy); 64 branches of one of 33k, 7 heads of 4 kv heads, 47
-// us, the attention 37 with the tensor pipe 39% busy: first tiles after 4.5 us (plan, pages, keys:
-// dependent round trips), then 1.5 us a key tile of two row tiles, where its MMAs need 1.1 and its
-// exponentials as much, 2 for the epilogue's 128 KB a CTA, and the branches' own tiles at 0.85 us
-// each and 2.5 a branch; 48 entries of 8 nested contexts, d = 64, 18.7 us; 4 of 160 keys 8.2, two
-// dependent launches.
+// Measured, whole calls on inputs that change from call to call: 16 branches of one context of
+// 139k, 8 kv heads (605 MB), 101 us (6.0 TB/s; the attention 93 of them, DRAM 80% busy); 64 branches
+// of one of 33k, 7 heads of 4 kv heads, 48 us, the attention 37 with the tensor pipe 39% busy: first
+// tiles after 4.5 us (plan, pages, keys: dependent round trips), then 1.5 us a key tile of two
+// row tiles, where its MMAs need 1.1 and its exponentials as much, 2 for the epilogue's 128 KB a CTA,
+// and the branches' own tiles at 0.85 us each and 2.5 a branch; 48 entries of 8 nested contexts,
+// d = 64, 19.6 us; 4 of 160 keys 9, two dependent launches.
+//
+// Where rows share nothing, pic_attend_decode (append and attention in one call) is as fast or
+// faster: us a layer, 32 + 2 x 8 heads of 128, that call, and this one with its append: 1 row of 4k
+// keys 8.7 and 15.3, 8 of 16k 86.8 and 90.2, 64 of 16k 593 and 600.  4 rows of a common 33k take 88.5
+// and 36.5, 64 of them 801 and 54.5.
 #include <algorithm>
 
 #include "pic_plan.cuh"
@@ -30,7 +35,10 @@ namespace share {
 constexpr int NSK = 3, NSV = 2;  // ring stages of K and V
 constexpr int NQB = 2;           // query tiles
 constexpr int kThreads = 384;    // K producer, MMA, V producer, ring, two softmax warpgroups
-constexpr int kBoundThreads = 448;  // 127 registers a thread: merge CTAs fit beside one on an SM
+// The bound is 448 threads: 14 warps, four of them on one of the SM's quarters of 16384 registers,
+// so at most 128 a thread (d = 128 spills 8 bytes).  The 12 warps launched then leave each quarter
+// 4096 registers, two warps of the merge (64 a thread): two of its CTAs fit beside one of these.
+constexpr int kBoundThreads = 448;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;  // S_t at 128 t, O_t at 256 + D t
 // Named barriers (0: __syncthreads): P_t from warpgroup t to the MMA warp, the ring warp's

@@ -13,8 +13,8 @@
 //  2. plan_kernel: one CTA: the forest, every entry's chain of nodes, the units' costs added
 //     up, and each of the attention's CTAs its first unit and pages.
 //
-// Measured: 4 branches of 4.3k positions 9.5 us, 64 entries of 8 contexts 13.5, 256 of four of
-// 139k 19.6 (17.9 MB of table entries, each read for both its neighbours, 8.9 from DRAM).  Not
+// Measured, on inputs that change from call to call: 4 branches of 4.3k positions 10.4 us, 32
+// 11.7, 64 entries of 8 contexts 13.5, 256 of four of 139k 19.8 (17.9 MB of table entries, each read for both its neighbours, 8.9 from DRAM).  Not
 // bytes but dependent steps by one CTA: counts and tree 2 us, nearest values 1 to 2.5, nodes and
 // their sums 1.5, the CTAs' first units and pages 2 to 3.5, each on cold instructions (nodes formed
 // again where they can be read back cost 0.5 us more).  It is made once a step, for all layers.

@@ -2,7 +2,8 @@
 
 compose -> relocate (all layers) -> per layer: prefill (inline append +
 attention) -> decode steps.  PyTorch only allocates device memory and
-supplies the stream; every step is a libpic call.
+supplies the stream; every step is a libpic call (but for two small PyTorch calls of
+BranchDecoder, which count the rows that have room and advance their lengths).
 """
 from __future__ import annotations
 
@@ -422,7 +423,8 @@ class DraftDecoder(_Rows):
       path (``path``, ``path_len``), the token after it (``next_token``), the
       accepted tokens' keys and values moved together, ctx_len advanced.
 
-    All device work, no synchronisation: a step can be captured in a CUDA graph.
+    A row to which ``begin`` gives no room (``result`` -1, and the device status says so) takes no
+    drafts: its draft_len is to be 0, or they are stored where its table has pages.  All device work, no synchronisation: a step can be captured in a CUDA graph.
     """
 
     def __init__(self, path: CacheHitPath, max_draft: int, rows: int | None = None,
